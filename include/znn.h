@@ -280,6 +280,54 @@ int  znn_sgd_update(int64_t count, float eta, const float* g, float* p, void* st
 int  znn_accumulate(int64_t count, const float* x, float* y, void* stream);
 
 /*
+ * Dropout, layer norm and the residual join, which nets deeper than a few layers train with.  Operands are dense
+ * [rows][cols] arrays of any extents >= 1.  `axis` says over what the norm is taken:
+ *   0  every column over the rows: images [map][voxel], each voxel over the maps
+ *   1  every row over its columns: rows of features
+ * A norm's features (n) are the elements it is taken over, its positions the columns or rows it is taken for.
+ *
+ * znn_dropout : y = x / (1 - p) where an element is kept, 0 where it is dropped (whatever x holds there).  The call is
+ *   its own Jacobian: on the gradient, with the same state, site and extents, it drops the same elements.
+ *   No mask is stored: whether element (row, col) is kept follows from its place.  `state` is a DEVICE pointer (8-byte
+ *   aligned) to two numbers {seed, round}, `site` tells the calls of a round apart.  The words are those of
+ *   Philox4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", SC 2011),
+ *   key (seed mod 2^32, seed / 2^32), counter (col / 4, row, site, round mod 2^32), word col mod 4; an element is kept where
+ *   its word is less than K = 2^32 - floor(p 2^32 + 1/2), and then multiplied by 2^32 / K.  0 <= p <= 1; with p = 0
+ *   `state` may be NULL and y = x.
+ * znn_random_advance : round += 1 on the device, behind a round: replays of a recorded round then drop other elements.
+ *
+ * znn_layernorm_fwd : y = w (x - m) s + b, m the mean of the n features of a position, s = 1 / sqrt(v + eps), v the
+ *   mean of (x - m)^2; w [n], b [n], eps > 0.  `stats` [2][positions] receives m and s for the backward pass; NULL in
+ *   prediction, which has no use for them.
+ * znn_layernorm_bwd : with h = (x - m) s from `stats` and a = w gy,
+ *     gx = s (a - mean(a) - h mean(a h)) (means over the features),  gw = sum of gy h,  gb = sum of gy (over the positions).
+ *   Sums are taken in an order that follows from the extents alone: results repeat themselves to the bit.
+ *
+ * znn_residual_norm_fwd : the end of a residual branch, r = x + dropout(h) and y = layernorm(r), in one pass over memory.
+ *   r is what the node sum of the two edges gives, to the bit.
+ * znn_residual_norm_bwd : gy and gr are the gradients of y and of r (NULL: r is used by the norm alone);
+ *     gx = (layer norm's Jacobian of gy) + gr,  gh = dropout(gx),  gw and gb as above.
+ *   gh may be NULL if p = 0, where it equals gx.
+ *
+ * The backward calls take a workspace of znn_layernorm_workspace_bytes (256-byte aligned; may be NULL if that is 0).
+ * ZNN_EUNSUPPORTED: 2^32 rows or more, more than 2^34 columns, or more than 2^28 features.
+ */
+int  znn_random_advance(uint64_t* state, void* stream);
+int  znn_dropout(int64_t rows, int64_t cols, double p, const uint64_t* state, uint32_t site, const float* x, float* y,
+                 void* stream);
+int  znn_layernorm_workspace_bytes(int64_t rows, int64_t cols, int32_t axis, size_t* bytes);
+int  znn_layernorm_fwd(int64_t rows, int64_t cols, int32_t axis, float eps, const float* x, const float* w, const float* b,
+                       float* y, float* stats, void* stream);
+int  znn_layernorm_bwd(int64_t rows, int64_t cols, int32_t axis, const float* gy, const float* x, const float* w,
+                       const float* stats, float* gx, float* gw, float* gb, void* ws, size_t ws_bytes, void* stream);
+int  znn_residual_norm_fwd(int64_t rows, int64_t cols, int32_t axis, float eps, double p, const uint64_t* state, uint32_t site,
+                           const float* h, const float* x, const float* w, const float* b, float* r, float* y, float* stats,
+                           void* stream);
+int  znn_residual_norm_bwd(int64_t rows, int64_t cols, int32_t axis, double p, const uint64_t* state, uint32_t site,
+                           const float* gy, const float* gr, const float* r, const float* w, const float* stats, float* gx,
+                           float* gh, float* gw, float* gb, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Layer-wise choice between the direct and the FFT method (Section 4): times
  * forward + backward + kernel gradient in both methods on the given shape
  * (2 warm-up rounds, 5 timed), stores the faster one in a process-wide cache

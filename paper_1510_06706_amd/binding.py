@@ -36,6 +36,8 @@ EXPORTS = [
     "znn_plan_set_spectra_layout", "znn_plan_spectra_layout", "znn_plan_tiles", "znn_conv3d_fwd_static",
     "znn_program_create", "znn_program_destroy", "znn_program_scratch_bytes", "znn_program_run",
     "znn_plan_set_round_memory",
+    "znn_random_advance", "znn_dropout", "znn_layernorm_workspace_bytes", "znn_layernorm_fwd", "znn_layernorm_bwd",
+    "znn_residual_norm_fwd", "znn_residual_norm_bwd",
 ]
 STATIC_SCRATCH_BYTES = 32 * 1024 * 1024
 SPECTRA_LAYOUTS = {"auto": 0, "full": 1, "folded": 2}
@@ -132,6 +134,14 @@ def lib():
         L.znn_program_destroy.restype = None
         L.znn_program_scratch_bytes.argtypes = [vp, ctypes.POINTER(sz)]
         L.znn_program_run.argtypes = [vp, ctypes.POINTER(vp), vp, sz, ctypes.c_float, ctypes.POINTER(vp)]
+        u32, f32, f64 = ctypes.c_uint32, ctypes.c_float, ctypes.c_double
+        L.znn_random_advance.argtypes = [vp, vp]
+        L.znn_dropout.argtypes = [i64, i64, f64, vp, u32, vp, vp, vp]
+        L.znn_layernorm_workspace_bytes.argtypes = [i64, i64, i32, ctypes.POINTER(sz)]
+        L.znn_layernorm_fwd.argtypes = [i64, i64, i32, f32] + [vp] * 6
+        L.znn_layernorm_bwd.argtypes = [i64, i64, i32] + [vp] * 8 + [sz, vp]
+        L.znn_residual_norm_fwd.argtypes = [i64, i64, i32, f32, f64, vp, u32] + [vp] * 8
+        L.znn_residual_norm_bwd.argtypes = [i64, i64, i32, f64, vp, u32] + [vp] * 10 + [sz, vp]
         for name in EXPORTS:
             if name not in ("znn_last_error", "znn_plan_destroy", "znn_program_destroy"):
                 getattr(L, name).restype = ctypes.c_int
@@ -456,6 +466,134 @@ def sgd_update(p, g, eta, stream=None):
     _check(lib().znn_sgd_update(p.numel(), float(eta), _ptr(g, torch.float32), _ptr(p, torch.float32),
                                 _stream_ptr(stream)))
     return p
+
+
+# ---------------------------------------------------------------- dropout, layer norm, residual join
+# Arrays are tensors [rows, ...] with all dimensions behind the first as their columns: images [map][z][y][x] with axis 0
+# (every voxel over the maps), rows of features with axis 1.
+def random_state(seed, device="cuda:0"):
+    """{seed, round} on the device: what dropout goes by.  ``random_advance`` behind a round makes the next one drop others."""
+    seed = int(seed) & 0xFFFFFFFFFFFFFFFF
+    return torch.tensor([seed - (1 << 64) if seed >> 63 else seed, 0], dtype=torch.int64, device=device)
+
+
+def random_advance(state, stream=None):
+    _check(lib().znn_random_advance(_state_ptr(state), _stream_ptr(stream)))
+    return state
+
+
+def _state_ptr(state):
+    if state is not None and state.numel() != 2:
+        raise ValueError("a random state holds two numbers")
+    return _ptr(state, torch.int64)
+
+
+def _extents(t):
+    if t.dim() < 1 or t.shape[0] < 1:
+        raise ValueError("expected an array [rows, ...], got %s" % (tuple(t.shape),))
+    return t.shape[0], t.numel() // t.shape[0]
+
+
+def _like(t, *others):
+    for o in others:
+        if o is not None and o.shape != t.shape:
+            raise ValueError("expected shape %s, got %s" % (tuple(t.shape), tuple(o.shape)))
+
+
+def _features(rows, cols, axis, *params):
+    """Positions of a norm, whose parameters are checked."""
+    if axis not in (0, 1):
+        raise ValueError("axis must be 0 or 1, got %r" % (axis,))
+    n, positions = (cols, rows) if axis else (rows, cols)
+    for p in params:
+        if p.numel() != n:
+            raise ValueError("expected %d parameters, got %d" % (n, p.numel()))
+    return positions
+
+
+def _empty(stream, device, *shapes):
+    """Tensors that belong to the stream that works on them."""
+    if stream is None:
+        return [torch.empty(s, dtype=torch.float32, device=device) for s in shapes]
+    with torch.cuda.stream(stream):
+        return [torch.empty(s, dtype=torch.float32, device=device) for s in shapes]
+
+
+def dropout(x, p, state=None, site=0, stream=None):
+    """x / (1 - p) where an element is kept, 0 elsewhere; on a gradient, with the same state and site, the Jacobian."""
+    rows, cols = _extents(x)
+    y, = _empty(stream, x.device, x.shape)
+    _check(lib().znn_dropout(rows, cols, p, _state_ptr(state), site, _ptr(x, torch.float32), _ptr(y), _stream_ptr(stream)))
+    return y
+
+
+def layernorm_fwd(x, w, b, eps=1e-5, axis=0, stats=True, stream=None):
+    """(y, stats): stats, for ``layernorm_bwd``, holds mean and 1 / deviation of every position (None if not asked for)."""
+    rows, cols = _extents(x)
+    positions = _features(rows, cols, axis, w, b)
+    y, *kept = _empty(stream, x.device, x.shape, *([(2, positions)] if stats else []))
+    kept = kept[0] if stats else None
+    _check(lib().znn_layernorm_fwd(rows, cols, axis, eps, _ptr(x, torch.float32), _ptr(w, torch.float32), _ptr(b, torch.float32),
+                                   _ptr(y), _ptr(kept), _stream_ptr(stream)))
+    return y, kept
+
+
+def layernorm_workspace_bytes(rows, cols, axis):
+    b = ctypes.c_size_t(0)
+    _check(lib().znn_layernorm_workspace_bytes(rows, cols, axis, ctypes.byref(b)))
+    return b.value
+
+
+def _norm_workspace(rows, cols, axis, stream, device):
+    need = layernorm_workspace_bytes(rows, cols, axis)
+    if not need:
+        return None, None, 0
+    ws, = _empty(stream, device, (need + 256) // 4)
+    return ws, (ws.data_ptr() + 255) & ~255, need
+
+
+def layernorm_bwd(gy, x, w, stats, axis=0, stream=None):
+    """(gx, gw, gb) from the input and the statistics of the forward pass."""
+    rows, cols = _extents(x)
+    _like(x, gy)
+    positions = _features(rows, cols, axis, w)
+    if stats.numel() != 2 * positions:
+        raise ValueError("expected statistics of %d positions, got %s" % (positions, tuple(stats.shape)))
+    gx, gw, gb = _empty(stream, x.device, x.shape, w.shape, w.shape)
+    ws, at, need = _norm_workspace(rows, cols, axis, stream, x.device)
+    _check(lib().znn_layernorm_bwd(rows, cols, axis, _ptr(gy, torch.float32), _ptr(x, torch.float32), _ptr(w, torch.float32),
+                                   _ptr(stats, torch.float32), _ptr(gx), _ptr(gw), _ptr(gb), at, need, _stream_ptr(stream)))
+    return gx, gw, gb
+
+
+def residual_norm_fwd(h, x, w, b, p=0.0, state=None, site=0, eps=1e-5, axis=0, stats=True, stream=None):
+    """(r, y, stats) with r = x + dropout(h), y = layernorm(r): the end of a residual branch in one pass."""
+    rows, cols = _extents(x)
+    _like(x, h)
+    positions = _features(rows, cols, axis, w, b)
+    r, y, *kept = _empty(stream, x.device, x.shape, x.shape, *([(2, positions)] if stats else []))
+    kept = kept[0] if stats else None
+    _check(lib().znn_residual_norm_fwd(rows, cols, axis, eps, p, _state_ptr(state), site, _ptr(h, torch.float32),
+                                       _ptr(x, torch.float32), _ptr(w, torch.float32), _ptr(b, torch.float32), _ptr(r), _ptr(y),
+                                       _ptr(kept), _stream_ptr(stream)))
+    return r, y, kept
+
+
+def residual_norm_bwd(gy, gr, r, w, stats, p=0.0, state=None, site=0, axis=0, stream=None):
+    """(gx, gh, gw, gb): gradients of x, h and the parameters.  gr, the gradient that reaches r beside the norm, may be
+    None.  Where p is 0, gh is gx."""
+    rows, cols = _extents(r)
+    _like(r, gy, gr)
+    positions = _features(rows, cols, axis, w)
+    if stats.numel() != 2 * positions:
+        raise ValueError("expected statistics of %d positions, got %s" % (positions, tuple(stats.shape)))
+    gx, gw, gb, *gh = _empty(stream, r.device, r.shape, w.shape, w.shape, *([r.shape] if p != 0 else []))
+    gh = gh[0] if p != 0 else None
+    ws, at, need = _norm_workspace(rows, cols, axis, stream, r.device)
+    _check(lib().znn_residual_norm_bwd(rows, cols, axis, p, _state_ptr(state), site, _ptr(gy, torch.float32), _ptr(gr, torch.float32),
+                                       _ptr(r, torch.float32), _ptr(w, torch.float32), _ptr(stats, torch.float32), _ptr(gx), _ptr(gh),
+                                       _ptr(gw), _ptr(gb), at, need, _stream_ptr(stream)))
+    return gx, gx if gh is None else gh, gw, gb
 
 
 def autotune_workspace_bytes(desc: ConvDesc) -> int:
