@@ -310,7 +310,7 @@ int  znn_accumulate(int64_t count, const float* x, float* y, void* stream);
  *   gh may be NULL if p = 0, where it equals gx.
  *
  * The backward calls take a workspace of znn_layernorm_workspace_bytes (256-byte aligned; may be NULL if that is 0).
- * ZNN_EUNSUPPORTED: 2^32 rows or more, more than 2^34 columns, or more than 2^28 features.
+ * ZNN_EUNSUPPORTED: 2^32 rows or more, more than 2^34 columns, or more than 2^26 features.
  */
 int  znn_random_advance(uint64_t* state, void* stream);
 int  znn_dropout(int64_t rows, int64_t cols, double p, const uint64_t* state, uint32_t site, const float* x, float* y,

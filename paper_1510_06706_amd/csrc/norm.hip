@@ -8,6 +8,7 @@
 // (d = x - m0, m = m0 + mean(d), variance mean(d^2) - mean(d)^2), so neither a mean far from zero nor m0's rounding costs digits.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "random.h"
 #include "znn_internal.h"
@@ -93,6 +94,404 @@ __device__ __forceinline__ float2 group_sum(float a, float b, float2* red)
     return v;
 }
 
+// ---------------------------------------------------------------- columns held in registers
+// TX lanes side by side take VEC neighbouring columns each, TY of them one below the other the rows ty, ty + TY, ..., at most K of
+// them, so that an operand is read once.  Sums over a column: over the lanes of a wave, then over the waves by LDS.
+template <int VEC> struct Vec { float v[VEC]; };
+template <int VEC> __device__ __forceinline__ Vec<VEC> load_vec(const float* p, int count)
+{
+    Vec<VEC> r;
+    if constexpr (VEC == 4) {
+        const floatu4 v = load4(p, count);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.v[e] = v[e];
+    } else r.v[0] = count > 0 ? *p : 0.f;
+    return r;
+}
+template <int VEC> __device__ __forceinline__ void store_vec(float* p, int count, const Vec<VEC>& r)
+{
+    if constexpr (VEC == 4) store4(p, count, floatu4{r.v[0], r.v[1], r.v[2], r.v[3]});
+    else if (count > 0) *p = r.v[0];
+}
+// columns c .. c + VEC - 1 of row m; c divisible by VEC
+template <int VEC> __device__ __forceinline__ void drop_vec(const DropKey& K, long c, long m, Vec<VEC>& r)
+{
+    const Words u = drop_words(K, (unsigned)(c >> 2), (unsigned)m);
+    if constexpr (VEC == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.v[e] = dropped(K, u.w[e], r.v[e]);
+    } else {
+        const int e = (int)(c & 3);
+        r.v[0] = dropped(K, e == 0 ? u.w[0] : e == 1 ? u.w[1] : e == 2 ? u.w[2] : u.w[3], r.v[0]);
+    }
+}
+
+// Sums of N values over ty, for all threads.  `red` must not be that of the call before: a thread may still read it.
+template <int TX, int TY, int N> __device__ __forceinline__ void sum_over_ty(float (&v)[N], float (*red)[TX][N])
+{
+    constexpr int WAVES = TX * TY / 64;
+#pragma unroll
+    for (int s = TX; s < 64; s <<= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], s);
+    if constexpr (WAVES > 1) {
+        const int tx = threadIdx.x % TX, wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) < TX)
+#pragma unroll
+            for (int i = 0; i < N; ++i) red[wave][tx][i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = red[0][tx][i];
+#pragma unroll
+        for (int q = 1; q < WAVES; ++q)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += red[q][tx][i];
+    }
+}
+
+template <int MODE, int VEC, int TX, int TY, int K>
+__global__ void __launch_bounds__(TX * TY) k_norm_cols(NormFwd A, long tiles)
+{
+    constexpr int WAVES = TX * TY / 64;
+    __shared__ float red[WAVES][TX][VEC], red2[WAVES][TX][2 * VEC];
+    DropKey D = {};
+    if (MODE == JOIN_DROP) D = drop_key(A.drop);
+    const int tx = threadIdx.x % TX, ty = threadIdx.x / TX, rows = (int)A.rows;
+    const float inv = 1.0f / (float)rows;
+    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const long c = (tile * TX + tx) * VEC;
+        auto body = [&](auto whole) {
+            const int count = whole.value ? VEC : (int)max(0L, min((long)VEC, A.cols - c));
+            Vec<VEC> v[K];
+            float sum[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[e] = 0.f;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int m = ty + TY * k;
+                if (TY * k < rows) v[k] = load_vec<VEC>(A.x + (long)min(m, rows - 1) * A.cols + c, count);
+            }
+            if (MODE != PLAIN) {
+                Vec<VEC> h[K];
+#pragma unroll
+                for (int k = 0; k < K; ++k)
+                    if (TY * k < rows) h[k] = load_vec<VEC>(A.h + (long)min(ty + TY * k, rows - 1) * A.cols + c, count);
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const int m = ty + TY * k;
+                    if (TY * k < rows) {
+                        if (MODE == JOIN_DROP) drop_vec<VEC>(D, c, m, h[k]);
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) v[k].v[e] = joined(v[k].v[e], h[k].v[e]);
+                        if (m < rows) store_vec<VEC>(A.r + (long)m * A.cols + c, count, v[k]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (TY * k < rows && ty + TY * k < rows)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[e] += v[k].v[e];
+            sum_over_ty<TX, TY, VEC>(sum, red);
+            float d[2 * VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) { sum[e] *= inv; d[e] = d[VEC + e] = 0.f; }
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (TY * k < rows && ty + TY * k < rows)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        v[k].v[e] -= sum[e];
+                        d[e] += v[k].v[e];
+                        d[VEC + e] += v[k].v[e] * v[k].v[e];
+                    }
+            sum_over_ty<TX, TY, 2 * VEC>(d, red2);
+            float rstd[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) { d[e] *= inv; rstd[e] = inverse_deviation(d[VEC + e] * inv, d[e], A.eps); }
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int m = ty + TY * k;
+                if (TY * k < rows && m < rows) {
+                    const float w = A.w[m], b = A.b[m];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) v[k].v[e] = (v[k].v[e] - d[e]) * rstd[e] * w + b;
+                    store_vec<VEC>(A.y + (long)m * A.cols + c, count, v[k]);
+                }
+            }
+            if (A.stats && ty == 0) {
+                Vec<VEC> m, s;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) { m.v[e] = sum[e] + d[e]; s.v[e] = rstd[e]; }
+                store_vec<VEC>(A.stats + c, count, m);
+                store_vec<VEC>(A.stats + A.cols + c, count, s);
+            }
+        };
+        if ((tile + 1) * TX * VEC <= A.cols) body(std::integral_constant<bool, true>{});      // uniform
+        else body(std::integral_constant<bool, false>{});
+    }
+}
+
+// A workgroup takes every gridDim.x-th tile and adds up what its columns give to the parameters' gradients in registers.
+template <int MODE, int VEC, int TX, int TY, int K>
+__global__ void __launch_bounds__(TX * TY) k_norm_cols_bwd(NormBwd A, long tiles, float* __restrict__ parts)
+{
+    constexpr int WAVES = TX * TY / 64;
+    __shared__ float red[2][WAVES][TX][2 * VEC];
+    DropKey D = {};
+    if (MODE == JOIN_DROP) D = drop_key(A.drop);
+    const int tx = threadIdx.x % TX, ty = threadIdx.x / TX, rows = (int)A.rows;
+    const float inv = 1.0f / (float)rows;
+    float gw[K], gb[K], w[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        gw[k] = gb[k] = 0.f;
+        w[k] = ty + TY * k < rows ? A.w[ty + TY * k] : 0.f;
+    }
+    int turn = 0;
+    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1) {
+        const long c = (tile * TX + tx) * VEC;
+        auto body = [&](auto whole) {
+            const int count = whole.value ? VEC : (int)max(0L, min((long)VEC, A.cols - c));
+            Vec<VEC> x[K], g[K];
+            const Vec<VEC> mean = load_vec<VEC>(A.stats + c, count), rstd = load_vec<VEC>(A.stats + A.cols + c, count);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (TY * k < rows) {
+                    const long t = (long)min(ty + TY * k, rows - 1) * A.cols + c;
+                    x[k] = load_vec<VEC>(A.x + t, count);
+                    g[k] = load_vec<VEC>(A.gy + t, count);
+                }
+            float s[2 * VEC];
+#pragma unroll
+            for (int e = 0; e < 2 * VEC; ++e) s[e] = 0.f;
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (TY * k < rows && ty + TY * k < rows)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const float h = (x[k].v[e] - mean.v[e]) * rstd.v[e], gy = g[k].v[e], a = gy * w[k];     // gy = 0 behind the columns
+                        x[k].v[e] = h;
+                        gw[k] += gy * h;
+                        gb[k] += gy;
+                        g[k].v[e] = a;
+                        s[e] += a;
+                        s[VEC + e] += a * h;
+                    }
+            sum_over_ty<TX, TY, 2 * VEC>(s, red[turn]);
+#pragma unroll
+            for (int e = 0; e < 2 * VEC; ++e) s[e] *= inv;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int m = ty + TY * k;
+                if (TY * k < rows && m < rows) {
+                    const long t = (long)m * A.cols + c;
+                    Vec<VEC> v;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) v.v[e] = rstd.v[e] * (g[k].v[e] - s[e] - x[k].v[e] * s[VEC + e]);
+                    if (MODE != PLAIN && A.gr) {
+                        const Vec<VEC> r = load_vec<VEC>(A.gr + t, count);
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) v.v[e] += r.v[e];
+                    }
+                    store_vec<VEC>(A.gx + t, count, v);
+                    if (MODE == JOIN_DROP) drop_vec<VEC>(D, c, m, v);
+                    if (MODE != PLAIN && A.gh) store_vec<VEC>(A.gh + t, count, v);
+                }
+            }
+        };
+        if ((tile + 1) * TX * VEC <= A.cols) body(std::integral_constant<bool, true>{});      // uniform
+        else body(std::integral_constant<bool, false>{});
+    }
+    float* part = parts + (long)blockIdx.x * 2 * rows;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (TY * k < rows) {
+            float a = gw[k], b = gb[k];
+#pragma unroll
+            for (int i = 1; i < TX; i <<= 1) { a += __shfl_xor(a, i); b += __shfl_xor(b, i); }
+            const int m = ty + TY * k;
+            if (tx == 0 && m < rows) { part[m] = a; part[rows + m] = b; }
+        }
+}
+
+// ---------------------------------------------------------------- rows held in registers
+// L lanes take a row, NV times four neighbouring columns each: lanes of a wave (the sums stay in it) or a whole workgroup.
+template <int L> struct RowGroup { static constexpr int threads = L > 256 ? L : 256, rows = threads / L, waves = L > 64 ? L / 64 : 1; };
+
+template <int L> __device__ __forceinline__ float2 row_sum(float a, float b, float2* red)
+{
+#pragma unroll
+    for (int s = 1; s < (L < 64 ? L : 64); s <<= 1) { a += __shfl_xor(a, s); b += __shfl_xor(b, s); }
+    if constexpr (L > 64) {
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = make_float2(a, b);
+        __syncthreads();
+        float2 v = red[0];
+#pragma unroll
+        for (int i = 1; i < L / 64; ++i) { v.x += red[i].x; v.y += red[i].y; }
+        return v;
+    }
+    return make_float2(a, b);
+}
+// columns 4 (lane + L j) .. + 3 of a row; only the last quads of a row may lie behind it
+template <int L> __device__ __forceinline__ int quad_count(int j, int lane, int cols)
+{
+    return 4 * L * (j + 1) <= cols ? 4 : max(0, min(4, cols - 4 * (lane + L * j)));
+}
+
+template <int MODE, int L, int NV>
+__global__ void __launch_bounds__(RowGroup<L>::threads) k_norm_rows(NormFwd A)
+{
+    __shared__ float2 red[2][RowGroup<L>::waves];
+    DropKey D = {};
+    if (MODE == JOIN_DROP) D = drop_key(A.drop);
+    const int lane = threadIdx.x % L, cols = (int)A.cols;
+    const float inv = 1.0f / (float)cols;
+    floatu4 w[NV], b[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int count = quad_count<L>(j, lane, cols);
+        w[j] = load4(A.w + 4 * (lane + L * j), count);
+        b[j] = load4(A.b + 4 * (lane + L * j), count);
+    }
+    for (long row0 = (long)blockIdx.x * RowGroup<L>::rows; row0 < A.rows; row0 += (long)gridDim.x * RowGroup<L>::rows) {
+        const long row = row0 + threadIdx.x / L, base = min(row, A.rows - 1) * cols;
+        const bool live = row < A.rows;
+        floatu4 v[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) v[j] = load4(A.x + base + 4 * (lane + L * j), quad_count<L>(j, lane, cols));
+        if (MODE != PLAIN) {
+            floatu4 h[NV];
+#pragma unroll
+            for (int j = 0; j < NV; ++j) h[j] = load4(A.h + base + 4 * (lane + L * j), quad_count<L>(j, lane, cols));
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (MODE == JOIN_DROP) h[j] = dropped4(D, (unsigned)(lane + L * j), (unsigned)row, h[j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[j][e] = joined(v[j][e], h[j][e]);
+                if (live) store4(A.r + base + 4 * (lane + L * j), quad_count<L>(j, lane, cols), v[j]);
+            }
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) sum += (v[j][0] + v[j][1]) + (v[j][2] + v[j][3]);
+        const float m0 = row_sum<L>(sum, 0.f, red[0]).x * inv;
+        float d1 = 0.f, d2 = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float d = e < quad_count<L>(j, lane, cols) ? v[j][e] - m0 : 0.f;
+                v[j][e] = d;
+                d1 += d;
+                d2 += d * d;
+            }
+        const float2 s = row_sum<L>(d1, d2, red[1]);
+        const float delta = s.x * inv, rstd = inverse_deviation(s.y * inv, delta, A.eps);
+        if (live) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[j][e] = (v[j][e] - delta) * rstd * w[j][e] + b[j][e];
+                store4(A.y + base + 4 * (lane + L * j), quad_count<L>(j, lane, cols), v[j]);
+            }
+            if (A.stats && lane == 0) { A.stats[row] = m0 + delta; A.stats[A.rows + row] = rstd; }
+        }
+    }
+}
+
+template <int MODE, int L, int NV>
+__global__ void __launch_bounds__(RowGroup<L>::threads) k_norm_rows_bwd(NormBwd A, float* __restrict__ parts)
+{
+    constexpr int ROWS = RowGroup<L>::rows;
+    __shared__ float2 red[2][RowGroup<L>::waves];
+    __shared__ float sums[ROWS > 1 ? (ROWS - 1) * L * NV * 8 : 1];
+    DropKey D = {};
+    if (MODE == JOIN_DROP) D = drop_key(A.drop);
+    const int lane = threadIdx.x % L, group = threadIdx.x / L, cols = (int)A.cols;
+    const float inv = 1.0f / (float)cols;
+    floatu4 w[NV], gw[NV], gb[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        w[j] = load4(A.w + 4 * (lane + L * j), quad_count<L>(j, lane, cols));
+        gw[j] = gb[j] = floatu4{0.f, 0.f, 0.f, 0.f};
+    }
+    int turn = 0;
+    for (long row0 = (long)blockIdx.x * ROWS; row0 < A.rows; row0 += (long)gridDim.x * ROWS, turn ^= 1) {
+        const bool live = row0 + group < A.rows;
+        const long row = min(row0 + group, A.rows - 1), base = row * cols;
+        const float mean = A.stats[row], rstd = A.stats[A.rows + row];
+        floatu4 x[NV], g[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int count = quad_count<L>(j, lane, cols);
+            x[j] = load4(A.x + base + 4 * (lane + L * j), count);
+            g[j] = load4(A.gy + base + 4 * (lane + L * j), live ? count : 0);       // gy = 0 behind the row and behind the rows
+        }
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool in = live && e < quad_count<L>(j, lane, cols);
+                const float h = in ? (x[j][e] - mean) * rstd : 0.f, a = g[j][e] * w[j][e];
+                x[j][e] = h;
+                gw[j][e] += g[j][e] * h;
+                gb[j][e] += g[j][e];
+                g[j][e] = a;
+                s1 += a;
+                s2 += a * h;
+            }
+        const float2 s = row_sum<L>(s1, s2, red[turn]);
+        const float m1 = s.x * inv, m2 = s.y * inv;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int count = live ? quad_count<L>(j, lane, cols) : 0;
+            const long t = base + 4 * (lane + L * j);
+            floatu4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = rstd * (g[j][e] - m1 - x[j][e] * m2);
+            if (MODE != PLAIN && A.gr) {
+                const floatu4 r = load4(A.gr + t, count);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += r[e];
+            }
+            store4(A.gx + t, count, v);
+            if (MODE == JOIN_DROP) v = dropped4(D, (unsigned)(lane + L * j), (unsigned)row, v);
+            if (MODE != PLAIN && A.gh) store4(A.gh + t, count, v);
+        }
+    }
+    // the sums of the workgroup's rows side by side, the first group's last
+    if constexpr (ROWS > 1) {
+        if (group > 0)
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sums[(((group - 1) * NV + j) * 8 + e) * L + lane] = gw[j][e];
+                    sums[(((group - 1) * NV + j) * 8 + 4 + e) * L + lane] = gb[j][e];
+                }
+        __syncthreads();
+        if (group > 0) return;
+        for (int q = 0; q < ROWS - 1; ++q)
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    gw[j][e] += sums[((q * NV + j) * 8 + e) * L + lane];
+                    gb[j][e] += sums[((q * NV + j) * 8 + 4 + e) * L + lane];
+                }
+    }
+    float* part = parts + (long)blockIdx.x * 2 * cols;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int count = quad_count<L>(j, lane, cols);
+        store4(part + 4 * (lane + L * j), count, gw[j]);
+        store4(part + cols + 4 * (lane + L * j), count, gb[j]);
+    }
+}
+
+// ---------------------------------------------------------------- positions of any size
 // Rows of any length: a workgroup walks a row three times.
 template <int MODE>
 __global__ void __launch_bounds__(1024) k_norm_rows_any(NormFwd A)
@@ -313,13 +712,22 @@ __global__ void __launch_bounds__(256) k_norm_params_cols(NormParams A)
     }
 }
 
-__global__ void __launch_bounds__(256)
+// 64 of the 2 x features values by sixteen slices of the shares
+__global__ void __launch_bounds__(1024)
 k_norm_params(long features, int shares, const float* __restrict__ parts, float* __restrict__ gw, float* __restrict__ gb)
 {
-    const long t = (long)blockIdx.x * 256 + threadIdx.x;
-    if (t >= 2 * features) return;
+    __shared__ float red[16][64];
+    const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+    const long t = (long)blockIdx.x * 64 + tx;
     float v = 0.f;
-    for (int s = 0; s < shares; ++s) v += parts[(long)s * 2 * features + t];
+    if (t < 2 * features)
+#pragma unroll 8
+        for (int s = ty; s < shares; s += 16) v += parts[(long)s * 2 * features + t];
+    red[ty][tx] = v;
+    __syncthreads();
+    if (ty > 0 || t >= 2 * features) return;
+#pragma unroll
+    for (int q = 1; q < 16; ++q) v += red[q][tx];
     if (t < features) gw[t] = v; else gb[t - features] = v;
 }
 
@@ -333,9 +741,46 @@ Shares param_shares(long rows, long cols, int axis)
     return Shares{(int)((positions + span - 1) / span), span};
 }
 
+// How an array is taken, by its extents alone: kernels that hold a position in registers (`held`) where one fits.
+struct Shape { bool held; int vec, tx, ty; long tiles; int lanes, quads; };
+Shape norm_shape(long rows, long cols, int axis)
+{
+    Shape S = {};
+    if (axis) {
+        const int lanes[] = {4, 16, 32, 64, 64, 64, 256, 256, 1024, 1024}, quads[] = {1, 1, 1, 1, 2, 4, 2, 4, 2, 4};
+        for (int i = 0; i < 10 && !S.held; ++i)
+            if (cols <= 4L * lanes[i] * quads[i]) { S.held = true; S.lanes = lanes[i]; S.quads = quads[i]; }
+        return S;
+    }
+    if (rows > 512) return S;
+    S.held = true;
+    if (rows <= 32) { S.tx = 64; S.ty = 4; }
+    else if (rows <= 64) { S.tx = 32; S.ty = 8; }
+    else if (rows <= 128) { S.tx = 32; S.ty = 16; }
+    else if (rows <= 256) { S.tx = 32; S.ty = 32; }
+    else { S.tx = 16; S.ty = 64; }
+    S.vec = cols >= 4L * S.tx * 512 ? 4 : 1;
+    S.tiles = (cols + S.tx * S.vec - 1) / (S.tx * S.vec);
+    return S;
+}
+int row_groups(const Shape& S) { return S.lanes > 256 ? 1 : 256 / S.lanes; }
+
+// Workgroups of a backward pass, each of which leaves a share of the parameters' gradients
+long bwd_groups(const Shape& S, long rows)
+{
+    if (S.lanes) return std::min((rows + row_groups(S) - 1) / row_groups(S), S.lanes > 256 ? 256L : 512L);
+    return std::min(S.tiles, 512L);
+}
+
+int norm_share_count(long rows, long cols, int axis)
+{
+    const Shape S = norm_shape(rows, cols, axis);
+    return S.held ? (int)bwd_groups(S, rows) : param_shares(rows, cols, axis).count;
+}
+
 size_t norm_workspace(long rows, long cols, int axis)
 {
-    return sizeof(float) * 2 * param_shares(rows, cols, axis).count * (axis ? cols : rows);
+    return sizeof(float) * 2 * norm_share_count(rows, cols, axis) * (axis ? cols : rows);
 }
 
 unsigned groups_of(long work, long each, long most) { return (unsigned)std::min((work + each - 1) / each, most); }
@@ -354,15 +799,67 @@ int check_axis(int64_t rows, int64_t cols, int32_t axis)
 {
     if (axis != 0 && axis != 1) return fail(ZNN_EINVAL, "axis must be 0 (over the rows) or 1 (over the columns)");
     int rc = check_array(rows, cols);
-    if (rc == ZNN_OK && (axis ? cols : rows) > 268435456LL)
+    if (rc == ZNN_OK && (axis ? cols : rows) > 67108864LL)
         rc = fail(ZNN_EUNSUPPORTED, "a norm over %lld elements is too large", (long long)(axis ? cols : rows));
     return rc;
+}
+
+// Calls f with the constants of a shape.
+template <int... N> struct Numbers {};
+template <class F> void with_cols(const Shape& S, F f)
+{
+    auto vec = [&](auto v) {
+        if (S.ty == 4) f(v, Numbers<64, 4>{});
+        else if (S.ty == 8) f(v, Numbers<32, 8>{});
+        else if (S.ty == 16) f(v, Numbers<32, 16>{});
+        else if (S.ty == 32) f(v, Numbers<32, 32>{});
+        else f(v, Numbers<16, 64>{});
+    };
+    if (S.vec == 4) vec(std::integral_constant<int, 4>{}); else vec(std::integral_constant<int, 1>{});
+}
+template <class F> void with_rows(const Shape& S, F f)
+{
+    switch (S.lanes * 8 + S.quads) {
+        case 4 * 8 + 1: return f(Numbers<4, 1>{});
+        case 16 * 8 + 1: return f(Numbers<16, 1>{});
+        case 32 * 8 + 1: return f(Numbers<32, 1>{});
+        case 64 * 8 + 1: return f(Numbers<64, 1>{});
+        case 64 * 8 + 2: return f(Numbers<64, 2>{});
+        case 64 * 8 + 4: return f(Numbers<64, 4>{});
+        case 256 * 8 + 2: return f(Numbers<256, 2>{});
+        case 256 * 8 + 4: return f(Numbers<256, 4>{});
+        case 1024 * 8 + 2: return f(Numbers<1024, 2>{});
+        default: return f(Numbers<1024, 4>{});
+    }
+}
+
+template <int MODE, int VEC, int TX, int TY>
+void cols_fwd(const NormFwd& A, const Shape& S, std::integral_constant<int, VEC>, Numbers<TX, TY>, hipStream_t s)
+{
+    ZNN_LAUNCH("layer norm forward", s, (k_norm_cols<MODE, VEC, TX, TY, 8>), dim3(groups_of(S.tiles, 1, 1L << 20)), dim3(TX * TY), 0, A, S.tiles);
+}
+template <int MODE, int VEC, int TX, int TY>
+void cols_bwd(const NormBwd& A, const Shape& S, std::integral_constant<int, VEC>, Numbers<TX, TY>, float* parts, hipStream_t s)
+{
+    ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd<MODE, VEC, TX, TY, 8>), dim3((unsigned)bwd_groups(S, A.rows)), dim3(TX * TY), 0, A,
+               S.tiles, parts);
+}
+template <int MODE, int L, int NV> void rows_fwd(const NormFwd& A, Numbers<L, NV>, hipStream_t s)
+{
+    ZNN_LAUNCH("layer norm forward", s, (k_norm_rows<MODE, L, NV>), dim3(groups_of(A.rows, RowGroup<L>::rows, 4096)), dim3(RowGroup<L>::threads), 0, A);
+}
+template <int MODE, int L, int NV> void rows_bwd(const NormBwd& A, const Shape& S, Numbers<L, NV>, float* parts, hipStream_t s)
+{
+    ZNN_LAUNCH("layer norm backward", s, (k_norm_rows_bwd<MODE, L, NV>), dim3((unsigned)bwd_groups(S, A.rows)), dim3(RowGroup<L>::threads), 0, A, parts);
 }
 
 template <int MODE>
 int norm_fwd(const NormFwd& A, int axis, hipStream_t s)
 {
-    if (axis) ZNN_LAUNCH("layer norm forward", s, k_norm_rows_any<MODE>, dim3(groups_of(A.rows, 1, 1L << 20)), dim3(1024), 0, A);
+    const Shape S = norm_shape(A.rows, A.cols, axis);
+    if (S.held && axis) with_rows(S, [&](auto n) { rows_fwd<MODE>(A, n, s); });
+    else if (S.held) with_cols(S, [&](auto v, auto n) { cols_fwd<MODE>(A, S, v, n, s); });
+    else if (axis) ZNN_LAUNCH("layer norm forward", s, k_norm_rows_any<MODE>, dim3(groups_of(A.rows, 1, 1L << 20)), dim3(1024), 0, A);
     else ZNN_LAUNCH("layer norm forward", s, k_norm_cols_any<MODE>, dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
     return check_launch("layer norm forward");
 }
@@ -370,18 +867,23 @@ int norm_fwd(const NormFwd& A, int axis, hipStream_t s)
 template <int MODE>
 int norm_bwd(const NormBwd& A, int axis, float* gw, float* gb, void* ws, hipStream_t s)
 {
-    const Shares S = param_shares(A.rows, A.cols, axis);
+    const Shape H = norm_shape(A.rows, A.cols, axis);
     const long features = axis ? A.cols : A.rows;
-    const NormParams P = {A.rows, A.cols, A.gy, A.x, A.stats, (float*)ws, S.count, S.span};
-    if (axis) {
-        ZNN_LAUNCH("layer norm backward", s, k_norm_rows_bwd_any<MODE>, dim3(groups_of(A.rows, 1, 1L << 20)), dim3(1024), 0, A);
-        ZNN_LAUNCH("layer norm parameters", s, k_norm_params_rows, dim3((unsigned)((A.cols + 63) / 64), (unsigned)S.count), dim3(256), 0, P);
-    } else {
-        ZNN_LAUNCH("layer norm backward", s, k_norm_cols_bwd_any<MODE>, dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
-        ZNN_LAUNCH("layer norm parameters", s, k_norm_params_cols, dim3(groups_of(A.rows, 1, 1L << 20), (unsigned)S.count), dim3(256), 0, P);
+    if (H.held && axis) with_rows(H, [&](auto n) { rows_bwd<MODE>(A, H, n, (float*)ws, s); });
+    else if (H.held) with_cols(H, [&](auto v, auto n) { cols_bwd<MODE>(A, H, v, n, (float*)ws, s); });
+    else {
+        const Shares S = param_shares(A.rows, A.cols, axis);
+        const NormParams P = {A.rows, A.cols, A.gy, A.x, A.stats, (float*)ws, S.count, S.span};
+        if (axis) {
+            ZNN_LAUNCH("layer norm backward", s, k_norm_rows_bwd_any<MODE>, dim3(groups_of(A.rows, 1, 1L << 20)), dim3(1024), 0, A);
+            ZNN_LAUNCH("layer norm parameters", s, k_norm_params_rows, dim3((unsigned)((A.cols + 63) / 64), (unsigned)S.count), dim3(256), 0, P);
+        } else {
+            ZNN_LAUNCH("layer norm backward", s, k_norm_cols_bwd_any<MODE>, dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
+            ZNN_LAUNCH("layer norm parameters", s, k_norm_params_cols, dim3(groups_of(A.rows, 1, 1L << 20), (unsigned)S.count), dim3(256), 0, P);
+        }
     }
-    ZNN_LAUNCH("layer norm parameters", s, k_norm_params, dim3((unsigned)((2 * features + 255) / 256)), dim3(256), 0, features, S.count,
-               (const float*)ws, gw, gb);
+    ZNN_LAUNCH("layer norm parameters", s, k_norm_params, dim3((unsigned)((2 * features + 63) / 64)), dim3(1024), 0, features,
+               norm_share_count(A.rows, A.cols, axis), (const float*)ws, gw, gb);
     return check_launch("layer norm backward");
 }
 
