@@ -8,6 +8,7 @@
 // (d = x - m0, m = m0 + mean(d), variance mean(d^2) - mean(d)^2), so neither a mean far from zero nor m0's rounding costs digits.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <type_traits>
 
 #include "random.h"
@@ -95,36 +96,87 @@ __device__ __forceinline__ float2 group_sum(float a, float b, float2* red)
 }
 
 // ---------------------------------------------------------------- columns held in registers
-// TX lanes side by side take VEC neighbouring columns each, TY of them one below the other the rows ty, ty + TY, ..., at most K of
-// them, so that an operand is read once.  Sums over a column: over the lanes of a wave, then over the waves by LDS.
-template <int VEC> struct Vec { float v[VEC]; };
-template <int VEC> __device__ __forceinline__ Vec<VEC> load_vec(const float* p, int count)
+// TX lanes side by side take four neighbouring columns each, TY of them one below the other the rows ty, ty + TY, ... (kRowsHeld of
+// them at most), so that an operand is read once.  Sums over a column: over the lanes of a wave, then over the waves by LDS.
+constexpr int kRowsHeld = 4;
+constexpr unsigned kBufferWord3 = 0x00020000u;      // raw 32-bit buffer elements
+typedef unsigned word4 __attribute__((ext_vector_type(4)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+
+// Stores of whole 128-byte lines (STREAM) leave the cache at once: it would write them back when the kernel ends, with nothing else left
+// to do: 120 x 262144 backward 90 -> 72 us, 120 x 32768 forward 8.7 -> 6.9.  Of parts of lines it would write each on its own: 120 x 262143
+// forward 44 -> 90.
+template <bool STREAM> __device__ __forceinline__ void store_buffer(__amdgpu_buffer_rsrc_t b, unsigned at, float4v v)
 {
-    Vec<VEC> r;
-    if constexpr (VEC == 4) {
-        const floatu4 v = load4(p, count);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r.v[e] = v[e];
-    } else r.v[0] = count > 0 ? *p : 0.f;
-    return r;
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(word4, v), b, (int)at, 0, STREAM ? 2 : 0);
 }
-template <int VEC> __device__ __forceinline__ void store_vec(float* p, int count, const Vec<VEC>& r)
+__device__ __forceinline__ float4v load_buffer(__amdgpu_buffer_rsrc_t b, unsigned at)
 {
-    if constexpr (VEC == 4) store4(p, count, floatu4{r.v[0], r.v[1], r.v[2], r.v[3]});
-    else if (count > 0) *p = r.v[0];
+    return __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(b, (int)at, 0, 0));
 }
-// columns c .. c + VEC - 1 of row m; c divisible by VEC
-template <int VEC> __device__ __forceinline__ void drop_vec(const DropKey& K, long c, long m, Vec<VEC>& r)
-{
-    const Words u = drop_words(K, (unsigned)(c >> 2), (unsigned)m);
-    if constexpr (VEC == 4) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r.v[e] = dropped(K, u.w[e], r.v[e]);
-    } else {
-        const int e = (int)(c & 3);
-        r.v[0] = dropped(K, e == 0 ? u.w[0] : e == 1 ? u.w[1] : e == 2 ? u.w[2] : u.w[3], r.v[0]);
+
+// Where a thread's elements lie.  Its row number k is row TY k + ty: a buffer that begins with row TY k, whose end cuts off what the
+// last rows are short of TY (loads give 0, stores go nowhere), and 32 bits of the thread's own, so that an operand costs no registers
+// for addresses (norm_shape keeps TY rows below 2^32 bytes).  At the right border the columns move left until four of them are there;
+// the first `skip` of them are then another thread's too, which computes and stores the same values.
+template <int TX, int TY> struct ColumnTile {
+    long cols, first;           // first: column at which the buffers begin
+    int rows, ty, skip;
+    unsigned along, at;         // columns from `first` on; bytes from a buffer's begin
+    bool border;                // uniform: some thread skips columns
+    __device__ __forceinline__ ColumnTile(long rows_, long cols_, long tile) : cols(cols_), first(tile * TX * 4), rows((int)rows_)
+    {
+        const int tx = threadIdx.x % TX * 4, last = (int)min(TX * 4L, cols - first) - 4;        // where the last thread may begin: -3 or more
+        ty = threadIdx.x / TX;
+        border = last < (TX - 1) * 4;
+        const int back = border && tile > 0 ? 4 : 0;        // so that the base lies left of every thread
+        skip = max(0, tx - last);
+        along = (unsigned)(tx - skip + back);
+        first -= back;
+        at = 4u * ((unsigned)ty * (unsigned)cols + along);
     }
-}
+    __device__ __forceinline__ bool any(int k) const { return TY * k < rows; }                                  // uniform
+    __device__ __forceinline__ bool has(int k) const { return TY * (k + 1) <= rows || TY * k + ty < rows; }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const float* p, int k) const
+    {
+        const unsigned bytes = TY * (k + 1) <= rows ? 0xffffffffu : 4u * ((unsigned)(rows - TY * k) * (unsigned)cols - (unsigned)first);
+        return __builtin_amdgcn_make_buffer_rsrc((void*)(p + ((long)TY * k * cols + first)), 0, (int)bytes, kBufferWord3);
+    }
+    __device__ __forceinline__ float4v load(const float* p, int k) const { return load_buffer(buffer(p, k), at); }
+    template <bool STREAM> __device__ __forceinline__ void store(float* p, int k, float4v v) const { store_buffer<STREAM>(buffer(p, k), at, v); }
+    // an array with one value per column
+    __device__ __forceinline__ float4v load_columns(const float* p) const
+    {
+        return load_buffer(__builtin_amdgcn_make_buffer_rsrc((void*)(p + first), 0, -1, kBufferWord3), 4u * along);
+    }
+    __device__ __forceinline__ void store_columns(float* p, float4v v) const
+    {
+        store_buffer<false>(__builtin_amdgcn_make_buffer_rsrc((void*)(p + first), 0, -1, kBufferWord3), 4u * along, v);
+    }
+    __device__ __forceinline__ float4v drop(const DropKey& K, int k, float4v v) const
+    {
+        const long c = first + along;
+        const unsigned m = TY * k + ty;
+        const Words u = drop_words(K, (unsigned)(c >> 2), m);
+        if (border) {           // columns of two quads
+            const Words n = drop_words(K, (unsigned)(c >> 2) + 1, m);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int q = e + (int)(c & 3);
+                v[e] = dropped(K, q == 0 ? u.w[0] : q == 1 ? u.w[1] : q == 2 ? u.w[2] : q == 3 ? u.w[3] : q == 4 ? n.w[0] : q == 5 ? n.w[1] : n.w[2], v[e]);
+            }
+        } else
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = dropped(K, u.w[e], v[e]);
+        return v;
+    }
+};
+
+// Tiles in the order of the workgroups, or (`apart`) an eighth of them to every XCD, so that rows that begin in the middle of a line find
+// its other part in the same cache: 36 x 105225 forward 9.8 -> 8.8 us, backward 17 -> 14; 200 x 30690 17 -> 14 and 26 -> 19.
+struct Tiles { long count; int apart; };
+__device__ __forceinline__ long tile_turns(Tiles T) { return T.apart ? (T.count + 7) / 8 * 8 : T.count; }
+__device__ __forceinline__ long tile_of(Tiles T, long turn) { return T.apart ? (turn & 7) * ((T.count + 7) / 8) + (turn >> 3) : turn; }
 
 // Sums of N values over ty, for all threads.  `red` must not be that of the call before: a thread may still read it.
 template <int TX, int TY, int N> __device__ __forceinline__ void sum_over_ty(float (&v)[N], float (*red)[TX][N])
@@ -149,95 +201,82 @@ template <int TX, int TY, int N> __device__ __forceinline__ void sum_over_ty(flo
     }
 }
 
-template <int MODE, int VEC, int TX, int TY, int K>
-__global__ void __launch_bounds__(TX * TY) k_norm_cols(NormFwd A, long tiles)
+template <int MODE, int TX, int TY, bool STREAM>
+__global__ void __launch_bounds__(TX * TY, 4) k_norm_cols(NormFwd A, Tiles tiles)
 {
-    constexpr int WAVES = TX * TY / 64;
-    __shared__ float red[WAVES][TX][VEC], red2[WAVES][TX][2 * VEC];
+    constexpr int WAVES = TX * TY / 64, K = kRowsHeld;
+    __shared__ float red[WAVES][TX][4], red2[WAVES][TX][8];
     DropKey D = {};
     if (MODE == JOIN_DROP) D = drop_key(A.drop);
-    const int tx = threadIdx.x % TX, ty = threadIdx.x / TX, rows = (int)A.rows;
-    const float inv = 1.0f / (float)rows;
-    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const long c = (tile * TX + tx) * VEC;
-        auto body = [&](auto whole) {
-            const int count = whole.value ? VEC : (int)max(0L, min((long)VEC, A.cols - c));
-            Vec<VEC> v[K];
-            float sum[VEC];
+    const float inv = 1.0f / (float)A.rows;
+    for (long turn = blockIdx.x; turn < tile_turns(tiles); turn += gridDim.x) {
+        const long tile = tile_of(tiles, turn);
+        if (tile >= tiles.count) continue;      // uniform
+        const ColumnTile<TX, TY> T(A.rows, A.cols, tile);
+        float4v v[K];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) sum[e] = 0.f;
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int m = ty + TY * k;
-                if (TY * k < rows) v[k] = load_vec<VEC>(A.x + (long)min(m, rows - 1) * A.cols + c, count);
-            }
-            if (MODE != PLAIN) {
-                Vec<VEC> h[K];
-#pragma unroll
-                for (int k = 0; k < K; ++k)
-                    if (TY * k < rows) h[k] = load_vec<VEC>(A.h + (long)min(ty + TY * k, rows - 1) * A.cols + c, count);
-#pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    const int m = ty + TY * k;
-                    if (TY * k < rows) {
-                        if (MODE == JOIN_DROP) drop_vec<VEC>(D, c, m, h[k]);
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) v[k].v[e] = joined(v[k].v[e], h[k].v[e]);
-                        if (m < rows) store_vec<VEC>(A.r + (long)m * A.cols + c, count, v[k]);
-                    }
-                }
-            }
+        for (int k = 0; k < K; ++k)
+            if (T.any(k)) v[k] = T.load(A.x, k);
+        if (MODE != PLAIN) {
+            float4v h[K];
 #pragma unroll
             for (int k = 0; k < K; ++k)
-                if (TY * k < rows && ty + TY * k < rows)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) sum[e] += v[k].v[e];
-            sum_over_ty<TX, TY, VEC>(sum, red);
-            float d[2 * VEC];
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) { sum[e] *= inv; d[e] = d[VEC + e] = 0.f; }
+                if (T.any(k)) h[k] = T.load(A.h, k);
 #pragma unroll
             for (int k = 0; k < K; ++k)
-                if (TY * k < rows && ty + TY * k < rows)
+                if (T.any(k)) {
+                    if (MODE == JOIN_DROP) h[k] = T.drop(D, k, h[k]);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        v[k].v[e] -= sum[e];
-                        d[e] += v[k].v[e];
-                        d[VEC + e] += v[k].v[e] * v[k].v[e];
-                    }
-            sum_over_ty<TX, TY, 2 * VEC>(d, red2);
-            float rstd[VEC];
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) { d[e] *= inv; rstd[e] = inverse_deviation(d[VEC + e] * inv, d[e], A.eps); }
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int m = ty + TY * k;
-                if (TY * k < rows && m < rows) {
-                    const float w = A.w[m], b = A.b[m];
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) v[k].v[e] = (v[k].v[e] - d[e]) * rstd[e] * w + b;
-                    store_vec<VEC>(A.y + (long)m * A.cols + c, count, v[k]);
+                    for (int e = 0; e < 4; ++e) v[k][e] = joined(v[k][e], h[k][e]);
+                    T.template store<STREAM>(A.r, k, v[k]);
                 }
-            }
-            if (A.stats && ty == 0) {
-                Vec<VEC> m, s;
+        }
+        float sum[4], d[8], rstd[4];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) { m.v[e] = sum[e] + d[e]; s.v[e] = rstd[e]; }
-                store_vec<VEC>(A.stats + c, count, m);
-                store_vec<VEC>(A.stats + A.cols + c, count, s);
+        for (int e = 0; e < 4; ++e) sum[e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (T.any(k))
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] += v[k][e];          // 0 where there is no row
+        sum_over_ty<TX, TY, 4>(sum, red);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { sum[e] *= inv; d[e] = d[4 + e] = 0.f; }
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (T.any(k))
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float a = T.has(k) ? v[k][e] - sum[e] : 0.f;
+                    v[k][e] = a;
+                    d[e] += a;
+                    d[4 + e] += a * a;
+                }
+        sum_over_ty<TX, TY, 8>(d, red2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { d[e] *= inv; rstd[e] = inverse_deviation(d[4 + e] * inv, d[e], A.eps); }
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (T.any(k)) {
+                const int m = min(TY * k + T.ty, T.rows - 1);
+                const float w = A.w[m], b = A.b[m];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[k][e] = (v[k][e] - d[e]) * rstd[e] * w + b;
+                T.template store<STREAM>(A.y, k, v[k]);
             }
-        };
-        if ((tile + 1) * TX * VEC <= A.cols) body(std::integral_constant<bool, true>{});      // uniform
-        else body(std::integral_constant<bool, false>{});
+        if (A.stats && T.ty == 0) {
+            T.store_columns(A.stats, float4v{sum[0] + d[0], sum[1] + d[1], sum[2] + d[2], sum[3] + d[3]});
+            T.store_columns(A.stats + A.cols, float4v{rstd[0], rstd[1], rstd[2], rstd[3]});
+        }
     }
 }
 
 // A workgroup takes every gridDim.x-th tile and adds up what its columns give to the parameters' gradients in registers.
-template <int MODE, int VEC, int TX, int TY, int K>
-__global__ void __launch_bounds__(TX * TY) k_norm_cols_bwd(NormBwd A, long tiles, float* __restrict__ parts)
+template <int MODE, int TX, int TY, bool STREAM>
+__global__ void __launch_bounds__(TX * TY, 4) k_norm_cols_bwd(NormBwd A, Tiles tiles, float* __restrict__ parts)
 {
-    constexpr int WAVES = TX * TY / 64;
-    __shared__ float red[2][WAVES][TX][2 * VEC];
+    constexpr int WAVES = TX * TY / 64, K = kRowsHeld;
+    __shared__ float red[2][WAVES][TX][8];
     DropKey D = {};
     if (MODE == JOIN_DROP) D = drop_key(A.drop);
     const int tx = threadIdx.x % TX, ty = threadIdx.x / TX, rows = (int)A.rows;
@@ -248,60 +287,58 @@ __global__ void __launch_bounds__(TX * TY) k_norm_cols_bwd(NormBwd A, long tiles
         gw[k] = gb[k] = 0.f;
         w[k] = ty + TY * k < rows ? A.w[ty + TY * k] : 0.f;
     }
-    int turn = 0;
-    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1) {
-        const long c = (tile * TX + tx) * VEC;
-        auto body = [&](auto whole) {
-            const int count = whole.value ? VEC : (int)max(0L, min((long)VEC, A.cols - c));
-            Vec<VEC> x[K], g[K];
-            const Vec<VEC> mean = load_vec<VEC>(A.stats + c, count), rstd = load_vec<VEC>(A.stats + A.cols + c, count);
+    int side = 0;
+    for (long turn = blockIdx.x; turn < tile_turns(tiles); turn += gridDim.x) {
+        const long tile = tile_of(tiles, turn);
+        if (tile >= tiles.count) continue;      // uniform
+        const ColumnTile<TX, TY> T(A.rows, A.cols, tile);
+        float4v x[K], g[K], r[K];
+        const float4v mean = T.load_columns(A.stats), rstd = T.load_columns(A.stats + A.cols);
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-                if (TY * k < rows) {
-                    const long t = (long)min(ty + TY * k, rows - 1) * A.cols + c;
-                    x[k] = load_vec<VEC>(A.x + t, count);
-                    g[k] = load_vec<VEC>(A.gy + t, count);
-                }
-            float s[2 * VEC];
-#pragma unroll
-            for (int e = 0; e < 2 * VEC; ++e) s[e] = 0.f;
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-                if (TY * k < rows && ty + TY * k < rows)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float h = (x[k].v[e] - mean.v[e]) * rstd.v[e], gy = g[k].v[e], a = gy * w[k];     // gy = 0 behind the columns
-                        x[k].v[e] = h;
-                        gw[k] += gy * h;
-                        gb[k] += gy;
-                        g[k].v[e] = a;
-                        s[e] += a;
-                        s[VEC + e] += a * h;
-                    }
-            sum_over_ty<TX, TY, 2 * VEC>(s, red[turn]);
-#pragma unroll
-            for (int e = 0; e < 2 * VEC; ++e) s[e] *= inv;
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int m = ty + TY * k;
-                if (TY * k < rows && m < rows) {
-                    const long t = (long)m * A.cols + c;
-                    Vec<VEC> v;
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) v.v[e] = rstd.v[e] * (g[k].v[e] - s[e] - x[k].v[e] * s[VEC + e]);
-                    if (MODE != PLAIN && A.gr) {
-                        const Vec<VEC> r = load_vec<VEC>(A.gr + t, count);
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) v.v[e] += r.v[e];
-                    }
-                    store_vec<VEC>(A.gx + t, count, v);
-                    if (MODE == JOIN_DROP) drop_vec<VEC>(D, c, m, v);
-                    if (MODE != PLAIN && A.gh) store_vec<VEC>(A.gh + t, count, v);
-                }
+        for (int k = 0; k < K; ++k)
+            if (T.any(k)) {
+                x[k] = T.load(A.x, k);
+                g[k] = T.load(A.gy, k);
             }
-        };
-        if ((tile + 1) * TX * VEC <= A.cols) body(std::integral_constant<bool, true>{});      // uniform
-        else body(std::integral_constant<bool, false>{});
+        const bool more = MODE != PLAIN && A.gr;
+        if (more)
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (T.any(k)) r[k] = T.load(A.gr, k);
+        float s[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (T.any(k))
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float gy = g[k][e], own = e >= T.skip ? gy : 0.f, a = gy * w[k];      // 0 where there is no row
+                    const float h = T.has(k) ? (x[k][e] - mean[e]) * rstd[e] : 0.f;
+                    x[k][e] = h;
+                    gw[k] += own * h;
+                    gb[k] += own;
+                    g[k][e] = a;
+                    s[e] += a;
+                    s[4 + e] += a * h;
+                }
+        sum_over_ty<TX, TY, 8>(s, red[side]);
+        side ^= 1;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] *= inv;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (T.any(k)) {
+                float4v v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = rstd[e] * (g[k][e] - s[e] - x[k][e] * s[4 + e]);
+                if (more)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] += r[k][e];
+                T.template store<STREAM>(A.gx, k, v);
+                if (MODE == JOIN_DROP) v = T.drop(D, k, v);
+                if (MODE != PLAIN && A.gh) T.template store<STREAM>(A.gh, k, v);
+            }
     }
     float* part = parts + (long)blockIdx.x * 2 * rows;
 #pragma unroll
@@ -712,18 +749,20 @@ __global__ void __launch_bounds__(256) k_norm_params_cols(NormParams A)
     }
 }
 
-// 64 of the 2 x features values by sixteen slices of the shares
+// 16 of the 2 x features values by 64 slices of the shares
 __global__ void __launch_bounds__(1024)
 k_norm_params(long features, int shares, const float* __restrict__ parts, float* __restrict__ gw, float* __restrict__ gb)
 {
-    __shared__ float red[16][64];
-    const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-    const long t = (long)blockIdx.x * 64 + tx;
+    __shared__ float red[16][16];
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const long t = (long)blockIdx.x * 16 + tx;
     float v = 0.f;
     if (t < 2 * features)
 #pragma unroll 8
-        for (int s = ty; s < shares; s += 16) v += parts[(long)s * 2 * features + t];
-    red[ty][tx] = v;
+        for (int s = ty; s < shares; s += 64) v += parts[(long)s * 2 * features + t];
+    v += __shfl_xor(v, 16);
+    v += __shfl_xor(v, 32);
+    if ((threadIdx.x & 63) < 16) red[threadIdx.x >> 6][tx] = v;
     __syncthreads();
     if (ty > 0 || t >= 2 * features) return;
 #pragma unroll
@@ -742,8 +781,8 @@ Shares param_shares(long rows, long cols, int axis)
 }
 
 // How an array is taken, by its extents alone: kernels that hold a position in registers (`held`) where one fits.
-struct Shape { bool held; int vec, tx, ty; long tiles; int lanes, quads; };
-Shape norm_shape(long rows, long cols, int axis)
+struct Shape { bool held; int tx, ty; Tiles tiles; long most; int lanes, quads; };
+Shape norm_shape(long rows, long cols, int axis, bool backward)
 {
     Shape S = {};
     if (axis) {
@@ -752,15 +791,16 @@ Shape norm_shape(long rows, long cols, int axis)
             if (cols <= 4L * lanes[i] * quads[i]) { S.held = true; S.lanes = lanes[i]; S.quads = quads[i]; }
         return S;
     }
-    if (rows > 512) return S;
+    // Tiles of eight lanes (a line of every row) leave the least to wait for at the end of a launch; sums of the parameters' gradients
+    // want fewer, wider ones.  us, TX = 8 and 16: 200 x 30690 forward 13.8 and 17.8, backward 19.4 and 27.0; 120 x 262143 forward 43.9 and 45.7,
+    // backward 101 and 87; 40 x 216000 13.6 and 14.3, 31 and 24.  Eight and four rows a thread: 120 x 96^3 forward with dropout 384 and 351.
+    S.ty = rows <= 16 ? 4 : rows <= 32 ? 8 : rows <= 64 ? 16 : rows <= 128 ? 32 : rows <= 256 ? 64 : 128;
+    S.tx = rows <= 16 ? 64 : rows <= 32 ? 32 : rows <= 128 && backward ? 16 : 8;
+    S.most = S.ty == 16 ? 1024 : S.ty == 128 ? 256 : 512;       // of 128 to 1024 threads: what a chip holds at once
+    S.tiles.apart = cols % 32 != 0 || (!backward && S.tx == 8); // rows on 128-byte lines: 120 x 96^3 backward 265 us in order, 277 apart
+    if (rows > S.ty * kRowsHeld || cols < 4 || S.ty * cols >= (1L << 30) - 16) return Shape{};
     S.held = true;
-    if (rows <= 32) { S.tx = 64; S.ty = 4; }
-    else if (rows <= 64) { S.tx = 32; S.ty = 8; }
-    else if (rows <= 128) { S.tx = 32; S.ty = 16; }
-    else if (rows <= 256) { S.tx = 32; S.ty = 32; }
-    else { S.tx = 16; S.ty = 64; }
-    S.vec = cols >= 4L * S.tx * 512 ? 4 : 1;
-    S.tiles = (cols + S.tx * S.vec - 1) / (S.tx * S.vec);
+    S.tiles.count = (cols + 4 * S.tx - 1) / (4 * S.tx);
     return S;
 }
 int row_groups(const Shape& S) { return S.lanes > 256 ? 1 : 256 / S.lanes; }
@@ -769,12 +809,12 @@ int row_groups(const Shape& S) { return S.lanes > 256 ? 1 : 256 / S.lanes; }
 long bwd_groups(const Shape& S, long rows)
 {
     if (S.lanes) return std::min((rows + row_groups(S) - 1) / row_groups(S), S.lanes > 256 ? 256L : 512L);
-    return std::min(S.tiles, 512L);
+    return std::min((S.tiles.count + 7) / 8 * 8, S.most);
 }
 
 int norm_share_count(long rows, long cols, int axis)
 {
-    const Shape S = norm_shape(rows, cols, axis);
+    const Shape S = norm_shape(rows, cols, axis, true);
     return S.held ? (int)bwd_groups(S, rows) : param_shares(rows, cols, axis).count;
 }
 
@@ -806,16 +846,16 @@ int check_axis(int64_t rows, int64_t cols, int32_t axis)
 
 // Calls f with the constants of a shape.
 template <int... N> struct Numbers {};
-template <class F> void with_cols(const Shape& S, F f)
+template <bool BACKWARD, class F> void with_cols(const Shape& S, F f)
 {
-    auto vec = [&](auto v) {
-        if (S.ty == 4) f(v, Numbers<64, 4>{});
-        else if (S.ty == 8) f(v, Numbers<32, 8>{});
-        else if (S.ty == 16) f(v, Numbers<32, 16>{});
-        else if (S.ty == 32) f(v, Numbers<32, 32>{});
-        else f(v, Numbers<16, 64>{});
-    };
-    if (S.vec == 4) vec(std::integral_constant<int, 4>{}); else vec(std::integral_constant<int, 1>{});
+    switch (S.ty) {
+        case 4: return f(Numbers<64, 4>{});
+        case 8: return f(Numbers<32, 8>{});
+        case 16: return f(Numbers<BACKWARD ? 16 : 8, 16>{});
+        case 32: return f(Numbers<BACKWARD ? 16 : 8, 32>{});
+        case 64: return f(Numbers<8, 64>{});
+        default: return f(Numbers<8, 128>{});
+    }
 }
 template <class F> void with_rows(const Shape& S, F f)
 {
@@ -833,16 +873,24 @@ template <class F> void with_rows(const Shape& S, F f)
     }
 }
 
-template <int MODE, int VEC, int TX, int TY>
-void cols_fwd(const NormFwd& A, const Shape& S, std::integral_constant<int, VEC>, Numbers<TX, TY>, hipStream_t s)
+bool on_lines(std::initializer_list<const float*> arrays)
 {
-    ZNN_LAUNCH("layer norm forward", s, (k_norm_cols<MODE, VEC, TX, TY, 8>), dim3(groups_of(S.tiles, 1, 1L << 20)), dim3(TX * TY), 0, A, S.tiles);
+    for (const float* p : arrays) if ((uintptr_t)p & 127) return false;
+    return true;
 }
-template <int MODE, int VEC, int TX, int TY>
-void cols_bwd(const NormBwd& A, const Shape& S, std::integral_constant<int, VEC>, Numbers<TX, TY>, float* parts, hipStream_t s)
+template <int MODE, int TX, int TY> void cols_fwd(const NormFwd& A, const Shape& S, Numbers<TX, TY>, hipStream_t s)
 {
-    ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd<MODE, VEC, TX, TY, 8>), dim3((unsigned)bwd_groups(S, A.rows)), dim3(TX * TY), 0, A,
-               S.tiles, parts);
+    const dim3 grid(groups_of((S.tiles.count + 7) / 8 * 8, 1, 1L << 20));
+    if (A.cols % 32 == 0 && on_lines({A.r, A.y}))
+        ZNN_LAUNCH("layer norm forward", s, (k_norm_cols<MODE, TX, TY, true>), grid, dim3(TX * TY), 0, A, S.tiles);
+    else ZNN_LAUNCH("layer norm forward", s, (k_norm_cols<MODE, TX, TY, false>), grid, dim3(TX * TY), 0, A, S.tiles);
+}
+template <int MODE, int TX, int TY> void cols_bwd(const NormBwd& A, const Shape& S, Numbers<TX, TY>, float* parts, hipStream_t s)
+{
+    const dim3 grid((unsigned)bwd_groups(S, A.rows));
+    if (A.cols % 32 == 0 && on_lines({A.gx, A.gh}))
+        ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd<MODE, TX, TY, true>), grid, dim3(TX * TY), 0, A, S.tiles, parts);
+    else ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd<MODE, TX, TY, false>), grid, dim3(TX * TY), 0, A, S.tiles, parts);
 }
 template <int MODE, int L, int NV> void rows_fwd(const NormFwd& A, Numbers<L, NV>, hipStream_t s)
 {
@@ -856,9 +904,9 @@ template <int MODE, int L, int NV> void rows_bwd(const NormBwd& A, const Shape& 
 template <int MODE>
 int norm_fwd(const NormFwd& A, int axis, hipStream_t s)
 {
-    const Shape S = norm_shape(A.rows, A.cols, axis);
+    const Shape S = norm_shape(A.rows, A.cols, axis, false);
     if (S.held && axis) with_rows(S, [&](auto n) { rows_fwd<MODE>(A, n, s); });
-    else if (S.held) with_cols(S, [&](auto v, auto n) { cols_fwd<MODE>(A, S, v, n, s); });
+    else if (S.held) with_cols<false>(S, [&](auto n) { cols_fwd<MODE>(A, S, n, s); });
     else if (axis) ZNN_LAUNCH("layer norm forward", s, k_norm_rows_any<MODE>, dim3(groups_of(A.rows, 1, 1L << 20)), dim3(1024), 0, A);
     else ZNN_LAUNCH("layer norm forward", s, k_norm_cols_any<MODE>, dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
     return check_launch("layer norm forward");
@@ -867,10 +915,10 @@ int norm_fwd(const NormFwd& A, int axis, hipStream_t s)
 template <int MODE>
 int norm_bwd(const NormBwd& A, int axis, float* gw, float* gb, void* ws, hipStream_t s)
 {
-    const Shape H = norm_shape(A.rows, A.cols, axis);
+    const Shape H = norm_shape(A.rows, A.cols, axis, true);
     const long features = axis ? A.cols : A.rows;
     if (H.held && axis) with_rows(H, [&](auto n) { rows_bwd<MODE>(A, H, n, (float*)ws, s); });
-    else if (H.held) with_cols(H, [&](auto v, auto n) { cols_bwd<MODE>(A, H, v, n, (float*)ws, s); });
+    else if (H.held) with_cols<true>(H, [&](auto n) { cols_bwd<MODE>(A, H, n, (float*)ws, s); });
     else {
         const Shares S = param_shares(A.rows, A.cols, axis);
         const NormParams P = {A.rows, A.cols, A.gy, A.x, A.stats, (float*)ws, S.count, S.span};
@@ -882,7 +930,7 @@ int norm_bwd(const NormBwd& A, int axis, float* gw, float* gb, void* ws, hipStre
             ZNN_LAUNCH("layer norm parameters", s, k_norm_params_cols, dim3(groups_of(A.rows, 1, 1L << 20), (unsigned)S.count), dim3(256), 0, P);
         }
     }
-    ZNN_LAUNCH("layer norm parameters", s, k_norm_params, dim3((unsigned)((2 * features + 63) / 64)), dim3(1024), 0, features,
+    ZNN_LAUNCH("layer norm parameters", s, k_norm_params, dim3((unsigned)((2 * features + 15) / 16)), dim3(1024), 0, features,
                norm_share_count(A.rows, A.cols, axis), (const float*)ws, gw, gb);
     return check_launch("layer norm backward");
 }
