@@ -6,7 +6,9 @@ library has not been built, loading raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -168,7 +170,8 @@ def make_desc(fan_in, fan_out, image, kernel, mode="direct", sparsity=(1, 1, 1))
 
 
 def _stream_ptr(stream=None):
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+    """The stream's handle; without one that of torch's current stream (0.3 us; 2.7 as a ``torch.cuda.Stream``)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
 
 
 def _ptr(t, dtype=None):
@@ -488,111 +491,115 @@ def _state_ptr(state):
     return _ptr(state, torch.int64)
 
 
-def _extents(t):
-    if t.dim() < 1 or t.shape[0] < 1:
-        raise ValueError("expected an array [rows, ...], got %s" % (tuple(t.shape),))
-    return t.shape[0], t.numel() // t.shape[0]
+def _extents(x, axis, *params):
+    """(rows, columns, positions of the norm) of an array whose parameters are checked."""
+    rows = x.shape[0] if x.dim() else 0
+    if rows < 1:
+        raise ValueError("expected an array [rows, ...], got %s" % (tuple(x.shape),))
+    cols = x.numel() // rows
+    if axis == 0:
+        n, positions = rows, cols
+    elif axis == 1:
+        n, positions = cols, rows
+    else:
+        raise ValueError("axis must be 0 or 1, got %r" % (axis,))
+    for p in params:
+        if p.numel() != n:
+            raise ValueError("expected %d parameters, got %d" % (n, p.numel()))
+    return rows, cols, positions
 
 
-def _like(t, *others):
+def _same_shape(t, *others):
     for o in others:
         if o is not None and o.shape != t.shape:
             raise ValueError("expected shape %s, got %s" % (tuple(t.shape), tuple(o.shape)))
 
 
-def _features(rows, cols, axis, *params):
-    """Positions of a norm, whose parameters are checked."""
-    if axis not in (0, 1):
-        raise ValueError("axis must be 0 or 1, got %r" % (axis,))
-    n, positions = (cols, rows) if axis else (rows, cols)
-    for p in params:
-        if p.numel() != n:
-            raise ValueError("expected %d parameters, got %d" % (n, p.numel()))
-    return positions
+_HERE = contextlib.nullcontext()
 
 
-def _empty(stream, device, *shapes):
-    """Tensors that belong to the stream that works on them."""
-    if stream is None:
-        return [torch.empty(s, dtype=torch.float32, device=device) for s in shapes]
-    with torch.cuda.stream(stream):
-        return [torch.empty(s, dtype=torch.float32, device=device) for s in shapes]
+def _on(stream):
+    """What is made inside belongs to the stream that works on it."""
+    return _HERE if stream is None else torch.cuda.stream(stream)
 
 
 def dropout(x, p, state=None, site=0, stream=None):
     """x / (1 - p) where an element is kept, 0 elsewhere; on a gradient, with the same state and site, the Jacobian."""
-    rows, cols = _extents(x)
-    y, = _empty(stream, x.device, x.shape)
-    _check(lib().znn_dropout(rows, cols, p, _state_ptr(state), site, _ptr(x, torch.float32), _ptr(y), _stream_ptr(stream)))
+    rows, cols, _ = _extents(x, 0)
+    with _on(stream):
+        y = torch.empty_like(x)
+    _check(lib().znn_dropout(rows, cols, p, _state_ptr(state), site, _ptr(x, torch.float32), y.data_ptr(), _stream_ptr(stream)))
     return y
 
 
 def layernorm_fwd(x, w, b, eps=1e-5, axis=0, stats=True, stream=None):
     """(y, stats): stats, for ``layernorm_bwd``, holds mean and 1 / deviation of every position (None if not asked for)."""
-    rows, cols = _extents(x)
-    positions = _features(rows, cols, axis, w, b)
-    y, *kept = _empty(stream, x.device, x.shape, *([(2, positions)] if stats else []))
-    kept = kept[0] if stats else None
+    rows, cols, positions = _extents(x, axis, w, b)
+    with _on(stream):
+        y = torch.empty_like(x)
+        kept = x.new_empty((2, positions)) if stats else None
     _check(lib().znn_layernorm_fwd(rows, cols, axis, eps, _ptr(x, torch.float32), _ptr(w, torch.float32), _ptr(b, torch.float32),
-                                   _ptr(y), _ptr(kept), _stream_ptr(stream)))
+                                   y.data_ptr(), _ptr(kept), _stream_ptr(stream)))
     return y, kept
 
 
+@functools.lru_cache(maxsize=1024)
 def layernorm_workspace_bytes(rows, cols, axis):
     b = ctypes.c_size_t(0)
     _check(lib().znn_layernorm_workspace_bytes(rows, cols, axis, ctypes.byref(b)))
     return b.value
 
 
-def _norm_workspace(rows, cols, axis, stream, device):
+def _norm_workspace(x, rows, cols, axis):
+    """(tensor that holds it, aligned address, bytes)"""
     need = layernorm_workspace_bytes(rows, cols, axis)
     if not need:
         return None, None, 0
-    ws, = _empty(stream, device, (need + 256) // 4)
+    ws = x.new_empty(need // 4 + 64)
     return ws, (ws.data_ptr() + 255) & ~255, need
 
 
 def layernorm_bwd(gy, x, w, stats, axis=0, stream=None):
     """(gx, gw, gb) from the input and the statistics of the forward pass."""
-    rows, cols = _extents(x)
-    _like(x, gy)
-    positions = _features(rows, cols, axis, w)
+    rows, cols, positions = _extents(x, axis, w)
+    _same_shape(x, gy)
     if stats.numel() != 2 * positions:
         raise ValueError("expected statistics of %d positions, got %s" % (positions, tuple(stats.shape)))
-    gx, gw, gb = _empty(stream, x.device, x.shape, w.shape, w.shape)
-    ws, at, need = _norm_workspace(rows, cols, axis, stream, x.device)
+    with _on(stream):
+        gx, gw, gb = torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
+        ws, at, need = _norm_workspace(x, rows, cols, axis)
     _check(lib().znn_layernorm_bwd(rows, cols, axis, _ptr(gy, torch.float32), _ptr(x, torch.float32), _ptr(w, torch.float32),
-                                   _ptr(stats, torch.float32), _ptr(gx), _ptr(gw), _ptr(gb), at, need, _stream_ptr(stream)))
+                                   _ptr(stats, torch.float32), gx.data_ptr(), gw.data_ptr(), gb.data_ptr(), at, need, _stream_ptr(stream)))
     return gx, gw, gb
 
 
 def residual_norm_fwd(h, x, w, b, p=0.0, state=None, site=0, eps=1e-5, axis=0, stats=True, stream=None):
     """(r, y, stats) with r = x + dropout(h), y = layernorm(r): the end of a residual branch in one pass."""
-    rows, cols = _extents(x)
-    _like(x, h)
-    positions = _features(rows, cols, axis, w, b)
-    r, y, *kept = _empty(stream, x.device, x.shape, x.shape, *([(2, positions)] if stats else []))
-    kept = kept[0] if stats else None
+    rows, cols, positions = _extents(x, axis, w, b)
+    _same_shape(x, h)
+    with _on(stream):
+        r, y = torch.empty_like(x), torch.empty_like(x)
+        kept = x.new_empty((2, positions)) if stats else None
     _check(lib().znn_residual_norm_fwd(rows, cols, axis, eps, p, _state_ptr(state), site, _ptr(h, torch.float32),
-                                       _ptr(x, torch.float32), _ptr(w, torch.float32), _ptr(b, torch.float32), _ptr(r), _ptr(y),
-                                       _ptr(kept), _stream_ptr(stream)))
+                                       _ptr(x, torch.float32), _ptr(w, torch.float32), _ptr(b, torch.float32), r.data_ptr(),
+                                       y.data_ptr(), _ptr(kept), _stream_ptr(stream)))
     return r, y, kept
 
 
 def residual_norm_bwd(gy, gr, r, w, stats, p=0.0, state=None, site=0, axis=0, stream=None):
     """(gx, gh, gw, gb): gradients of x, h and the parameters.  gr, the gradient that reaches r beside the norm, may be
     None.  Where p is 0, gh is gx."""
-    rows, cols = _extents(r)
-    _like(r, gy, gr)
-    positions = _features(rows, cols, axis, w)
+    rows, cols, positions = _extents(r, axis, w)
+    _same_shape(r, gy, gr)
     if stats.numel() != 2 * positions:
         raise ValueError("expected statistics of %d positions, got %s" % (positions, tuple(stats.shape)))
-    gx, gw, gb, *gh = _empty(stream, r.device, r.shape, w.shape, w.shape, *([r.shape] if p != 0 else []))
-    gh = gh[0] if p != 0 else None
-    ws, at, need = _norm_workspace(rows, cols, axis, stream, r.device)
+    with _on(stream):
+        gx, gw, gb = torch.empty_like(r), torch.empty_like(w), torch.empty_like(w)
+        gh = torch.empty_like(r) if p != 0 else None
+        ws, at, need = _norm_workspace(r, rows, cols, axis)
     _check(lib().znn_residual_norm_bwd(rows, cols, axis, p, _state_ptr(state), site, _ptr(gy, torch.float32), _ptr(gr, torch.float32),
-                                       _ptr(r, torch.float32), _ptr(w, torch.float32), _ptr(stats, torch.float32), _ptr(gx), _ptr(gh),
-                                       _ptr(gw), _ptr(gb), at, need, _stream_ptr(stream)))
+                                       _ptr(r, torch.float32), _ptr(w, torch.float32), _ptr(stats, torch.float32), gx.data_ptr(),
+                                       _ptr(gh), gw.data_ptr(), gb.data_ptr(), at, need, _stream_ptr(stream)))
     return gx, gx if gh is None else gh, gw, gb
 
 

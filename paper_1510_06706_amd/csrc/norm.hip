@@ -29,6 +29,15 @@ int make_drop(double p, const uint64_t* state, uint32_t site, Drop* drop, bool* 
 
 namespace {
 
+// Rows lie one behind the other, so that the stores of neighbouring lanes fill lines but at a row's ends.  They leave the cache at once, which
+// would write them back when the kernel ends, with nothing else left to do.  us before and after: dropout on 36 x 84987 5.6 -> 5.1, norm on
+// 16384 x 512 12.4 -> 11.0, on 1000 x 3505 6.5 -> 5.7, joined 10.8 -> 8.9, join on 8192 x 2048 backward 67 -> 57.
+__device__ __forceinline__ void store_row(float* p, int count, floatu4 v)
+{
+    if (count >= 4) __builtin_nontemporal_store(v, reinterpret_cast<floatu4*>(p));
+    else store4(p, count, v);
+}
+
 // ---------------------------------------------------------------- dropout
 __global__ void __launch_bounds__(256)
 k_dropout(long rows, long cols, long quads, Drop D, const float* __restrict__ x, float* __restrict__ y)
@@ -37,7 +46,7 @@ k_dropout(long rows, long cols, long quads, Drop D, const float* __restrict__ x,
     for (long t = (long)blockIdx.x * 256 + threadIdx.x; t < rows * quads; t += (long)gridDim.x * 256) {
         const long row = t / quads, q = t - row * quads, at = row * cols + 4 * q;
         const int count = (int)min(4L, cols - 4 * q);
-        store4(y + at, count, dropped4(K, (unsigned)q, (unsigned)row, load4(x + at, count)));
+        store_row(y + at, count, dropped4(K, (unsigned)q, (unsigned)row, load4(x + at, count)));
     }
 }
 
@@ -103,8 +112,7 @@ constexpr unsigned kBufferWord3 = 0x00020000u;      // raw 32-bit buffer element
 typedef unsigned word4 __attribute__((ext_vector_type(4)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
-// Stores of whole 128-byte lines (STREAM) leave the cache at once: it would write them back when the kernel ends, with nothing else left
-// to do: 120 x 262144 backward 90 -> 72 us, 120 x 32768 forward 8.7 -> 6.9.  Of parts of lines it would write each on its own: 120 x 262143
+// Stores of whole 128-byte lines (STREAM) leave the cache at once, as those of rows do (store_row): 120 x 262144 backward 90 -> 72 us, 120 x 32768 forward 8.7 -> 6.9.  Of parts of lines it would write each on its own: 120 x 262143
 // forward 44 -> 90.
 template <bool STREAM> __device__ __forceinline__ void store_buffer(__amdgpu_buffer_rsrc_t b, unsigned at, float4v v)
 {
@@ -271,12 +279,36 @@ __global__ void __launch_bounds__(TX * TY, 4) k_norm_cols(NormFwd A, Tiles tiles
     }
 }
 
-// A workgroup takes every gridDim.x-th tile and adds up what its columns give to the parameters' gradients in registers.
-template <int MODE, int TX, int TY, bool STREAM>
-__global__ void __launch_bounds__(TX * TY, 4) k_norm_cols_bwd(NormBwd A, Tiles tiles, float* __restrict__ parts)
+// Gradients of weight and bias of one feature by one workgroup, over all columns: for few columns, where a launch that adds shares up
+// would take as long again.
+template <int T> __device__ __forceinline__ void row_params(const NormBwd& A, long m, float* gw, float* gb, float2* red)
+{
+    float a = 0.f, b = 0.f;
+    for (long q = threadIdx.x; 4 * q < A.cols; q += T) {
+        const int count = (int)min(4L, A.cols - 4 * q);
+        const floatu4 g = load4(A.gy + m * A.cols + 4 * q, count), x = load4(A.x + m * A.cols + 4 * q, count);
+        const floatu4 mean = load4(A.stats + 4 * q, count), rstd = load4(A.stats + A.cols + 4 * q, count);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < count) { a += g[e] * ((x[e] - mean[e]) * rstd[e]); b += g[e]; }
+    }
+    const float2 s = group_sum<T / 64>(a, b, red);
+    if (threadIdx.x == 0) { gw[m] = s.x; gb[m] = s.y; }
+}
+
+// PARTS: a workgroup takes every gridDim.x-th tile, adds up what its columns give to the parameters' gradients in registers and leaves its
+// share.  Otherwise the first workgroups take a feature each (row_params).
+template <int MODE, int TX, int TY, bool STREAM, bool PARTS>
+__global__ void __launch_bounds__(TX * TY, 4) k_norm_cols_bwd(NormBwd A, Tiles tiles, float* __restrict__ parts, float* __restrict__ pw, float* __restrict__ pb)
 {
     constexpr int WAVES = TX * TY / 64, K = kRowsHeld;
     __shared__ float red[2][WAVES][TX][8];
+    const unsigned others = PARTS ? 0 : (unsigned)A.rows;
+    if (blockIdx.x < others) {
+        row_params<TX * TY>(A, blockIdx.x, pw, pb, (float2*)red);
+        return;
+    }
+    const unsigned block = blockIdx.x - others, blocks = gridDim.x - others;
     DropKey D = {};
     if (MODE == JOIN_DROP) D = drop_key(A.drop);
     const int tx = threadIdx.x % TX, ty = threadIdx.x / TX, rows = (int)A.rows;
@@ -288,7 +320,7 @@ __global__ void __launch_bounds__(TX * TY, 4) k_norm_cols_bwd(NormBwd A, Tiles t
         w[k] = ty + TY * k < rows ? A.w[ty + TY * k] : 0.f;
     }
     int side = 0;
-    for (long turn = blockIdx.x; turn < tile_turns(tiles); turn += gridDim.x) {
+    for (long turn = block; turn < tile_turns(tiles); turn += blocks) {
         const long tile = tile_of(tiles, turn);
         if (tile >= tiles.count) continue;      // uniform
         const ColumnTile<TX, TY> T(A.rows, A.cols, tile);
@@ -316,8 +348,10 @@ __global__ void __launch_bounds__(TX * TY, 4) k_norm_cols_bwd(NormBwd A, Tiles t
                     const float gy = g[k][e], own = e >= T.skip ? gy : 0.f, a = gy * w[k];      // 0 where there is no row
                     const float h = T.has(k) ? (x[k][e] - mean[e]) * rstd[e] : 0.f;
                     x[k][e] = h;
-                    gw[k] += own * h;
-                    gb[k] += own;
+                    if (PARTS) {
+                        gw[k] += own * h;
+                        gb[k] += own;
+                    }
                     g[k][e] = a;
                     s[e] += a;
                     s[4 + e] += a * h;
@@ -340,7 +374,8 @@ __global__ void __launch_bounds__(TX * TY, 4) k_norm_cols_bwd(NormBwd A, Tiles t
                 if (MODE != PLAIN && A.gh) T.template store<STREAM>(A.gh, k, v);
             }
     }
-    float* part = parts + (long)blockIdx.x * 2 * rows;
+    if constexpr (!PARTS) return;
+    float* part = parts + (long)block * 2 * rows;
 #pragma unroll
     for (int k = 0; k < K; ++k)
         if (TY * k < rows) {
@@ -353,14 +388,13 @@ __global__ void __launch_bounds__(TX * TY, 4) k_norm_cols_bwd(NormBwd A, Tiles t
 }
 
 // ---------------------------------------------------------------- rows held in registers
-// L lanes take a row, NV times four neighbouring columns each: lanes of a wave (the sums stay in it) or a whole workgroup.
-template <int L> struct RowGroup { static constexpr int threads = L > 256 ? L : 256, rows = threads / L, waves = L > 64 ? L / 64 : 1; };
-
+// L lanes take a row, NV times four neighbouring columns each: lanes of a wave (the sums stay in it) or a whole workgroup of L.
+// T threads in a workgroup, T / L rows at a time.
 template <int L> __device__ __forceinline__ float2 row_sum(float a, float b, float2* red)
 {
 #pragma unroll
     for (int s = 1; s < (L < 64 ? L : 64); s <<= 1) { a += __shfl_xor(a, s); b += __shfl_xor(b, s); }
-    if constexpr (L > 64) {
+    if constexpr (L > 64) {         // `red` must not be that of the call before: a thread may still read it
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = make_float2(a, b);
         __syncthreads();
         float2 v = red[0];
@@ -375,24 +409,35 @@ template <int L> __device__ __forceinline__ int quad_count(int j, int lane, int 
 {
     return 4 * L * (j + 1) <= cols ? 4 : max(0, min(4, cols - 4 * (lane + L * j)));
 }
-
-template <int MODE, int L, int NV>
-__global__ void __launch_bounds__(RowGroup<L>::threads) k_norm_rows(NormFwd A)
+// the row of a wave, which the compiler then knows to be one
+template <int L> __device__ __forceinline__ long wave_row(long row)
 {
-    __shared__ float2 red[2][RowGroup<L>::waves];
+    if constexpr (L >= 64) return (long)__builtin_amdgcn_readfirstlane((int)row) & 0xffffffffL;     // rows have 32 bits
+    return row;
+}
+
+template <int MODE, int L, int NV, int T>
+__global__ void __launch_bounds__(T) k_norm_rows(NormFwd A)
+{
+    constexpr int ROWS = T / L;
+    constexpr bool KEEP = L * NV <= 2048;       // weights of longer rows come from the cache for every row: their registers let a second workgroup in
+    __shared__ float2 red[2][L > 64 ? L / 64 : 1];
     DropKey D = {};
     if (MODE == JOIN_DROP) D = drop_key(A.drop);
     const int lane = threadIdx.x % L, cols = (int)A.cols;
     const float inv = 1.0f / (float)cols;
     floatu4 w[NV], b[NV];
+    auto weights = [&]() {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int count = quad_count<L>(j, lane, cols);
-        w[j] = load4(A.w + 4 * (lane + L * j), count);
-        b[j] = load4(A.b + 4 * (lane + L * j), count);
-    }
-    for (long row0 = (long)blockIdx.x * RowGroup<L>::rows; row0 < A.rows; row0 += (long)gridDim.x * RowGroup<L>::rows) {
-        const long row = row0 + threadIdx.x / L, base = min(row, A.rows - 1) * cols;
+        for (int j = 0; j < NV; ++j) {
+            const int count = quad_count<L>(j, lane, cols);
+            w[j] = load4(A.w + 4 * (lane + L * j), count);
+            b[j] = load4(A.b + 4 * (lane + L * j), count);
+        }
+    };
+    if (KEEP) weights();
+    for (long row0 = (long)blockIdx.x * ROWS; row0 < A.rows; row0 += (long)gridDim.x * ROWS) {
+        const long row = wave_row<L>(row0 + threadIdx.x / L), base = min(row, A.rows - 1) * cols;
         const bool live = row < A.rows;
         floatu4 v[NV];
 #pragma unroll
@@ -406,7 +451,7 @@ __global__ void __launch_bounds__(RowGroup<L>::threads) k_norm_rows(NormFwd A)
                 if (MODE == JOIN_DROP) h[j] = dropped4(D, (unsigned)(lane + L * j), (unsigned)row, h[j]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[j][e] = joined(v[j][e], h[j][e]);
-                if (live) store4(A.r + base + 4 * (lane + L * j), quad_count<L>(j, lane, cols), v[j]);
+                if (live) store_row(A.r + base + 4 * (lane + L * j), quad_count<L>(j, lane, cols), v[j]);
             }
         }
         float sum = 0.f;
@@ -423,6 +468,7 @@ __global__ void __launch_bounds__(RowGroup<L>::threads) k_norm_rows(NormFwd A)
                 d1 += d;
                 d2 += d * d;
             }
+        if (!KEEP) weights();
         const float2 s = row_sum<L>(d1, d2, red[1]);
         const float delta = s.x * inv, rstd = inverse_deviation(s.y * inv, delta, A.eps);
         if (live) {
@@ -430,19 +476,52 @@ __global__ void __launch_bounds__(RowGroup<L>::threads) k_norm_rows(NormFwd A)
             for (int j = 0; j < NV; ++j) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[j][e] = (v[j][e] - delta) * rstd * w[j][e] + b[j][e];
-                store4(A.y + base + 4 * (lane + L * j), quad_count<L>(j, lane, cols), v[j]);
+                store_row(A.y + base + 4 * (lane + L * j), quad_count<L>(j, lane, cols), v[j]);
             }
             if (A.stats && lane == 0) { A.stats[row] = m0 + delta; A.stats[A.rows + row] = rstd; }
         }
     }
 }
 
-template <int MODE, int L, int NV>
-__global__ void __launch_bounds__(RowGroup<L>::threads) k_norm_rows_bwd(NormBwd A, float* __restrict__ parts)
+// Gradients of weight and bias of 32 features by one workgroup, over all rows: for few rows, where shares of the workgroups would be as
+// large as the operands.  red: T / 32 x 32 float2.
+template <int T> __device__ __forceinline__ void column_params(const NormBwd& A, long c0, float* gw, float* gb, float2 (*red)[32])
 {
-    constexpr int ROWS = RowGroup<L>::rows;
-    __shared__ float2 red[2][RowGroup<L>::waves];
-    __shared__ float sums[ROWS > 1 ? (ROWS - 1) * L * NV * 8 : 1];
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    const long c = c0 + tx;
+    float a = 0.f, b = 0.f;
+    if (c < A.cols)
+#pragma unroll 4
+        for (long r = ty; r < A.rows; r += T / 32) {
+            const float g = A.gy[r * A.cols + c];
+            a += g * ((A.x[r * A.cols + c] - A.stats[r]) * A.stats[A.rows + r]);
+            b += g;
+        }
+    red[ty][tx] = make_float2(a, b);
+    __syncthreads();
+    if (ty > 0 || c >= A.cols) return;
+#pragma unroll 8
+    for (int q = 1; q < T / 32; ++q) { a += red[q][tx].x; b += red[q][tx].y; }
+    gw[c] = a;
+    gb[c] = b;
+}
+
+// PARTS: the workgroup adds up what its rows give to the parameters' gradients, in registers or, of long rows, in LDS, and leaves its share.
+// Otherwise the first workgroups take 32 features each (column_params).
+template <int MODE, int L, int NV, int T, bool PARTS>
+__global__ void __launch_bounds__(T) k_norm_rows_bwd(NormBwd A, float* __restrict__ parts, float* __restrict__ pw, float* __restrict__ pb)
+{
+    constexpr int ROWS = T / L;
+    __shared__ float2 red[2][L > 64 ? L / 64 : 1];
+    constexpr bool IN_LDS = PARTS && L * NV > 2048;
+    __shared__ float sums[IN_LDS ? L * NV * 8 : !PARTS ? T * 2 : ROWS > 1 ? (ROWS - 1) * L * NV * 4 : 1];
+    const unsigned others = PARTS ? 0 : (unsigned)((A.cols + 31) / 32);
+    if (blockIdx.x < others) {
+        column_params<T>(A, (long)blockIdx.x * 32, pw, pb, (float2 (*)[32])sums);
+        return;
+    }
+    const unsigned block = blockIdx.x - others, blocks = gridDim.x - others;
+    floatu4* held = reinterpret_cast<floatu4*>(sums) + threadIdx.x;     // IN_LDS: the thread's own, gw and gb by turns, T apart
     DropKey D = {};
     if (MODE == JOIN_DROP) D = drop_key(A.drop);
     const int lane = threadIdx.x % L, group = threadIdx.x / L, cols = (int)A.cols;
@@ -452,33 +531,43 @@ __global__ void __launch_bounds__(RowGroup<L>::threads) k_norm_rows_bwd(NormBwd 
     for (int j = 0; j < NV; ++j) {
         w[j] = load4(A.w + 4 * (lane + L * j), quad_count<L>(j, lane, cols));
         gw[j] = gb[j] = floatu4{0.f, 0.f, 0.f, 0.f};
+        if (IN_LDS) held[2 * j * T] = held[(2 * j + 1) * T] = gw[j];
     }
     int turn = 0;
-    for (long row0 = (long)blockIdx.x * ROWS; row0 < A.rows; row0 += (long)gridDim.x * ROWS, turn ^= 1) {
-        const bool live = row0 + group < A.rows;
-        const long row = min(row0 + group, A.rows - 1), base = row * cols;
+    for (long row0 = (long)block * ROWS; row0 < A.rows; row0 += (long)blocks * ROWS, turn ^= 1) {
+        const long at = wave_row<L>(row0 + group), row = min(at, A.rows - 1), base = row * cols;
+        const bool live = at < A.rows;
         const float mean = A.stats[row], rstd = A.stats[A.rows + row];
-        floatu4 x[NV], g[NV];
+        floatu4 x[NV], g[NV], r[NV];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int count = quad_count<L>(j, lane, cols);
             x[j] = load4(A.x + base + 4 * (lane + L * j), count);
             g[j] = load4(A.gy + base + 4 * (lane + L * j), live ? count : 0);       // gy = 0 behind the row and behind the rows
         }
+        const bool more = MODE != PLAIN && A.gr;
+        if (more)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) r[j] = load4(A.gr + base + 4 * (lane + L * j), quad_count<L>(j, lane, cols));
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
+        for (int j = 0; j < NV; ++j) {
+            if (IN_LDS) { gw[j] = held[2 * j * T]; gb[j] = held[(2 * j + 1) * T]; }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const bool in = live && e < quad_count<L>(j, lane, cols);
                 const float h = in ? (x[j][e] - mean) * rstd : 0.f, a = g[j][e] * w[j][e];
                 x[j][e] = h;
-                gw[j][e] += g[j][e] * h;
-                gb[j][e] += g[j][e];
+                if (PARTS) {
+                    gw[j][e] += g[j][e] * h;
+                    gb[j][e] += g[j][e];
+                }
                 g[j][e] = a;
                 s1 += a;
                 s2 += a * h;
             }
+            if (IN_LDS) { held[2 * j * T] = gw[j]; held[(2 * j + 1) * T] = gb[j]; }
+        }
         const float2 s = row_sum<L>(s1, s2, red[turn]);
         const float m1 = s.x * inv, m2 = s.y * inv;
 #pragma unroll
@@ -488,43 +577,40 @@ __global__ void __launch_bounds__(RowGroup<L>::threads) k_norm_rows_bwd(NormBwd 
             floatu4 v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = rstd * (g[j][e] - m1 - x[j][e] * m2);
-            if (MODE != PLAIN && A.gr) {
-                const floatu4 r = load4(A.gr + t, count);
+            if (more)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += r[e];
-            }
-            store4(A.gx + t, count, v);
+                for (int e = 0; e < 4; ++e) v[e] += r[j][e];
+            store_row(A.gx + t, count, v);
             if (MODE == JOIN_DROP) v = dropped4(D, (unsigned)(lane + L * j), (unsigned)row, v);
-            if (MODE != PLAIN && A.gh) store4(A.gh + t, count, v);
+            if (MODE != PLAIN && A.gh) store_row(A.gh + t, count, v);
         }
     }
-    // the sums of the workgroup's rows side by side, the first group's last
-    if constexpr (ROWS > 1) {
-        if (group > 0)
+    if constexpr (!PARTS) return;
+    // the sums of the workgroup's rows side by side, in the order of the groups: first those of the weight, then those of the bias
+    float* part = parts + (long)block * 2 * cols;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        floatu4 (&v)[NV] = which ? gb : gw;
+        if constexpr (ROWS > 1) {
+            if (which) __syncthreads();
+            if (group > 0)
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sums[(((group - 1) * NV + j) * 4 + e) * L + lane] = v[j][e];
+            __syncthreads();
+            if (group == 0)
+#pragma unroll 1
+                for (int q = 0; q < ROWS - 1; ++q)
+#pragma unroll
+                    for (int j = 0; j < NV; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[j][e] += sums[((q * NV + j) * 4 + e) * L + lane];
+        }
+        if (group == 0)
 #pragma unroll
             for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sums[(((group - 1) * NV + j) * 8 + e) * L + lane] = gw[j][e];
-                    sums[(((group - 1) * NV + j) * 8 + 4 + e) * L + lane] = gb[j][e];
-                }
-        __syncthreads();
-        if (group > 0) return;
-        for (int q = 0; q < ROWS - 1; ++q)
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    gw[j][e] += sums[((q * NV + j) * 8 + e) * L + lane];
-                    gb[j][e] += sums[((q * NV + j) * 8 + 4 + e) * L + lane];
-                }
-    }
-    float* part = parts + (long)blockIdx.x * 2 * cols;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int count = quad_count<L>(j, lane, cols);
-        store4(part + 4 * (lane + L * j), count, gw[j]);
-        store4(part + cols + 4 * (lane + L * j), count, gb[j]);
+                store4(part + which * cols + 4 * (lane + L * j), quad_count<L>(j, lane, cols), IN_LDS ? held[(2 * j + which) * T] : v[j]);
     }
 }
 
@@ -781,41 +867,68 @@ Shares param_shares(long rows, long cols, int axis)
 }
 
 // How an array is taken, by its extents alone: kernels that hold a position in registers (`held`) where one fits.
-struct Shape { bool held; int tx, ty; Tiles tiles; long most; int lanes, quads; };
-Shape norm_shape(long rows, long cols, int axis, bool backward)
+struct Shape {
+    bool held;
+    int tx, ty; Tiles tiles;                // axis 0
+    int lanes, quads, threads;              // axis 1
+    long most;                              // workgroups that walk over the positions, at most
+    bool few;                               // backward: the parameters' gradients by workgroups of their own, in the same launch
+};
+Shape rows_shape(long rows, long cols, bool backward)
 {
     Shape S = {};
-    if (axis) {
-        const int lanes[] = {4, 16, 32, 64, 64, 64, 256, 256, 1024, 1024}, quads[] = {1, 1, 1, 1, 2, 4, 2, 4, 2, 4};
-        for (int i = 0; i < 10 && !S.held; ++i)
-            if (cols <= 4L * lanes[i] * quads[i]) { S.held = true; S.lanes = lanes[i]; S.quads = quads[i]; }
-        return S;
-    }
+    // Few rows: as many as would make the shares of the parameters' gradients as large as the operands.  us, by shares and not: 64 x 1000
+    // 6.7 and 2.8, 512 x 1024 7.3 and 4.8, 300 x 12000 25 and 13.5, 1000 x 3505 16.7 and 15.3, 1000 x 1000 8.5 and 11.8.
+    S.few = backward && (rows <= 512 || (rows <= 1024 && cols > 2048));
+    struct Way { int lanes, quads, threads; long most; };
+    // Forward: waves for themselves as long as four quads a lane do.  Backward: a quad or two a lane where the sums of the parameters take
+    // registers as well (8192 x 2048 join backward: 256 lanes 64 us, 512 lanes 57), and no more shares than their reading is worth.
+    static constexpr Way forward_ways[] = {{4, 1, 256, 4096}, {16, 1, 256, 4096}, {32, 1, 256, 4096}, {64, 1, 256, 4096}, {64, 2, 256, 4096}, {64, 4, 256, 4096},
+                                           {256, 2, 256, 4096}, {256, 4, 256, 4096}, {1024, 2, 1024, 4096}, {1024, 3, 1024, 512}, {1024, 4, 1024, 512}};
+    static constexpr Way backward_ways[] = {{4, 1, 256, 512}, {16, 1, 256, 1024}, {32, 1, 512, 512}, {64, 1, 512, 512}, {64, 2, 512, 512}, {64, 4, 512, 256},
+                                            {512, 1, 512, 512}, {512, 2, 512, 512}, {1024, 2, 1024, 256}, {1024, 3, 1024, 256}, {1024, 4, 1024, 256}};
+    static constexpr Way few_ways[] = {{256, 1, 256, 1024}, {512, 1, 512, 1024}, {512, 2, 512, 1024}, {1024, 2, 1024, 1024}, {1024, 3, 1024, 1024},
+                                       {1024, 4, 1024, 1024}};
+    auto take = [&](auto& ways) {
+        for (const Way& w : ways)
+            if (!S.held && cols <= 4L * w.lanes * w.quads) { S.held = true; S.lanes = w.lanes; S.quads = w.quads; S.threads = w.threads; S.most = w.most; }
+    };
+    if (!backward) take(forward_ways);
+    else if (S.few) take(few_ways);
+    else take(backward_ways);
+    if (backward && S.lanes == 512 && rows < 4096) S.most = 256;
+    return S;
+}
+Shape cols_shape(long rows, long cols, bool backward)
+{
+    Shape S = {};
     // Tiles of eight lanes (a line of every row) leave the least to wait for at the end of a launch; sums of the parameters' gradients
     // want fewer, wider ones.  us, TX = 8 and 16: 200 x 30690 forward 13.8 and 17.8, backward 19.4 and 27.0; 120 x 262143 forward 43.9 and 45.7,
     // backward 101 and 87; 40 x 216000 13.6 and 14.3, 31 and 24.  Eight and four rows a thread: 120 x 96^3 forward with dropout 384 and 351.
     S.ty = rows <= 16 ? 4 : rows <= 32 ? 8 : rows <= 64 ? 16 : rows <= 128 ? 32 : rows <= 256 ? 64 : 128;
     S.tx = rows <= 16 ? 64 : rows <= 32 ? 32 : rows <= 128 && backward ? 16 : 8;
-    S.most = S.ty == 16 ? 1024 : S.ty == 128 ? 256 : 512;       // of 128 to 1024 threads: what a chip holds at once
+    S.most = !backward ? 1L << 20 : S.ty == 16 ? 1024 : S.ty == 128 ? 256 : 512;   // backward, of 256 to 1024 threads: what a chip holds at once
     S.tiles.apart = cols % 32 != 0 || (!backward && S.tx == 8); // rows on 128-byte lines: 120 x 96^3 backward 265 us in order, 277 apart
-    if (rows > S.ty * kRowsHeld || cols < 4 || S.ty * cols >= (1L << 30) - 16) return Shape{};
-    S.held = true;
+    // us, by shares and not: 40 x 1728 6.3 and 3.5, 120 x 8000 8.0 and 4.7, 40 x 32768 7.7 and 18.9, 400 x 8000 12.4 and 14.1
+    S.few = backward && cols <= 12288 && rows <= 256;
+    S.held = rows <= S.ty * kRowsHeld && cols >= 4 && S.ty * cols < (1L << 30) - 16;
     S.tiles.count = (cols + 4 * S.tx - 1) / (4 * S.tx);
     return S;
 }
-int row_groups(const Shape& S) { return S.lanes > 256 ? 1 : 256 / S.lanes; }
+Shape norm_shape(long rows, long cols, int axis, bool backward) { return axis ? rows_shape(rows, cols, backward) : cols_shape(rows, cols, backward); }
 
-// Workgroups of a backward pass, each of which leaves a share of the parameters' gradients
-long bwd_groups(const Shape& S, long rows)
+// Workgroups that walk over the positions.  Backward each leaves a share of the parameters' gradients.
+long position_groups(const Shape& S, long rows)
 {
-    if (S.lanes) return std::min((rows + row_groups(S) - 1) / row_groups(S), S.lanes > 256 ? 256L : 512L);
+    if (S.lanes) return std::min((rows + S.threads / S.lanes - 1) / (S.threads / S.lanes), S.most);
     return std::min((S.tiles.count + 7) / 8 * 8, S.most);
 }
 
+// Shares of the parameters' gradients, 0 where none are left
 int norm_share_count(long rows, long cols, int axis)
 {
     const Shape S = norm_shape(rows, cols, axis, true);
-    return S.held ? (int)bwd_groups(S, rows) : param_shares(rows, cols, axis).count;
+    return !S.held ? param_shares(rows, cols, axis).count : S.few ? 0 : (int)position_groups(S, rows);
 }
 
 size_t norm_workspace(long rows, long cols, int axis)
@@ -857,20 +970,29 @@ template <bool BACKWARD, class F> void with_cols(const Shape& S, F f)
         default: return f(Numbers<8, 128>{});
     }
 }
-template <class F> void with_rows(const Shape& S, F f)
+template <bool BACKWARD, bool FEW, class F> void with_rows(const Shape& S, F f)
 {
-    switch (S.lanes * 8 + S.quads) {
-        case 4 * 8 + 1: return f(Numbers<4, 1>{});
-        case 16 * 8 + 1: return f(Numbers<16, 1>{});
-        case 32 * 8 + 1: return f(Numbers<32, 1>{});
-        case 64 * 8 + 1: return f(Numbers<64, 1>{});
-        case 64 * 8 + 2: return f(Numbers<64, 2>{});
-        case 64 * 8 + 4: return f(Numbers<64, 4>{});
-        case 256 * 8 + 2: return f(Numbers<256, 2>{});
-        case 256 * 8 + 4: return f(Numbers<256, 4>{});
-        case 1024 * 8 + 2: return f(Numbers<1024, 2>{});
-        default: return f(Numbers<1024, 4>{});
+    if constexpr (!FEW) {
+        switch (S.lanes * 8 + S.quads) {
+            case 4 * 8 + 1: return f(Numbers<4, 1, 256>{});
+            case 16 * 8 + 1: return f(Numbers<16, 1, 256>{});
+            case 32 * 8 + 1: return f(Numbers<32, 1, BACKWARD ? 512 : 256>{});
+            case 64 * 8 + 1: return f(Numbers<64, 1, BACKWARD ? 512 : 256>{});
+            case 64 * 8 + 2: return f(Numbers<64, 2, BACKWARD ? 512 : 256>{});
+            case 64 * 8 + 4: return f(Numbers<64, 4, BACKWARD ? 512 : 256>{});
+        }
+        if constexpr (!BACKWARD) {
+            if (S.lanes == 256 && S.quads == 2) return f(Numbers<256, 2, 256>{});
+            if (S.lanes == 256) return f(Numbers<256, 4, 256>{});
+        }
+    } else if (S.lanes == 256) return f(Numbers<256, 1, 256>{});
+    if constexpr (BACKWARD) {
+        if (S.lanes == 512 && S.quads == 1) return f(Numbers<512, 1, 512>{});
+        if (S.lanes == 512) return f(Numbers<512, 2, 512>{});
     }
+    if (S.quads == 2) return f(Numbers<1024, 2, 1024>{});
+    if (S.quads == 3) return f(Numbers<1024, 3, 1024>{});
+    return f(Numbers<1024, 4, 1024>{});
 }
 
 bool on_lines(std::initializer_list<const float*> arrays)
@@ -880,32 +1002,45 @@ bool on_lines(std::initializer_list<const float*> arrays)
 }
 template <int MODE, int TX, int TY> void cols_fwd(const NormFwd& A, const Shape& S, Numbers<TX, TY>, hipStream_t s)
 {
-    const dim3 grid(groups_of((S.tiles.count + 7) / 8 * 8, 1, 1L << 20));
+    const dim3 grid((unsigned)position_groups(S, A.rows));
     if (A.cols % 32 == 0 && on_lines({A.r, A.y}))
         ZNN_LAUNCH("layer norm forward", s, (k_norm_cols<MODE, TX, TY, true>), grid, dim3(TX * TY), 0, A, S.tiles);
     else ZNN_LAUNCH("layer norm forward", s, (k_norm_cols<MODE, TX, TY, false>), grid, dim3(TX * TY), 0, A, S.tiles);
 }
-template <int MODE, int TX, int TY> void cols_bwd(const NormBwd& A, const Shape& S, Numbers<TX, TY>, float* parts, hipStream_t s)
+template <int MODE, int TX, int TY, bool PARTS>
+void cols_bwd(const NormBwd& A, const Shape& S, Numbers<TX, TY>, float* parts, float* gw, float* gb, hipStream_t s)
 {
-    const dim3 grid((unsigned)bwd_groups(S, A.rows));
+    const dim3 grid((unsigned)(position_groups(S, A.rows) + (PARTS ? 0 : A.rows)));
     if (A.cols % 32 == 0 && on_lines({A.gx, A.gh}))
-        ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd<MODE, TX, TY, true>), grid, dim3(TX * TY), 0, A, S.tiles, parts);
-    else ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd<MODE, TX, TY, false>), grid, dim3(TX * TY), 0, A, S.tiles, parts);
+        ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd<MODE, TX, TY, true, PARTS>), grid, dim3(TX * TY), 0, A, S.tiles, parts, gw, gb);
+    else ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd<MODE, TX, TY, false, PARTS>), grid, dim3(TX * TY), 0, A, S.tiles, parts, gw, gb);
 }
-template <int MODE, int L, int NV> void rows_fwd(const NormFwd& A, Numbers<L, NV>, hipStream_t s)
+template <int MODE, int TX, int TY> void few_cols_bwd(const NormBwd& A, const Shape& S, Numbers<TX, TY> n, float* gw, float* gb, hipStream_t s)
 {
-    ZNN_LAUNCH("layer norm forward", s, (k_norm_rows<MODE, L, NV>), dim3(groups_of(A.rows, RowGroup<L>::rows, 4096)), dim3(RowGroup<L>::threads), 0, A);
+    cols_bwd<MODE, TX, TY, false>(A, S, n, nullptr, gw, gb, s);
 }
-template <int MODE, int L, int NV> void rows_bwd(const NormBwd& A, const Shape& S, Numbers<L, NV>, float* parts, hipStream_t s)
+template <int MODE, int TX, int TY>
+void sum_cols_bwd(const NormBwd& A, const Shape& S, Numbers<TX, TY> n, float* parts, float* gw, float* gb, hipStream_t s)
 {
-    ZNN_LAUNCH("layer norm backward", s, (k_norm_rows_bwd<MODE, L, NV>), dim3((unsigned)bwd_groups(S, A.rows)), dim3(RowGroup<L>::threads), 0, A, parts);
+    cols_bwd<MODE, TX, TY, true>(A, S, n, parts, gw, gb, s);
+}
+template <int MODE, int L, int NV, int T> void rows_fwd(const NormFwd& A, const Shape& S, Numbers<L, NV, T>, hipStream_t s)
+{
+    ZNN_LAUNCH("layer norm forward", s, (k_norm_rows<MODE, L, NV, T>), dim3((unsigned)position_groups(S, A.rows)), dim3(T), 0, A);
+}
+template <int MODE, bool PARTS, int L, int NV, int T>
+void rows_bwd(const NormBwd& A, const Shape& S, Numbers<L, NV, T>, float* parts, float* gw, float* gb, hipStream_t s)
+{
+    const long others = PARTS ? 0 : (A.cols + 31) / 32;
+    ZNN_LAUNCH("layer norm backward", s, (k_norm_rows_bwd<MODE, L, NV, T, PARTS>), dim3((unsigned)(position_groups(S, A.rows) + others)), dim3(T), 0, A,
+               parts, gw, gb);
 }
 
 template <int MODE>
 int norm_fwd(const NormFwd& A, int axis, hipStream_t s)
 {
     const Shape S = norm_shape(A.rows, A.cols, axis, false);
-    if (S.held && axis) with_rows(S, [&](auto n) { rows_fwd<MODE>(A, n, s); });
+    if (S.held && axis) with_rows<false, false>(S, [&](auto n) { rows_fwd<MODE>(A, S, n, s); });
     else if (S.held) with_cols<false>(S, [&](auto n) { cols_fwd<MODE>(A, S, n, s); });
     else if (axis) ZNN_LAUNCH("layer norm forward", s, k_norm_rows_any<MODE>, dim3(groups_of(A.rows, 1, 1L << 20)), dim3(1024), 0, A);
     else ZNN_LAUNCH("layer norm forward", s, k_norm_cols_any<MODE>, dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
@@ -917,11 +1052,17 @@ int norm_bwd(const NormBwd& A, int axis, float* gw, float* gb, void* ws, hipStre
 {
     const Shape H = norm_shape(A.rows, A.cols, axis, true);
     const long features = axis ? A.cols : A.rows;
-    if (H.held && axis) with_rows(H, [&](auto n) { rows_bwd<MODE>(A, H, n, (float*)ws, s); });
-    else if (H.held) with_cols<true>(H, [&](auto n) { cols_bwd<MODE>(A, H, n, (float*)ws, s); });
+    float* const parts = (float*)ws;
+    if (H.held && H.few) {
+        if (axis) with_rows<true, true>(H, [&](auto n) { rows_bwd<MODE, false>(A, H, n, parts, gw, gb, s); });
+        else with_cols<true>(H, [&](auto n) { few_cols_bwd<MODE>(A, H, n, gw, gb, s); });
+        return check_launch("layer norm backward");
+    }
+    if (H.held && axis) with_rows<true, false>(H, [&](auto n) { rows_bwd<MODE, true>(A, H, n, parts, gw, gb, s); });
+    else if (H.held) with_cols<true>(H, [&](auto n) { sum_cols_bwd<MODE>(A, H, n, parts, gw, gb, s); });
     else {
         const Shares S = param_shares(A.rows, A.cols, axis);
-        const NormParams P = {A.rows, A.cols, A.gy, A.x, A.stats, (float*)ws, S.count, S.span};
+        const NormParams P = {A.rows, A.cols, A.gy, A.x, A.stats, parts, S.count, S.span};
         if (axis) {
             ZNN_LAUNCH("layer norm backward", s, k_norm_rows_bwd_any<MODE>, dim3(groups_of(A.rows, 1, 1L << 20)), dim3(1024), 0, A);
             ZNN_LAUNCH("layer norm parameters", s, k_norm_params_rows, dim3((unsigned)((A.cols + 63) / 64), (unsigned)S.count), dim3(256), 0, P);
@@ -931,7 +1072,7 @@ int norm_bwd(const NormBwd& A, int axis, float* gw, float* gb, void* ws, hipStre
         }
     }
     ZNN_LAUNCH("layer norm parameters", s, k_norm_params, dim3((unsigned)((2 * features + 15) / 16)), dim3(1024), 0, features,
-               norm_share_count(A.rows, A.cols, axis), (const float*)ws, gw, gb);
+               norm_share_count(A.rows, A.cols, axis), (const float*)parts, gw, gb);
     return check_launch("layer norm backward");
 }
 
