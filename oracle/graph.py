@@ -20,6 +20,8 @@ Edges (tuples; ``name`` keys the edge's parameters):
   ("transfer", name, src, dst[, fn])           params {"b": [f]}
   ("maxfilter", name, src, dst, win[, s])
   ("maxpool", name, src, dst, p)
+  ("layernorm", name, src, dst[, eps])         params {"w": [f], "b": [f]}
+  ("dropout", name, src, dst, p)               times the round's factors of the edge (`factors`), or nothing without them
 The graph is {"inputs": {node: shape}, "edges": [...], "outputs": [node, ...]}; every
 edge's source must be complete before the edge runs, so edges are visited in an order
 in which each node's incoming edges all precede its outgoing ones (checked).
@@ -29,6 +31,7 @@ from __future__ import annotations
 import numpy as np
 
 import oracle
+from oracle.net import normalise, normalise_back
 
 ONES = (1, 1, 1)
 
@@ -60,7 +63,7 @@ def order(graph):
     return out
 
 
-def forward(graph, params, inputs):
+def forward(graph, params, inputs, factors=None):
     """Returns (node images, per-edge auxiliaries: argmax offsets of filters and pools, the
     own output of every transfer edge)."""
     img = {n: np.asarray(v, dtype=np.float64) for n, v in inputs.items()}
@@ -76,13 +79,17 @@ def forward(graph, params, inputs):
             y, aux[name] = oracle.maxfilter3d_fwd(a, e[4], _opt(e, 5, ONES))
         elif kind == "maxpool":
             y, aux[name] = oracle.maxpool3d_fwd(a, e[4])
+        elif kind == "layernorm":
+            y, aux[name] = normalise(a, params[name], _opt(e, 4, 1e-5))
+        elif kind == "dropout":
+            y = a * factors[name] if factors and name in factors else a
         else:
             raise ValueError(e)
         img[dst] = y if dst not in img else img[dst] + y
     return img, aux
 
 
-def backward(graph, params, img, aux, gout):
+def backward(graph, params, img, aux, gout, factors=None):
     """``gout`` maps every output node to d loss / d image.  Returns (parameter gradients
     per edge name, backward images per node)."""
     back = {n: np.asarray(g, dtype=np.float64) for n, g in gout.items()}
@@ -101,19 +108,23 @@ def backward(graph, params, img, aux, gout):
             grads[name] = {"b": gs.reshape(gs.shape[0], -1).sum(axis=1)}
         elif kind == "maxfilter":
             gs = oracle.maxfilter3d_bwd(g, aux[name], img[src].shape[1:], e[4], _opt(e, 5, ONES))
+        elif kind == "layernorm":
+            gs, grads[name] = normalise_back(g, img[src], params[name], aux[name])
+        elif kind == "dropout":
+            gs = g * factors[name] if factors and name in factors else g
         else:
             gs = oracle.maxpool3d_bwd(g, aux[name], img[src].shape[1:], e[4])
         back[src] = gs if src not in back else back[src] + gs
     return grads, back
 
 
-def train_round(graph, params, inputs, targets, eta, loss="square"):
+def train_round(graph, params, inputs, targets, eta, loss="square", factors=None):
     """One round; the loss is summed over the output nodes.  Returns
     (loss value, node images, aux, gradients, updated params)."""
-    img, aux = forward(graph, params, inputs)
+    img, aux = forward(graph, params, inputs, factors)
     value = sum(oracle.loss_value(img[n], targets[n], loss) for n in graph["outputs"])
     gout = {n: oracle.loss_grad(img[n], targets[n], loss) for n in graph["outputs"]}
-    grads, _ = backward(graph, params, img, aux, gout)
+    grads, _ = backward(graph, params, img, aux, gout, factors)
     new = {name: {k: np.asarray(v, dtype=np.float64) - eta * grads[name][k] for k, v in p.items()}
            for name, p in params.items()}
     return value, img, aux, grads, new

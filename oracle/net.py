@@ -15,12 +15,15 @@ Layer specs (tuples; trailing fields optional):
   ("transfer"[, fn])           bias + "rectify" (default) | "logistic" | "tanh"
   ("maxfilter", win[, s])      sliding-window maximum, window taps s apart
   ("maxpool", p)               block maximum
+  ("layernorm"[, eps])         every voxel normalised over the maps (params "w", "b")
+  ("dropout", p)               times the factors of the round (`factors`, by layer), or nothing without them
 """
 from __future__ import annotations
 
 import numpy as np
 
 import oracle
+from oracle import norm
 
 
 ONES = (1, 1, 1)
@@ -30,7 +33,18 @@ def _opt(spec, i, default):
     return spec[i] if len(spec) > i else default
 
 
-def forward(layers, params, x):
+def normalise(a, p, eps):
+    y, m, s = norm.layernorm_fwd(a.reshape(a.shape[0], -1), p["w"], p["b"], eps, 0)
+    return y.reshape(a.shape), (m, s)
+
+
+def normalise_back(g, a, p, stats):
+    rows = a.shape[0]
+    gx, gw, gb = norm.layernorm_bwd(g.reshape(rows, -1), a.reshape(rows, -1), p["w"], *stats, 0)
+    return gx.reshape(a.shape), {"w": gw, "b": gb}
+
+
+def forward(layers, params, x, factors=None):
     """Returns the list of node images: acts[0] = input, acts[l+1] = output of layer l.
     For max-filter layers the argmax offsets are kept in aux[l]."""
     acts = [np.asarray(x, dtype=np.float64)]
@@ -45,13 +59,17 @@ def forward(layers, params, x):
             y, aux[l] = oracle.maxfilter3d_fwd(a, spec[1], _opt(spec, 2, ONES))
         elif spec[0] == "maxpool":
             y, aux[l] = oracle.maxpool3d_fwd(a, spec[1])
+        elif spec[0] == "layernorm":
+            y, aux[l] = normalise(a, params[l], _opt(spec, 1, 1e-5))
+        elif spec[0] == "dropout":
+            y = a if factors is None else a * factors[l]
         else:
             raise ValueError(spec)
         acts.append(y)
     return acts, aux
 
 
-def backward(layers, params, acts, aux, gout):
+def backward(layers, params, acts, aux, gout, factors=None):
     """Gradients of the loss w.r.t. every parameter, given d loss / d output."""
     grads = [None] * len(layers)
     g = np.asarray(gout, dtype=np.float64)
@@ -68,14 +86,18 @@ def backward(layers, params, acts, aux, gout):
             g = oracle.maxfilter3d_bwd(g, aux[l], acts[l].shape[1:], spec[1], _opt(spec, 2, ONES))
         elif spec[0] == "maxpool":
             g = oracle.maxpool3d_bwd(g, aux[l], acts[l].shape[1:], spec[1])
+        elif spec[0] == "layernorm":
+            g, grads[l] = normalise_back(g, acts[l], params[l], aux[l])
+        elif spec[0] == "dropout":
+            g = g if factors is None else g * factors[l]
     return grads
 
 
-def train_round(layers, params, x, target, eta, loss="square"):
+def train_round(layers, params, x, target, eta, loss="square", factors=None):
     """One round; returns (loss value, acts, aux, grads, updated params)."""
-    acts, aux = forward(layers, params, x)
+    acts, aux = forward(layers, params, x, factors)
     value = oracle.loss_value(acts[-1], target, loss)
-    grads = backward(layers, params, acts, aux, oracle.loss_grad(acts[-1], target, loss))
+    grads = backward(layers, params, acts, aux, oracle.loss_grad(acts[-1], target, loss), factors)
     loss = value
     new = []
     for p, g in zip(params, grads):

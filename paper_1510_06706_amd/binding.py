@@ -45,6 +45,7 @@ STATIC_SCRATCH_BYTES = 32 * 1024 * 1024
 SPECTRA_LAYOUTS = {"auto": 0, "full": 1, "folded": 2}
 STRATEGIES = ("direct", "fft", "fft_memo")
 TRANSFER_FNS = {"rectify": 0, "logistic": 1, "tanh": 2}
+NORM_EPS = 1e-5
 
 
 class Vec3(ctypes.Structure):
@@ -532,7 +533,7 @@ def dropout(x, p, state=None, site=0, stream=None):
     return y
 
 
-def layernorm_fwd(x, w, b, eps=1e-5, axis=0, stats=True, stream=None):
+def layernorm_fwd(x, w, b, eps=NORM_EPS, axis=0, stats=True, stream=None):
     """(y, stats): stats, for ``layernorm_bwd``, holds mean and 1 / deviation of every position (None if not asked for)."""
     rows, cols, positions = _extents(x, axis, w, b)
     with _on(stream):
@@ -573,7 +574,7 @@ def layernorm_bwd(gy, x, w, stats, axis=0, stream=None):
     return gx, gw, gb
 
 
-def residual_norm_fwd(h, x, w, b, p=0.0, state=None, site=0, eps=1e-5, axis=0, stats=True, stream=None):
+def residual_norm_fwd(h, x, w, b, p=0.0, state=None, site=0, eps=NORM_EPS, axis=0, stats=True, stream=None):
     """(r, y, stats) with r = x + dropout(h), y = layernorm(r): the end of a residual branch in one pass."""
     rows, cols, positions = _extents(x, axis, w, b)
     _same_shape(x, h)

@@ -16,15 +16,20 @@
 
 namespace znn {
 
-int make_drop(double p, const uint64_t* state, uint32_t site, Drop* drop, bool* drops)
+// dropped: how many of 2^32
+static int make_drop_parts(double dropped, const uint64_t* state, uint32_t site, Drop* drop, bool* drops)
 {
-    if (!(p >= 0.0 && p <= 1.0)) return fail(ZNN_EINVAL, "the probability to drop must lie in [0, 1]");
-    const double keep = 4294967296.0 - std::floor(p * 4294967296.0 + 0.5);
-    *drops = keep < 4294967296.0;
+    const double keep = 4294967296.0 - dropped;
+    *drops = dropped > 0.0;
     *drop = Drop{state, site, *drops ? (unsigned)keep : 0u, keep > 0.0 ? (float)(4294967296.0 / keep) : 0.f};
     if (*drops && !state) return fail(ZNN_EINVAL, "dropout needs a random state");
     if (*drops && ((uintptr_t)state & 7)) return fail(ZNN_EINVAL, "the random state is not 8-byte aligned");
     return ZNN_OK;
+}
+static int make_drop(double p, const uint64_t* state, uint32_t site, Drop* drop, bool* drops)
+{
+    if (!(p >= 0.0 && p <= 1.0)) return fail(ZNN_EINVAL, "the probability to drop must lie in [0, 1]");
+    return make_drop_parts(std::floor(p * 4294967296.0 + 0.5), state, site, drop, drops);
 }
 
 namespace {
@@ -931,10 +936,6 @@ int norm_share_count(long rows, long cols, int axis)
     return !S.held ? param_shares(rows, cols, axis).count : S.few ? 0 : (int)position_groups(S, rows);
 }
 
-size_t norm_workspace(long rows, long cols, int axis)
-{
-    return sizeof(float) * 2 * norm_share_count(rows, cols, axis) * (axis ? cols : rows);
-}
 
 unsigned groups_of(long work, long each, long most) { return (unsigned)std::min((work + each - 1) / each, most); }
 
@@ -1076,7 +1077,28 @@ int norm_bwd(const NormBwd& A, int axis, float* gw, float* gb, void* ws, hipStre
     return check_launch("layer norm backward");
 }
 
+int launch_dropout(long rows, long cols, const Drop& D, bool drops, const float* x, float* y, hipStream_t s)
+{
+    const long quads = (cols + 3) / 4;
+    if (drops) ZNN_LAUNCH("dropout", s, k_dropout, dim3(groups_of(rows * quads, 256, 1L << 20)), dim3(256), 0, rows, cols, quads, D, x, y);
+    else ZNN_LAUNCH("dropout", s, k_copy, dim3(groups_of(rows * cols, 256, 1L << 20)), dim3(256), 0, rows * cols, x, y);
+    return check_launch("dropout");
+}
+
 }  // namespace
+
+size_t norm_workspace(long rows, long cols, int axis)
+{
+    return sizeof(float) * 2 * norm_share_count(rows, cols, axis) * (axis ? cols : rows);
+}
+
+int dropout_parts(long rows, long cols, unsigned dropped, const uint64_t* state, uint32_t site, const float* x, float* y, hipStream_t s)
+{
+    Drop D;
+    bool drops;
+    const int rc = make_drop_parts(dropped, state, site, &D, &drops);
+    return rc != ZNN_OK ? rc : launch_dropout(rows, cols, D, drops, x, y, s);
+}
 
 }  // namespace znn
 
@@ -1101,11 +1123,7 @@ int znn_dropout(int64_t rows, int64_t cols, double p, const uint64_t* state, uin
     bool drops;
     rc = make_drop(p, state, site, &D, &drops);
     if (rc != ZNN_OK) return rc;
-    const hipStream_t s = (hipStream_t)stream;
-    const long quads = (cols + 3) / 4;
-    if (drops) ZNN_LAUNCH("dropout", s, k_dropout, dim3(groups_of(rows * quads, 256, 1L << 20)), dim3(256), 0, (long)rows, (long)cols, quads, D, x, y);
-    else ZNN_LAUNCH("dropout", s, k_copy, dim3(groups_of(rows * cols, 256, 1L << 20)), dim3(256), 0, (long)(rows * cols), x, y);
-    return check_launch("dropout");
+    return launch_dropout((long)rows, (long)cols, D, drops, x, y, (hipStream_t)stream);
 }
 
 int znn_layernorm_workspace_bytes(int64_t rows, int64_t cols, int32_t axis, size_t* bytes)

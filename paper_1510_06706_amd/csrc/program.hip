@@ -17,6 +17,7 @@
 // Six-layer 3D net on a 12^3 patch: 78 -> 31 launches, 617 -> 413 us on the fp32 direct kernels, 268 us on those on split operands: chains
 // of kernels of 4 to 26 us (direct passes 144 us, gradients with their copies and sums 85 us, the rest 2 to 9 us each).
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <new>
 #include <vector>
@@ -193,6 +194,7 @@ struct Layer {
 
 long elements(const znn_op& o) { return (long)o.maps * o.n.z * o.n.y * o.n.x; }
 long voxels(const znn_op& o) { return (long)o.n.z * o.n.y * o.n.x; }
+float norm_eps(const znn_op& o) { float v; memcpy(&v, &o.window.x, sizeof v); return v; }
 int bias_spans(const znn_op& o) { return (int)((voxels(o) + kBiasSpan - 1) / kBiasSpan); }
 
 }  // namespace
@@ -240,6 +242,10 @@ constexpr Form kForm[] = {
     {7u, 4, 0x03u, 0x0cu},      // LOSS_GRAD
     {3u, 8, 0xfeu, 0x01u},      // NODE_SUM
     {3u, 2, 0x03u, 0x02u},      // UPDATE
+    {0x0fu, 5, 0x07u, 0x18u},   // NORM_FWD
+    {0x7fu, 7, 0x0fu, 0x70u},   // NORM_BWD
+    {7u, 3, 0x03u, 0x04u},      // DROPOUT
+    {1u, 1, 0x01u, 0x01u},      // RANDOM_ADVANCE
 };
 
 bool uses(const Step& s, unsigned positions, int buffer)
@@ -269,7 +275,7 @@ bool touched_between(const znn_program& P, int buffer, int first, int last)
 
 int check_op(const znn_op& o, int i, int buffers, int streams)
 {
-    if (o.kind < ZNN_OP_CONV_FWD || o.kind > ZNN_OP_UPDATE) return fail(ZNN_EINVAL, "operation %d: unknown kind %d", i, o.kind);
+    if (o.kind < ZNN_OP_CONV_FWD || o.kind > ZNN_OP_RANDOM_ADVANCE) return fail(ZNN_EINVAL, "operation %d: unknown kind %d", i, o.kind);
     if (o.stream < 0 || o.stream >= streams) return fail(ZNN_EINVAL, "operation %d: no stream %d", i, o.stream);
     const Form& form = kForm[o.kind];
     for (int b = 0; b < 8; ++b) {
@@ -292,6 +298,8 @@ int check_op(const znn_op& o, int i, int buffers, int streams)
     if (o.maps < 1 || o.n.z < 1 || o.n.y < 1 || o.n.x < 1) return fail(ZNN_EINVAL, "operation %d: maps and extents must be >= 1", i);
     if ((double)o.maps * o.n.z * o.n.y * o.n.x / 256 >= 2147483647.0)
         return fail(ZNN_EUNSUPPORTED, "operation %d: too many elements for one launch", i);
+    if (o.kind == ZNN_OP_NORM_FWD && !(norm_eps(o) > 0.f && norm_eps(o) < INFINITY))
+        return fail(ZNN_EINVAL, "operation %d: eps must be positive and finite", i);
     if (o.kind == ZNN_OP_FILTER_FWD || o.kind == ZNN_OP_FILTER_BWD || o.kind == ZNN_OP_POOL_FWD || o.kind == ZNN_OP_POOL_BWD)
         return check_filter(o.maps, o.n, o.window, o.sparsity, o.kind == ZNN_OP_POOL_FWD || o.kind == ZNN_OP_POOL_BWD);
     return ZNN_OK;
@@ -347,7 +355,8 @@ int place_steps(znn_program& P, const znn_op* ops, int count)
         int i = u - 1;
         while (i >= 0 && !uses(P.steps[i], writes(P.steps[i]), o.buf[0])) --i;
         const Step* made = i < 0 ? nullptr : &P.steps[i];
-        const long have = !made ? -1 : made->kind == ZNN_OP_BIAS_GRAD ? made->op.maps
+        const bool of_norm = made && made->kind == ZNN_OP_NORM_BWD && made->op.buf[4] != o.buf[0];
+        const long have = !made ? -1 : made->kind == ZNN_OP_BIAS_GRAD || of_norm ? made->op.maps
                         : made->kind == ZNN_OP_CONV_WGRAD ? (long)made->op.plan->g.f * made->op.plan->g.fo * made->op.plan->g.kvol() : -1;
         if (have >= 0 && have != elements(o))
             return fail(ZNN_EINVAL, "operation %d: an update of %ld elements from a gradient of %ld", u - 1, elements(o), have);
@@ -452,6 +461,7 @@ int place_steps(znn_program& P, const znn_op* ops, int count)
     // scratch of the passes: one area per stream
     std::vector<size_t> need(P.streams, 0);
     for (Step& s : P.steps) {
+        if (s.kind == ZNN_OP_NORM_BWD) need[s.stream] = std::max(need[s.stream], align256(norm_workspace(s.op.maps, voxels(s.op), 0)));
         if (s.layer < 0 || s.copies != kNone || (s.kind == ZNN_OP_CONV_WGRAD && P.layers[s.layer].joined)) continue;
         const Layer& L = P.layers[s.layer];
         const Geom& g = L.plan.g;
@@ -763,6 +773,12 @@ int run_step(znn_program& P, Step& t, float* const* buf, char* scratch, float et
             ZNN_LAUNCH("loss gradient", s, k_loss_finish, dim3(blocks_of(count)), dim3(256), 0, count, at(0), at(1), at(2), at(3), o.loss, o.fn);
             return check_launch("loss gradient");
         case ZNN_OP_UPDATE: return znn_sgd_update(count, eta, at(0), at(1), s);
+        case ZNN_OP_NORM_FWD: return znn_layernorm_fwd(o.maps, voxels(o), 0, norm_eps(o), at(0), at(1), at(2), at(3), at(4), s);
+        case ZNN_OP_NORM_BWD:
+            return znn_layernorm_bwd(o.maps, voxels(o), 0, at(0), at(1), at(2), at(3), at(4), at(5), at(6), scratch + P.area[t.stream],
+                                     norm_workspace(o.maps, voxels(o), 0), s);
+        case ZNN_OP_DROPOUT: return dropout_parts(o.maps, voxels(o), (unsigned)o.sparsity.x, (const uint64_t*)at(1), (uint32_t)o.window.x, at(0), at(2), s);
+        case ZNN_OP_RANDOM_ADVANCE: return znn_random_advance((uint64_t*)at(0), s);
         case ZNN_OP_NODE_SUM: {
             SumArgs A = {};
             for (int q = 1; q < 7 && o.buf[q] >= 0; ++q) A.part[A.parts++] = at(q);

@@ -69,7 +69,4 @@ __device__ __forceinline__ void store4(float* p, int count, floatu4 v)
     if (count > 2) p[2] = v[2];
 }
 
-// Checks p and the state and says what is dropped; `drops` is false where nothing is (p = 0, or less than half of 2^-32).
-int make_drop(double p, const uint64_t* state, uint32_t site, Drop* drop, bool* drops);
-
 }  // namespace znn

@@ -286,6 +286,9 @@ int fill_pattern(float* p, long count, float scale, hipStream_t s);
 // max-filter backward, times the derivative of the transfer function that gave y (y may be NULL)
 int maxfilter_bwd(int32_t maps, znn_vec3 n, znn_vec3 win, znn_vec3 sp, const float* gout, const int32_t* idx, float* gin,
                   const float* y, int fn, hipStream_t s);
+// dropout of `dropped` parts in 2^32, and what a backward layer norm takes as its workspace
+int dropout_parts(long rows, long cols, unsigned dropped, const uint64_t* state, uint32_t site, const float* x, float* y, hipStream_t s);
+size_t norm_workspace(long rows, long cols, int axis);
 int check_filter(int32_t maps, znn_vec3 n, znn_vec3 win, znn_vec3 sp, bool pool);
 
 // ---------------------------------------------------------------- passes of a plan with buffers given by the caller

@@ -67,7 +67,11 @@ class GraphNet:
     reused while another stream still reads it.
 
     ``streams`` is the number of side streams.  None stands for four, of which a round uses all or, where it is
-    small, none; a number is kept to by every round."""
+    small, none; a number is kept to by every round.
+
+    Layer norms (every voxel over the maps) and dropout are edges like the others.  Dropout drops in rounds and in passes
+    with ``train``, by the device's {seed, round} in ``random`` (``seed`` sets it, a round moves it on by one); with p = 0
+    it hands its image on: the edge that a residual branch passes by."""
 
     # Multiply-adds of a round's convolutions by the direct method, times two, from which on several streams may be the faster ones.  Multi-scale nets, us a round
     # on several streams and on one: width 8, 20^3 443 and 164; 16, 40^3 (6e9) 483 and 311; 32, 40^3 (2.4e10) 543 and 510; 40, 36^3 (2.5e10) 551 and 555;
@@ -76,7 +80,7 @@ class GraphNet:
     # two to eight, two to four layers deep, 2D and 3D, either method (1e8 to 5.5e10), one took 0.35 to 0.98 of the time of several.
     SEVERAL_STREAMS = 3e10
 
-    def __init__(self, graph, params, mode="auto", device="cuda:0", streams=None):
+    def __init__(self, graph, params, mode="auto", device="cuda:0", streams=None, seed=0):
         import torch
         self.graph = graph
         self.device = device
@@ -87,6 +91,10 @@ class GraphNet:
         self.streams = [torch.cuda.Stream(device=device) for _ in range(4 if streams is None else max(1, int(streams)))]
         self._given_streams = streams is not None
         self._programs = {}
+        for e in self.edges:
+            if e[0] == "dropout":
+                zp.drop_parts(e[4])
+        self.random = znn.random_state(seed, device) if any(e[0] == "dropout" for e in self.edges) else None
         self._events, self._next_event = [], 0      # events are reused from round to round
         self.incoming, self.outgoing = {}, {}
         for e in self.edges:
@@ -137,8 +145,9 @@ class GraphNet:
         return total
 
     # ------------------------------------------------------------ passes
-    def forward(self, inputs):
-        """inputs: {node: CUDA tensor}.  Returns (node images, per-edge aux, node events)."""
+    def forward(self, inputs, train=False):
+        """inputs: {node: CUDA tensor}.  Returns (node images, per-edge aux, node events).  ``train``: as in a training
+        round, with dropout and what ``backward`` needs of norms."""
         import torch
         main = torch.cuda.current_stream()
         self._next_event = 0
@@ -158,6 +167,11 @@ class GraphNet:
                 y = aux[name] = znn.transfer_fwd(a, self.params[name]["b"], _opt(e, 4, "rectify"), stream=s)
             elif kind == "maxfilter":
                 y, aux[name] = znn.maxfilter3d_fwd(a, e[4], _opt(e, 5, ONES), stream=s)
+            elif kind == "layernorm":
+                y, aux[name] = znn.layernorm_fwd(a, self.params[name]["w"], self.params[name]["b"], _opt(e, 4, znn.NORM_EPS), stats=train,
+                                                 stream=s)
+            elif kind == "dropout":
+                y = znn.dropout(a, e[4], self.random, i, stream=s) if train and e[4] != 0 else a
             else:
                 y, aux[name] = znn.maxpool3d_fwd(a, e[4], stream=s)
             parts.setdefault(dst, {})[name] = y
@@ -208,6 +222,11 @@ class GraphNet:
                 grads[name] = {"b": znn.bias_grad(gs, stream=s)}
             elif kind == "maxfilter":
                 gs = znn.maxfilter3d_bwd(g, aux[name], self.shapes[src][1:], e[4], _opt(e, 5, ONES), stream=s)
+            elif kind == "layernorm":
+                gs, gw, gb = znn.layernorm_bwd(g, img[src], self.params[name]["w"], aux[name], stream=s)
+                grads[name] = {"w": gw, "b": gb}
+            elif kind == "dropout":
+                gs = znn.dropout(g, e[4], self.random, len(self.edges) - 1 - i, stream=s) if e[4] != 0 else g
             else:
                 gs = znn.maxpool3d_bwd(g, aux[name], self.shapes[src][1:], e[4], stream=s)
             ev = self._event(s)
@@ -246,6 +265,9 @@ class GraphNet:
                 given[e[1], "w"] = P.buffer("given", (e[4], shape[e[2]][0]) + tuple(e[5]))
             elif e[0] == "transfer":
                 given[e[1], "b"] = P.buffer("given", shape[e[2]][:1])
+            elif e[0] == "layernorm":
+                given[e[1], "w"], given[e[1], "b"] = P.buffer("given", shape[e[2]][:1]), P.buffer("given", shape[e[2]][:1])
+        random = None if self.random is None else P.buffer("given", (4,))
         by_name = {e[1]: e for e in E}
 
         def parts_sum(out, parts, at, dims):
@@ -262,7 +284,9 @@ class GraphNet:
         for i, e in enumerate(E):
             kind, name, src, dst = e[:4]
             how = dict(stream=stream(i), maps=shape[src][0], n=shape[src][1:])
-            if name not in part:                # a transfer edge may have been taken over by the convolution before it
+            if kind == "dropout" and e[4] == 0:
+                part[name] = img[src]
+            elif name not in part:              # a transfer edge may have been taken over by the convolution before it
                 y = part[name] = P.buffer("fresh" if alone(dst) or kind == "transfer" else "kept", shape[dst])
                 if kind == "conv":
                     op = P.add(zp.CONV_FWD, (img[src], given[name, "w"], y), stream=stream(i), plan=self.plans[name])
@@ -273,6 +297,12 @@ class GraphNet:
                 elif kind == "transfer":
                     aux[name] = y
                     P.add(zp.TRANSFER_FWD, (img[src], given[name, "b"], y), fn=_opt(e, 4, "rectify"), **how)
+                elif kind == "layernorm":
+                    aux[name] = P.buffer("fresh", (2, math.prod(shape[src][1:])))
+                    P.add(zp.NORM_FWD, (img[src], given[name, "w"], given[name, "b"], y, aux[name]), window=zp.eps_bits(_opt(e, 4, znn.NORM_EPS)),
+                          **how)
+                elif kind == "dropout":
+                    P.add(zp.DROPOUT, (img[src], random, y), window=(0, 0, i), sparsity=zp.drop_parts(e[4]), **how)
                 else:
                     aux[name] = P.buffer("fresh", shape[dst], True)
                     P.add(zp.FILTER_FWD if kind == "maxfilter" else zp.POOL_FWD, (img[src], y, aux[name]), window=e[4],
@@ -332,6 +362,16 @@ class GraphNet:
                     gop = P.add(zp.TRANSFER_BWD, (b, aux[name], gs), fn=_opt(e, 4, "rectify"), **how)
                 grads[name] = {"b": P.buffer("gradient", (shape[src][0],))}
                 P.add(zp.BIAS_GRAD, (gs, grads[name]["b"]), **how)
+            elif kind == "layernorm":
+                gs = P.buffer("kept", shape[src])
+                grads[name] = {k: P.buffer("gradient", shape[src][:1]) for k in ("w", "b")}
+                gop = P.add(zp.NORM_BWD, (b, img[src], given[name, "w"], aux[name], gs, grads[name]["w"], grads[name]["b"]), **how)
+            elif kind == "dropout":
+                if e[4] == 0:
+                    gs, gop = b, dict(op, kind=None)
+                elif needed:
+                    gs = P.buffer("kept", shape[src])
+                    gop = P.add(zp.DROPOUT, (b, random, gs), window=(0, 0, len(E) - 1 - i), sparsity=zp.drop_parts(e[4]), **how)
             elif needed:
                 gs = P.buffer("kept", shape[src])
                 gop = P.add(zp.FILTER_BWD if kind == "maxfilter" else zp.POOL_BWD, (b, aux[name], gs), window=e[4],
@@ -344,6 +384,9 @@ class GraphNet:
         for n, d in grads.items():
             for k in d:
                 P.add(zp.UPDATE, (d[k], given[n, k]), n=(1, 1, math.prod(P.shapes[d[k]])))
+        if random is not None:
+            P.add(zp.RANDOM_ADVANCE, (random,))
+            given["random", "state"] = random
         return P.build(), given, targets, img, aux, gout, grads
 
     def train_round(self, inputs, targets, eta, loss="square"):
@@ -356,7 +399,9 @@ class GraphNet:
         P, given, target, img, aux, gout, grads = self._programs[loss]
         tensors = {given[n, "x"]: zp.check_input(inputs[n], self.shapes[n]) for n in self.graph["inputs"]}
         for (n, k), b in given.items():
-            if k != "x":
+            if k == "state":
+                tensors[b] = self.random
+            elif k != "x":
                 tensors[b] = zp.check_parameter(self.params[n][k], k, P.shapes[b])
         for n, b in target.items():
             tensors[b] = zp.check_input(targets[n], count=math.prod(self.shapes[n]))

@@ -25,9 +25,13 @@ class Net:
     fastest one whose buffers fit ``memory_budget`` bytes (per layer; None = no limit).  "fft_memo"
     (in a list) attaches memo buffers to the layer's plan, and rounds go layer by layer to leave the
     spectra there; rounds of tuned nets are programs, which memoize in their own memory.
+
+    Beside the paper's layers: ("layernorm"[, eps]) normalises every voxel over its maps, with parameters "w" and "b", and
+    ("dropout", p) drops elements in training rounds (nothing in a forward pass alone).  What is dropped follows from
+    ``random``, the device's {seed, round}, which a round moves on by one; ``seed`` sets it.
     """
 
-    def __init__(self, layers, in_shape, params, mode="auto", device="cuda:0", memory_budget=None):
+    def __init__(self, layers, in_shape, params, mode="auto", device="cuda:0", memory_budget=None, seed=0):
         import torch
         self.layers = list(layers)
         self.shapes = shapes(layers, in_shape)
@@ -59,6 +63,10 @@ class Net:
             else:
                 self.plans.append(None)
         self._programs = {}
+        for spec in self.layers:
+            if spec[0] == "dropout":
+                zp.drop_parts(spec[1])
+        self.random = znn.random_state(seed, device) if any(s[0] == "dropout" for s in self.layers) else None
 
     @property
     def _by_layer(self):
@@ -88,8 +96,17 @@ class Net:
                 given[l, "w"] = P.buffer("given", (spec[2], spec[1]) + tuple(spec[3]))
             elif spec[0] == "transfer":
                 given[l, "b"] = P.buffer("given", shape[l][:1])
+            elif spec[0] == "layernorm":
+                given[l, "w"], given[l, "b"] = P.buffer("given", shape[l][:1]), P.buffer("given", shape[l][:1])
+        random = None
+        if loss is not None and self.random is not None:
+            random = given["random", "x"] = P.buffer("given", (4,))
         act, aux, conv = [given[0, "x"]], [None] * len(L), None
         for l, spec in enumerate(L):
+            if spec[0] == "dropout" and (random is None or spec[1] == 0):       # nothing is dropped
+                act.append(act[-1])
+                conv = None
+                continue
             kind, y = spec[0], P.buffer("fresh", shape[l + 1])
             if kind == "conv":
                 conv = P.add(zp.CONV_FWD, (act[-1], given[l, "w"], y), plan=self.plans[l])
@@ -97,6 +114,13 @@ class Net:
                 fn = _opt(spec, 1, "rectify")
                 if conv is None or not P.attach(conv, fn, y, given[l, "b"]):
                     P.add(zp.TRANSFER_FWD, (act[-1], given[l, "b"], y), fn=fn, maps=shape[l][0], n=shape[l][1:])
+            elif kind == "layernorm":
+                if loss is not None:
+                    aux[l] = P.buffer("fresh", (2, math.prod(shape[l][1:])))
+                P.add(zp.NORM_FWD, (act[-1], given[l, "w"], given[l, "b"], y, -1 if aux[l] is None else aux[l]), maps=shape[l][0],
+                      n=shape[l][1:], window=zp.eps_bits(_opt(spec, 1, znn.NORM_EPS)))
+            elif kind == "dropout":
+                P.add(zp.DROPOUT, (act[-1], random, y), maps=shape[l][0], n=shape[l][1:], window=(0, 0, l), sparsity=zp.drop_parts(spec[1]))
             else:
                 aux[l] = P.buffer("fresh", shape[l + 1], True)
                 P.add(zp.FILTER_FWD if kind == "maxfilter" else zp.POOL_FWD, (act[-1], y, aux[l]), maps=shape[l][0],
@@ -130,6 +154,16 @@ class Net:
                         g = below()
                         op = P.add(zp.CONV_BWD, (ready, given[l, "w"], g), plan=self.plans[l])
                     P.add(zp.CONV_WGRAD, (act[l], ready, grads[l]["w"]), plan=self.plans[l])
+                elif kind == "layernorm":
+                    grads[l] = {k: P.buffer("gradient", shape[l][:1]) for k in ("w", "b")}
+                    h = below()
+                    op = P.add(zp.NORM_BWD, (g, act[l], given[l, "w"], aux[l], h, grads[l]["w"], grads[l]["b"]), **how)
+                    g = h
+                elif kind == "dropout":
+                    if spec[1] != 0 and l > 0:
+                        h = below()
+                        op = P.add(zp.DROPOUT, (g, random, h), window=(0, 0, l), sparsity=zp.drop_parts(spec[1]), **how)
+                        g = h
                 elif l > 0:
                     h = below()
                     op = P.add(zp.FILTER_BWD if kind == "maxfilter" else zp.POOL_BWD, (g, aux[l], h), window=spec[1],
@@ -138,6 +172,8 @@ class Net:
             for l, d in enumerate(grads):
                 for k in d or ():
                     P.add(zp.UPDATE, (d[k], given[l, k]), n=(1, 1, math.prod(P.shapes[d[k]])))
+            if random is not None:
+                P.add(zp.RANDOM_ADVANCE, (random,))
         self._programs[loss] = P.build(), given, act, aux, target, gout, grads
         return self._programs[loss]
 
@@ -145,22 +181,26 @@ class Net:
         P, given, act, aux, t, gout, grads = self._program(loss)
         tensors = {given[0, "x"]: zp.check_input(x, self.shapes[0])}
         for (l, k), b in given.items():
-            if k != "x":
+            if l == "random":
+                tensors[b] = self.random
+            elif k != "x":
                 tensors[b] = zp.check_parameter(self.params[l][k], k, P.shapes[b])
         if loss is not None:
             tensors[t] = zp.check_input(target, count=math.prod(self.shapes[-1]))
         out = P.run(tensors, float(eta))
+        out[given[0, "x"]] = x          # what a layer that drops nothing hands on
         return ([x] + [out[b] for b in act[1:]], [None if b is None else out[b] for b in aux],
                 None if gout is None else out[gout],
                 [None if d is None else {k: out[b] for k, b in d.items()} for d in grads])
 
-    def forward(self, x):
+    def forward(self, x, train=False):
+        """(node images, per-layer aux).  ``train``: as in a training round, with dropout and what ``backward`` needs of norms."""
         # without convolutions, inputs of any extent pass
-        if self._by_layer or tuple(x.shape) != tuple(self.shapes[0]):
-            return self._forward_by_layer(x)
+        if train or self._by_layer or tuple(x.shape) != tuple(self.shapes[0]):
+            return self._forward_by_layer(x, train)
         return self._run(None, x)[:2]
 
-    def _forward_by_layer(self, x):
+    def _forward_by_layer(self, x, train=True):
         """One library call per layer: what plans with memoized spectra of their own need before ``backward``."""
         acts, aux = [x], [None] * len(self.layers)
         for l, spec in enumerate(self.layers):
@@ -174,6 +214,10 @@ class Net:
                 y = znn.transfer_fwd(a, self.params[l]["b"], _opt(spec, 1, "rectify"))
             elif spec[0] == "maxfilter":
                 y, aux[l] = znn.maxfilter3d_fwd(a, spec[1], _opt(spec, 2, ONES))
+            elif spec[0] == "layernorm":
+                y, aux[l] = znn.layernorm_fwd(a, self.params[l]["w"], self.params[l]["b"], _opt(spec, 1, znn.NORM_EPS), stats=train)
+            elif spec[0] == "dropout":
+                y = znn.dropout(a, spec[1], self.random, l) if train and spec[1] != 0 else a
             else:
                 y, aux[l] = znn.maxpool3d_fwd(a, spec[1])
             acts.append(y)
@@ -199,6 +243,12 @@ class Net:
                 grads[l] = {"b": znn.bias_grad(g)}
             elif spec[0] == "maxfilter":
                 g = znn.maxfilter3d_bwd(g, aux[l], self.shapes[l][1:], spec[1], _opt(spec, 2, ONES))
+            elif spec[0] == "layernorm":
+                g, gw, gb = znn.layernorm_bwd(g, acts[l], self.params[l]["w"], aux[l])
+                grads[l] = {"w": gw, "b": gb}
+            elif spec[0] == "dropout":
+                if spec[1] != 0:
+                    g = znn.dropout(g, spec[1], self.random, l)
             else:
                 g = znn.maxpool3d_bwd(g, aux[l], self.shapes[l][1:], spec[1])
         return grads
@@ -215,6 +265,8 @@ class Net:
             if p is not None:
                 for k in p:
                     znn.sgd_update(p[k], g[k], eta)
+        if self.random is not None:
+            znn.random_advance(self.random)
         return acts, aux, gout, grads
 
     def capture_round(self, x, target, eta, loss="square"):
@@ -229,7 +281,10 @@ class Net:
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):       # warm-up outside the graph: plans grow their workspaces
             saved = [None if p is None else {k: v.clone() for k, v in p.items()} for p in self.params]
+            random = None if self.random is None else self.random.clone()
             self.train_round(x, target, eta, loss=loss)
+            if random is not None:
+                self.random.copy_(random)
             for p, q in zip(self.params, saved):
                 if p is not None:
                     for k in p:

@@ -14,7 +14,7 @@ from . import binding as znn
 from .binding import TRANSFER_FNS
 
 (CONV_FWD, CONV_BWD, CONV_WGRAD, TRANSFER_FWD, TRANSFER_BWD, BIAS_GRAD, FILTER_FWD, FILTER_BWD, POOL_FWD, POOL_BWD,
- LOSS_GRAD, NODE_SUM, UPDATE) = range(13)
+ LOSS_GRAD, NODE_SUM, UPDATE, NORM_FWD, NORM_BWD, DROPOUT, RANDOM_ADVANCE) = range(17)
 LOSSES = {"square": 0, "cross_entropy": 1}
 OP = struct.Struct("@22iP")         # the fields of binding.Op
 assert OP.size == ctypes.sizeof(znn.Op)
@@ -169,6 +169,19 @@ class Program:
             shape = self.shapes[b]
             out[b] = slab[at // 4:at // 4 + math.prod(shape)].view(shape)
         return out
+
+
+def eps_bits(eps):
+    """What an operation takes as its `window`: eps as the bits of a float."""
+    return (0, 0, struct.unpack("i", struct.pack("f", eps))[0])
+
+
+def drop_parts(p):
+    """What an operation takes as its `sparsity`: how many of 2^32 elements are dropped, as 32 bits."""
+    n = math.floor(p * 2 ** 32 + 0.5) if 0 <= p < 1 else 1 << 32
+    if n >> 32:
+        raise ValueError("the probability to drop must lie in [0, 1), got %r" % (p,))
+    return (0, 0, n - (1 << 32) if n >> 31 else n)
 
 
 def check_input(t, shape=None, count=None):

@@ -154,7 +154,7 @@ def shapes(layers, in_shape):
         if spec[0] == "conv":
             assert spec[1] == m
             out.append((spec[2],) + tuple(a - s * (b - 1) for a, b, s in zip(n, spec[3], _opt(spec, 4, ONES))))
-        elif spec[0] == "transfer":
+        elif spec[0] in ("transfer", "layernorm", "dropout"):
             out.append(out[-1])
         elif spec[0] == "maxfilter":
             out.append((m,) + tuple(a - s * (b - 1) for a, b, s in zip(n, spec[1], _opt(spec, 2, ONES))))
@@ -167,7 +167,8 @@ def shapes(layers, in_shape):
 
 
 def synthetic_params(layers, seed):
-    """fp32 kernels uniform[-1,1) * sqrt(6 / (f k^3)) and biases uniform[-0.1,0.1), seeded per layer."""
+    """fp32 kernels uniform[-1,1) * sqrt(6 / (f k^3)), biases uniform[-0.1,0.1) and weights of norms within 0.1 of 1, seeded
+    per layer."""
     params = []
     for l, spec in enumerate(layers):
         if spec[0] == "conv":
@@ -177,6 +178,10 @@ def synthetic_params(layers, seed):
         elif spec[0] == "transfer":
             maps = [s for s in layers[:l] if s[0] == "conv"][-1][2]
             params.append({"b": uniform_pm1(seed + 17 * l, STREAM_BIAS, (maps,), 0.1)})
+        elif spec[0] == "layernorm":
+            maps = [s for s in layers[:l] if s[0] == "conv"][-1][2]
+            params.append({"w": 1 + uniform_pm1(seed + 17 * l, STREAM_KERNEL, (maps,), 0.1),
+                           "b": uniform_pm1(seed + 17 * l, STREAM_BIAS, (maps,), 0.1)})
         else:
             params.append(None)
     return params
@@ -222,6 +227,7 @@ def config3_sparse_tensors():
 # Nodes are groups of images, edges are bundles of operations between two groups:
 #   ("conv", name, src, dst, f_out, k[, s]) | ("transfer", name, src, dst[, fn])
 #   ("maxfilter", name, src, dst, win[, s]) | ("maxpool", name, src, dst, p)
+#   ("layernorm", name, src, dst[, eps]) | ("dropout", name, src, dst, p)
 # A node's image is the sum of its incoming edges' outputs, so all of them must agree in shape.
 def graph_shapes(graph):
     """Shape [maps, z, y, x] of every node, by propagating the input shapes along the edges."""
@@ -237,7 +243,7 @@ def graph_shapes(graph):
             m, n = shape[src][0], shape[src][1:]
             if kind == "conv":
                 out = (e[4],) + tuple(a - s * (b - 1) for a, b, s in zip(n, e[5], _opt(e, 6, ONES)))
-            elif kind == "transfer":
+            elif kind in ("transfer", "layernorm", "dropout"):
                 out = shape[src]
             elif kind == "maxfilter":
                 out = (m,) + tuple(a - s * (b - 1) for a, b, s in zip(n, e[4], _opt(e, 5, ONES)))
@@ -266,6 +272,9 @@ def graph_params(graph, seed):
             params[name] = {"w": uniform_pm1(seed + 17 * i, STREAM_KERNEL, (fo, f) + k, scale)}
         elif kind == "transfer":
             params[name] = {"b": uniform_pm1(seed + 17 * i, STREAM_BIAS, (shape[src][0],), 0.1)}
+        elif kind == "layernorm":
+            params[name] = {"w": 1 + uniform_pm1(seed + 17 * i, STREAM_KERNEL, (shape[src][0],), 0.1),
+                            "b": uniform_pm1(seed + 17 * i, STREAM_BIAS, (shape[src][0],), 0.1)}
     return params
 
 

@@ -62,3 +62,28 @@ def test_gradients_against_differences(rows, cols, axis):
             slope = (8 * (moved(d) - moved(-d)) - (moved(2 * d) - moved(-2 * d))) / (12 * d)
             scale = max(1.0, float(s.max()) ** 5)       # the fifth derivative grows with 1 / deviation where it is that small
             assert abs(slope - got[at]) < 1e-9 * scale, (which, at)
+
+
+def test_gradients_of_a_net_with_norms_and_dropout():
+    """A round's gradients against differences of its loss, with the round's factors held."""
+    from oracle import net as onet
+    layers = [("conv", 1, 3, (1, 2, 2)), ("layernorm", 1e-3), ("transfer", "tanh"), ("dropout", 0.4), ("conv", 3, 2, (1, 2, 2)),
+              ("layernorm",), ("transfer", "logistic")]
+    rs = np.random.RandomState(3)
+    x, t = rs.randn(1, 1, 5, 6), rs.rand(2, 1, 3, 4)
+    params = [{"w": rs.randn(3, 1, 1, 2, 2)}, {"w": 1 + 0.2 * rs.randn(3), "b": rs.randn(3)}, {"b": rs.randn(3)}, None,
+              {"w": rs.randn(2, 3, 1, 2, 2)}, {"w": 1 + 0.2 * rs.randn(2), "b": rs.randn(2)}, {"b": rs.randn(2)}]
+    factors = {3: norm.dropout_factor(3, 20, 0.4, 5, 1, 3).reshape(3, 1, 4, 5)}
+    assert (factors[3] == 0).any() and (factors[3] > 0).any()
+    grads = onet.train_round(layers, params, x, t, 0.0, factors=factors)[3]
+    for l, p in enumerate(params):
+        for k in p or ():
+            for at in np.ndindex(p[k].shape):
+                def moved(d):
+                    q = [None if v is None else {n: a.copy() for n, a in v.items()} for v in params]
+                    q[l][k][at] += d
+                    return onet.train_round(layers, q, x, t, 0.0, factors=factors)[0]
+                d = 1e-4
+                slope = (8 * (moved(d) - moved(-d)) - (moved(2 * d) - moved(-2 * d))) / (12 * d)
+                # two maps normalise to +-1 steeply where they are near each other: eps = 1e-5 makes fifth derivatives of 1e7 at worst
+                assert abs(slope - grads[l][k][at]) < 1e-6 * max(1.0, abs(grads[l][k][at])), (l, k, at)
