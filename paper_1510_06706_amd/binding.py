@@ -6,7 +6,6 @@ library has not been built, loading raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import functools
 import os
@@ -516,31 +515,32 @@ def _same_shape(t, *others):
             raise ValueError("expected shape %s, got %s" % (tuple(t.shape), tuple(o.shape)))
 
 
-_HERE = contextlib.nullcontext()
-
-
-def _on(stream):
-    """What is made inside belongs to the stream that works on it."""
-    return _HERE if stream is None else torch.cuda.stream(stream)
+def _here(x):
+    """The stream that works on a GPU tensor: the current one of its device."""
+    return torch._C._cuda_getCurrentRawStream(x.get_device())
 
 
 def dropout(x, p, state=None, site=0, stream=None):
     """x / (1 - p) where an element is kept, 0 elsewhere; on a gradient, with the same state and site, the Jacobian."""
+    if stream is not None:          # what is made belongs to the stream that works on it
+        with torch.cuda.stream(stream):
+            return dropout(x, p, state, site)
     rows, cols, _ = _extents(x, 0)
-    with _on(stream):
-        y = torch.empty_like(x)
-    _check(lib().znn_dropout(rows, cols, p, _state_ptr(state), site, _ptr(x, torch.float32), y.data_ptr(), _stream_ptr(stream)))
+    y = torch.empty_like(x)
+    _check(lib().znn_dropout(rows, cols, p, _state_ptr(state), site, _ptr(x, torch.float32), y.data_ptr(), _here(x)))
     return y
 
 
 def layernorm_fwd(x, w, b, eps=NORM_EPS, axis=0, stats=True, stream=None):
     """(y, stats): stats, for ``layernorm_bwd``, holds mean and 1 / deviation of every position (None if not asked for)."""
+    if stream is not None:          # what is made belongs to the stream that works on it
+        with torch.cuda.stream(stream):
+            return layernorm_fwd(x, w, b, eps, axis, stats)
     rows, cols, positions = _extents(x, axis, w, b)
-    with _on(stream):
-        y = torch.empty_like(x)
-        kept = x.new_empty((2, positions)) if stats else None
+    y = torch.empty_like(x)
+    kept = x.new_empty((2, positions)) if stats else None
     _check(lib().znn_layernorm_fwd(rows, cols, axis, eps, _ptr(x, torch.float32), _ptr(w, torch.float32), _ptr(b, torch.float32),
-                                   y.data_ptr(), _ptr(kept), _stream_ptr(stream)))
+                                   y.data_ptr(), _ptr(kept), _here(x)))
     return y, kept
 
 
@@ -562,45 +562,51 @@ def _norm_workspace(x, rows, cols, axis):
 
 def layernorm_bwd(gy, x, w, stats, axis=0, stream=None):
     """(gx, gw, gb) from the input and the statistics of the forward pass."""
+    if stream is not None:          # what is made belongs to the stream that works on it
+        with torch.cuda.stream(stream):
+            return layernorm_bwd(gy, x, w, stats, axis)
     rows, cols, positions = _extents(x, axis, w)
     _same_shape(x, gy)
     if stats.numel() != 2 * positions:
         raise ValueError("expected statistics of %d positions, got %s" % (positions, tuple(stats.shape)))
-    with _on(stream):
-        gx, gw, gb = torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
-        ws, at, need = _norm_workspace(x, rows, cols, axis)
+    gx, gw, gb = torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
+    ws, at, need = _norm_workspace(x, rows, cols, axis)
     _check(lib().znn_layernorm_bwd(rows, cols, axis, _ptr(gy, torch.float32), _ptr(x, torch.float32), _ptr(w, torch.float32),
-                                   _ptr(stats, torch.float32), gx.data_ptr(), gw.data_ptr(), gb.data_ptr(), at, need, _stream_ptr(stream)))
+                                   _ptr(stats, torch.float32), gx.data_ptr(), gw.data_ptr(), gb.data_ptr(), at, need, _here(x)))
     return gx, gw, gb
 
 
 def residual_norm_fwd(h, x, w, b, p=0.0, state=None, site=0, eps=NORM_EPS, axis=0, stats=True, stream=None):
     """(r, y, stats) with r = x + dropout(h), y = layernorm(r): the end of a residual branch in one pass."""
+    if stream is not None:          # what is made belongs to the stream that works on it
+        with torch.cuda.stream(stream):
+            return residual_norm_fwd(h, x, w, b, p, state, site, eps, axis, stats)
     rows, cols, positions = _extents(x, axis, w, b)
     _same_shape(x, h)
-    with _on(stream):
-        r, y = torch.empty_like(x), torch.empty_like(x)
-        kept = x.new_empty((2, positions)) if stats else None
+    r, y = torch.empty_like(x), torch.empty_like(x)
+    kept = x.new_empty((2, positions)) if stats else None
     _check(lib().znn_residual_norm_fwd(rows, cols, axis, eps, p, _state_ptr(state), site, _ptr(h, torch.float32),
                                        _ptr(x, torch.float32), _ptr(w, torch.float32), _ptr(b, torch.float32), r.data_ptr(),
-                                       y.data_ptr(), _ptr(kept), _stream_ptr(stream)))
+                                       y.data_ptr(), _ptr(kept), _here(x)))
     return r, y, kept
 
 
 def residual_norm_bwd(gy, gr, r, w, stats, p=0.0, state=None, site=0, axis=0, stream=None):
     """(gx, gh, gw, gb): gradients of x, h and the parameters.  gr, the gradient that reaches r beside the norm, may be
     None.  Where p is 0, gh is gx."""
+    if stream is not None:          # what is made belongs to the stream that works on it
+        with torch.cuda.stream(stream):
+            return residual_norm_bwd(gy, gr, r, w, stats, p, state, site, axis)
     rows, cols, positions = _extents(r, axis, w)
     _same_shape(r, gy, gr)
     if stats.numel() != 2 * positions:
         raise ValueError("expected statistics of %d positions, got %s" % (positions, tuple(stats.shape)))
-    with _on(stream):
-        gx, gw, gb = torch.empty_like(r), torch.empty_like(w), torch.empty_like(w)
-        gh = torch.empty_like(r) if p != 0 else None
-        ws, at, need = _norm_workspace(r, rows, cols, axis)
+    gx, gw, gb = torch.empty_like(r), torch.empty_like(w), torch.empty_like(w)
+    gh = torch.empty_like(r) if p != 0 else None
+    ws, at, need = _norm_workspace(r, rows, cols, axis)
     _check(lib().znn_residual_norm_bwd(rows, cols, axis, p, _state_ptr(state), site, _ptr(gy, torch.float32), _ptr(gr, torch.float32),
                                        _ptr(r, torch.float32), _ptr(w, torch.float32), _ptr(stats, torch.float32), gx.data_ptr(),
-                                       _ptr(gh), gw.data_ptr(), gb.data_ptr(), at, need, _stream_ptr(stream)))
+                                       _ptr(gh), gw.data_ptr(), gb.data_ptr(), at, need, _here(r)))
     return gx, gx if gh is None else gh, gw, gb
 
 

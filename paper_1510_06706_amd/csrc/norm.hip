@@ -849,8 +849,14 @@ k_norm_params(long features, int shares, const float* __restrict__ parts, float*
     const long t = (long)blockIdx.x * 16 + tx;
     float v = 0.f;
     if (t < 2 * features)
-#pragma unroll 8
-        for (int s = ty; s < shares; s += 64) v += parts[(long)s * 2 * features + t];
+        for (int s0 = ty; s0 < shares; s0 += 8 * 64) {      // eight requests at once
+            float a[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] = parts[(long)min(s0 + 64 * i, shares - 1) * 2 * features + t];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] = s0 + 64 * i < shares ? a[i] : 0.f;
+            v += ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7]));
+        }
     v += __shfl_xor(v, 16);
     v += __shfl_xor(v, 32);
     if ((threadIdx.x & 63) < 16) red[threadIdx.x >> 6][tx] = v;
