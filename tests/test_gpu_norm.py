@@ -26,6 +26,9 @@ SHAPES = [(1, 1, 0), (1, 1, 1), (1, 7, 0), (1, 7, 1), (6, 1, 0), (6, 1, 1), (3, 
           (2, 70003, 0), (129, 3001, 0), (500, 1021, 0), (3, 262147, 0),
           (1, 1024, 1), (7, 63, 1), (64, 64, 1), (5, 255, 1), (5, 256, 1), (5, 257, 1), (33, 1001, 1), (16, 4096, 1), (3, 4097, 1), (9, 8200, 1),
           (2, 16385, 1), (2, 40003, 1), (1, 131075, 1), (2049, 24, 1), (70001, 3, 1), (5003, 130, 1), (1000, 513, 1), (300, 2047, 1)]
+# what the shapes above leave out of the backward passes that add up shares: tiles of every height, on lines and not, and rows by every number of lanes
+SHARED = [(20, 12301, 0), (33, 16384, 0), (40, 12299, 0), (100, 13001, 0), (120, 12320, 0), (146, 12289, 0), (200, 12800, 0), (256, 12303, 0), (512, 1000, 0),
+          (600, 40, 1), (513, 100, 1), (700, 250, 1), (520, 500, 1), (700, 1500, 1), (1030, 3001, 1), (1025, 8000, 1), (1025, 9001, 1), (1025, 16383, 1)]
 
 
 def arrays(rows, cols, axis, seed, *scales):
@@ -93,7 +96,7 @@ def check_grads(gx, gw, gb, gy, x, w, stats, axis, gr=None):
     assert (np.abs(gb - wb) <= TOL * np.abs(gy).sum(other)).all()
 
 
-@pytest.mark.parametrize("rows,cols,axis", SHAPES)
+@pytest.mark.parametrize("rows,cols,axis", SHAPES + SHARED)
 def test_layernorm(rows, cols, axis):
     (x, gy), w, b = arrays(rows, cols, axis, rows + cols, 1.0, 0.1)
     y, stats = znn.layernorm_fwd(put(x), put(w), put(b), EPS, axis)
@@ -126,6 +129,11 @@ def test_residual_join(rows, cols, axis, p, use_gr):
     assert (gh is gx) == (p == 0)
     again = znn.residual_norm_bwd(put(gy), put(gr) if use_gr else None, r, put(w), stats, p, state, 5, axis)
     assert all(torch.equal(u, v) for u, v in zip(got, again))
+
+
+@pytest.mark.parametrize("rows,cols,axis", SHARED)
+def test_residual_join_with_shares(rows, cols, axis):
+    test_residual_join(rows, cols, axis, 0.3, True)
 
 
 @pytest.mark.parametrize("p", [0.0, 0.1, 0.5, 0.999, 1.0, 1e-12])
