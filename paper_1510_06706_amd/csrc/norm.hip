@@ -117,8 +117,8 @@ constexpr unsigned kBufferWord3 = 0x00020000u;      // raw 32-bit buffer element
 typedef unsigned word4 __attribute__((ext_vector_type(4)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
-// Stores of whole 128-byte lines (STREAM) leave the cache at once, as those of rows do (store_row): 120 x 262144 backward 90 -> 72 us, 120 x 32768 forward 8.7 -> 6.9.  Of parts of lines it would write each on its own: 120 x 262143
-// forward 44 -> 90.
+// Stores of whole 128-byte lines (STREAM) leave the cache at once, as those of rows do (store_row): 120 x 262144 backward 90 -> 72 us,
+// 120 x 32768 forward 8.7 -> 6.9.  Parts of lines would be written each on its own: 120 x 262143 forward 44 -> 90.
 template <bool STREAM> __device__ __forceinline__ void store_buffer(__amdgpu_buffer_rsrc_t b, unsigned at, float4v v)
 {
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(word4, v), b, (int)at, 0, STREAM ? 2 : 0);
@@ -137,7 +137,9 @@ template <int TX, int TY> struct ColumnTile {
     int rows, ty, skip;
     unsigned along, at;         // columns from `first` on; bytes from a buffer's begin
     bool border;                // uniform: some thread skips columns
-    __device__ __forceinline__ ColumnTile(long rows_, long cols_, long tile) : cols(cols_), first(tile * TX * 4), rows((int)rows_)
+    long row0;                  // the tile's rows are those from row0 on of the array, and the pointers begin there
+    __device__ __forceinline__ ColumnTile(long rows_, long cols_, long tile, long row0_ = 0)
+        : cols(cols_), first(tile * TX * 4), rows((int)rows_), row0(row0_)
     {
         const int tx = threadIdx.x % TX * 4, last = (int)min(TX * 4L, cols - first) - 4;        // where the last thread may begin: -3 or more
         ty = threadIdx.x / TX;
@@ -169,7 +171,7 @@ template <int TX, int TY> struct ColumnTile {
     __device__ __forceinline__ float4v drop(const DropKey& K, int k, float4v v) const
     {
         const long c = first + along;
-        const unsigned m = TY * k + ty;
+        const unsigned m = (unsigned)row0 + TY * k + ty;
         const Words u = drop_words(K, (unsigned)(c >> 2), m);
         if (border) {           // columns of two quads
             const Words n = drop_words(K, (unsigned)(c >> 2) + 1, m);
@@ -284,21 +286,19 @@ __global__ void __launch_bounds__(TX * TY, 4) k_norm_cols(NormFwd A, Tiles tiles
     }
 }
 
-// Gradients of weight and bias of one feature by one workgroup, over all columns: for few columns, where a launch that adds shares up
-// would take as long again.
-template <int T> __device__ __forceinline__ void row_params(const NormBwd& A, long m, float* gw, float* gb, float2* red)
+// What the columns from c0 to c1 give to the gradients of weight and bias of one feature, by one workgroup.  Over all columns: for few of
+// them, where a launch that adds shares up would take as long again.
+template <int T> __device__ __forceinline__ float2 row_params(const float* gy, const float* x, const float* mean, const float* rstd, long c0, long c1, float2* red)
 {
     float a = 0.f, b = 0.f;
-    for (long q = threadIdx.x; 4 * q < A.cols; q += T) {
-        const int count = (int)min(4L, A.cols - 4 * q);
-        const floatu4 g = load4(A.gy + m * A.cols + 4 * q, count), x = load4(A.x + m * A.cols + 4 * q, count);
-        const floatu4 mean = load4(A.stats + 4 * q, count), rstd = load4(A.stats + A.cols + 4 * q, count);
+    for (long c = c0 + 4 * threadIdx.x; c < c1; c += 4 * T) {
+        const int count = (int)min(4L, c1 - c);
+        const floatu4 g = load4(gy + c, count), v = load4(x + c, count), m = load4(mean + c, count), q = load4(rstd + c, count);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (e < count) { a += g[e] * ((x[e] - mean[e]) * rstd[e]); b += g[e]; }
+            if (e < count) { a += g[e] * ((v[e] - m[e]) * q[e]); b += g[e]; }
     }
-    const float2 s = group_sum<T / 64>(a, b, red);
-    if (threadIdx.x == 0) { gw[m] = s.x; gb[m] = s.y; }
+    return group_sum<T / 64>(a, b, red);
 }
 
 // PARTS: a workgroup takes every gridDim.x-th tile, adds up what its columns give to the parameters' gradients in registers and leaves its
@@ -310,7 +310,9 @@ __global__ void __launch_bounds__(TX * TY, 4) k_norm_cols_bwd(NormBwd A, Tiles t
     __shared__ float red[2][WAVES][TX][8];
     const unsigned others = PARTS ? 0 : (unsigned)A.rows;
     if (blockIdx.x < others) {
-        row_params<TX * TY>(A, blockIdx.x, pw, pb, (float2*)red);
+        const long m = blockIdx.x;
+        const float2 s = row_params<TX * TY>(A.gy + m * A.cols, A.x + m * A.cols, A.stats, A.stats + A.cols, 0, A.cols, (float2*)red);
+        if (threadIdx.x == 0) { pw[m] = s.x; pb[m] = s.y; }
         return;
     }
     const unsigned block = blockIdx.x - others, blocks = gridDim.x - others;
@@ -620,6 +622,15 @@ __global__ void __launch_bounds__(T) k_norm_rows_bwd(NormBwd A, float* __restric
 }
 
 // ---------------------------------------------------------------- positions of any size
+// Calls f(quad, columns) for the quads of a row that are the thread's, several of them without a branch in between.
+template <class F> __device__ __forceinline__ void row_quads(long cols, F f)
+{
+    const long whole = cols / 4;
+#pragma unroll 4
+    for (long q = threadIdx.x; q < whole; q += 1024) f(q, 4);
+    if ((cols & 3) && threadIdx.x == whole % 1024) f(whole, (int)(cols & 3));
+}
+
 // Rows of any length: a workgroup walks a row three times.
 template <int MODE>
 __global__ void __launch_bounds__(1024) k_norm_rows_any(NormFwd A)
@@ -627,14 +638,12 @@ __global__ void __launch_bounds__(1024) k_norm_rows_any(NormFwd A)
     __shared__ float2 red[16];
     DropKey K = {};
     if (MODE == JOIN_DROP) K = drop_key(A.drop);
-    const long quads = (A.cols + 3) / 4;
     const float inv = 1.0f / (float)A.cols;
     for (long row = blockIdx.x; row < A.rows; row += gridDim.x) {
         const long base = row * A.cols;
-        const float* src = MODE == PLAIN ? A.x : A.r;
-        float sum = 0.f;
-        for (long q = threadIdx.x; q < quads; q += 1024) {
-            const int count = (int)min(4L, A.cols - 4 * q);
+        const float* src = (MODE == PLAIN ? A.x : A.r) + base;
+        float sum = 0.f, d1 = 0.f, d2 = 0.f;
+        row_quads(A.cols, [&](long q, int count) {
             floatu4 v = load4(A.x + base + 4 * q, count);
             if (MODE != PLAIN) {
                 floatu4 h = load4(A.h + base + 4 * q, count);
@@ -644,26 +653,23 @@ __global__ void __launch_bounds__(1024) k_norm_rows_any(NormFwd A)
                 store4(A.r + base + 4 * q, count, v);
             }
             sum += (v[0] + v[1]) + (v[2] + v[3]);       // 0 behind the row
-        }
+        });
         const float m0 = group_sum<16>(sum, 0.f, red).x * inv;
-        float d1 = 0.f, d2 = 0.f;
-        for (long q = threadIdx.x; q < quads; q += 1024) {
-            const int count = (int)min(4L, A.cols - 4 * q);
-            const floatu4 v = load4(src + base + 4 * q, count);
+        row_quads(A.cols, [&](long q, int count) {
+            const floatu4 v = load4(src + 4 * q, count);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (e < count) { const float d = v[e] - m0; d1 += d; d2 += d * d; }
-        }
+        });
         const float2 s = group_sum<16>(d1, d2, red);
         const float delta = s.x * inv, rstd = inverse_deviation(s.y * inv, delta, A.eps);
-        for (long q = threadIdx.x; q < quads; q += 1024) {
-            const int count = (int)min(4L, A.cols - 4 * q);
-            floatu4 v = load4(src + base + 4 * q, count);
+        row_quads(A.cols, [&](long q, int count) {
+            floatu4 v = load4(src + 4 * q, count);
             const floatu4 w = load4(A.w + 4 * q, count), b = load4(A.b + 4 * q, count);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = ((v[e] - m0) - delta) * rstd * w[e] + b[e];
-            store4(A.y + base + 4 * q, count, v);
-        }
+            store_row(A.y + base + 4 * q, count, v);
+        });
         if (A.stats && threadIdx.x == 0) { A.stats[row] = m0 + delta; A.stats[A.rows + row] = rstd; }
     }
 }
@@ -674,23 +680,20 @@ __global__ void __launch_bounds__(1024) k_norm_rows_bwd_any(NormBwd A)
     __shared__ float2 red[16];
     DropKey K = {};
     if (MODE == JOIN_DROP) K = drop_key(A.drop);
-    const long quads = (A.cols + 3) / 4;
     const float inv = 1.0f / (float)A.cols;
     for (long row = blockIdx.x; row < A.rows; row += gridDim.x) {
         const long base = row * A.cols;
         const float mean = A.stats[row], rstd = A.stats[A.rows + row];
         float s1 = 0.f, s2 = 0.f;
-        for (long q = threadIdx.x; q < quads; q += 1024) {
-            const int count = (int)min(4L, A.cols - 4 * q);
+        row_quads(A.cols, [&](long q, int count) {
             const floatu4 x = load4(A.x + base + 4 * q, count), g = load4(A.gy + base + 4 * q, count), w = load4(A.w + 4 * q, count);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (e < count) { const float a = g[e] * w[e]; s1 += a; s2 += a * ((x[e] - mean) * rstd); }
-        }
+        });
         const float2 s = group_sum<16>(s1, s2, red);
         const float m1 = s.x * inv, m2 = s.y * inv;
-        for (long q = threadIdx.x; q < quads; q += 1024) {
-            const int count = (int)min(4L, A.cols - 4 * q);
+        row_quads(A.cols, [&](long q, int count) {
             const floatu4 x = load4(A.x + base + 4 * q, count), g = load4(A.gy + base + 4 * q, count), w = load4(A.w + 4 * q, count);
             floatu4 v;
 #pragma unroll
@@ -700,14 +703,180 @@ __global__ void __launch_bounds__(1024) k_norm_rows_bwd_any(NormBwd A)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] += r[e];
             }
-            store4(A.gx + base + 4 * q, count, v);
+            store_row(A.gx + base + 4 * q, count, v);
             if (MODE == JOIN_DROP) v = dropped4(K, (unsigned)q, (unsigned)row, v);
-            if (MODE != PLAIN && A.gh) store4(A.gh + base + 4 * q, count, v);
+            if (MODE != PLAIN && A.gh) store_row(A.gh + base + 4 * q, count, v);
+        });
+    }
+}
+
+// Columns of any height: tiles of 32 columns by 128 threads below each other, which walk blocks of 512 rows three times.
+constexpr int kTallX = 8, kTallY = 128, kTallRows = kTallY * kRowsHeld;
+typedef ColumnTile<kTallX, kTallY> TallTile;
+
+template <int MODE>
+__global__ void __launch_bounds__(1024) k_norm_cols_tall(NormFwd A, Tiles tiles)
+{
+    constexpr int K = kRowsHeld;
+    __shared__ float red[16][kTallX][4], red2[16][kTallX][8];
+    DropKey D = {};
+    if (MODE == JOIN_DROP) D = drop_key(A.drop);
+    const float inv = 1.0f / (float)A.rows;
+    for (long turn = blockIdx.x; turn < tile_turns(tiles); turn += gridDim.x) {
+        const long tile = tile_of(tiles, turn);
+        if (tile >= tiles.count) continue;      // uniform
+        const float* src = MODE == PLAIN ? A.x : A.r;
+        float sum[4], d[8], rstd[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] = d[e] = d[4 + e] = 0.f;
+#pragma unroll 1
+        for (long r0 = 0; r0 < A.rows; r0 += kTallRows) {
+            const TallTile T(min((long)kTallRows, A.rows - r0), A.cols, tile, r0);
+            const long off = r0 * A.cols;
+            float4v v[K], h[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (T.any(k)) {
+                    v[k] = T.load(A.x + off, k);
+                    if (MODE != PLAIN) h[k] = T.load(A.h + off, k);
+                }
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (T.any(k)) {
+                    if (MODE != PLAIN) {
+                        if (MODE == JOIN_DROP) h[k] = T.drop(D, k, h[k]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[k][e] = joined(v[k][e], h[k][e]);
+                        T.template store<false>(A.r + off, k, v[k]);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[e] += v[k][e];      // 0 where there is no row
+                }
+        }
+        sum_over_ty<kTallX, kTallY, 4>(sum, red);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] *= inv;
+#pragma unroll 1
+        for (long r0 = 0; r0 < A.rows; r0 += kTallRows) {
+            const TallTile T(min((long)kTallRows, A.rows - r0), A.cols, tile, r0);
+            float4v v[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (T.any(k)) v[k] = T.load(src + r0 * A.cols, k);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (T.any(k))
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float a = T.has(k) ? v[k][e] - sum[e] : 0.f;
+                        d[e] += a;
+                        d[4 + e] += a * a;
+                    }
+        }
+        sum_over_ty<kTallX, kTallY, 8>(d, red2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { d[e] *= inv; rstd[e] = inverse_deviation(d[4 + e] * inv, d[e], A.eps); }
+#pragma unroll 1
+        for (long r0 = 0; r0 < A.rows; r0 += kTallRows) {
+            const TallTile T(min((long)kTallRows, A.rows - r0), A.cols, tile, r0);
+            float4v v[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (T.any(k)) v[k] = T.load(src + r0 * A.cols, k);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (T.any(k)) {
+                    const long m = min(r0 + kTallY * k + T.ty, A.rows - 1);
+                    const float w = A.w[m], b = A.b[m];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[k][e] = ((v[k][e] - sum[e]) - d[e]) * rstd[e] * w + b;
+                    T.template store<false>(A.y + r0 * A.cols, k, v[k]);
+                }
+            if (A.stats && r0 == 0 && T.ty == 0) {
+                T.store_columns(A.stats, float4v{sum[0] + d[0], sum[1] + d[1], sum[2] + d[2], sum[3] + d[3]});
+                T.store_columns(A.stats + A.cols, float4v{rstd[0], rstd[1], rstd[2], rstd[3]});
+            }
         }
     }
 }
 
-// Columns of any height: 64 columns by four slices of the rows, which a workgroup walks three times.
+template <int MODE>
+__global__ void __launch_bounds__(1024) k_norm_cols_bwd_tall(NormBwd A, Tiles tiles)
+{
+    constexpr int K = MODE == PLAIN ? kRowsHeld : 2;        // four of three operands leave no registers: 1024 x 110592 1141 us, two 821
+    constexpr long BLOCK = kTallY * K;
+    __shared__ float red[2][16][kTallX][8];
+    DropKey D = {};
+    if (MODE == JOIN_DROP) D = drop_key(A.drop);
+    const float inv = 1.0f / (float)A.rows;
+    int side = 0;
+    for (long turn = blockIdx.x; turn < tile_turns(tiles); turn += gridDim.x) {
+        const long tile = tile_of(tiles, turn);
+        if (tile >= tiles.count) continue;      // uniform
+        float s[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = 0.f;
+        float4v mean, rstd;
+#pragma unroll 1
+        for (long r0 = 0; r0 < A.rows; r0 += BLOCK) {
+            const TallTile T(min(BLOCK, A.rows - r0), A.cols, tile, r0);
+            if (r0 == 0) { mean = T.load_columns(A.stats); rstd = T.load_columns(A.stats + A.cols); }
+            float4v x[K], g[K];
+            float w[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (T.any(k)) {
+                    x[k] = T.load(A.x + r0 * A.cols, k);
+                    g[k] = T.load(A.gy + r0 * A.cols, k);
+                    w[k] = A.w[min(r0 + kTallY * k + T.ty, A.rows - 1)];
+                }
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (T.any(k))
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float a = g[k][e] * w[k];         // 0 where there is no row
+                        s[e] += a;
+                        s[4 + e] += T.has(k) ? a * ((x[k][e] - mean[e]) * rstd[e]) : 0.f;
+                    }
+        }
+        sum_over_ty<kTallX, kTallY, 8>(s, red[side]);
+        side ^= 1;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] *= inv;
+#pragma unroll 1
+        for (long r0 = 0; r0 < A.rows; r0 += BLOCK) {
+            const TallTile T(min(BLOCK, A.rows - r0), A.cols, tile, r0);
+            const long off = r0 * A.cols;
+            const bool more = MODE != PLAIN && A.gr;
+            float4v x[K], g[K], r[K];
+            float w[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (T.any(k)) {
+                    x[k] = T.load(A.x + off, k);
+                    g[k] = T.load(A.gy + off, k);
+                    if (more) r[k] = T.load(A.gr + off, k);
+                    w[k] = A.w[min(r0 + kTallY * k + T.ty, A.rows - 1)];
+                }
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (T.any(k)) {
+                    float4v v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[e] = rstd[e] * (g[k][e] * w[k] - s[e] - (x[k][e] - mean[e]) * rstd[e] * s[4 + e]);
+                        if (more) v[e] += r[k][e];
+                    }
+                    T.template store<false>(A.gx + off, k, v);
+                    if (MODE == JOIN_DROP) v = T.drop(D, k, v);
+                    if (MODE != PLAIN && A.gh) T.template store<false>(A.gh + off, k, v);
+                }
+        }
+    }
+}
+
+// Columns of any height where there are no four of them, or 128 rows pass 2^32 bytes: 64 columns by four slices of the rows.
 __device__ __forceinline__ float2 slices_sum(float a, float b, float2 (*red)[64])
 {
     const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
@@ -798,7 +967,7 @@ struct NormParams {
     long rows, cols;
     const float *gy, *x, *stats;
     float* parts;
-    int shares; long span;          // positions of a share
+    long span;                      // positions of a share
 };
 
 __global__ void __launch_bounds__(256) k_norm_params_rows(NormParams A)
@@ -825,13 +994,7 @@ __global__ void __launch_bounds__(256) k_norm_params_cols(NormParams A)
     __shared__ float2 red[4];
     const long c0 = blockIdx.y * A.span, end = min(A.cols, c0 + A.span);
     for (long m = blockIdx.x; m < A.rows; m += gridDim.x) {
-        float gw = 0.f, gb = 0.f;
-        for (long c = c0 + threadIdx.x; c < end; c += 256) {
-            const float g = A.gy[m * A.cols + c];
-            gw += g * ((A.x[m * A.cols + c] - A.stats[c]) * A.stats[A.cols + c]);
-            gb += g;
-        }
-        const float2 s = group_sum<4>(gw, gb, red);
+        const float2 s = row_params<256>(A.gy + m * A.cols, A.x + m * A.cols, A.stats, A.stats + A.cols, c0, end, red);
         if (threadIdx.x == 0) {
             float* part = A.parts + (long)blockIdx.y * 2 * A.rows;
             part[m] = s.x;
@@ -884,6 +1047,7 @@ struct Shape {
     int lanes, quads, threads;              // axis 1
     long most;                              // workgroups that walk over the positions, at most
     bool few;                               // backward: the parameters' gradients by workgroups of their own, in the same launch
+    bool tall;                              // axis 0, not held: tiles that are walked several times
 };
 Shape rows_shape(long rows, long cols, bool backward)
 {
@@ -922,7 +1086,9 @@ Shape cols_shape(long rows, long cols, bool backward)
     S.tiles.apart = cols % 32 != 0 || (!backward && S.tx == 8); // rows on 128-byte lines: 120 x 96^3 backward 265 us in order, 277 apart
     // us, by shares and not: 40 x 1728 6.3 and 3.5, 120 x 8000 8.0 and 4.7, 40 x 32768 7.7 and 18.9, 400 x 8000 12.4 and 14.1
     S.few = backward && cols <= 12288 && rows <= 256;
-    S.held = rows <= S.ty * kRowsHeld && cols >= 4 && S.ty * cols < (1L << 30) - 16;
+    const bool tiled = cols >= 4 && S.ty * cols < (1L << 30) - 16;
+    S.held = tiled && rows <= S.ty * kRowsHeld;
+    S.tall = tiled && !S.held;
     S.tiles.count = (cols + 4 * S.tx - 1) / (4 * S.tx);
     return S;
 }
@@ -941,7 +1107,6 @@ int norm_share_count(long rows, long cols, int axis)
     const Shape S = norm_shape(rows, cols, axis, true);
     return !S.held ? param_shares(rows, cols, axis).count : S.few ? 0 : (int)position_groups(S, rows);
 }
-
 
 unsigned groups_of(long work, long each, long most) { return (unsigned)std::min((work + each - 1) / each, most); }
 
@@ -1050,6 +1215,7 @@ int norm_fwd(const NormFwd& A, int axis, hipStream_t s)
     if (S.held && axis) with_rows<false, false>(S, [&](auto n) { rows_fwd<MODE>(A, S, n, s); });
     else if (S.held) with_cols<false>(S, [&](auto n) { cols_fwd<MODE>(A, S, n, s); });
     else if (axis) ZNN_LAUNCH("layer norm forward", s, k_norm_rows_any<MODE>, dim3(groups_of(A.rows, 1, 1L << 20)), dim3(1024), 0, A);
+    else if (S.tall) ZNN_LAUNCH("layer norm forward", s, k_norm_cols_tall<MODE>, dim3((unsigned)position_groups(S, A.rows)), dim3(1024), 0, A, S.tiles);
     else ZNN_LAUNCH("layer norm forward", s, k_norm_cols_any<MODE>, dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
     return check_launch("layer norm forward");
 }
@@ -1069,12 +1235,13 @@ int norm_bwd(const NormBwd& A, int axis, float* gw, float* gb, void* ws, hipStre
     else if (H.held) with_cols<true>(H, [&](auto n) { sum_cols_bwd<MODE>(A, H, n, parts, gw, gb, s); });
     else {
         const Shares S = param_shares(A.rows, A.cols, axis);
-        const NormParams P = {A.rows, A.cols, A.gy, A.x, A.stats, parts, S.count, S.span};
+        const NormParams P = {A.rows, A.cols, A.gy, A.x, A.stats, parts, S.span};
         if (axis) {
             ZNN_LAUNCH("layer norm backward", s, k_norm_rows_bwd_any<MODE>, dim3(groups_of(A.rows, 1, 1L << 20)), dim3(1024), 0, A);
             ZNN_LAUNCH("layer norm parameters", s, k_norm_params_rows, dim3((unsigned)((A.cols + 63) / 64), (unsigned)S.count), dim3(256), 0, P);
         } else {
-            ZNN_LAUNCH("layer norm backward", s, k_norm_cols_bwd_any<MODE>, dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
+            if (H.tall) ZNN_LAUNCH("layer norm backward", s, k_norm_cols_bwd_tall<MODE>, dim3((unsigned)position_groups(H, A.rows)), dim3(1024), 0, A, H.tiles);
+            else ZNN_LAUNCH("layer norm backward", s, k_norm_cols_bwd_any<MODE>, dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
             ZNN_LAUNCH("layer norm parameters", s, k_norm_params_cols, dim3(groups_of(A.rows, 1, 1L << 20), (unsigned)S.count), dim3(256), 0, P);
         }
     }

@@ -26,9 +26,11 @@ SHAPES = [(1, 1, 0), (1, 1, 1), (1, 7, 0), (1, 7, 1), (6, 1, 0), (6, 1, 1), (3, 
           (2, 70003, 0), (129, 3001, 0), (500, 1021, 0), (3, 262147, 0),
           (1, 1024, 1), (7, 63, 1), (64, 64, 1), (5, 255, 1), (5, 256, 1), (5, 257, 1), (33, 1001, 1), (16, 4096, 1), (3, 4097, 1), (9, 8200, 1),
           (2, 16385, 1), (2, 40003, 1), (1, 131075, 1), (2049, 24, 1), (70001, 3, 1), (5003, 130, 1), (1000, 513, 1), (300, 2047, 1)]
-# what the shapes above leave out of the backward passes that add up shares: tiles of every height, on lines and not, and rows by every number of lanes
+# what the shapes above leave out of the backward passes that add up shares: tiles of every height, on lines and not, rows by every number
+# of lanes, and positions that no workgroup holds
 SHARED = [(20, 12301, 0), (33, 16384, 0), (40, 12299, 0), (100, 13001, 0), (120, 12320, 0), (146, 12289, 0), (200, 12800, 0), (256, 12303, 0), (512, 1000, 0),
-          (600, 40, 1), (513, 100, 1), (700, 250, 1), (520, 500, 1), (700, 1500, 1), (1030, 3001, 1), (1025, 8000, 1), (1025, 9001, 1), (1025, 16383, 1)]
+          (600, 40, 1), (513, 100, 1), (700, 250, 1), (520, 500, 1), (700, 1500, 1), (1030, 3001, 1), (1025, 8000, 1), (1025, 9001, 1), (1025, 16383, 1),
+          (513, 37, 0), (1024, 160, 0), (2047, 131, 0), (1100, 4097, 0), (3000, 4, 0), (5000, 3, 0), (700, 20001, 1)]
 
 
 def arrays(rows, cols, axis, seed, *scales):
