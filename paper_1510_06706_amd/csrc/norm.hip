@@ -521,7 +521,7 @@ __global__ void __launch_bounds__(T) k_norm_rows_bwd(NormBwd A, float* __restric
     constexpr int ROWS = T / L;
     __shared__ float2 red[2][L > 64 ? L / 64 : 1];
     constexpr bool IN_LDS = PARTS && L * NV > 2048;
-    __shared__ float sums[IN_LDS ? L * NV * 8 : !PARTS ? T * 2 : ROWS > 1 ? (ROWS - 1) * L * NV * 4 : 1];
+    __shared__ __align__(16) float sums[IN_LDS ? L * NV * 8 : !PARTS ? T * 2 : ROWS > 1 ? T * NV * 4 : 1];
     const unsigned others = PARTS ? 0 : (unsigned)((A.cols + 31) / 32);
     if (blockIdx.x < others) {
         column_params<T>(A, (long)blockIdx.x * 32, pw, pb, (float2 (*)[32])sums);
@@ -593,31 +593,27 @@ __global__ void __launch_bounds__(T) k_norm_rows_bwd(NormBwd A, float* __restric
         }
     }
     if constexpr (!PARTS) return;
-    // the sums of the workgroup's rows side by side, in the order of the groups: first those of the weight, then those of the bias
     float* part = parts + (long)block * 2 * cols;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        floatu4 (&v)[NV] = which ? gb : gw;
-        if constexpr (ROWS > 1) {
+        const floatu4 (&v)[NV] = which ? gb : gw;
+        if constexpr (ROWS > 1) {       // the sums of the workgroup's rows below each other, which all threads add up
+            constexpr int W = L * NV * 4;
             if (which) __syncthreads();
-            if (group > 0)
 #pragma unroll
-                for (int j = 0; j < NV; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sums[(((group - 1) * NV + j) * 4 + e) * L + lane] = v[j][e];
+            for (int j = 0; j < NV; ++j) *reinterpret_cast<floatu4*>(sums + group * W + 4 * (lane + L * j)) = v[j];
             __syncthreads();
-            if (group == 0)
-#pragma unroll 1
-                for (int q = 0; q < ROWS - 1; ++q)
+            for (int c = threadIdx.x; c < cols; c += T) {
+                float a = sums[c];
 #pragma unroll
-                    for (int j = 0; j < NV; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[j][e] += sums[((q * NV + j) * 4 + e) * L + lane];
-        }
-        if (group == 0)
+                for (int q = 1; q < ROWS; ++q) a += sums[q * W + c];
+                part[which * cols + c] = a;
+            }
+        } else {
 #pragma unroll
             for (int j = 0; j < NV; ++j)
                 store4(part + which * cols + 4 * (lane + L * j), quad_count<L>(j, lane, cols), IN_LDS ? held[(2 * j + which) * T] : v[j]);
+        }
     }
 }
 
