@@ -59,7 +59,10 @@ k_dropout(long rows, long cols, long quads, Drop D, const float* __restrict__ x,
 
 __global__ void __launch_bounds__(256) k_copy(long count, const float* __restrict__ x, float* __restrict__ y)
 {
-    for (long t = (long)blockIdx.x * 256 + threadIdx.x; t < count; t += (long)gridDim.x * 256) y[t] = x[t];
+    for (long t = 4 * ((long)blockIdx.x * 256 + threadIdx.x); t < count; t += 4L * gridDim.x * 256) {
+        const int n = (int)min(4L, count - t);
+        store_row(y + t, n, load4(x + t, n));
+    }
 }
 
 __global__ void k_random_advance(uint64_t* state) { state[1] += 1; }
@@ -1260,7 +1263,7 @@ int launch_dropout(long rows, long cols, const Drop& D, bool drops, const float*
 {
     const long quads = (cols + 3) / 4;
     if (drops) ZNN_LAUNCH("dropout", s, k_dropout, dim3(groups_of(rows * quads, 256, 1L << 20)), dim3(256), 0, rows, cols, quads, D, x, y);
-    else ZNN_LAUNCH("dropout", s, k_copy, dim3(groups_of(rows * cols, 256, 1L << 20)), dim3(256), 0, rows * cols, x, y);
+    else ZNN_LAUNCH("dropout", s, k_copy, dim3(groups_of(rows * cols, 1024, 1L << 20)), dim3(256), 0, rows * cols, x, y);
     return check_launch("dropout");
 }
 

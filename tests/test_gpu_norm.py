@@ -29,6 +29,8 @@ SHAPES = [(1, 1, 0), (1, 1, 1), (1, 7, 0), (1, 7, 1), (6, 1, 0), (6, 1, 1), (3, 
 # what the shapes above leave out of the backward passes that add up shares: tiles of every height, on lines and not, rows by every number
 # of lanes, and positions that no workgroup holds
 SHARED = [(20, 12301, 0), (33, 16384, 0), (40, 12299, 0), (100, 13001, 0), (120, 12320, 0), (146, 12289, 0), (200, 12800, 0), (256, 12303, 0), (512, 1000, 0),
+          # one to three columns in the last tile
+          (30, 12419, 0), (40, 12354, 0), (100, 13057, 0), (300, 4099, 0), (2, 12545, 0),
           (600, 40, 1), (513, 100, 1), (700, 250, 1), (520, 500, 1), (700, 1500, 1), (1030, 3001, 1), (1025, 8000, 1), (1025, 9001, 1), (1025, 16383, 1),
           (513, 37, 0), (1024, 160, 0), (2047, 131, 0), (1100, 4097, 0), (3000, 4, 0), (5000, 3, 0), (700, 20001, 1)]
 
