@@ -413,7 +413,9 @@ int  znn_autotune_round(const znn_conv_desc* desc, uint64_t memory_budget, void*
  *   NODE_SUM       out, part, ?part x 5, ?y   the parts in that order (positions 1 to 6), times fn'(y) (position 7)
  *   UPDATE         g, p                       p = p - eta g, maps x n elements: those of the gradient
  *   NORM_FWD       x, w, b, y, ?stats         layer norm over the maps of every voxel; window.x: eps, as the bits of a float
- *   NORM_BWD       gy, x, w, stats, gx, gw, gb
+ *   NORM_BWD       gy, x, w, stats, gx, gw, gb, ?gr      gx plus gr, where x is used beside the norm
+ *   JOIN_FWD       h, x, state, w, b, r, y, ?stats       r = x + dropout(h), y its layer norm: window.x: eps, window.y: the site, sparsity.x as
+ *                                                        for DROPOUT
  *   DROPOUT        x, state, y                window.x: the site; sparsity.x: how many of 2^32 are dropped, as the bits of a uint32
  *   RANDOM_ADVANCE state                      (two numbers of 64 bits, as znn_dropout takes them)
  */
@@ -421,7 +423,8 @@ typedef enum znn_op_kind {
     ZNN_OP_CONV_FWD = 0, ZNN_OP_CONV_BWD = 1, ZNN_OP_CONV_WGRAD = 2, ZNN_OP_TRANSFER_FWD = 3, ZNN_OP_TRANSFER_BWD = 4,
     ZNN_OP_BIAS_GRAD = 5, ZNN_OP_FILTER_FWD = 6, ZNN_OP_FILTER_BWD = 7, ZNN_OP_POOL_FWD = 8, ZNN_OP_POOL_BWD = 9,
     ZNN_OP_LOSS_GRAD = 10, ZNN_OP_NODE_SUM = 11, ZNN_OP_UPDATE = 12,
-    ZNN_OP_NORM_FWD = 13, ZNN_OP_NORM_BWD = 14, ZNN_OP_DROPOUT = 15, ZNN_OP_RANDOM_ADVANCE = 16
+    ZNN_OP_NORM_FWD = 13, ZNN_OP_NORM_BWD = 14, ZNN_OP_DROPOUT = 15, ZNN_OP_RANDOM_ADVANCE = 16,
+    ZNN_OP_JOIN_FWD = 17
 } znn_op_kind;
 
 typedef enum znn_loss { ZNN_LOSS_SQUARE = 0, ZNN_LOSS_CROSS_ENTROPY = 1 } znn_loss;

@@ -515,11 +515,6 @@ def _same_shape(t, *others):
             raise ValueError("expected shape %s, got %s" % (tuple(t.shape), tuple(o.shape)))
 
 
-def _here(x):
-    """The stream that works on a GPU tensor: the current one of its device."""
-    return torch._C._cuda_getCurrentRawStream(x.get_device())
-
-
 def dropout(x, p, state=None, site=0, stream=None):
     """x / (1 - p) where an element is kept, 0 elsewhere; on a gradient, with the same state and site, the Jacobian."""
     if stream is not None:          # what is made belongs to the stream that works on it
@@ -527,7 +522,7 @@ def dropout(x, p, state=None, site=0, stream=None):
             return dropout(x, p, state, site)
     rows, cols, _ = _extents(x, 0)
     y = torch.empty_like(x)
-    _check(lib().znn_dropout(rows, cols, p, _state_ptr(state), site, _ptr(x, torch.float32), y.data_ptr(), _here(x)))
+    _check(lib().znn_dropout(rows, cols, p, _state_ptr(state), site, _ptr(x, torch.float32), y.data_ptr(), _stream_ptr()))
     return y
 
 
@@ -540,7 +535,7 @@ def layernorm_fwd(x, w, b, eps=NORM_EPS, axis=0, stats=True, stream=None):
     y = torch.empty_like(x)
     kept = x.new_empty((2, positions)) if stats else None
     _check(lib().znn_layernorm_fwd(rows, cols, axis, eps, _ptr(x, torch.float32), _ptr(w, torch.float32), _ptr(b, torch.float32),
-                                   y.data_ptr(), _ptr(kept), _here(x)))
+                                   y.data_ptr(), _ptr(kept), _stream_ptr()))
     return y, kept
 
 
@@ -572,7 +567,7 @@ def layernorm_bwd(gy, x, w, stats, axis=0, stream=None):
     gx, gw, gb = torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
     ws, at, need = _norm_workspace(x, rows, cols, axis)
     _check(lib().znn_layernorm_bwd(rows, cols, axis, _ptr(gy, torch.float32), _ptr(x, torch.float32), _ptr(w, torch.float32),
-                                   _ptr(stats, torch.float32), gx.data_ptr(), gw.data_ptr(), gb.data_ptr(), at, need, _here(x)))
+                                   _ptr(stats, torch.float32), gx.data_ptr(), gw.data_ptr(), gb.data_ptr(), at, need, _stream_ptr()))
     return gx, gw, gb
 
 
@@ -587,7 +582,7 @@ def residual_norm_fwd(h, x, w, b, p=0.0, state=None, site=0, eps=NORM_EPS, axis=
     kept = x.new_empty((2, positions)) if stats else None
     _check(lib().znn_residual_norm_fwd(rows, cols, axis, eps, p, _state_ptr(state), site, _ptr(h, torch.float32),
                                        _ptr(x, torch.float32), _ptr(w, torch.float32), _ptr(b, torch.float32), r.data_ptr(),
-                                       y.data_ptr(), _ptr(kept), _here(x)))
+                                       y.data_ptr(), _ptr(kept), _stream_ptr()))
     return r, y, kept
 
 
@@ -606,7 +601,7 @@ def residual_norm_bwd(gy, gr, r, w, stats, p=0.0, state=None, site=0, axis=0, st
     ws, at, need = _norm_workspace(r, rows, cols, axis)
     _check(lib().znn_residual_norm_bwd(rows, cols, axis, p, _state_ptr(state), site, _ptr(gy, torch.float32), _ptr(gr, torch.float32),
                                        _ptr(r, torch.float32), _ptr(w, torch.float32), _ptr(stats, torch.float32), gx.data_ptr(),
-                                       _ptr(gh), gw.data_ptr(), gb.data_ptr(), at, need, _here(r)))
+                                       _ptr(gh), gw.data_ptr(), gb.data_ptr(), at, need, _stream_ptr()))
     return gx, gx if gh is None else gh, gw, gb
 
 

@@ -1282,6 +1282,17 @@ int dropout_parts(long rows, long cols, unsigned dropped, const uint64_t* state,
     return rc != ZNN_OK ? rc : launch_dropout(rows, cols, D, drops, x, y, s);
 }
 
+int join_parts(long rows, long cols, float eps, unsigned dropped, const uint64_t* state, uint32_t site, const float* h, const float* x,
+               const float* w, const float* b, float* r, float* y, float* stats, hipStream_t s)
+{
+    Drop D;
+    bool drops;
+    const int rc = make_drop_parts(dropped, state, site, &D, &drops);
+    if (rc != ZNN_OK) return rc;
+    const NormFwd A = {rows, cols, h, x, w, b, r, y, stats, eps, D};
+    return drops ? norm_fwd<JOIN_DROP>(A, 0, s) : norm_fwd<JOIN>(A, 0, s);
+}
+
 }  // namespace znn
 
 using namespace znn;

@@ -243,9 +243,10 @@ constexpr Form kForm[] = {
     {3u, 8, 0xfeu, 0x01u},      // NODE_SUM
     {3u, 2, 0x03u, 0x02u},      // UPDATE
     {0x0fu, 5, 0x07u, 0x18u},   // NORM_FWD
-    {0x7fu, 7, 0x0fu, 0x70u},   // NORM_BWD
+    {0x7fu, 8, 0x8fu, 0x70u},   // NORM_BWD
     {7u, 3, 0x03u, 0x04u},      // DROPOUT
     {1u, 1, 0x01u, 0x01u},      // RANDOM_ADVANCE
+    {0x7fu, 8, 0x1fu, 0xe0u},   // JOIN_FWD
 };
 
 bool uses(const Step& s, unsigned positions, int buffer)
@@ -275,7 +276,7 @@ bool touched_between(const znn_program& P, int buffer, int first, int last)
 
 int check_op(const znn_op& o, int i, int buffers, int streams)
 {
-    if (o.kind < ZNN_OP_CONV_FWD || o.kind > ZNN_OP_RANDOM_ADVANCE) return fail(ZNN_EINVAL, "operation %d: unknown kind %d", i, o.kind);
+    if (o.kind < ZNN_OP_CONV_FWD || o.kind > ZNN_OP_JOIN_FWD) return fail(ZNN_EINVAL, "operation %d: unknown kind %d", i, o.kind);
     if (o.stream < 0 || o.stream >= streams) return fail(ZNN_EINVAL, "operation %d: no stream %d", i, o.stream);
     const Form& form = kForm[o.kind];
     for (int b = 0; b < 8; ++b) {
@@ -298,7 +299,7 @@ int check_op(const znn_op& o, int i, int buffers, int streams)
     if (o.maps < 1 || o.n.z < 1 || o.n.y < 1 || o.n.x < 1) return fail(ZNN_EINVAL, "operation %d: maps and extents must be >= 1", i);
     if ((double)o.maps * o.n.z * o.n.y * o.n.x / 256 >= 2147483647.0)
         return fail(ZNN_EUNSUPPORTED, "operation %d: too many elements for one launch", i);
-    if (o.kind == ZNN_OP_NORM_FWD && !(norm_eps(o) > 0.f && norm_eps(o) < INFINITY))
+    if ((o.kind == ZNN_OP_NORM_FWD || o.kind == ZNN_OP_JOIN_FWD) && !(norm_eps(o) > 0.f && norm_eps(o) < INFINITY))
         return fail(ZNN_EINVAL, "operation %d: eps must be positive and finite", i);
     if (o.kind == ZNN_OP_FILTER_FWD || o.kind == ZNN_OP_FILTER_BWD || o.kind == ZNN_OP_POOL_FWD || o.kind == ZNN_OP_POOL_BWD)
         return check_filter(o.maps, o.n, o.window, o.sparsity, o.kind == ZNN_OP_POOL_FWD || o.kind == ZNN_OP_POOL_BWD);
@@ -774,9 +775,12 @@ int run_step(znn_program& P, Step& t, float* const* buf, char* scratch, float et
             return check_launch("loss gradient");
         case ZNN_OP_UPDATE: return znn_sgd_update(count, eta, at(0), at(1), s);
         case ZNN_OP_NORM_FWD: return znn_layernorm_fwd(o.maps, voxels(o), 0, norm_eps(o), at(0), at(1), at(2), at(3), at(4), s);
-        case ZNN_OP_NORM_BWD:
-            return znn_layernorm_bwd(o.maps, voxels(o), 0, at(0), at(1), at(2), at(3), at(4), at(5), at(6), scratch + P.area[t.stream],
-                                     norm_workspace(o.maps, voxels(o), 0), s);
+        case ZNN_OP_NORM_BWD:       // with nothing dropped and no gr, the join is the norm
+            return znn_residual_norm_bwd(o.maps, voxels(o), 0, 0.0, nullptr, 0, at(0), at(7), at(1), at(2), at(3), at(4), nullptr, at(5), at(6),
+                                         scratch + P.area[t.stream], norm_workspace(o.maps, voxels(o), 0), s);
+        case ZNN_OP_JOIN_FWD:
+            return join_parts(o.maps, voxels(o), norm_eps(o), (unsigned)o.sparsity.x, (const uint64_t*)at(2), (uint32_t)o.window.y, at(0), at(1), at(3),
+                              at(4), at(5), at(6), at(7), s);
         case ZNN_OP_DROPOUT: return dropout_parts(o.maps, voxels(o), (unsigned)o.sparsity.x, (const uint64_t*)at(1), (uint32_t)o.window.x, at(0), at(2), s);
         case ZNN_OP_RANDOM_ADVANCE: return znn_random_advance((uint64_t*)at(0), s);
         case ZNN_OP_NODE_SUM: {

@@ -286,8 +286,10 @@ int fill_pattern(float* p, long count, float scale, hipStream_t s);
 // max-filter backward, times the derivative of the transfer function that gave y (y may be NULL)
 int maxfilter_bwd(int32_t maps, znn_vec3 n, znn_vec3 win, znn_vec3 sp, const float* gout, const int32_t* idx, float* gin,
                   const float* y, int fn, hipStream_t s);
-// dropout of `dropped` parts in 2^32, and what a backward layer norm takes as its workspace
+// dropout of `dropped` parts in 2^32, the residual join with it over the maps, and what a backward layer norm takes as its workspace
 int dropout_parts(long rows, long cols, unsigned dropped, const uint64_t* state, uint32_t site, const float* x, float* y, hipStream_t s);
+int join_parts(long rows, long cols, float eps, unsigned dropped, const uint64_t* state, uint32_t site, const float* h, const float* x,
+               const float* w, const float* b, float* r, float* y, float* stats, hipStream_t s);
 size_t norm_workspace(long rows, long cols, int axis);
 int check_filter(int32_t maps, znn_vec3 n, znn_vec3 win, znn_vec3 sp, bool pool);
 

@@ -269,6 +269,13 @@ class GraphNet:
                 given[e[1], "w"], given[e[1], "b"] = P.buffer("given", shape[e[2]][:1]), P.buffer("given", shape[e[2]][:1])
         random = None if self.random is None else P.buffer("given", (4,))
         by_name = {e[1]: e for e in E}
+        # node: (edge that hands its image on, edge that drops, norm behind their sum), which one operation takes together
+        joins = {}
+        for n, names in self.incoming.items():
+            ways = sorted((by_name[k] for k in names if by_name[k][0] == "dropout"), key=lambda e: e[4] != 0)
+            norm = next((by_name[k] for k in self.outgoing.get(n, ()) if by_name[k][0] == "layernorm"), None)
+            if len(names) == len(ways) == 2 and ways[0][4] == 0 and ways[1][4] != 0 and norm is not None:
+                joins[n] = (ways[0], ways[1], norm)
 
         def parts_sum(out, parts, at, dims):
             """Operation(s) that add `parts` in order into buffer `out`; the last one."""
@@ -284,7 +291,7 @@ class GraphNet:
         for i, e in enumerate(E):
             kind, name, src, dst = e[:4]
             how = dict(stream=stream(i), maps=shape[src][0], n=shape[src][1:])
-            if kind == "dropout" and e[4] == 0:
+            if kind == "dropout" and (e[4] == 0 or dst in joins):
                 part[name] = img[src]
             elif name not in part:              # a transfer edge may have been taken over by the convolution before it
                 y = part[name] = P.buffer("fresh" if alone(dst) or kind == "transfer" else "kept", shape[dst])
@@ -310,16 +317,23 @@ class GraphNet:
             if all(n in part for n in self.incoming[dst]) and dst not in img:
                 if alone(dst):
                     img[dst] = part[name]
+                elif dst in joins:
+                    skip, drop, then = joins[dst]
+                    img[dst], aux[then[1]] = P.buffer("fresh", shape[dst]), P.buffer("fresh", (2, math.prod(shape[dst][1:])))
+                    part[then[1]] = P.buffer("fresh" if alone(then[3]) else "kept", shape[dst])
+                    P.add(zp.JOIN_FWD, (part[drop[1]], part[skip[1]], random, given[then[1], "w"], given[then[1], "b"], img[dst], part[then[1]],
+                                        aux[then[1]]), stream=stream(i), maps=shape[dst][0], n=shape[dst][1:],
+                          window=zp.eps_bits(_opt(then, 4, znn.NORM_EPS), E.index(drop)), sparsity=zp.drop_parts(drop[4]))
                 else:
                     img[dst] = P.buffer("fresh", shape[dst])
                     parts_sum(img[dst], [part[n] for n in self.incoming[dst]], stream(i), shape[dst])
 
         # backward: back[n] is node n's backward image, `below` the transfer edge whose derivative it already holds
-        gout, targets, back, below, gpart, grads = {}, {}, {}, {}, {}, {}
+        gout, targets, back, below, gpart, grads, added = {}, {}, {}, {}, {}, {}, {}
         outgoing = lambda n: list(reversed(self.outgoing.get(n, [])))  # noqa: E731
 
         def finish(node, at):
-            order = ["loss"] * (node in gout) + outgoing(node)
+            order = ["loss"] * (node in gout) + [k for k in outgoing(node) if k in gpart[node]]
             buf, op = gpart[node][order[0]]
             if len(order) > 1:
                 buf = P.buffer("kept", shape[node])
@@ -365,7 +379,12 @@ class GraphNet:
             elif kind == "layernorm":
                 gs = P.buffer("kept", shape[src])
                 grads[name] = {k: P.buffer("gradient", shape[src][:1]) for k in ("w", "b")}
-                gop = P.add(zp.NORM_BWD, (b, img[src], given[name, "w"], aux[name], gs, grads[name]["w"], grads[name]["b"]), **how)
+                # the gradient by the one other edge out of the node, which the operation adds
+                other = [k for k in self.outgoing[src] if k != name]
+                more = gpart.get(src, {}).pop(other[0], None) if len(other) == 1 and src not in gout else None
+                gop = P.add(zp.NORM_BWD, (b, img[src], given[name, "w"], aux[name], gs, grads[name]["w"], grads[name]["b"],
+                                          -1 if more is None else more[0]), **how)
+                added[src] = more is not None
             elif kind == "dropout":
                 if e[4] == 0:
                     gs, gop = b, dict(op, kind=None)
@@ -379,7 +398,7 @@ class GraphNet:
             if gs is None or not needed:
                 continue
             gpart.setdefault(src, {})[name] = (gs, gop)
-            if len(gpart[src]) == len(self.outgoing[src]) + (src in gout):
+            if len(gpart[src]) == len(self.outgoing[src]) - added.get(src, False) + (src in gout):
                 finish(src, s)
         for n, d in grads.items():
             for k in d:

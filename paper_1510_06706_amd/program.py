@@ -14,7 +14,7 @@ from . import binding as znn
 from .binding import TRANSFER_FNS
 
 (CONV_FWD, CONV_BWD, CONV_WGRAD, TRANSFER_FWD, TRANSFER_BWD, BIAS_GRAD, FILTER_FWD, FILTER_BWD, POOL_FWD, POOL_BWD,
- LOSS_GRAD, NODE_SUM, UPDATE, NORM_FWD, NORM_BWD, DROPOUT, RANDOM_ADVANCE) = range(17)
+ LOSS_GRAD, NODE_SUM, UPDATE, NORM_FWD, NORM_BWD, DROPOUT, RANDOM_ADVANCE, JOIN_FWD) = range(18)
 LOSSES = {"square": 0, "cross_entropy": 1}
 OP = struct.Struct("@22iP")         # the fields of binding.Op
 assert OP.size == ctypes.sizeof(znn.Op)
@@ -171,9 +171,9 @@ class Program:
         return out
 
 
-def eps_bits(eps):
-    """What an operation takes as its `window`: eps as the bits of a float."""
-    return (0, 0, struct.unpack("i", struct.pack("f", eps))[0])
+def eps_bits(eps, site=0):
+    """What an operation takes as its `window`: eps as the bits of a float, and the site of a join."""
+    return (0, site, struct.unpack("i", struct.pack("f", eps))[0])
 
 
 def drop_parts(p):

@@ -179,6 +179,43 @@ def test_rounds_of_a_graph_with_residual_branches():
     assert rel_err(host(plain["y"]), want["y"]) <= 1e-4
 
 
+def test_the_end_of_a_branch_is_one_operation():
+    """Dropout, the sum with what passes the branch by, and the norm behind it; backward, the norm adds the other gradient."""
+    from paper_1510_06706_amd import program as zp
+    g = residual_graph()
+    inputs, targets, params = synth.graph_tensors(g, 32)
+    net = zgraph.GraphNet(g, params, "direct", seed=SEED)
+    net.train_round({n: dev(v) for n, v in inputs.items()}, {n: dev(v) for n, v in targets.items()}, 0.0)
+    kinds = [op["kind"] for op in net._programs["square"][0].ops]
+    assert kinds.count(zp.JOIN_FWD) == 2 and kinds.count(zp.NODE_SUM) == 0
+    assert kinds.count(zp.NORM_FWD) == 1 and kinds.count(zp.NORM_BWD) == 3
+    assert kinds.count(zp.DROPOUT) == 2                 # backward
+    assert sum(op["kind"] == zp.NORM_BWD and op["buf"][7] >= 0 for op in net._programs["square"][0].ops) == 2
+
+
+def test_joins_that_lead_to_a_sum_and_to_two_norms():
+    """A join whose norm ends in a node with another edge, beside a second norm of the same node, which is an output too."""
+    k1 = (1, 1, 1)
+    g = {"inputs": {"x": (3, 2, 5, 6)},
+         "edges": [("conv", "c", "x", "h", 4, k1), ("conv", "c2", "x", "a", 4, k1), ("dropout", "d", "h", "s", 0.4), ("dropout", "i", "a", "s", 0.0),
+                   ("layernorm", "n", "s", "u"), ("layernorm", "m", "s", "v", 1e-2), ("conv", "e", "a", "u", 4, k1), ("conv", "f", "v", "u", 4, k1),
+                   ("transfer", "t", "u", "y", "tanh")],
+         "outputs": ["y", "s"]}
+    inputs, targets, params = synth.graph_tensors(g, 33)
+    p64 = {n: {k: v.astype(np.float64) for k, v in p.items()} for n, p in params.items()}
+    nets = [zgraph.GraphNet(g, params, "direct", streams=s, seed=SEED) for s in (None, 3)]
+    site = [e[1] for e in zgraph.edge_order(g)].index("d")
+    factors = {"d": norm.dropout_factor(4, 60, 0.4, SEED, 0, site).reshape(4, 2, 5, 6)}
+    _, r_img, _, r_grads, _ = ograph.train_round(g, p64, inputs, targets, 0.0, "square", factors)
+    results = [net.train_round({n: dev(v) for n, v in inputs.items()}, {n: dev(v) for n, v in targets.items()}, 0.0) for net in nets]
+    for img, _, _, grads in results:
+        for n in r_img:
+            assert rel_err(host(img[n]), r_img[n]) <= 1e-4, n
+        for n, d in r_grads.items():
+            for k in d:
+                assert rel_err(host(grads[n][k]), d[k]) <= 1e-4, (n, k)
+
+
 @pytest.mark.parametrize("p", [-0.1, 1.0, 1.5, float("nan")])
 def test_probabilities_that_nets_refuse(p):
     layers = [("conv", 1, 2, (1, 1, 1)), ("dropout", p), ("transfer",)]

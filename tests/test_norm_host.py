@@ -117,10 +117,15 @@ def test_operations_of_programs():
     assert program_rc((zp.RANDOM_ADVANCE, (), {})) == znn.ZNN_EINVAL
     for bad in (0.0, -1.0, NAN, INF):
         assert program_rc((zp.NORM_FWD, (0, 1, 2, 3, 4), dict(how, window=zp.eps_bits(bad)))) == znn.ZNN_EINVAL
+    join = (0, 1, 9, 2, 3, 4, 5, 6)
+    assert program_rc((zp.JOIN_FWD, join, eps)) == program_rc((zp.JOIN_FWD, join[:7], eps)) == znn.ZNN_OK      # without statistics
+    assert program_rc((zp.JOIN_FWD, join[:6], eps)) == znn.ZNN_EINVAL
+    assert program_rc((zp.JOIN_FWD, join, dict(how, window=zp.eps_bits(0.0)))) == znn.ZNN_EINVAL
+    assert program_rc((zp.NORM_BWD, (5, 0, 1, 4, 6, 7, 8, 3), how)) == znn.ZNN_OK            # with a gradient to add
     # an update of another extent than the norm's gradient
     assert program_rc(backward, (zp.UPDATE, (7, 1), dict(n=(1, 1, 2)))) == znn.ZNN_OK
     assert program_rc(backward, (zp.UPDATE, (7, 1), dict(n=(1, 1, 3)))) == znn.ZNN_EINVAL
-    assert program_rc((max(zp.RANDOM_ADVANCE, zp.UPDATE) + 1, (0,), {})) == znn.ZNN_EINVAL
+    assert program_rc((zp.JOIN_FWD + 1, (0,), {})) == znn.ZNN_EINVAL
 
 
 @pytest.mark.parametrize("p,parts", [(0.0, 0), (0.5, -2 ** 31), (0.25, 2 ** 30), (1e-12, 0), (1 - 2.0 ** -32, -1)])
