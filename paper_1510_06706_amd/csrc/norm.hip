@@ -114,6 +114,10 @@ __device__ __forceinline__ float2 group_sum(float a, float b, float2* red)
     return v;
 }
 
+// Additions that follow each other in a sum over a position of any length.  The sums of such chains are added up in a chain of their own: one
+// chain of 2^18 squares of normal values is 955 half-ulps low, because what is less than half an ulp of the sum is lost.
+constexpr int kChain = 256;
+
 // ---------------------------------------------------------------- columns held in registers
 // TX lanes side by side take four neighbouring columns each, TY of them one below the other the rows ty, ty + TY, ... (kRowsHeld of
 // them at most), so that an operand is read once.  Sums over a column: over the lanes of a wave, then over the waves by LDS.
@@ -884,77 +888,85 @@ __global__ void __launch_bounds__(1024) k_norm_cols_bwd_tall(NormBwd A, Tiles ti
     }
 }
 
-// Columns of any height where there are no four of them, or 128 rows pass 2^32 bytes: 64 columns by four slices of the rows.
-__device__ __forceinline__ float2 slices_sum(float a, float b, float2 (*red)[64])
+// Columns of any height where there are no four of them, or 128 rows pass 2^32 bytes: TX columns by TY slices of the rows.
+template <int MODE, int TX, int TY>
+__global__ void __launch_bounds__(TX * TY) k_norm_cols_any(NormFwd A)
 {
-    const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-    __syncthreads();
-    red[ty][tx] = make_float2(a, b);
-    __syncthreads();
-    const float2 v0 = red[0][tx], v1 = red[1][tx], v2 = red[2][tx], v3 = red[3][tx];
-    return make_float2((v0.x + v1.x) + (v2.x + v3.x), (v0.y + v1.y) + (v2.y + v3.y));
-}
-
-template <int MODE>
-__global__ void __launch_bounds__(256) k_norm_cols_any(NormFwd A)
-{
-    __shared__ float2 red[4][64];
+    constexpr int WAVES = TX * TY / 64;
+    __shared__ float red[WAVES][TX][1], red2[WAVES][TX][2];
     DropKey K = {};
     if (MODE == JOIN_DROP) K = drop_key(A.drop);
-    const int ty = threadIdx.x >> 6;
+    const int tx = threadIdx.x % TX, ty = threadIdx.x / TX;
     const float inv = 1.0f / (float)A.rows;
-    for (long c0 = (long)blockIdx.x * 64; c0 < A.cols; c0 += (long)gridDim.x * 64) {
-        const long c = c0 + (threadIdx.x & 63);
+    for (long c0 = (long)blockIdx.x * TX; c0 < A.cols; c0 += (long)gridDim.x * TX) {
+        const long c = c0 + tx;
         const long mine = c < A.cols ? A.rows : 0;       // rows that this thread's column has
         const float* src = MODE == PLAIN ? A.x : A.r;
-        float sum = 0.f;
-        for (long m = ty; m < mine; m += 4) {
-            const long t = m * A.cols + c;
-            float v = A.x[t];
-            if (MODE != PLAIN) {
-                float h = A.h[t];
-                if (MODE == JOIN_DROP) {
-                    const Words u = drop_words(K, (unsigned)(c >> 2), (unsigned)m);
-                    const int e = (int)(c & 3);
-                    h = dropped(K, e == 0 ? u.w[0] : e == 1 ? u.w[1] : e == 2 ? u.w[2] : u.w[3], h);
+        float sum[1] = {0.f}, d[2] = {0.f, 0.f};
+        for (long m = ty; m < mine;) {
+            float part = 0.f;
+            for (int i = 0; i < kChain && m < mine; ++i, m += TY) {
+                const long t = m * A.cols + c;
+                float v = A.x[t];
+                if (MODE != PLAIN) {
+                    float h = A.h[t];
+                    if (MODE == JOIN_DROP) {
+                        const Words u = drop_words(K, (unsigned)(c >> 2), (unsigned)m);
+                        const int e = (int)(c & 3);
+                        h = dropped(K, e == 0 ? u.w[0] : e == 1 ? u.w[1] : e == 2 ? u.w[2] : u.w[3], h);
+                    }
+                    v = joined(v, h);
+                    A.r[t] = v;
                 }
-                v = joined(v, h);
-                A.r[t] = v;
+                part += v;
             }
-            sum += v;
+            sum[0] += part;
         }
-        const float m0 = slices_sum(sum, 0.f, red).x * inv;
-        float d1 = 0.f, d2 = 0.f;
-        for (long m = ty; m < mine; m += 4) { const float d = src[m * A.cols + c] - m0; d1 += d; d2 += d * d; }
-        const float2 s = slices_sum(d1, d2, red);
-        const float delta = s.x * inv, rstd = inverse_deviation(s.y * inv, delta, A.eps);
-        for (long m = ty; m < mine; m += 4)
+        sum_over_ty<TX, TY, 1>(sum, red);
+        const float m0 = sum[0] * inv;
+        for (long m = ty; m < mine;) {
+            float p1 = 0.f, p2 = 0.f;
+            for (int i = 0; i < kChain && m < mine; ++i, m += TY) { const float v = src[m * A.cols + c] - m0; p1 += v; p2 += v * v; }
+            d[0] += p1;
+            d[1] += p2;
+        }
+        sum_over_ty<TX, TY, 2>(d, red2);
+        const float delta = d[0] * inv, rstd = inverse_deviation(d[1] * inv, delta, A.eps);
+        for (long m = ty; m < mine; m += TY)
             A.y[m * A.cols + c] = ((src[m * A.cols + c] - m0) - delta) * rstd * A.w[m] + A.b[m];
         if (A.stats && mine && ty == 0) { A.stats[c] = m0 + delta; A.stats[A.cols + c] = rstd; }
     }
 }
 
-template <int MODE>
-__global__ void __launch_bounds__(256) k_norm_cols_bwd_any(NormBwd A)
+template <int MODE, int TX, int TY>
+__global__ void __launch_bounds__(TX * TY) k_norm_cols_bwd_any(NormBwd A)
 {
-    __shared__ float2 red[4][64];
+    constexpr int WAVES = TX * TY / 64;
+    __shared__ float red[2][WAVES][TX][2];
     DropKey K = {};
     if (MODE == JOIN_DROP) K = drop_key(A.drop);
-    const int ty = threadIdx.x >> 6;
+    const int tx = threadIdx.x % TX, ty = threadIdx.x / TX;
     const float inv = 1.0f / (float)A.rows;
-    for (long c0 = (long)blockIdx.x * 64; c0 < A.cols; c0 += (long)gridDim.x * 64) {
-        const long c = c0 + (threadIdx.x & 63);
+    int side = 0;
+    for (long c0 = (long)blockIdx.x * TX; c0 < A.cols; c0 += (long)gridDim.x * TX) {
+        const long c = c0 + tx;
         const long mine = c < A.cols ? A.rows : 0;
         const float mean = mine ? A.stats[c] : 0.f, rstd = mine ? A.stats[A.cols + c] : 0.f;
-        float s1 = 0.f, s2 = 0.f;
-        for (long m = ty; m < mine; m += 4) {
-            const float a = A.gy[m * A.cols + c] * A.w[m];
-            s1 += a;
-            s2 += a * ((A.x[m * A.cols + c] - mean) * rstd);
+        float s[2] = {0.f, 0.f};
+        for (long m = ty; m < mine;) {
+            float p1 = 0.f, p2 = 0.f;
+            for (int i = 0; i < kChain && m < mine; ++i, m += TY) {
+                const float a = A.gy[m * A.cols + c] * A.w[m];
+                p1 += a;
+                p2 += a * ((A.x[m * A.cols + c] - mean) * rstd);
+            }
+            s[0] += p1;
+            s[1] += p2;
         }
-        const float2 s = slices_sum(s1, s2, red);
-        const float m1 = s.x * inv, m2 = s.y * inv;
-        for (long m = ty; m < mine; m += 4) {
+        sum_over_ty<TX, TY, 2>(s, red[side]);
+        side ^= 1;
+        const float m1 = s[0] * inv, m2 = s[1] * inv;
+        for (long m = ty; m < mine; m += TY) {
             const long t = m * A.cols + c;
             float v = rstd * (A.gy[t] * A.w[m] - m1 - (A.x[t] - mean) * rstd * m2);
             if (MODE != PLAIN && A.gr) v += A.gr[t];
@@ -977,6 +989,17 @@ struct NormParams {
     float* parts;
     long span;                      // positions of a share
 };
+
+// sums over the four waves of a workgroup, lane by lane
+__device__ __forceinline__ float2 slices_sum(float a, float b, float2 (*red)[64])
+{
+    const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+    __syncthreads();
+    red[ty][tx] = make_float2(a, b);
+    __syncthreads();
+    const float2 v0 = red[0][tx], v1 = red[1][tx], v2 = red[2][tx], v3 = red[3][tx];
+    return make_float2((v0.x + v1.x) + (v2.x + v3.x), (v0.y + v1.y) + (v2.y + v3.y));
+}
 
 __global__ void __launch_bounds__(256) k_norm_params_rows(NormParams A)
 {
@@ -1225,7 +1248,8 @@ int norm_fwd(const NormFwd& A, int axis, hipStream_t s)
     else if (S.held) with_cols<false>(S, [&](auto n) { cols_fwd<MODE>(A, S, n, s); });
     else if (axis) ZNN_LAUNCH("layer norm forward", s, k_norm_rows_any<MODE>, dim3(groups_of(A.rows, 1, 1L << 20)), dim3(1024), 0, A);
     else if (S.tall) ZNN_LAUNCH("layer norm forward", s, k_norm_cols_tall<MODE>, dim3((unsigned)position_groups(S, A.rows)), dim3(1024), 0, A, S.tiles);
-    else ZNN_LAUNCH("layer norm forward", s, k_norm_cols_any<MODE>, dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
+    else if (A.cols < 4) ZNN_LAUNCH("layer norm forward", s, (k_norm_cols_any<MODE, 4, 256>), dim3(1), dim3(1024), 0, A);
+    else ZNN_LAUNCH("layer norm forward", s, (k_norm_cols_any<MODE, 64, 4>), dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
     return check_launch("layer norm forward");
 }
 
@@ -1250,7 +1274,8 @@ int norm_bwd(const NormBwd& A, int axis, float* gw, float* gb, void* ws, hipStre
             ZNN_LAUNCH("layer norm parameters", s, k_norm_params_rows, dim3((unsigned)((A.cols + 63) / 64), (unsigned)S.count), dim3(256), 0, P);
         } else {
             if (H.tall) ZNN_LAUNCH("layer norm backward", s, k_norm_cols_bwd_tall<MODE>, dim3((unsigned)position_groups(H, A.rows)), dim3(1024), 0, A, H.tiles);
-            else ZNN_LAUNCH("layer norm backward", s, k_norm_cols_bwd_any<MODE>, dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
+            else if (A.cols < 4) ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd_any<MODE, 4, 256>), dim3(1), dim3(1024), 0, A);
+            else ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd_any<MODE, 64, 4>), dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
             ZNN_LAUNCH("layer norm parameters", s, k_norm_params_cols, dim3(groups_of(A.rows, 1, 1L << 20), (unsigned)S.count), dim3(256), 0, P);
         }
     }

@@ -1,0 +1,77 @@
+"""Norms over long positions: sums of millions of elements against 64 bits.
+
+Tolerances in units of u = 2^-24 and of the terms a result is the sum of.  A sum is made of chains of a few hundred additions, whose
+sums are added in chains again, then by trees: the roundings of n additions of like terms add up to about sqrt(n / 3) u of the sum
+(15 u for 512 and less for the average over many threads), what follows adds one u an operation.  64 u hold for that.  One chain of
+2^18 squares of normal values is 955 u low, because terms below half an ulp of the sum are lost: 480 u of 1 / deviation.
+"""
+import pytest
+import torch
+
+from paper_1510_06706_amd import binding as znn
+
+pytestmark = pytest.mark.gpu
+
+TOL = 64 * 2.0 ** -24
+EPS = 1e-5
+DEV = "cuda:0"
+
+
+def values(rows, cols, axis, seed, power=1):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    make = lambda *n: torch.randn(*n, generator=gen, device=DEV)  # noqa: E731
+    n = (rows, cols)[axis]
+    # gradients of one sign, so that what a chain loses is not made up for
+    return make(rows, cols) ** power, make(rows, cols) ** 2, 1 + 0.2 * make(n), 0.2 * make(n)
+
+
+def wide(t, axis):
+    """[features, positions] in 64 bits"""
+    t = t.double()
+    return t if axis == 0 else t.t()
+
+
+def check_forward(y, stats, x, w, b, axis):
+    x, y, w, b, stats = wide(x, axis), wide(y, axis), w.double()[:, None], b.double()[:, None], stats.double()
+    m = x.mean(0)
+    s = 1 / torch.sqrt(((x - m) ** 2).mean(0) + EPS)
+    assert bool(((stats[0] - m).abs() <= TOL * x.abs().mean(0)).all()), ((stats[0] - m) / x.abs().mean(0) / TOL).tolist()
+    assert bool(((stats[1] - s).abs() <= TOL * s).all()), ((stats[1] / s - 1) / TOL).tolist()
+    h = (x - m) * s
+    assert bool(((y - (h * w + b)).abs() <= TOL * ((1 + h.abs()) * w.abs() + b.abs())).all())
+
+
+def check_backward(got, gy, x, w, stats, axis, gr=None):
+    gx, gy, x, w, stats = wide(got[0], axis), wide(gy, axis), wide(x, axis), w.double()[:, None], stats.double()
+    h = (x - stats[0]) * stats[1]
+    a = gy * w
+    want = stats[1] * (a - a.mean(0) - h * (a * h).mean(0))
+    terms = stats[1] * (a.abs() + a.abs().mean(0) + h.abs() * (a * h).abs().mean(0))
+    if gr is not None:
+        want, terms = want + wide(gr, axis), terms + wide(gr, axis).abs()
+    assert bool(((gx - want).abs() <= TOL * terms).all()), float(((gx - want).abs() / terms).max() / TOL)
+    gw, gb = got[-2].double(), got[-1].double()
+    assert bool(((gw - (gy * h).sum(1)).abs() <= TOL * (gy * h).abs().sum(1)).all())
+    assert bool(((gb - gy.sum(1)).abs() <= TOL * gy.abs().sum(1)).all())
+
+
+@pytest.mark.parametrize("rows,cols", [(1 << 20, 1), (1 << 20, 2), ((1 << 20) + 3, 3), ((1 << 22) + 1, 1)])
+def test_a_few_columns_of_many_rows(rows, cols):
+    x, gy, w, b = values(rows, cols, 0, rows + cols)
+    y, stats = znn.layernorm_fwd(x, w, b, EPS, 0)
+    check_forward(y, stats, x, w, b, 0)
+    check_backward(znn.layernorm_bwd(gy, x, w, stats, 0), gy, x, w, stats, 0)
+
+
+@pytest.mark.parametrize("p", [0.0, 0.3])
+def test_a_join_of_a_few_columns_of_many_rows(p):
+    rows, cols = (1 << 20) + 1, 3
+    x, gy, w, b = values(rows, cols, 0, 5)
+    h, gr, _, _ = values(rows, cols, 0, 6)
+    state = znn.random_state(77) if p else None
+    r, y, stats = znn.residual_norm_fwd(h, x, w, b, p, state, 4, EPS, 0)
+    assert torch.equal(r, x + znn.dropout(h, p, state, 4))
+    check_forward(y, stats, r, w, b, 0)
+    gx, gh, gw, gb = znn.residual_norm_bwd(gy, gr, r, w, stats, p, state, 4, 0)
+    check_backward((gx, gw, gb), gy, r, w, stats, 0, gr)
+    assert torch.equal(gh, znn.dropout(gx, p, state, 4))
