@@ -147,10 +147,12 @@ class GraphNet:
     # ------------------------------------------------------------ passes
     def forward(self, inputs, train=False):
         """inputs: {node: CUDA tensor}.  Returns (node images, per-edge aux, node events).  ``train``: as in a training
-        round, with dropout and what ``backward`` needs of norms."""
+        round, with dropout and what ``backward`` needs of norms; the aux of an edge that drops is then a copy of the
+        {seed, round} it went by."""
         import torch
         main = torch.cuda.current_stream()
         self._next_event = 0
+        random = self.random.clone() if train and self.random is not None else None
         img, aux, ready = dict(inputs), {}, {}
         first = self._event(main)
         for n in inputs:
@@ -171,7 +173,8 @@ class GraphNet:
                 y, aux[name] = znn.layernorm_fwd(a, self.params[name]["w"], self.params[name]["b"], _opt(e, 4, znn.NORM_EPS), stats=train,
                                                  stream=s)
             elif kind == "dropout":
-                y = znn.dropout(a, e[4], self.random, i, stream=s) if train and e[4] != 0 else a
+                aux[name] = random if train and e[4] != 0 else None
+                y = a if aux[name] is None else znn.dropout(a, e[4], random, i, stream=s)
             else:
                 y, aux[name] = znn.maxpool3d_fwd(a, e[4], stream=s)
             parts.setdefault(dst, {})[name] = y
@@ -185,8 +188,14 @@ class GraphNet:
 
     def backward(self, img, aux, gout):
         """gout: {output node: d loss / d image} (valid on the current stream).  Returns
-        (parameter gradients per edge name, backward images per node)."""
+        (parameter gradients per edge name, backward images per node) of the pass that `img` and `aux` come from: what it
+        dropped is dropped, and nothing where it dropped nothing."""
         import torch
+        for e in self.edges:
+            if e[0] == "dropout" and e[4] != 0 and aux.get(e[1]) is not None and aux[e[1]] is self.random:
+                raise ValueError("edge %r: what a finished round dropped is not known any more; forward(inputs, train=True) keeps it" % (e[1],))
+            if e[0] == "layernorm" and aux[e[1]] is None:
+                raise ValueError("edge %r: the forward pass kept no statistics; forward(inputs, train=True) does" % (e[1],))
         main = torch.cuda.current_stream()
         back, ready, grads, grad_ev = {}, {}, {}, []
         parts, part_ev = {}, {}
@@ -226,7 +235,7 @@ class GraphNet:
                 gs, gw, gb = znn.layernorm_bwd(g, img[src], self.params[name]["w"], aux[name], stream=s)
                 grads[name] = {"w": gw, "b": gb}
             elif kind == "dropout":
-                gs = znn.dropout(g, e[4], self.random, len(self.edges) - 1 - i, stream=s) if e[4] != 0 else g
+                gs = g if aux.get(name) is None else znn.dropout(g, e[4], aux[name], len(self.edges) - 1 - i, stream=s)
             else:
                 gs = znn.maxpool3d_bwd(g, aux[name], self.shapes[src][1:], e[4], stream=s)
             ev = self._event(s)
@@ -426,5 +435,7 @@ class GraphNet:
             tensors[b] = zp.check_input(targets[n], count=math.prod(self.shapes[n]))
         out = P.run(tensors, float(eta), self.streams[:P.streams - 1])
         out.update({given[n, "x"]: inputs[n] for n in self.graph["inputs"]})
-        return ({n: out[b] for n, b in img.items()}, {n: out[b] for n, b in aux.items()}, {n: out[b] for n, b in gout.items()},
+        kept = {n: out[b] for n, b in aux.items()}
+        kept.update((e[1], self.random) for e in self.edges if e[0] == "dropout" and e[4] != 0)     # which the round has moved on
+        return ({n: out[b] for n, b in img.items()}, kept, {n: out[b] for n, b in gout.items()},
                 {n: {k: out[b] for k, b in d.items()} for n, d in grads.items()})

@@ -189,18 +189,23 @@ class Net:
             tensors[t] = zp.check_input(target, count=math.prod(self.shapes[-1]))
         out = P.run(tensors, float(eta))
         out[given[0, "x"]] = x          # what a layer that drops nothing hands on
-        return ([x] + [out[b] for b in act[1:]], [None if b is None else out[b] for b in aux],
+        kept = [None if b is None else out[b] for b in aux]
+        for l, spec in enumerate(self.layers):
+            if loss is not None and spec[0] == "dropout" and spec[1] != 0:
+                kept[l] = self.random       # which the round has moved on
+        return ([x] + [out[b] for b in act[1:]], kept,
                 None if gout is None else out[gout],
                 [None if d is None else {k: out[b] for k, b in d.items()} for d in grads])
 
     def forward(self, x, train=False):
-        """(node images, per-layer aux).  ``train``: as in a training round, with dropout and what ``backward`` needs of norms."""
+        """(node images, per-layer aux).  ``train``: as in a training round, with dropout and what ``backward`` needs of norms;
+        the aux of a layer that drops is then a copy of the {seed, round} it went by."""
         # without convolutions, inputs of any extent pass
         if train or self._by_layer or tuple(x.shape) != tuple(self.shapes[0]):
-            return self._forward_by_layer(x, train)
+            return self._forward_by_layer(x, train, self.random.clone() if train and self.random is not None else None)
         return self._run(None, x)[:2]
 
-    def _forward_by_layer(self, x, train=True):
+    def _forward_by_layer(self, x, train=False, random=None):
         """One library call per layer: what plans with memoized spectra of their own need before ``backward``."""
         acts, aux = [x], [None] * len(self.layers)
         for l, spec in enumerate(self.layers):
@@ -217,14 +222,24 @@ class Net:
             elif spec[0] == "layernorm":
                 y, aux[l] = znn.layernorm_fwd(a, self.params[l]["w"], self.params[l]["b"], _opt(spec, 1, znn.NORM_EPS), stats=train)
             elif spec[0] == "dropout":
-                y = znn.dropout(a, spec[1], self.random, l) if train and spec[1] != 0 else a
+                aux[l] = random if train and spec[1] != 0 else None
+                y = a if aux[l] is None else znn.dropout(a, spec[1], random, l)
             else:
                 y, aux[l] = znn.maxpool3d_fwd(a, spec[1])
             acts.append(y)
         return acts, aux
 
     def backward(self, acts, aux, gout, record=None):
-        """`record`, if a list, receives (layer, gradient arriving at that layer's output)."""
+        """The gradients of the pass that `acts` and `aux` come from: what it dropped is dropped, and nothing where it dropped
+        nothing.  `record`, if a list, receives (layer, gradient arriving at that layer's output)."""
+        for l, spec in enumerate(self.layers):
+            if spec[0] == "dropout" and spec[1] != 0 and aux[l] is not None and aux[l] is self.random:
+                raise ValueError("layer %d: what a finished round dropped is not known any more; forward(x, train=True) keeps it" % l)
+            if spec[0] == "layernorm" and aux[l] is None:
+                raise ValueError("layer %d: the forward pass kept no statistics; forward(x, train=True) does" % l)
+        return self._backward(acts, aux, gout, record)
+
+    def _backward(self, acts, aux, gout, record=None):
         grads = [None] * len(self.layers)
         g = gout
         for l in range(len(self.layers) - 1, -1, -1):
@@ -247,8 +262,8 @@ class Net:
                 g, gw, gb = znn.layernorm_bwd(g, acts[l], self.params[l]["w"], aux[l])
                 grads[l] = {"w": gw, "b": gb}
             elif spec[0] == "dropout":
-                if spec[1] != 0:
-                    g = znn.dropout(g, spec[1], self.random, l)
+                if aux[l] is not None:
+                    g = znn.dropout(g, spec[1], aux[l], l)
             else:
                 g = znn.maxpool3d_bwd(g, aux[l], self.shapes[l][1:], spec[1])
         return grads
@@ -258,9 +273,9 @@ class Net:
             raise ValueError(loss)
         if record is None and not self._by_layer:
             return self._run(loss, x, target, eta)
-        acts, aux = self._forward_by_layer(x)
+        acts, aux = self._forward_by_layer(x, True, self.random)
         gout = znn.loss_grad(acts[-1], target, loss)
-        grads = self.backward(acts, aux, gout, record)
+        grads = self._backward(acts, aux, gout, record)
         for p, g in zip(self.params, grads):
             if p is not None:
                 for k in p:
