@@ -1035,31 +1035,36 @@ __global__ void __launch_bounds__(256) k_norm_params_cols(NormParams A)
 }
 
 // 16 of the 2 x features values by 64 slices of the shares, each in ascending order of its shares, eight at a time, then the slices by a fixed
-// tree.  Bound by the latency of what other caches just wrote: 2 to 4 us.
+// tree.  Bound by the latency of what other caches just wrote: 2 to 4 us.  Workgroups walk from 2^23 features on: one for every 16 values would be 2^32
+// threads at 2^25, more than a launch may have.
 __global__ void __launch_bounds__(1024)
 k_norm_params(long features, int shares, const float* __restrict__ parts, float* __restrict__ gw, float* __restrict__ gb)
 {
     __shared__ float red[16][16];
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const long t = (long)blockIdx.x * 16 + tx;
-    float v = 0.f;
-    if (t < 2 * features)
-        for (int s0 = ty; s0 < shares; s0 += 8 * 64) {      // eight requests at once
-            float a[8];
+    for (long t0 = (long)blockIdx.x * 16; t0 < 2 * features; t0 += (long)gridDim.x * 16) {
+        const long t = t0 + tx;
+        float v = 0.f;
+        if (t < 2 * features)
+            for (int s0 = ty; s0 < shares; s0 += 8 * 64) {      // eight requests at once
+                float a[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) a[i] = parts[(long)min(s0 + 64 * i, shares - 1) * 2 * features + t];
+                for (int i = 0; i < 8; ++i) a[i] = parts[(long)min(s0 + 64 * i, shares - 1) * 2 * features + t];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) a[i] = s0 + 64 * i < shares ? a[i] : 0.f;
-            v += ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7]));
+                for (int i = 0; i < 8; ++i) a[i] = s0 + 64 * i < shares ? a[i] : 0.f;
+                v += ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7]));
+            }
+        v += __shfl_xor(v, 16);
+        v += __shfl_xor(v, 32);
+        if ((threadIdx.x & 63) < 16) red[threadIdx.x >> 6][tx] = v;
+        __syncthreads();
+        if (ty == 0 && t < 2 * features) {
+#pragma unroll
+            for (int q = 1; q < 16; ++q) v += red[q][tx];
+            if (t < features) gw[t] = v; else gb[t - features] = v;
         }
-    v += __shfl_xor(v, 16);
-    v += __shfl_xor(v, 32);
-    if ((threadIdx.x & 63) < 16) red[threadIdx.x >> 6][tx] = v;
-    __syncthreads();
-    if (ty > 0 || t >= 2 * features) return;
-#pragma unroll
-    for (int q = 1; q < 16; ++q) v += red[q][tx];
-    if (t < features) gw[t] = v; else gb[t - features] = v;
+        __syncthreads();
+    }
 }
 
 struct Shares { int count; long span; };
@@ -1279,7 +1284,7 @@ int norm_bwd(const NormBwd& A, int axis, float* gw, float* gb, void* ws, hipStre
             ZNN_LAUNCH("layer norm parameters", s, k_norm_params_cols, dim3(groups_of(A.rows, 1, 1L << 20), (unsigned)S.count), dim3(256), 0, P);
         }
     }
-    ZNN_LAUNCH("layer norm parameters", s, k_norm_params, dim3((unsigned)((2 * features + 15) / 16)), dim3(1024), 0, features,
+    ZNN_LAUNCH("layer norm parameters", s, k_norm_params, dim3(groups_of(2 * features, 16, 1L << 20)), dim3(1024), 0, features,
                norm_share_count(A.rows, A.cols, axis), (const float*)parts, gw, gb);
     return check_launch("layer norm backward");
 }

@@ -75,3 +75,12 @@ def test_a_join_of_a_few_columns_of_many_rows(p):
     gx, gh, gw, gb = znn.residual_norm_bwd(gy, gr, r, w, stats, p, state, 4, 0)
     check_backward((gx, gw, gb), gy, r, w, stats, 0, gr)
     assert torch.equal(gh, znn.dropout(gx, p, state, 4))
+
+
+@pytest.mark.parametrize("rows,cols,axis", [(1, (1 << 25) + 5, 1), (2, (1 << 25) + 5, 1), ((1 << 25) + 5, 1, 0)])
+def test_gradients_of_more_parameters_than_one_launch_counts(rows, cols, axis):
+    """Sums of 2^25 features' shares by 1024 threads for 16 values would be 2^32 threads: more than a launch may have."""
+    x, gy, w, b = values(rows, cols, axis, 9)
+    y, stats = znn.layernorm_fwd(x, w, b, EPS, axis)
+    check_forward(y, stats, x, w, b, axis)
+    check_backward(znn.layernorm_bwd(gy, x, w, stats, axis), gy, x, w, stats, axis)
