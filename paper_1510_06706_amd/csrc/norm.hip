@@ -117,6 +117,7 @@ __device__ __forceinline__ float2 group_sum(float a, float b, float2* red)
 // Additions that follow each other in a sum over a position of any length.  The sums of such chains are added up in a chain of their own: one
 // chain of 2^18 squares of normal values is 955 half-ulps low, because what is less than half an ulp of the sum is lost.
 constexpr int kChain = 256;
+constexpr long kLongRow = 1024L * kChain;       // columns of which each of 1024 threads adds up kChain
 
 // ---------------------------------------------------------------- columns held in registers
 // TX lanes side by side take four neighbouring columns each, TY of them one below the other the rows ty, ty + TY, ... (kRowsHeld of
@@ -633,17 +634,28 @@ __global__ void __launch_bounds__(T) k_norm_rows_bwd(NormBwd A, float* __restric
 }
 
 // ---------------------------------------------------------------- positions of any size
-// Calls f(quad, columns) for the quads of a row that are the thread's, several of them without a branch in between.
-template <class F> __device__ __forceinline__ void row_quads(long cols, F f)
+// Calls f(quad, columns) for the quads of a row that are the thread's, several of them without a branch in between; LONG: and aside() between
+// kChain values and the next.
+template <bool LONG, class F, class G> __device__ __forceinline__ void row_quads(long cols, F f, G aside)
 {
     const long whole = cols / 4;
+    if constexpr (!LONG) {
 #pragma unroll 4
-    for (long q = threadIdx.x; q < whole; q += 1024) f(q, 4);
+        for (long q = threadIdx.x; q < whole; q += 1024) f(q, 4);
+    } else
+        for (long q0 = 0; q0 < whole; q0 += kLongRow / 4) {
+            if (q0 > 0) aside();
+            const long end = min(whole, q0 + kLongRow / 4);
+#pragma unroll 4
+            for (long q = q0 + threadIdx.x; q < end; q += 1024) f(q, 4);
+        }
     if ((cols & 3) && threadIdx.x == whole % 1024) f(whole, (int)(cols & 3));
 }
+template <class F> __device__ __forceinline__ void row_quads(long cols, F f) { row_quads<false>(cols, f, [] {}); }
 
-// Rows of any length: a workgroup walks a row three times, backward twice.  2000 x 20000 71 us at a floor of 60.
-template <int MODE>
+// Rows of any length: a workgroup walks a row three times, backward twice.  2000 x 20000 71 us at a floor of 60.  Those of more than kLongRow columns
+// by instances of their own, as setting aside costs the others: joined with dropout 2000 x 20000 149 us without, 159 with it.
+template <int MODE, bool LONG>
 __global__ void __launch_bounds__(1024) k_norm_rows_any(NormFwd A)
 {
     __shared__ float2 red[16];
@@ -653,8 +665,8 @@ __global__ void __launch_bounds__(1024) k_norm_rows_any(NormFwd A)
     for (long row = blockIdx.x; row < A.rows; row += gridDim.x) {
         const long base = row * A.cols;
         const float* src = (MODE == PLAIN ? A.x : A.r) + base;
-        float sum = 0.f, d1 = 0.f, d2 = 0.f;
-        row_quads(A.cols, [&](long q, int count) {
+        float sum = 0.f, d1 = 0.f, d2 = 0.f, far1 = 0.f, far2 = 0.f;        // far: the chains set aside
+        row_quads<LONG>(A.cols, [&](long q, int count) {
             floatu4 v = load4(A.x + base + 4 * q, count);
             if (MODE != PLAIN) {
                 floatu4 h = load4(A.h + base + 4 * q, count);
@@ -664,14 +676,17 @@ __global__ void __launch_bounds__(1024) k_norm_rows_any(NormFwd A)
                 store4(A.r + base + 4 * q, count, v);
             }
             sum += (v[0] + v[1]) + (v[2] + v[3]);       // 0 behind the row
-        });
+        }, [&] { far1 += sum; sum = 0.f; });
+        if (LONG) sum += far1;
         const float m0 = group_sum<16>(sum, 0.f, red).x * inv;
-        row_quads(A.cols, [&](long q, int count) {
+        far1 = 0.f;
+        row_quads<LONG>(A.cols, [&](long q, int count) {
             const floatu4 v = load4(src + 4 * q, count);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (e < count) { const float d = v[e] - m0; d1 += d; d2 += d * d; }
-        });
+        }, [&] { far1 += d1; far2 += d2; d1 = d2 = 0.f; });
+        if (LONG) { d1 += far1; d2 += far2; }
         const float2 s = group_sum<16>(d1, d2, red);
         const float delta = s.x * inv, rstd = inverse_deviation(s.y * inv, delta, A.eps);
         row_quads(A.cols, [&](long q, int count) {
@@ -685,7 +700,7 @@ __global__ void __launch_bounds__(1024) k_norm_rows_any(NormFwd A)
     }
 }
 
-template <int MODE>
+template <int MODE, bool LONG>
 __global__ void __launch_bounds__(1024) k_norm_rows_bwd_any(NormBwd A)
 {
     __shared__ float2 red[16];
@@ -695,13 +710,14 @@ __global__ void __launch_bounds__(1024) k_norm_rows_bwd_any(NormBwd A)
     for (long row = blockIdx.x; row < A.rows; row += gridDim.x) {
         const long base = row * A.cols;
         const float mean = A.stats[row], rstd = A.stats[A.rows + row];
-        float s1 = 0.f, s2 = 0.f;
-        row_quads(A.cols, [&](long q, int count) {
+        float s1 = 0.f, s2 = 0.f, far1 = 0.f, far2 = 0.f;
+        row_quads<LONG>(A.cols, [&](long q, int count) {
             const floatu4 x = load4(A.x + base + 4 * q, count), g = load4(A.gy + base + 4 * q, count), w = load4(A.w + 4 * q, count);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (e < count) { const float a = g[e] * w[e]; s1 += a; s2 += a * ((x[e] - mean) * rstd); }
-        });
+        }, [&] { far1 += s1; far2 += s2; s1 = s2 = 0.f; });
+        if (LONG) { s1 += far1; s2 += far2; }
         const float2 s = group_sum<16>(s1, s2, red);
         const float m1 = s.x * inv, m2 = s.y * inv;
         row_quads(A.cols, [&](long q, int count) {
@@ -726,11 +742,31 @@ __global__ void __launch_bounds__(1024) k_norm_rows_bwd_any(NormBwd A)
 constexpr int kTallX = 8, kTallY = 128, kTallRows = kTallY * kRowsHeld;
 typedef ColumnTile<kTallX, kTallY> TallTile;
 
-template <int MODE>
+// LONG, for more than kLongColumn rows: chains of a thread's sums are set aside in LDS, [value][thread].  Instances of their own, as it costs the others
+// registers: 1024 x 110592 joined 457 us without, 473 with it.
+constexpr long kLongColumn = (long)kTallY * kChain;
+typedef float TallAside[8][1024];
+template <int N> __device__ __forceinline__ void set_aside(long r0, long block, TallAside& far, float (&v)[N])
+{
+    if ((r0 + block) % kLongColumn != 0) return;        // uniform
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        far[i][threadIdx.x] = r0 + block == kLongColumn ? v[i] : far[i][threadIdx.x] + v[i];
+        v[i] = 0.f;
+    }
+}
+template <int N> __device__ __forceinline__ void add_aside(const TallAside& far, float (&v)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += far[i][threadIdx.x];
+}
+
+template <int MODE, bool LONG>
 __global__ void __launch_bounds__(1024) k_norm_cols_tall(NormFwd A, Tiles tiles)
 {
     constexpr int K = kRowsHeld;
     __shared__ float red[16][kTallX][4], red2[16][kTallX][8];
+    __shared__ float far[LONG ? 8 : 1][LONG ? 1024 : 1];
     DropKey D = {};
     if (MODE == JOIN_DROP) D = drop_key(A.drop);
     const float inv = 1.0f / (float)A.rows;
@@ -764,7 +800,9 @@ __global__ void __launch_bounds__(1024) k_norm_cols_tall(NormFwd A, Tiles tiles)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) sum[e] += v[k][e];      // 0 where there is no row
                 }
+            if constexpr (LONG) set_aside<4>(r0, kTallRows, far, sum);
         }
+        if constexpr (LONG) add_aside<4>(far, sum);
         sum_over_ty<kTallX, kTallY, 4>(sum, red);
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] *= inv;
@@ -784,7 +822,9 @@ __global__ void __launch_bounds__(1024) k_norm_cols_tall(NormFwd A, Tiles tiles)
                         d[e] += a;
                         d[4 + e] += a * a;
                     }
+            if constexpr (LONG) set_aside<8>(r0, kTallRows, far, d);
         }
+        if constexpr (LONG) add_aside<8>(far, d);
         sum_over_ty<kTallX, kTallY, 8>(d, red2);
 #pragma unroll
         for (int e = 0; e < 4; ++e) { d[e] *= inv; rstd[e] = inverse_deviation(d[4 + e] * inv, d[e], A.eps); }
@@ -812,12 +852,13 @@ __global__ void __launch_bounds__(1024) k_norm_cols_tall(NormFwd A, Tiles tiles)
     }
 }
 
-template <int MODE>
+template <int MODE, bool LONG>
 __global__ void __launch_bounds__(1024) k_norm_cols_bwd_tall(NormBwd A, Tiles tiles)
 {
     constexpr int K = MODE == PLAIN ? kRowsHeld : 2;        // four of three operands leave no registers: 1024 x 110592 1141 us, two 821
     constexpr long BLOCK = kTallY * K;
     __shared__ float red[2][16][kTallX][8];
+    __shared__ float far[LONG ? 8 : 1][LONG ? 1024 : 1];
     DropKey D = {};
     if (MODE == JOIN_DROP) D = drop_key(A.drop);
     const float inv = 1.0f / (float)A.rows;
@@ -851,7 +892,9 @@ __global__ void __launch_bounds__(1024) k_norm_cols_bwd_tall(NormBwd A, Tiles ti
                         s[e] += a;
                         s[4 + e] += T.has(k) ? a * ((x[k][e] - mean[e]) * rstd[e]) : 0.f;
                     }
+            if constexpr (LONG) set_aside<8>(r0, BLOCK, far, s);
         }
+        if constexpr (LONG) add_aside<8>(far, s);
         sum_over_ty<kTallX, kTallY, 8>(s, red[side]);
         side ^= 1;
 #pragma unroll
@@ -1251,9 +1294,15 @@ int norm_fwd(const NormFwd& A, int axis, hipStream_t s)
     const Shape S = norm_shape(A.rows, A.cols, axis, false);
     if (S.held && axis) with_rows<false, false>(S, [&](auto n) { rows_fwd<MODE>(A, S, n, s); });
     else if (S.held) with_cols<false>(S, [&](auto n) { cols_fwd<MODE>(A, S, n, s); });
-    else if (axis) ZNN_LAUNCH("layer norm forward", s, k_norm_rows_any<MODE>, dim3(groups_of(A.rows, 1, 1L << 20)), dim3(1024), 0, A);
-    else if (S.tall) ZNN_LAUNCH("layer norm forward", s, k_norm_cols_tall<MODE>, dim3((unsigned)position_groups(S, A.rows)), dim3(1024), 0, A, S.tiles);
-    else if (A.cols < 4) ZNN_LAUNCH("layer norm forward", s, (k_norm_cols_any<MODE, 4, 256>), dim3(1), dim3(1024), 0, A);
+    else if (axis) {
+        const dim3 grid(groups_of(A.rows, 1, 1L << 20));
+        if (A.cols > kLongRow) ZNN_LAUNCH("layer norm forward", s, (k_norm_rows_any<MODE, true>), grid, dim3(1024), 0, A);
+        else ZNN_LAUNCH("layer norm forward", s, (k_norm_rows_any<MODE, false>), grid, dim3(1024), 0, A);
+    } else if (S.tall) {
+        const dim3 grid((unsigned)position_groups(S, A.rows));
+        if (A.rows > kLongColumn) ZNN_LAUNCH("layer norm forward", s, (k_norm_cols_tall<MODE, true>), grid, dim3(1024), 0, A, S.tiles);
+        else ZNN_LAUNCH("layer norm forward", s, (k_norm_cols_tall<MODE, false>), grid, dim3(1024), 0, A, S.tiles);
+    } else if (A.cols < 4) ZNN_LAUNCH("layer norm forward", s, (k_norm_cols_any<MODE, 4, 256>), dim3(1), dim3(1024), 0, A);
     else ZNN_LAUNCH("layer norm forward", s, (k_norm_cols_any<MODE, 64, 4>), dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
     return check_launch("layer norm forward");
 }
@@ -1275,10 +1324,14 @@ int norm_bwd(const NormBwd& A, int axis, float* gw, float* gb, void* ws, hipStre
         const Shares S = param_shares(A.rows, A.cols, axis);
         const NormParams P = {A.rows, A.cols, A.gy, A.x, A.stats, parts, S.span};
         if (axis) {
-            ZNN_LAUNCH("layer norm backward", s, k_norm_rows_bwd_any<MODE>, dim3(groups_of(A.rows, 1, 1L << 20)), dim3(1024), 0, A);
+            const dim3 grid(groups_of(A.rows, 1, 1L << 20));
+            if (A.cols > kLongRow) ZNN_LAUNCH("layer norm backward", s, (k_norm_rows_bwd_any<MODE, true>), grid, dim3(1024), 0, A);
+            else ZNN_LAUNCH("layer norm backward", s, (k_norm_rows_bwd_any<MODE, false>), grid, dim3(1024), 0, A);
             ZNN_LAUNCH("layer norm parameters", s, k_norm_params_rows, dim3((unsigned)((A.cols + 63) / 64), (unsigned)S.count), dim3(256), 0, P);
         } else {
-            if (H.tall) ZNN_LAUNCH("layer norm backward", s, k_norm_cols_bwd_tall<MODE>, dim3((unsigned)position_groups(H, A.rows)), dim3(1024), 0, A, H.tiles);
+            const dim3 grid((unsigned)position_groups(H, A.rows));
+            if (H.tall && A.rows > kLongColumn) ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd_tall<MODE, true>), grid, dim3(1024), 0, A, H.tiles);
+            else if (H.tall) ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd_tall<MODE, false>), grid, dim3(1024), 0, A, H.tiles);
             else if (A.cols < 4) ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd_any<MODE, 4, 256>), dim3(1), dim3(1024), 0, A);
             else ZNN_LAUNCH("layer norm backward", s, (k_norm_cols_bwd_any<MODE, 64, 4>), dim3(groups_of(A.cols, 64, 1L << 20)), dim3(256), 0, A);
             ZNN_LAUNCH("layer norm parameters", s, k_norm_params_cols, dim3(groups_of(A.rows, 1, 1L << 20), (unsigned)S.count), dim3(256), 0, P);

@@ -84,3 +84,26 @@ def test_gradients_of_more_parameters_than_one_launch_counts(rows, cols, axis):
     y, stats = znn.layernorm_fwd(x, w, b, EPS, axis)
     check_forward(y, stats, x, w, b, axis)
     check_backward(znn.layernorm_bwd(gy, x, w, stats, axis), gy, x, w, stats, axis)
+
+
+# cubes of normal values: most terms are small beside the largest, and lost in a long chain
+@pytest.mark.parametrize("rows,cols,axis", [(1 << 24, 4, 0), ((1 << 22) + 77, 13, 0), (1, 1 << 26, 1), (2, (1 << 25) + 3, 1)])
+def test_positions_that_are_walked(rows, cols, axis):
+    x, gy, w, b = values(rows, cols, axis, rows + cols, 3)
+    y, stats = znn.layernorm_fwd(x, w, b, EPS, axis)
+    check_forward(y, stats, x, w, b, axis)
+    check_backward(znn.layernorm_bwd(gy, x, w, stats, axis), gy, x, w, stats, axis)
+
+
+@pytest.mark.parametrize("p", [0.0, 0.3])
+@pytest.mark.parametrize("rows,cols,axis", [((1 << 22) + 77, 7, 0), (1, (1 << 24) + 3, 1)])
+def test_joins_of_positions_that_are_walked(rows, cols, axis, p):
+    x, gy, w, b = values(rows, cols, axis, 7, 3)
+    h, gr, _, _ = values(rows, cols, axis, 8)
+    state = znn.random_state(78) if p else None
+    r, y, stats = znn.residual_norm_fwd(h, x, w, b, p, state, 4, EPS, axis)
+    assert torch.equal(r, x + znn.dropout(h, p, state, 4))
+    check_forward(y, stats, r, w, b, axis)
+    gx, gh, gw, gb = znn.residual_norm_bwd(gy, gr, r, w, stats, p, state, 4, axis)
+    check_backward((gx, gw, gb), gy, r, w, stats, axis, gr)
+    assert torch.equal(gh, znn.dropout(gx, p, state, 4))
