@@ -1,8 +1,8 @@
 """Norms over long positions: sums of millions of elements against 64 bits.
 
-Tolerances in units of u = 2^-24 and of the terms a result is the sum of.  A sum is made of chains of a few hundred additions, whose
-sums are added in chains again, then by trees: the roundings of n additions of like terms add up to about sqrt(n / 3) u of the sum
-(15 u for 512 and less for the average over many threads), what follows adds one u an operation.  64 u hold for that.  One chain of
+Tolerances in units of u = 2^-24 and of the terms a result is the sum of.  A sum is made of chains of at most 1024 additions,
+whose sums are added in chains again, then by trees: the roundings of n additions of like terms add up to about sqrt(n / 3) u of the
+sum (18 u for 1024, and less for the average over many threads), what follows adds one u an operation.  64 u hold for that.  One chain of
 2^18 squares of normal values is 955 u low, because terms below half an ulp of the sum are lost: 480 u of 1 / deviation.
 """
 import pytest
@@ -107,3 +107,26 @@ def test_joins_of_positions_that_are_walked(rows, cols, axis, p):
     gx, gh, gw, gb = znn.residual_norm_bwd(gy, gr, r, w, stats, p, state, 4, axis)
     check_backward((gx, gw, gb), gy, r, w, stats, axis, gr)
     assert torch.equal(gh, znn.dropout(gx, p, state, 4))
+
+
+# by tiles, walked, by four lanes, by a wave and by a workgroup a row: arrays whose positions are many times what a chip holds at once
+@pytest.mark.parametrize("rows,cols,axis", [(40, 20000003, 0), (129, 16700001, 0), (600, 1300001, 0), (30000001, 16, 1), (16700001, 129, 1), (500000, 2500, 1),
+                                            (40000, 20000, 1)])
+def test_gradients_of_parameters_over_many_positions(rows, cols, axis):
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    n, other = (rows, cols)[axis], 1 - axis
+    x, gy = torch.randn(rows, cols, generator=gen, device=DEV), torch.randn(rows, cols, generator=gen, device=DEV)
+    gy.mul_(gy).mul_(gy)            # fourth powers: most gradients are small beside the largest
+    w, b = torch.ones(n, device=DEV), torch.zeros(n, device=DEV)
+    _, stats = znn.layernorm_fwd(x, w, b, EPS, axis)
+    _, gw, gb = znn.layernorm_bwd(gy, x, w, stats, axis)
+    sums = torch.zeros(4, n, dtype=torch.float64, device=DEV)
+    step = max(1, (1 << 27) // n)   # so many positions at a time in 64 bits
+    for i in range(0, (cols, rows)[axis], step):
+        part = (slice(None), slice(i, i + step)) if axis == 0 else slice(i, i + step)
+        m, s = stats[:, i:i + step].double().unsqueeze(axis + 1)
+        g = gy[part].double()
+        h = (x[part].double() - m) * s * g
+        sums += torch.stack([h.sum(other), h.abs().sum(other), g.sum(other), g.abs().sum(other)])
+    assert bool(((gw - sums[0]).abs() <= TOL * sums[1]).all())
+    assert bool(((gb - sums[2]).abs() <= TOL * sums[3]).all())
