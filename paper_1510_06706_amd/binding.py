@@ -491,6 +491,13 @@ def _state_ptr(state):
     return _ptr(state, torch.int64)
 
 
+def _site(site):
+    """The calls of a round are told apart by 32 bits, of which ctypes would cut the rest off."""
+    if not 0 <= site < 1 << 32:
+        raise ValueError("a site has 32 bits, got %r" % (site,))
+    return site
+
+
 def _extents(x, axis, *params):
     """(rows, columns, positions of the norm) of an array whose parameters are checked."""
     rows = x.shape[0] if x.dim() else 0
@@ -522,7 +529,7 @@ def dropout(x, p, state=None, site=0, stream=None):
             return dropout(x, p, state, site)
     rows, cols, _ = _extents(x, 0)
     y = torch.empty_like(x)
-    _check(lib().znn_dropout(rows, cols, p, _state_ptr(state), site, _ptr(x, torch.float32), y.data_ptr(), _stream_ptr()))
+    _check(lib().znn_dropout(rows, cols, p, _state_ptr(state), _site(site), _ptr(x, torch.float32), y.data_ptr(), _stream_ptr()))
     return y
 
 
@@ -580,7 +587,7 @@ def residual_norm_fwd(h, x, w, b, p=0.0, state=None, site=0, eps=NORM_EPS, axis=
     _same_shape(x, h)
     r, y = torch.empty_like(x), torch.empty_like(x)
     kept = x.new_empty((2, positions)) if stats else None
-    _check(lib().znn_residual_norm_fwd(rows, cols, axis, eps, p, _state_ptr(state), site, _ptr(h, torch.float32),
+    _check(lib().znn_residual_norm_fwd(rows, cols, axis, eps, p, _state_ptr(state), _site(site), _ptr(h, torch.float32),
                                        _ptr(x, torch.float32), _ptr(w, torch.float32), _ptr(b, torch.float32), r.data_ptr(),
                                        y.data_ptr(), _ptr(kept), _stream_ptr()))
     return r, y, kept
@@ -599,8 +606,8 @@ def residual_norm_bwd(gy, gr, r, w, stats, p=0.0, state=None, site=0, axis=0, st
     gx, gw, gb = torch.empty_like(r), torch.empty_like(w), torch.empty_like(w)
     gh = torch.empty_like(r) if p != 0 else None
     ws, at, need = _norm_workspace(r, rows, cols, axis)
-    _check(lib().znn_residual_norm_bwd(rows, cols, axis, p, _state_ptr(state), site, _ptr(gy, torch.float32), _ptr(gr, torch.float32),
-                                       _ptr(r, torch.float32), _ptr(w, torch.float32), _ptr(stats, torch.float32), gx.data_ptr(),
+    _check(lib().znn_residual_norm_bwd(rows, cols, axis, p, _state_ptr(state), _site(site), _ptr(gy, torch.float32),
+                                       _ptr(gr, torch.float32), _ptr(r, torch.float32), _ptr(w, torch.float32), _ptr(stats, torch.float32), gx.data_ptr(),
                                        _ptr(gh), gw.data_ptr(), gb.data_ptr(), at, need, _stream_ptr()))
     return gx, gx if gh is None else gh, gw, gb
 
