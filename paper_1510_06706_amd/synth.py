@@ -166,6 +166,14 @@ def shapes(layers, in_shape):
     return out
 
 
+def _maps_at(layers, l):
+    """Maps before layer l: those the last convolution gave or, where there is none yet, those the first one takes."""
+    before, behind = ([s for s in part if s[0] == "conv"] for part in (layers[:l], layers[l:]))
+    if not before and not behind:
+        raise ValueError("no convolution tells the number of maps at layer %d" % l)
+    return before[-1][2] if before else behind[0][1]
+
+
 def synthetic_params(layers, seed):
     """fp32 kernels uniform[-1,1) * sqrt(6 / (f k^3)), biases uniform[-0.1,0.1) and weights of norms within 0.1 of 1, seeded
     per layer."""
@@ -176,10 +184,10 @@ def synthetic_params(layers, seed):
             scale = float(np.sqrt(6.0 / (f * int(np.prod(k)))))
             params.append({"w": uniform_pm1(seed + 17 * l, STREAM_KERNEL, (fo, f) + tuple(k), scale)})
         elif spec[0] == "transfer":
-            maps = [s for s in layers[:l] if s[0] == "conv"][-1][2]
+            maps = _maps_at(layers, l)
             params.append({"b": uniform_pm1(seed + 17 * l, STREAM_BIAS, (maps,), 0.1)})
         elif spec[0] == "layernorm":
-            maps = [s for s in layers[:l] if s[0] == "conv"][-1][2]
+            maps = _maps_at(layers, l)
             params.append({"w": 1 + uniform_pm1(seed + 17 * l, STREAM_KERNEL, (maps,), 0.1),
                            "b": uniform_pm1(seed + 17 * l, STREAM_BIAS, (maps,), 0.1)})
         else:
