@@ -1,0 +1,37 @@
+"""The largest norms: the last number of features that the calls take and the first that they refuse, without a GPU."""
+import ctypes
+
+import pytest
+
+from paper_1510_06706_amd import binding as znn
+
+LIMIT = 1 << 26
+
+
+def rc(rows, cols, axis):
+    return znn.lib().znn_layernorm_workspace_bytes(rows, cols, axis, ctypes.byref(ctypes.c_size_t(0)))
+
+
+@pytest.mark.parametrize("other", [1, 3, 100])
+def test_features(other):
+    assert rc(other, LIMIT, 1) == rc(LIMIT, other, 0) == znn.ZNN_OK
+    assert rc(other, LIMIT + 1, 1) == rc(LIMIT + 1, other, 0) == znn.ZNN_EUNSUPPORTED
+    # positions have limits of their own
+    assert rc(LIMIT + 1, other, 1) == rc(other, LIMIT + 1, 0) == znn.ZNN_OK
+
+
+def test_rows_and_columns():
+    assert rc((1 << 32) - 1, 1, 1) == rc(1, 1 << 34, 0) == znn.ZNN_OK
+    assert rc(1 << 32, 1, 1) == rc(1, (1 << 34) + 1, 0) == znn.ZNN_EUNSUPPORTED
+    assert rc((1 << 32) - 1, LIMIT, 1) == rc(LIMIT, 1 << 34, 0) == znn.ZNN_OK       # below 2^61 elements
+
+
+@pytest.mark.parametrize("axis", [0, 1])
+def test_every_call_asks(axis):
+    P = ctypes.c_void_p(1 << 20)        # never dereferenced: the calls are refused
+    rows, cols = (LIMIT + 1, 1) if axis == 0 else (1, LIMIT + 1)
+    L = znn.lib()
+    assert L.znn_layernorm_fwd(rows, cols, axis, 1e-5, P, P, P, P, P, None) == znn.ZNN_EUNSUPPORTED
+    assert L.znn_layernorm_bwd(rows, cols, axis, P, P, P, P, P, P, P, P, 1 << 40, None) == znn.ZNN_EUNSUPPORTED
+    assert L.znn_residual_norm_fwd(rows, cols, axis, 1e-5, 0.0, None, 0, P, P, P, P, P, P, P, None) == znn.ZNN_EUNSUPPORTED
+    assert L.znn_residual_norm_bwd(rows, cols, axis, 0.0, None, 0, P, None, P, P, P, P, P, P, P, P, 1 << 40, None) == znn.ZNN_EUNSUPPORTED
