@@ -301,6 +301,8 @@ int  znn_accumulate(int64_t count, const float* x, float* y, void* stream);
  *   prediction, which has no use for them.
  * znn_layernorm_bwd : with h = (x - m) s from `stats` and a = w gy,
  *     gx = s (a - mean(a) - h mean(a h)) (means over the features),  gw = sum of gy h,  gb = sum of gy (over the positions).
+ *   `stats` holds m in 32 bits, so that h is off by up to half an ulp of m times s: gradients lose digits where a mean is large
+ *   beside its deviation, which y does not.
  *   Sums are taken in an order that follows from the extents alone: results repeat themselves to the bit.
  *
  * znn_residual_norm_fwd : the end of a residual branch, r = x + dropout(h) and y = layernorm(r), in one pass over memory.

@@ -5,7 +5,8 @@
 //     m = sum x / n,  s = 1 / sqrt(sum (x - m)^2 / n + eps),  h = (x - m) s,  y = w h + b
 //     a = w gy,  gx = s (a - mean(a) - h mean(a h)),  gw = sum over positions of gy h,  gb = sum of gy
 // Sums are held in 32 bits.  The sum of squares is taken about a first mean m0 and corrected by what is left of the sum there
-// (d = x - m0, m = m0 + mean(d), variance mean(d^2) - mean(d)^2), so neither a mean far from zero nor m0's rounding costs digits.
+// (d = x - m0, m = m0 + mean(d), variance mean(d^2) - mean(d)^2), so neither a mean far from zero nor m0's rounding costs y digits.  Backward, h is that
+// of the statistics, which hold m in 32 bits: off by up to half an ulp of m times s, 2.4e-4 beside a mean of 4096 and a deviation of 1.
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
@@ -536,7 +537,7 @@ template <int T> __device__ __forceinline__ void column_params(const NormBwd& A,
 
 // PARTS: the workgroup adds up what its rows give to the parameters' gradients, in registers or, of long rows, in LDS, and leaves its share.
 // Otherwise the first workgroups take 32 features each (column_params).  Bound by memory: 20000 x 8000 (1.92 GB) 348 us = 5.5 TB/s, 5003 x 1001
-// (60 MB) 12 us and 3 for the shares' sums, 64 x 1000 2.8 us in one launch.
+// (60 MB) 16 us, of them 3 to 4 for the shares' sums, 64 x 1000 2.8 us in one launch.
 template <int MODE, int L, int NV, int T, bool PARTS>
 __global__ void __launch_bounds__(T) k_norm_rows_bwd(NormBwd A, float* __restrict__ parts, float* __restrict__ pw, float* __restrict__ pb)
 {
@@ -1142,7 +1143,7 @@ struct Shape {
     bool tall;                              // axis 0, not held: tiles that are walked several times
 };
 // Workgroups that leave shares: `most`, twice, four times as many and so on, until a thread adds up 1024 positions at most in one chain, `each` to a
-// turn.  From 256 on 10000000 x 64 backward takes 1540 us, so 1435.
+// turn.  With 1024 10000000 x 64 backward takes 1435 us, with 256 1540.
 long share_groups(long most, long positions, long each)
 {
     while (most < 65536 && positions > most * each * 1024) most *= 2;
@@ -1157,7 +1158,9 @@ Shape rows_shape(long rows, long cols, bool backward)
     S.few = backward && (rows <= 512 || (rows <= 1024 && cols > 2048));
     struct Way { int lanes, quads, threads; long most; };
     // Forward: waves for themselves as long as four quads a lane do.  Backward: a quad or two a lane where the sums of the parameters take
-    // registers as well (8192 x 2048 join backward: 256 lanes 64 us, 512 lanes 57), and no more shares than their reading is worth.
+    // registers as well (8192 x 2048 join backward: 256 lanes 64 us, 512 lanes 57).  The last number is the most workgroups that walk.  Forward four
+    // times as many give the same, a fourth 12.0 us for 11.2 (16384 x 512) and 580 for 345 (20000 x 10000); backward each leaves a share: twice as many
+    // 50000 x 16 8.0 us for 7.3, 5003 x 1001 18.6 for 16.2, 8192 x 2048 40.1 for 36.4, half 20000 x 8000 474 for 355 and 60000 x 60 13.1 for 11.8.
     static constexpr Way forward_ways[] = {{4, 1, 256, 4096}, {16, 1, 256, 4096}, {32, 1, 256, 4096}, {64, 1, 256, 4096}, {64, 2, 256, 4096}, {64, 4, 256, 4096},
                                            {256, 2, 256, 4096}, {256, 4, 256, 4096}, {1024, 2, 1024, 4096}, {1024, 3, 1024, 512}, {1024, 4, 1024, 512}};
     static constexpr Way backward_ways[] = {{4, 1, 256, 512}, {16, 1, 256, 1024}, {32, 1, 512, 512}, {64, 1, 512, 512}, {64, 2, 512, 512}, {64, 4, 512, 256},
@@ -1171,6 +1174,7 @@ Shape rows_shape(long rows, long cols, bool backward)
     if (!backward) take(forward_ways);
     else if (S.few) take(few_ways);
     else take(backward_ways);
+    // 512 of them: 1030 x 2000 backward 14.8 us for 12.4, 1200 x 4000 20.6 for 19.1, 1700 x 1700 15.6 for 15.2, but 3000 x 1500 17.6 for 20.4
     if (backward && S.lanes == 512 && rows < 4096) S.most = 256;
     if (backward && S.held) S.most = share_groups(S.most, rows, S.threads / S.lanes);
     return S;
@@ -1183,15 +1187,17 @@ Shape cols_shape(long rows, long cols, bool backward)
     // backward 101 and 87; 40 x 216000 13.6 and 14.3, 31 and 24.  Eight and four rows a thread: 120 x 96^3 forward with dropout 384 and 351.
     S.ty = rows <= 16 ? 4 : rows <= 32 ? 8 : rows <= 64 ? 16 : rows <= 128 ? 32 : rows <= 256 ? 64 : 128;
     S.tx = rows <= 16 ? 64 : rows <= 32 ? 32 : rows <= 128 && backward ? 16 : 8;
-    S.most = !backward ? 1L << 20 : S.ty == 16 ? 1024 : S.ty == 128 ? 256 : 512;   // backward, of 256 to 1024 threads: what a chip holds at once
-    S.tiles.apart = cols % 32 != 0 || (!backward && S.tx == 8); // rows on 128-byte lines: 120 x 96^3 backward 265 us in order, 277 apart
+    // backward what a chip holds at once of 256, 512 and 1024 threads, for four and eight rows half of it
+    S.most = !backward ? 1L << 20 : S.ty == 16 ? 1024 : S.ty == 128 ? 256 : 512;
+    // rows on 128-byte lines: 120 x 96^3 backward 265 us in order, 277 apart; forward 193 in order, 176 apart, joined 392 and 349
+    S.tiles.apart = cols % 32 != 0 || (!backward && S.tx == 8);
     // us, by shares and not: 40 x 1728 6.3 and 3.5, 120 x 8000 8.0 and 4.7, 40 x 32768 7.7 and 18.9, 400 x 8000 12.4 and 14.1
     S.few = backward && cols <= 12288 && rows <= 256;
     const bool tiled = cols >= 4 && S.ty * cols < (1L << 30) - 16;
     S.held = tiled && rows <= S.ty * kRowsHeld;
     S.tall = tiled && !S.held;
     S.tiles.count = (cols + 4 * S.tx - 1) / (4 * S.tx);
-    if (backward) S.most = share_groups(S.most, cols, S.tx);        // of a tile four columns a lane, one after another
+    if (backward && S.held) S.most = share_groups(S.most, cols, S.tx);      // of a tile four columns a lane, one after another
     return S;
 }
 Shape norm_shape(long rows, long cols, int axis, bool backward) { return axis ? rows_shape(rows, cols, backward) : cols_shape(rows, cols, backward); }
