@@ -1232,7 +1232,7 @@ int check_axis(int64_t rows, int64_t cols, int32_t axis)
 {
     if (axis != 0 && axis != 1) return fail(ZNN_EINVAL, "axis must be 0 (over the rows) or 1 (over the columns)");
     int rc = check_array(rows, cols);
-    if (rc == ZNN_OK && (axis ? cols : rows) > 67108864LL)
+    if (rc == ZNN_OK && (axis ? cols : rows) > kNormFeatures)
         rc = fail(ZNN_EUNSUPPORTED, "a norm over %lld elements is too large", (long long)(axis ? cols : rows));
     return rc;
 }

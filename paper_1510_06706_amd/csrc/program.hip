@@ -299,6 +299,8 @@ int check_op(const znn_op& o, int i, int buffers, int streams)
     if (o.maps < 1 || o.n.z < 1 || o.n.y < 1 || o.n.x < 1) return fail(ZNN_EINVAL, "operation %d: maps and extents must be >= 1", i);
     if ((double)o.maps * o.n.z * o.n.y * o.n.x / 256 >= 2147483647.0)
         return fail(ZNN_EUNSUPPORTED, "operation %d: too many elements for one launch", i);
+    if ((o.kind == ZNN_OP_NORM_FWD || o.kind == ZNN_OP_NORM_BWD || o.kind == ZNN_OP_JOIN_FWD) && o.maps > kNormFeatures)
+        return fail(ZNN_EUNSUPPORTED, "operation %d: a norm over %d maps is too large", i, o.maps);
     if ((o.kind == ZNN_OP_NORM_FWD || o.kind == ZNN_OP_JOIN_FWD) && !(norm_eps(o) > 0.f && norm_eps(o) < INFINITY))
         return fail(ZNN_EINVAL, "operation %d: eps must be positive and finite", i);
     if (o.kind == ZNN_OP_FILTER_FWD || o.kind == ZNN_OP_FILTER_BWD || o.kind == ZNN_OP_POOL_FWD || o.kind == ZNN_OP_POOL_BWD)

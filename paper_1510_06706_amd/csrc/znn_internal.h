@@ -291,6 +291,7 @@ int dropout_parts(long rows, long cols, unsigned dropped, const uint64_t* state,
 int join_parts(long rows, long cols, float eps, unsigned dropped, const uint64_t* state, uint32_t site, const float* h, const float* x,
                const float* w, const float* b, float* r, float* y, float* stats, hipStream_t s);
 size_t norm_workspace(long rows, long cols, int axis);
+constexpr long kNormFeatures = 1L << 26;       // the most that a norm is taken over
 int check_filter(int32_t maps, znn_vec3 n, znn_vec3 win, znn_vec3 sp, bool pool);
 
 // ---------------------------------------------------------------- passes of a plan with buffers given by the caller

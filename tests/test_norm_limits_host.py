@@ -35,3 +35,24 @@ def test_every_call_asks(axis):
     assert L.znn_layernorm_bwd(rows, cols, axis, P, P, P, P, P, P, P, P, 1 << 40, None) == znn.ZNN_EUNSUPPORTED
     assert L.znn_residual_norm_fwd(rows, cols, axis, 1e-5, 0.0, None, 0, P, P, P, P, P, P, P, None) == znn.ZNN_EUNSUPPORTED
     assert L.znn_residual_norm_bwd(rows, cols, axis, 0.0, None, 0, P, None, P, P, P, P, P, P, P, P, 1 << 40, None) == znn.ZNN_EUNSUPPORTED
+
+
+def test_programs_ask_before_a_round_runs():
+    """A round that begins would end behind half of its operations, and a join, which the program runs by itself, not at all."""
+    from paper_1510_06706_amd import program as zp
+
+    def built(kind, buf, maps):
+        P = zp.Program("cuda:0")
+        for _ in range(10):
+            P.buffer("given", (4,))
+        P.add(kind, buf, maps=maps, n=(1, 1, 1), window=zp.eps_bits(1e-5))
+        try:
+            P.build()
+        except znn.ZnnError as e:
+            return e.code
+        return znn.ZNN_OK
+
+    for kind, buf in ((zp.NORM_FWD, (0, 1, 2, 3, 4)), (zp.NORM_BWD, (5, 0, 1, 4, 6, 7, 8)), (zp.JOIN_FWD, (0, 1, 9, 2, 3, 4, 5, 6))):
+        assert built(kind, buf, LIMIT) == znn.ZNN_OK
+        assert built(kind, buf, LIMIT + 1) == znn.ZNN_EUNSUPPORTED
+    assert built(zp.DROPOUT, (0, 9, 3), LIMIT + 1) == znn.ZNN_OK        # dropout has no features
