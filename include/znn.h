@@ -330,6 +330,56 @@ int  znn_residual_norm_bwd(int64_t rows, int64_t cols, int32_t axis, double p, c
                            float* gh, float* gw, float* gb, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Gated unit: the product of the two halves of a fully connected layer with 2 f' output nodes and kernels of one voxel,
+ *     u = W x + b,  v = V x + c,  y = fn(u) v       (fn applied to u alone)
+ * over f features of every position.  w [2 f'][f] holds the rows of W before those of V, b [2 f'] the numbers b before c (NULL: zeros).
+ * `axis` says where the features lie:
+ *   0  images [map][voxel]: x [f][positions], y [f'][positions], kept [2 f'][positions]
+ *   1  rows of features: x [positions][f], y [positions][f'], kept [positions][2 f']
+ * znn_gated_fwd : `kept` receives u and v for the backward pass; NULL in prediction, which has no use for them.
+ * znn_gated_bwd : with du = gy v fn'(u) and dv = gy fn(u) from `kept`,
+ *     gx = W^T du + V^T dv,  gw = [du; dv] x^T (summed over the positions),  gb = sum of [du; dv].
+ *   gx may be NULL where nothing reads it, gb where there is no bias.
+ * Sums are taken in fp32 in an order that follows from the extents alone: results repeat themselves to the bit.
+ * Functions at infinity are their limits (SiLU and GELU are 0 at minus infinity); the rectifier is 0 at NaN, as its transfer function is.
+ * The calls take a workspace of znn_gated_workspace_bytes for their pass (ZNN_PASS_FWD or ZNN_PASS_BWD; 256-byte aligned; may be
+ * NULL if that is 0).  ZNN_EUNSUPPORTED: more than 2^20 features on either side, or more than 2^31 - 1 positions.
+ */
+typedef enum znn_gate_fn {
+    ZNN_GATE_RECTIFY  = 0,   /* max(u, 0)                       */
+    ZNN_GATE_LOGISTIC = 1,   /* 1 / (1 + exp(-u))               */
+    ZNN_GATE_TANH     = 2,   /* tanh(u)                         */
+    ZNN_GATE_SILU     = 3,   /* u / (1 + exp(-u))               */
+    ZNN_GATE_GELU     = 4    /* u (1 + erf(u / sqrt(2))) / 2    */
+} znn_gate_fn;
+int  znn_gated_workspace_bytes(int32_t fan_in, int32_t fan_out, int64_t positions, int32_t axis, int32_t pass, size_t* bytes);
+int  znn_gated_fwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t positions, int32_t axis, const float* x, const float* w,
+                   const float* b, float* y, float* kept, void* ws, size_t ws_bytes, void* stream);
+int  znn_gated_bwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t positions, int32_t axis, const float* gy, const float* x,
+                   const float* w, const float* kept, float* gx, float* gw, float* gb, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gated recurrence along lines: with f_t = 1 / (1 + exp(-z_t)),
+ *     h_t = f_t h_(t-1) + (1 - f_t) x_t
+ * for every line of an array [outer][length][inner], t its place along the middle extent: along any axis of images (outer = maps
+ * and slower axes, inner = faster axes), along the steps of [batch][step][feature].  `reverse` != 0 takes the steps from the last to the
+ * first.  h0 [outer][inner] is the state before the first step taken (NULL: zeros), so that one step of a running sequence is a call of length 1.
+ *   A gate that is shut (z = -inf, or so low that f_t is 0 in fp32) forgets the state whatever it holds: a line may hold several
+ * sequences one after another.  One that is wide open (1 - f_t = 0) keeps the state whatever x_t holds: padding.
+ * znn_recurrence_bwd : from gh, the gradient of every h_t, with G_t = gh_t + f_(t+1) G_(t+1):
+ *     gz = G_t (h_(t-1) - x_t) f_t (1 - f_t),  gx = G_t (1 - f_t),  gh0 = f_1 G_1 (may be NULL),
+ *   0 where a factor f_t or 1 - f_t is 0, whatever the others hold.
+ * A line is taken in pieces that follow from the extents alone: results repeat themselves to the bit.
+ * The calls take a workspace of znn_recurrence_workspace_bytes (256-byte aligned; may be NULL if that is 0).
+ * ZNN_EUNSUPPORTED: more than 2^34 elements along an extent, or more than 2^40 in all.
+ */
+int  znn_recurrence_workspace_bytes(int64_t outer, int64_t length, int64_t inner, size_t* bytes);
+int  znn_recurrence_fwd(int64_t outer, int64_t length, int64_t inner, int32_t reverse, const float* z, const float* x, const float* h0,
+                        float* h, void* ws, size_t ws_bytes, void* stream);
+int  znn_recurrence_bwd(int64_t outer, int64_t length, int64_t inner, int32_t reverse, const float* gh, const float* z, const float* x,
+                        const float* h, const float* h0, float* gz, float* gx, float* gh0, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Layer-wise choice between the direct and the FFT method (Section 4): times
  * forward + backward + kernel gradient in both methods on the given shape
  * (2 warm-up rounds, 5 timed), stores the faster one in a process-wide cache

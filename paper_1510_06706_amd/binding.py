@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -39,11 +40,14 @@ EXPORTS = [
     "znn_plan_set_round_memory",
     "znn_random_advance", "znn_dropout", "znn_layernorm_workspace_bytes", "znn_layernorm_fwd", "znn_layernorm_bwd",
     "znn_residual_norm_fwd", "znn_residual_norm_bwd",
+    "znn_gated_workspace_bytes", "znn_gated_fwd", "znn_gated_bwd",
+    "znn_recurrence_workspace_bytes", "znn_recurrence_fwd", "znn_recurrence_bwd",
 ]
 STATIC_SCRATCH_BYTES = 32 * 1024 * 1024
 SPECTRA_LAYOUTS = {"auto": 0, "full": 1, "folded": 2}
 STRATEGIES = ("direct", "fft", "fft_memo")
 TRANSFER_FNS = {"rectify": 0, "logistic": 1, "tanh": 2}
+GATE_FNS = {"rectify": 0, "logistic": 1, "tanh": 2, "silu": 3, "gelu": 4}
 NORM_EPS = 1e-5
 
 
@@ -144,6 +148,12 @@ def lib():
         L.znn_layernorm_bwd.argtypes = [i64, i64, i32] + [vp] * 8 + [sz, vp]
         L.znn_residual_norm_fwd.argtypes = [i64, i64, i32, f32, f64, vp, u32] + [vp] * 8
         L.znn_residual_norm_bwd.argtypes = [i64, i64, i32, f64, vp, u32] + [vp] * 10 + [sz, vp]
+        L.znn_gated_workspace_bytes.argtypes = [i32, i32, i64, i32, i32, ctypes.POINTER(sz)]
+        L.znn_gated_fwd.argtypes = [i32, i32, i32, i64, i32] + [vp] * 6 + [sz, vp]
+        L.znn_gated_bwd.argtypes = [i32, i32, i32, i64, i32] + [vp] * 8 + [sz, vp]
+        L.znn_recurrence_workspace_bytes.argtypes = [i64, i64, i64, ctypes.POINTER(sz)]
+        L.znn_recurrence_fwd.argtypes = [i64, i64, i64, i32] + [vp] * 5 + [sz, vp]
+        L.znn_recurrence_bwd.argtypes = [i64, i64, i64, i32] + [vp] * 9 + [sz, vp]
         for name in EXPORTS:
             if name not in ("znn_last_error", "znn_plan_destroy", "znn_program_destroy"):
                 getattr(L, name).restype = ctypes.c_int
@@ -610,6 +620,150 @@ def residual_norm_bwd(gy, gr, r, w, stats, p=0.0, state=None, site=0, axis=0, st
                                        _ptr(gr, torch.float32), _ptr(r, torch.float32), _ptr(w, torch.float32), _ptr(stats, torch.float32), gx.data_ptr(),
                                        _ptr(gh), gw.data_ptr(), gb.data_ptr(), at, need, _stream_ptr()))
     return gx, gx if gh is None else gh, gw, gb
+
+
+# ---------------------------------------------------------------- gated unit, gated recurrence
+def _take_workspace(like, need):
+    """(tensor that holds it, aligned address, bytes)"""
+    if not need:
+        return None, None, 0
+    ws = like.new_empty(need // 4 + 64)
+    return ws, (ws.data_ptr() + 255) & ~255, need
+
+
+def _operands(*tensors):
+    """Device pointers of fp32 tensors (None -> NULL), which have to live on the current device: the call runs on a stream of it."""
+    pointers = [_ptr(t, torch.float32) for t in tensors]
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("tensor lives on device %d, the current one is %d" % (t.get_device(), device))
+    return pointers
+
+
+def _gate_number(fn):
+    if fn not in GATE_FNS:
+        raise ValueError("a gate function is one of %s, got %r" % (", ".join(GATE_FNS), fn))
+    return GATE_FNS[fn]
+
+
+def _gated_extents(x, w, axis):
+    """(f, f', positions) of x with its features along ``axis`` and w [2 f', f], which may have axes of extent 1 behind these."""
+    if axis not in (0, 1):
+        raise ValueError("axis must be 0 or 1, got %r" % (axis,))
+    if x.dim() < 1 or x.numel() < 1:
+        raise ValueError("expected an array of features, got %s" % (tuple(x.shape),))
+    f = x.shape[0] if axis == 0 else x.shape[-1]
+    if w.dim() < 2 or w.shape[1] != f or w.shape[0] % 2 or w.numel() != w.shape[0] * f:
+        raise ValueError("expected weights [2 f', %d], got %s" % (f, tuple(w.shape)))
+    return f, w.shape[0] // 2, x.numel() // f
+
+
+def _gated_like(x, axis, features):
+    return x.new_empty((features,) + x.shape[1:] if axis == 0 else x.shape[:-1] + (features,))
+
+
+def _expect_shape(t, shape, what):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("expected %s of shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
+
+
+@functools.lru_cache(maxsize=1024)
+def gated_workspace_bytes(f, fo, positions, axis, which):
+    b = ctypes.c_size_t(0)
+    _check(lib().znn_gated_workspace_bytes(f, fo, positions, axis, which, ctypes.byref(b)))
+    return b.value
+
+
+def gated_fwd(x, w, b=None, fn="silu", axis=0, kept=True, stream=None):
+    """(y, kept) with y = fn(u) v, [u; v] = w x + b over the features of x: its first dimension (axis 0, images) or its last one
+    (axis 1, rows of features).  kept, for ``gated_bwd``, holds u and v (None if not asked for)."""
+    if stream is not None:          # what is made belongs to the stream that works on it
+        with torch.cuda.stream(stream):
+            return gated_fwd(x, w, b, fn, axis, kept)
+    number = _gate_number(fn)
+    f, fo, positions = _gated_extents(x, w, axis)
+    if b is not None and b.numel() != 2 * fo:
+        raise ValueError("expected %d biases, got %d" % (2 * fo, b.numel()))
+    operands = _operands(x, w, b)
+    y = _gated_like(x, axis, fo)
+    both = _gated_like(x, axis, 2 * fo) if kept else None
+    ws, at, need = _take_workspace(x, gated_workspace_bytes(f, fo, positions, axis, ZNN_PASS_FWD))
+    _check(lib().znn_gated_fwd(number, f, fo, positions, axis, *operands, y.data_ptr(), _ptr(both), at, need, _stream_ptr()))
+    return y, both
+
+
+def gated_bwd(gy, x, w, kept, fn="silu", axis=0, bias=True, need_gx=True, stream=None):
+    """(gx, gw, gb) from the input and what the forward pass kept; gb is None without ``bias``, gx without ``need_gx``."""
+    if stream is not None:          # what is made belongs to the stream that works on it
+        with torch.cuda.stream(stream):
+            return gated_bwd(gy, x, w, kept, fn, axis, bias, need_gx)
+    number = _gate_number(fn)
+    f, fo, positions = _gated_extents(x, w, axis)
+    outer = (lambda n: (n,) + x.shape[1:]) if axis == 0 else (lambda n: x.shape[:-1] + (n,))
+    _expect_shape(gy, outer(fo), "a gradient")
+    _expect_shape(kept, outer(2 * fo), "kept values")
+    operands = _operands(gy, x, w, kept)
+    gx, gw = torch.empty_like(x) if need_gx else None, torch.empty_like(w)
+    gb = w.new_empty(2 * fo) if bias else None
+    ws, at, need = _take_workspace(x, gated_workspace_bytes(f, fo, positions, axis, ZNN_PASS_BWD))
+    _check(lib().znn_gated_bwd(number, f, fo, positions, axis, *operands, _ptr(gx), gw.data_ptr(), _ptr(gb), at, need, _stream_ptr()))
+    return gx, gw, gb
+
+
+def _line_extents(z, dim, *others):
+    """(outer, length, inner) of the lines along a dimension."""
+    if not -z.dim() <= dim < z.dim():
+        raise ValueError("an array of %d dimensions has no dimension %r" % (z.dim(), dim))
+    if z.numel() < 1:
+        raise ValueError("expected an array of lines, got %s" % (tuple(z.shape),))
+    _same_shape(z, *others)
+    dim %= z.dim()
+    return math.prod(z.shape[:dim]), z.shape[dim], math.prod(z.shape[dim + 1:])
+
+
+@functools.lru_cache(maxsize=1024)
+def recurrence_workspace_bytes(outer, length, inner):
+    b = ctypes.c_size_t(0)
+    _check(lib().znn_recurrence_workspace_bytes(outer, length, inner, ctypes.byref(b)))
+    return b.value
+
+
+def _check_state(h0, z, dim):
+    if h0 is not None and h0.shape != z.shape[:dim % z.dim()] + z.shape[dim % z.dim() + 1:]:
+        raise ValueError("expected one state for every line along dimension %d of %s, got %s" % (dim, tuple(z.shape), tuple(h0.shape)))
+
+
+def recurrence_fwd(z, x, h0=None, dim=-1, reverse=False, out=None, stream=None):
+    """h with h_t = f_t h_(t-1) + (1 - f_t) x_t, f = logistic(z), along a dimension, from the state h0 (the shape without that
+    dimension; None: zeros).  One step of a running sequence is a call on one step, with the last state as h0."""
+    if stream is not None:          # what is made belongs to the stream that works on it
+        with torch.cuda.stream(stream):
+            return recurrence_fwd(z, x, h0, dim, reverse, out)
+    outer, length, inner = _line_extents(z, dim, x, out)
+    _check_state(h0, z, dim)
+    operands = _operands(z, x, h0, out)[:3]
+    h = torch.empty_like(z) if out is None else out
+    ws, at, need = _take_workspace(z, recurrence_workspace_bytes(outer, length, inner))
+    _check(lib().znn_recurrence_fwd(outer, length, inner, bool(reverse), *operands, h.data_ptr(), at, need, _stream_ptr()))
+    return h
+
+
+def recurrence_bwd(gh, z, x, h, h0=None, dim=-1, reverse=False, gz=None, gx=None, stream=None):
+    """(gz, gx, gh0) from the gradient of every h and the forward pass's operands and result; gh0 is None without h0."""
+    if stream is not None:          # what is made belongs to the stream that works on it
+        with torch.cuda.stream(stream):
+            return recurrence_bwd(gh, z, x, h, h0, dim, reverse, gz, gx)
+    outer, length, inner = _line_extents(z, dim, gh, x, h, gz, gx)
+    _check_state(h0, z, dim)
+    operands = _operands(gh, z, x, h, h0, gz, gx)[:5]
+    gz = torch.empty_like(z) if gz is None else gz
+    gx = torch.empty_like(x) if gx is None else gx
+    gh0 = None if h0 is None else torch.empty_like(h0)
+    ws, at, need = _take_workspace(z, recurrence_workspace_bytes(outer, length, inner))
+    _check(lib().znn_recurrence_bwd(outer, length, inner, bool(reverse), *operands, gz.data_ptr(), gx.data_ptr(), _ptr(gh0), at, need,
+                                    _stream_ptr()))
+    return gz, gx, gh0
 
 
 def autotune_workspace_bytes(desc: ConvDesc) -> int:

@@ -1,0 +1,214 @@
+"""The gated recurrence along lines, forward and backward, against the reference in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import gated
+from paper_1510_06706_amd import binding as znn
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to("cuda:0")
+
+
+def host(t):
+    return t.cpu().numpy().astype(np.float64)
+
+
+def operands(shape, seed, state=True, gates=2.0):
+    r = np.random.default_rng(seed)
+    z = (r.normal(size=shape) * 2 + gates).astype(np.float32)
+    x, gh = r.normal(size=shape).astype(np.float32), (r.normal(size=shape) * 0.01).astype(np.float32)
+    h0 = r.normal(size=(shape[0], shape[2])).astype(np.float32) if state else None     # [outer][inner]
+    return z, x, gh, h0
+
+
+def check(z, x, gh, h0, reverse, h=None):
+    """Both passes on the device within the bounds; returns (h, gz, gx, gh0)."""
+    dz, dx, dg, d0 = dev(z), dev(x), dev(gh), None if h0 is None else dev(h0)
+    got = znn.recurrence_fwd(dz, dx, d0, 1, reverse)
+    want, bound = gated.recurrence_fwd(z, x, h0, reverse)
+    compare(host(got), want, bound, "h")
+    grads = znn.recurrence_bwd(dg, dz, dx, got, d0, 1, reverse)
+    wants, bounds = gated.recurrence_bwd(gh, z, x, host(got), h0, reverse)
+    for name, g, w, b in zip(("gz", "gx", "gh0"), grads, wants, bounds):
+        if g is not None:
+            compare(host(g), w.reshape(tuple(g.shape)), b.reshape(tuple(g.shape)), name)
+    return (got,) + tuple(grads)
+
+
+def compare(got, want, bound, name):
+    same = np.isnan(want) == np.isnan(got)
+    assert same.all(), (name, "NaN at", np.argwhere(~same)[:4])
+    finite = np.isfinite(want)
+    assert (got[~finite & ~np.isnan(want)] == want[~finite & ~np.isnan(want)]).all(), name
+    off = np.abs(got - want)[finite] / bound[finite]
+    assert off.size == 0 or off.max() <= 1, (name, off.max())
+
+
+# [outer][length][inner]: single steps, lines of one element, fewer and more lines than a launch holds at once, along the fastest
+# extent and across, short lines side by side, lines longer than any piece, extents on no boundary
+SHAPES = [(1, 1, 1), (8, 1, 1000), (3, 2, 1), (70, 3, 1), (1, 5, 3), (1000, 60, 1), (257, 63, 1), (33, 64, 1), (31, 65, 1), (5, 1000, 1), (2, 4097, 1),
+          (1, 70001, 1), (3, 20000, 1), (4, 17, 2), (6, 100, 7), (40, 9, 63), (3, 50, 64), (2, 77, 65), (3, 1003, 129), (1, 4096, 256), (1, 9001, 36),
+          (2, 30, 5000), (1, 3, 70000), (7, 200, 1001), (9, 1, 1), (1, 1, 70001), (300, 256, 1), (301, 257, 1), (2, 513, 1), (1, 2049, 4)]
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("reverse,state", [(False, True), (True, False), (True, True), (False, False)])
+def test_shapes(shape, reverse, state):
+    print("case", shape, reverse, state, flush=True)
+    check(*operands(shape, 11, state), reverse)
+
+
+@pytest.mark.parametrize("shape", [(3, 700, 5), (4, 3000, 1), (1, 5000, 70), (500, 12, 1), (2, 40000, 1)])
+@pytest.mark.parametrize("gates", [-8.0, 9.0, 30.0])
+def test_gates_that_forget_at_once_and_that_remember_thousands_of_steps(shape, gates):
+    check(*operands(shape, 13, True, gates), False)
+
+
+@pytest.mark.parametrize("shape", [(3, 700, 5), (4, 3000, 1), (1, 5000, 70), (500, 12, 1), (2, 40000, 1), (2, 3000, 300)])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_sequences_in_a_line(shape, reverse):
+    """A shut gate forgets whatever the state held, an open one passes over whatever the operand holds."""
+    z, x, gh, h0 = operands(shape, 17)
+    r = np.random.default_rng(18)
+    z[r.random(shape) < 0.02] = -np.inf
+    padding = r.random(shape) < 0.05
+    z[padding] = np.inf
+    x[padding] = np.where(r.random(shape) < 0.5, np.nan, np.inf)[padding]
+    x[r.random(shape) < 0.005] = np.nan
+    x[r.random(shape) < 0.005] = np.inf
+    z[r.random(shape) < 0.01] = -3.4e38
+    z[r.random(shape) < 0.01] = 3.4e38
+    h0[0, 0] = np.nan
+    gh[r.random(shape) < 0.003] = np.nan
+    with np.errstate(invalid="ignore"):
+        check(z, x, gh, h0, reverse)
+
+
+@pytest.mark.parametrize("shape", [(3, 20000, 1), (1, 9000, 64)])
+def test_a_state_that_is_not_finite_stays_until_a_gate_is_shut(shape):
+    """Also where the product of the gates since then has left the range of fp32, in whatever piece of the line."""
+    for bad in (np.nan, np.inf, -np.inf):
+        z, x, gh, h0 = operands(shape, 19, True, 0.0)
+        x[:, 3] = bad
+        z[0, 15000 if shape[1] > 15000 else 8000] = -np.inf
+        with np.errstate(invalid="ignore"):
+            check(z, x, gh, h0, False)
+
+
+def test_no_state_to_begin_with_is_zero():
+    z, x, gh, _ = operands((4, 333, 9), 23)
+    a = check(z, x, gh, None, False)
+    b = check(z, x, gh, np.zeros((4, 9), np.float32), False)
+    assert all(torch.equal(p, q) for p, q in zip(a[:3], b[:3]))
+
+
+@pytest.mark.parametrize("shape,dim", [((4, 7, 9, 11), 0), ((4, 7, 9, 11), 1), ((4, 7, 9, 11), -2), ((4, 7, 9, 11), 3), ((50,), 0), ((3, 90), 0)])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_every_dimension_of_an_array(shape, dim, reverse):
+    r = np.random.default_rng(29)
+    z, x, gh = (r.normal(size=shape).astype(np.float32) for _ in range(3))
+    h0 = np.asarray(r.normal(size=shape[:dim % len(shape)] + shape[dim % len(shape) + 1:]), dtype=np.float32)
+    axis = dim % len(shape)
+    lines = lambda t: t.reshape(int(np.prod(shape[:axis])), shape[axis], -1)  # noqa: E731
+    got = znn.recurrence_fwd(dev(z), dev(x), dev(h0).view(h0.shape), dim, reverse)
+    want, bound = gated.recurrence_fwd(lines(z), lines(x), h0, reverse)
+    compare(lines(host(got)), want, bound, "h")
+    grads = znn.recurrence_bwd(dev(gh), dev(z), dev(x), got, dev(h0).view(h0.shape), dim, reverse)
+    wants, bounds = gated.recurrence_bwd(lines(gh), lines(z), lines(x), lines(host(got)), h0, reverse)
+    for name, g, w, b in zip(("gz", "gx", "gh0"), grads, wants, bounds):
+        compare(host(g).reshape(w.shape), w, b, name)
+    assert grads[2].shape == h0.shape
+
+
+@pytest.mark.parametrize("shape,pieces", [((2, 5000, 1), [1, 7, 2048, 2944]), ((1, 700, 96), [1] * 5 + [695]), ((8, 6, 1000), [1] * 6)])
+def test_a_running_sequence_goes_on_from_its_last_state(shape, pieces):
+    z, x, gh, h0 = operands(shape, 31)
+    want, bound = gated.recurrence_fwd(z, x, h0)
+    state, at = dev(h0), 0
+    for n in pieces:
+        h = znn.recurrence_fwd(dev(z[:, at:at + n]), dev(x[:, at:at + n]), state, 1)
+        compare(host(h), want[:, at:at + n], bound[:, at:at + n], at)
+        state, at = h[:, -1].contiguous(), at + n
+
+
+@pytest.mark.parametrize("shape", [(3, 1000, 1), (130, 61, 1), (2, 300, 60), (3, 50, 77), (1, 40000, 1)])
+def test_arrays_on_no_boundary_and_nothing_beside_them(shape):
+    """Operands that begin at any element; what lies before and behind the results stays as it is."""
+    z, x, gh, h0 = operands(shape, 37)
+    n = z.size
+
+    def place(a, first):
+        t = torch.full((a.size + 8,), 7.5, device="cuda:0")
+        t[first:first + a.size] = dev(a).reshape(-1)
+        return t, t[first:first + a.size].view(a.shape)
+
+    h = znn.recurrence_fwd(dev(z), dev(x), dev(h0), 1)
+    grads = znn.recurrence_bwd(dev(gh), dev(z), dev(x), h, dev(h0), 1)
+    for first in (1, 2, 3):
+        views = [place(a, (first + i) % 4)[1] for i, a in enumerate((z, x, gh, h0))]
+        held, out = place(np.zeros(shape), first)
+        assert torch.equal(znn.recurrence_fwd(views[0], views[1], views[3], 1, out=out), h)
+        assert bool((held[:first] == 7.5).all()) and bool((held[first + n:] == 7.5).all())
+        (hz, oz), (hx, ox) = place(np.zeros(shape), (first + 1) % 4), place(np.zeros(shape), first)
+        got = znn.recurrence_bwd(views[2], views[0], views[1], out, views[3], 1, gz=oz, gx=ox)
+        assert all(torch.equal(a, b) for a, b in zip(got, grads))
+        for t, f in ((hz, (first + 1) % 4), (hx, first)):
+            assert bool((t[:f] == 7.5).all()) and bool((t[f + n:] == 7.5).all())
+
+
+@pytest.mark.parametrize("shape", [(3, 70000, 1), (1, 9000, 96), (40, 60, 100), (700, 60, 1)])
+def test_calls_repeat_themselves_on_any_stream_and_in_a_graph(shape):
+    z, x, gh, h0 = (dev(a) for a in operands(shape, 41))
+    h = znn.recurrence_fwd(z, x, h0, 1)
+    grads = znn.recurrence_bwd(gh, z, x, h, h0, 1)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        a = znn.recurrence_fwd(z, x, h0, 1, stream=side)
+        b = znn.recurrence_bwd(gh, z, x, a, h0, 1, stream=side)
+        side.synchronize()
+        assert torch.equal(a, h) and all(torch.equal(p, q) for p, q in zip(b, grads))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a = znn.recurrence_fwd(z, x, h0, 1)
+        b = znn.recurrence_bwd(gh, z, x, a, h0, 1)
+    for number in range(4):
+        x.mul_(-1)
+        gh.mul_(-1)
+        graph.replay()
+        c = znn.recurrence_fwd(z, x, h0, 1)
+        d = znn.recurrence_bwd(gh, z, x, c, h0, 1)
+        torch.cuda.synchronize()
+        assert torch.equal(a, c) and all(torch.equal(p, q) for p, q in zip(b, d)), number
+
+
+def test_two_streams_at_once():
+    sets = [[dev(a) for a in operands((2, 60000, 1), 43 + i)] for i in range(2)] + [[dev(a) for a in operands((1, 9000, 128), 47 + i)] for i in range(2)]
+    wants = [znn.recurrence_fwd(z, x, h0, 1) for z, x, _, h0 in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    got = [[znn.recurrence_fwd(z, x, h0, 1, stream=s) for (z, x, _, h0), s in zip(sets, streams)] for _ in range(5)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for row in got for a, b in zip(row, wants))
+
+
+def test_gradients_against_differences():
+    shape = (2, 300, 3)
+    z, x, gh, h0 = operands(shape, 53)
+    h = znn.recurrence_fwd(dev(z), dev(x), dev(h0), 1)
+    grads = [host(g) for g in znn.recurrence_bwd(dev(gh), dev(z), dev(x), h, dev(h0), 1)]
+    value = lambda z, x, h0: (gated.recurrence_fwd(z, x, h0)[0] * gh).sum()  # noqa: E731
+    r = np.random.default_rng(54)
+    arrays = [t.astype(np.float64) for t in (z, x, h0)]
+    for which in range(3):
+        for _ in range(8):
+            way = [np.zeros_like(t) for t in arrays]
+            way[which] = r.normal(size=arrays[which].shape)
+            e = 1e-5
+            d = (value(*(t + e * w for t, w in zip(arrays, way))) - value(*(t - e * w for t, w in zip(arrays, way)))) / (2 * e)
+            terms = np.abs(grads[which] * way[which]).sum()
+            assert abs(d - (grads[which] * way[which]).sum()) <= 1e-5 * terms + 1e-9
