@@ -7,55 +7,607 @@ namespace znn {
 namespace {
 
 // f = 1 / (1 + exp(-z)) and k = 1 - f = 1 / (1 + exp(z)), each to its own last digits: 1 - f would have lost those of a gate that is nearly open.
+// exp(-|z|) is 2^t times a correction for what t, rounded, leaves of |z| / ln 2; the quotient takes one step of Newton's method.  Both are within a
+// few half-steps, in 14 instructions; expf and a division take 35, and along lines the arithmetic stands beside the memory's time.
 struct Gate { float f, k; };
 __device__ __forceinline__ Gate gate(float z)
 {
-    const float e = expf(-fabsf(z)), large = 1.f / (1.f + e), small = e * large;
-    return z < 0.f ? Gate{small, large} : Gate{large, small};
+    const float m = fminf(fabsf(z), 1e30f), t = m * -1.44269502f;
+    const float rest = fmaf(m, -1.44269502f, -t) + m * -1.92596299e-8f;     // of -|z| / ln 2 = -|z| (1.44269502 + 1.92596299e-8)
+    float e = __builtin_amdgcn_exp2f(t);
+    e = fmaf(e, rest * 0.693147182f, e);
+    const float d = 1.f + e, guess = __builtin_amdgcn_rcpf(d), large = fmaf(fmaf(-d, guess, 1.f), guess, guess), small = e * large;
+    const float f = z < 0.f ? small : large;
+    // a gate of NaN is NaN: the smaller of NaN and a number is the number
+    return z == z ? Gate{f, z < 0.f ? large : small} : Gate{z, z};
 }
 // A factor of 0 takes nothing, not even an infinity: that is how a sequence ends and how padding is passed over.
 __device__ __forceinline__ float times(float a, float v) { return a == 0.f ? 0.f : a * v; }
 
-struct Lines {
-    long outer, length, inner;
-    int reverse;
-};
-struct LinesFwd { Lines L; const float *z, *x, *h0; float* h; };
-struct LinesBwd { Lines L; const float *gh, *z, *x, *h, *h0; float *gz, *gx, *gh0; };
+struct Lines { long outer, length, inner; };
+// `mirror`: steps are taken from the last place of a line to the first.  Forward that is the caller's `reverse`; backward, where
+// gradients flow the other way, its opposite.
+struct LinesFwd { Lines L; int mirror; const float *z, *x, *h0; float* h; };
+struct LinesBwd { Lines L; int mirror; const float *gh, *z, *x, *h, *h0; float *gz, *gx, *gh0; };
 
-// One thread a line.
-__global__ void __launch_bounds__(256) k_lines_fwd(LinesFwd A)
+// What a run of steps makes of the state before it: state -> a state + b.  a is a product of gates: 0 exactly where one of them is (a state
+// of whatever kind is forgotten then), the smallest subnormal where it has only become too small (an infinite state stays one).
+struct Run { float a, b; };
+__device__ __forceinline__ float gates(float p, float q) { return fmaxf(p * q, fminf(fminf(p, q), 1.401298e-45f)); }
+__device__ __forceinline__ Run then(const Run& first, const Run& next)
 {
-    const long lines = A.L.outer * A.L.inner, step = A.L.reverse ? -A.L.inner : A.L.inner;
+    return Run{gates(first.a, next.a), times(next.a, first.b) + next.b};
+}
+__device__ __forceinline__ float after(const Run& r, float state) { return times(r.a, state) + r.b; }
+
+// ---------------------------------------------------------------- pieces of a line that wait for each other
+// A line too long for one workgroup is cut into pieces, and a workgroup takes a piece where its ticket says: the pieces before it have been taken by
+// workgroups that run already.  Each piece leaves what it makes of a state as soon as it has seen its own steps, for those behind it in its group of pieces,
+// and the last piece of a group leaves the state after the group.  The state before a piece follows from the state after the group before and from what the
+// pieces before it in its own group make of that, joined in one order: results do not depend on who came first.  A record is one word of 64 bits, so that
+// nothing has to be ordered with it; `kPending` is no factor (a factor is in 0 .. 1).  Everything is read once and written once; two launches that
+// read the operands twice would move 20 instead of 12 bytes an element forward, 32 instead of 24 backward.
+constexpr unsigned kPending = 0xffffffffu;
+constexpr int kPatience = 1 << 22;      // looks at a record: far more than any wait takes; then the state is NaN instead of a launch that never ends
+
+struct Chain { unsigned* ticket; unsigned long *runs, *states; };   // ticket NULL: no piece waits for another
+
+__global__ void __launch_bounds__(256) k_lines_begin(Chain C, long records)
+{
+    if (blockIdx.x == 0 && threadIdx.x == 0) *C.ticket = 0;
+    for (long i = blockIdx.x * 256L + threadIdx.x; i < records; i += gridDim.x * 256L) C.runs[i] = ~0ul;
+}
+
+__device__ __forceinline__ unsigned take_ticket(const Chain& C)
+{
+    __shared__ unsigned taken;
+    if (!C.ticket) return blockIdx.x;
+    if (threadIdx.x == 0) taken = __hip_atomic_fetch_add(C.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(taken);
+}
+__device__ __forceinline__ void leave(unsigned long* at, const Run& r)
+{
+    const unsigned long w = (unsigned long)__builtin_bit_cast(unsigned, r.b) << 32 | __builtin_bit_cast(unsigned, r.a);
+    __hip_atomic_store(at, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ unsigned long look(const unsigned long* at)
+{
+    return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ Run await(const unsigned long* at, unsigned long w)
+{
+    for (int n = 0; (unsigned)w == kPending; ++n) {
+        if (n == kPatience) return Run{0.f, __builtin_nanf("")};
+        __builtin_amdgcn_s_sleep(1);
+        w = look(at);
+    }
+    return Run{__builtin_bit_cast(float, (unsigned)w), __builtin_bit_cast(float, (unsigned)(w >> 32))};
+}
+
+// ---------------------------------------------------------------- across: a lane a line
+// Lanes are neighbouring lines, so that a step of 64 lines is one or a few runs of memory.  A wave holds P steps of its lines in registers, the
+// waves of a workgroup follow each other, W P steps in all; what the waves make of a state goes through shared memory.
+
+constexpr int kMostWaves = 16;
+
+struct Across { unsigned groups, pieces; int waves; Chain chain; };     // groups of 64 lines, pieces of a line
+
+constexpr int kAcrossGroup = 16;        // pieces of a group
+
+// The state before this wave's steps.  All waves of the workgroup call it with what their steps make of a state.
+__device__ __forceinline__ float state_before(const Run& mine, const Across& T, unsigned piece, long line, float first)
+{
+    __shared__ Run runs[kMostWaves][64];
+    __shared__ float states[64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float state = first;
+    if (T.waves > 1 || T.pieces > 1) {
+        runs[wave][lane] = mine;
+        __syncthreads();
+    }
+    if (T.pieces > 1) {
+        if (wave == 0) {
+            Run all = mine;
+            for (int w = 1; w < T.waves; ++w) all = then(all, runs[w][lane]);
+            // lines behind the last one have records of their own
+            const long row = (long)T.groups * 64;
+            const unsigned group = piece / kAcrossGroup, at = piece % kAcrossGroup;
+            unsigned long* const here = T.chain.runs + piece * row + line;
+            const bool last = piece + 1 == T.pieces;
+            if (at + 1 < kAcrossGroup && !last) leave(here, all);
+            unsigned long w[kAcrossGroup];
+            const unsigned long* const before = T.chain.states + ((long)group - 1) * row + line;
+            const unsigned long s = group ? look(before) : 0ul;
+#pragma unroll
+            for (int i = 0; i < kAcrossGroup; ++i) w[i] = i < (int)at ? look(here - ((int)at - i) * row) : 0ul;
+            Run seen = {1.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < kAcrossGroup; ++i)
+                if (i < (int)at) seen = then(seen, await(here - ((int)at - i) * row, w[i]));
+            all = then(seen, all);
+            if (group) state = await(before, s).b;
+            if (at + 1 == kAcrossGroup && !last) leave(T.chain.states + (long)group * row + line, Run{0.f, after(all, state)});
+            states[lane] = after(seen, state);
+        }
+        __syncthreads();
+        state = states[lane];
+    }
+    for (int w = 0; w < wave; ++w) state = after(runs[w][lane], state);
+    return state;
+}
+
+template <int P>
+__global__ void __launch_bounds__(1024) k_lines_across(LinesFwd A, Across T)
+{
+    const unsigned ticket = take_ticket(T.chain), piece = ticket / T.groups, group = ticket - piece * T.groups;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long lines = A.L.outer * A.L.inner, line = group * 64L + lane, l = line < lines ? line : lines - 1;
+    const long o = l / A.L.inner, step = A.mirror ? -A.L.inner : A.L.inner;
+    const long t0 = ((long)piece * T.waves + wave) * P, left = A.L.length - t0;
+    const int n = left > P ? P : left > 0 ? (int)left : 0;       // uniform in a wave
+    const long at = (o * A.L.length + (A.mirror ? A.L.length - 1 - t0 : t0)) * A.L.inner + (l - o * A.L.inner);
+    float f[P], b[P];
+    const float *pz = A.z + at, *px = A.x + at;
+#pragma unroll
+    for (int i = 0; i < P; ++i, pz += step, px += step)
+        if (i < n) { f[i] = *pz; b[i] = *px; }
+    Run mine = {1.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+        if (i < n) {
+            const Gate g = gate(f[i]);
+            f[i] = g.f;
+            b[i] = times(g.k, b[i]);
+            mine = then(mine, Run{f[i], b[i]});
+        }
+    float h = state_before(mine, T, piece, line, A.h0 ? A.h0[l] : 0.f);
+    if (line >= lines) return;
+    float* ph = A.h + at;
+#pragma unroll
+    for (int i = 0; i < P; ++i, ph += step)
+        if (i < n) *ph = h = times(f[i], h) + b[i];
+}
+
+// What flows backwards is q_t = f_t G_t with G_t = gh_t + q_(t+1): the factors of a step are its own.
+__device__ __forceinline__ float grads(const Gate& g, float G, float before, float x, float& gz)
+{
+    gz = g.f == 0.f || g.k == 0.f ? 0.f : G * (before - x) * (g.f * g.k);
+    return times(g.k, G);
+}
+
+template <int P>
+__global__ void __launch_bounds__(1024) k_lines_across_bwd(LinesBwd A, Across T)
+{
+    const unsigned ticket = take_ticket(T.chain), piece = ticket / T.groups, group = ticket - piece * T.groups;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long lines = A.L.outer * A.L.inner, line = group * 64L + lane, l = line < lines ? line : lines - 1;
+    const long o = l / A.L.inner, step = A.mirror ? -A.L.inner : A.L.inner;
+    const long t0 = ((long)piece * T.waves + wave) * P, left = A.L.length - t0;
+    const int n = left > P ? P : left > 0 ? (int)left : 0;
+    const long at = (o * A.L.length + (A.mirror ? A.L.length - 1 - t0 : t0)) * A.L.inner + (l - o * A.L.inner);
+    float z[P], gh[P], x[P], before[P];
+    const float h0 = A.h0 ? A.h0[l] : 0.f;
+    const float *pz = A.z + at, *pg = A.gh + at, *px = A.x + at, *ph = A.h + at + step;
+#pragma unroll
+    for (int i = 0; i < P; ++i, pz += step, pg += step)
+        if (i < n) { z[i] = *pz; gh[i] = *pg; }
+#pragma unroll
+    for (int i = 0; i < P; ++i, px += step, ph += step)
+        if (i < n) { x[i] = *px; before[i] = i < n - 1 || n < left ? *ph : h0; }
+    Run mine = {1.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+        if (i < n) {
+            const float f = gate(z[i]).f;
+            mine = then(mine, Run{f, times(f, gh[i])});
+        }
+    float q = state_before(mine, T, piece, line, 0.f);
+    if (line >= lines) return;
+    float *qx = A.gx + at, *qz = A.gz + at;
+#pragma unroll
+    for (int i = 0; i < P; ++i, qx += step, qz += step)
+        if (i < n) {
+            const Gate g = gate(z[i]);
+            const float G = gh[i] + q;
+            *qx = grads(g, G, before[i], x[i], *qz);
+            q = times(g.f, G);
+        }
+    if (A.gh0 && n > 0 && t0 + n == A.L.length) A.gh0[l] = q;
+}
+
+// ---------------------------------------------------------------- along: lanes follow a line
+// Lines along the fastest extent lie one behind the other, so that the array is one line of outer * length steps in which a line begins every
+// `length` steps: a step whose gate takes nothing of the state before it.  A lane holds quads of four neighbouring steps, a wave kQuads rows of
+// 64 quads, one after the other; the waves of a workgroup follow each other.
+
+constexpr int kQuads = 4, kWaveSteps = 256 * kQuads, kAlongWaves = 4, kFarOff = 1 << 30;
+typedef float floatu4 __attribute__((ext_vector_type(4), aligned(4)));      // lines begin at any element
+
+// steps in all and of a workgroup; min(length, kFarOff)
+struct Along { long steps; int tile; FastDiv line; Chain chain; };
+
+// The beginnings of lines in a tile.
+struct Tile {
+    long first;                 // the tile's first step
+    int count;                  // its steps
+    long line;                  // the line of the first one
+    int left;                   // steps of that line from there on, at most kFarOff
+    bool begins;                // with its first one
+};
+__device__ __forceinline__ Tile tile_of(const Lines& L, const Along& T, unsigned number)
+{
+    const long first = (long)number * T.tile, line = first / L.length, pos = first - line * L.length, left = L.length - pos;
+    return Tile{first, (int)(T.steps - first < T.tile ? T.steps - first : T.tile), line, left < kFarOff ? (int)left : kFarOff, pos == 0};
+}
+// From step `off` of the tile on: its line, whether that begins there, and in how many steps the next one does.
+struct Run4 { long line; int until; bool begins; };
+__device__ __forceinline__ Run4 place_in_line(const Tile& S, const FastDiv& length, int off)
+{
+    if (off < S.left) return Run4{S.line, S.left - off, S.begins && off == 0};
+    const unsigned u = (unsigned)(off - S.left), n = fdiv_any(u, length), pos = u - n * length.d;
+    return Run4{S.line + 1 + n, (int)(length.d - pos), pos == 0};
+}
+// Does a line begin at the j-th step from there?  Called for j = 1, 2, 3 (4) in order.
+__device__ __forceinline__ bool next_begins(Run4& R, const FastDiv& length, int j)
+{
+    if (j != R.until) return false;
+    R.until += (int)length.d;
+    ++R.line;
+    return true;
+}
+
+// Four steps from step e on; `most` of them are there.  Memory runs against the steps where mirrored: step 0 is element `last` then.
+__device__ __forceinline__ void load_steps(float (&v)[4], const float* p, long e, int most, bool mirror, long last)
+{
+    if (most >= 4) {
+        const floatu4 q = *(const floatu4*)(mirror ? p + (last - 3 - e) : p + e);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = mirror ? q[3 - j] : q[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = j < most ? (mirror ? p[last - e - j] : p[e + j]) : 0.f;
+    }
+}
+__device__ __forceinline__ void store_steps(const float (&v)[4], float* p, long e, int most, bool mirror, long last)
+{
+    if (most >= 4) {
+        floatu4 q;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[j] = mirror ? v[3 - j] : v[j];
+        *(floatu4*)(mirror ? p + (last - 3 - e) : p + e) = q;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < most) (mirror ? p[last - e - j] : p[e + j]) = v[j];
+    }
+}
+
+// The value of another lane, by the data path between lanes: `none` where there is no such lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float other_lane(float none, float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ Run other_lane(const Run& r) { return Run{other_lane<CTRL, ROWS>(1.f, r.a), other_lane<CTRL, ROWS>(0.f, r.b)}; }
+__device__ __forceinline__ float last_lane(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+
+// What this lane and those before it make of a state: rows of 16 lanes, then the last lane of the row and of the two rows before.
+__device__ __forceinline__ Run scan_lanes(Run r)
+{
+    r = then(other_lane<0x111>(r), r);          // one to eight lanes up in a row
+    r = then(other_lane<0x112>(r), r);
+    r = then(other_lane<0x114>(r), r);
+    r = then(other_lane<0x118>(r), r);
+    r = then(other_lane<0x142, 0xa>(r), r);     // lane 15 of the row before to rows 1 and 3
+    r = then(other_lane<0x143, 0xc>(r), r);     // lane 31 to rows 2 and 3
+    return r;
+}
+// The same without this lane (`before`) and for all lanes (the result).
+__device__ __forceinline__ Run scan_lanes(const Run& mine, Run& before)
+{
+    const Run r = scan_lanes(mine);
+    before = other_lane<0x138>(r);              // one lane up in the wave
+    return Run{last_lane(r.a), last_lane(r.b)};
+}
+
+constexpr int kAlongGroup = 64;         // pieces of a group: a lane a record
+
+// The state before this wave's steps.
+__device__ __forceinline__ float state_before(const Run& mine, const Along& T, const Tile& S, unsigned number)
+{
+    __shared__ Run runs[kMostWaves];
+    __shared__ float shared_state;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    if (lane == 0) runs[wave] = mine;
+    __syncthreads();
+    float state = 0.f;
+    if (T.chain.ticket) {
+        if (wave == 0) {
+            Run all = mine;
+            for (int w = 1; w < waves; ++w) all = then(all, runs[w]);
+            const unsigned group = number / kAlongGroup, at = number % kAlongGroup;
+            const bool leaves = at + 1 == kAlongGroup && number + 1 < gridDim.x;
+            if (lane == 0 && at + 1 < kAlongGroup) leave(T.chain.runs + number, all);
+            // nothing reaches a tile that begins with a line
+            if (!S.begins) {
+                const unsigned long* const from = T.chain.runs + (number - at + lane);
+                const Run r = scan_lanes(lane < (int)at ? await(from, look(from)) : Run{1.f, 0.f});
+                const Run seen = {last_lane(r.a), last_lane(r.b)};
+                if (seen.a != 0.f && group) {
+                    const unsigned long* const before = T.chain.states + (group - 1);
+                    state = await(before, look(before)).b;
+                }
+                state = after(seen, state);
+            }
+            if (lane == 0 && leaves) leave(T.chain.states + group, Run{0.f, after(all, state)});
+            if (lane == 0) shared_state = state;
+        }
+        __syncthreads();
+        state = shared_state;
+    }
+    for (int w = 0; w < wave; ++w) state = after(runs[w], state);
+    return state;
+}
+
+__global__ void __launch_bounds__(64 * kAlongWaves) k_lines_along(LinesFwd A, Along T)
+{
+    const unsigned number = take_ticket(T.chain);
+    const Tile S = tile_of(A.L, T, number);
+    const int off0 = (threadIdx.x >> 6) * kWaveSteps + (threadIdx.x & 63) * 4;
+    float f[kQuads][4], b[kQuads][4];
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) {
+        const int off = off0 + q * 256;
+        load_steps(f[q], A.z, S.first + off, S.count - off, A.mirror, T.steps - 1);
+        load_steps(b[q], A.x, S.first + off, S.count - off, A.mirror, T.steps - 1);
+    }
+    Run mine = {1.f, 0.f}, before[kQuads];
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) {
+        const int off = off0 + q * 256;
+        Run4 R = place_in_line(S, T.line, off);
+        Run r = {1.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool begins = j ? next_begins(R, T.line, j) : R.begins, there = off + j < S.count;
+            const Gate g = gate(f[q][j]);
+            f[q][j] = there ? g.f : 1.f;
+            b[q][j] = there ? times(g.k, b[q][j]) : 0.f;
+            if (begins && there) {
+                if (A.h0) b[q][j] += times(g.f, A.h0[A.mirror ? A.L.outer - 1 - R.line : R.line]);
+                f[q][j] = 0.f;
+            }
+            r = then(r, Run{f[q][j], b[q][j]});
+        }
+        const Run all = scan_lanes(r, before[q]);
+        before[q] = then(mine, before[q]);
+        mine = then(mine, all);
+    }
+    const float first = state_before(mine, T, S, number);
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) {
+        const int off = off0 + q * 256;
+        float h = after(before[q], first);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[q][j] = h = times(f[q][j], h) + b[q][j];
+        store_steps(b[q], A.h, S.first + off, S.count - off, A.mirror, T.steps - 1);
+    }
+}
+
+__global__ void __launch_bounds__(64 * kAlongWaves) k_lines_along_bwd(LinesBwd A, Along T)
+{
+    const unsigned number = take_ticket(T.chain);
+    const Tile S = tile_of(A.L, T, number);
+    const int off0 = (threadIdx.x >> 6) * kWaveSteps + (threadIdx.x & 63) * 4;
+    const long last = T.steps - 1;
+    float z[kQuads][4], gh[kQuads][4], x[kQuads][4], h[kQuads][4];
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) {
+        const int off = off0 + q * 256;
+        load_steps(z[q], A.z, S.first + off, S.count - off, A.mirror, last);
+        load_steps(gh[q], A.gh, S.first + off, S.count - off, A.mirror, last);
+        load_steps(x[q], A.x, S.first + off, S.count - off, A.mirror, last);
+        // the step before is the next one here
+        const long e = S.first + off + 1;
+        load_steps(h[q], A.h, e, off >= S.count ? 0 : T.steps - e < 4 ? (int)(T.steps - e) : 4, A.mirror, last);
+    }
+    Run mine = {1.f, 0.f}, before[kQuads];
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) {
+        const int off = off0 + q * 256;
+        Run4 R = place_in_line(S, T.line, off);
+        Run r = {1.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool begins = j ? next_begins(R, T.line, j) : R.begins, there = off + j < S.count;
+            const float f = gate(z[q][j]).f;
+            if (there) r = then(r, Run{begins ? 0.f : f, times(f, gh[q][j])});
+        }
+        const Run all = scan_lanes(r, before[q]);
+        before[q] = then(mine, before[q]);
+        mine = then(mine, all);
+    }
+    const float first = state_before(mine, T, S, number);
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) {
+        const int off = off0 + q * 256, most = S.count - off;
+        Run4 R = place_in_line(S, T.line, off);
+        float state = after(before[q], first);
+        if (R.begins) state = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const long line = A.mirror ? A.L.outer - 1 - R.line : R.line;
+            const bool ends = next_begins(R, T.line, j + 1);
+            const Gate g = gate(z[q][j]);
+            const float G = gh[q][j] + state;
+            if (ends && j < most) h[q][j] = A.h0 ? A.h0[line] : 0.f;
+            float gz;
+            x[q][j] = grads(g, G, h[q][j], x[q][j], gz);
+            z[q][j] = gz;
+            state = times(g.f, G);
+            if (ends) {
+                if (A.gh0 && j < most) A.gh0[line] = state;
+                state = 0.f;
+            }
+        }
+        store_steps(x[q], A.gx, S.first + off, most, A.mirror, last);
+        store_steps(z[q], A.gz, S.first + off, most, A.mirror, last);
+    }
+}
+
+// ---------------------------------------------------------------- many lines: a lane a line from its first step to its last
+// Where lines alone fill the chip nothing has to be joined: a lane walks its line, the operands of U steps requested together.
+
+template <int U>
+__global__ void __launch_bounds__(256) k_lines_walk(LinesFwd A)
+{
+    const long lines = A.L.outer * A.L.inner, step = A.mirror ? -A.L.inner : A.L.inner;
     for (long l = blockIdx.x * 256L + threadIdx.x; l < lines; l += gridDim.x * 256L) {
-        const long o = l / A.L.inner, i = l - o * A.L.inner;
-        long at = (o * A.L.length + (A.L.reverse ? A.L.length - 1 : 0)) * A.L.inner + i;
+        const long o = l / A.L.inner;
+        long at = (o * A.L.length + (A.mirror ? A.L.length - 1 : 0)) * A.L.inner + (l - o * A.L.inner);
         float h = A.h0 ? A.h0[l] : 0.f;
-        for (long t = 0; t < A.L.length; ++t, at += step) {
-            const Gate g = gate(A.z[at]);
-            h = times(g.f, h) + times(g.k, A.x[at]);
-            A.h[at] = h;
+        for (long t = 0; t < A.L.length; t += U, at += U * step) {
+            float z[U], x[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+                if (t + i < A.L.length) { z[i] = A.z[at + i * step]; x[i] = A.x[at + i * step]; }
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+                if (t + i < A.L.length) {
+                    const Gate g = gate(z[i]);
+                    h = times(g.f, h) + times(g.k, x[i]);
+                    A.h[at + i * step] = h;
+                }
         }
     }
 }
 
-// What flows backwards is q_t = f_t G_t, G_t = gh_t + q_(t+1): the factors of a step are its own.
-__global__ void __launch_bounds__(256) k_lines_bwd(LinesBwd A)
+template <int U>
+__global__ void __launch_bounds__(256) k_lines_walk_bwd(LinesBwd A)
 {
-    const long lines = A.L.outer * A.L.inner, step = A.L.reverse ? -A.L.inner : A.L.inner;
+    const long lines = A.L.outer * A.L.inner, step = A.mirror ? -A.L.inner : A.L.inner;
     for (long l = blockIdx.x * 256L + threadIdx.x; l < lines; l += gridDim.x * 256L) {
-        const long o = l / A.L.inner, i = l - o * A.L.inner;
-        long at = (o * A.L.length + (A.L.reverse ? 0 : A.L.length - 1)) * A.L.inner + i;
+        const long o = l / A.L.inner;
+        long at = (o * A.L.length + (A.mirror ? A.L.length - 1 : 0)) * A.L.inner + (l - o * A.L.inner);
+        const float h0 = A.h0 ? A.h0[l] : 0.f;
         float q = 0.f;
-        for (long t = A.L.length - 1; t >= 0; --t, at -= step) {
-            const Gate g = gate(A.z[at]);
-            const float G = A.gh[at] + q, before = t > 0 ? A.h[at - step] : A.h0 ? A.h0[l] : 0.f;
-            A.gx[at] = times(g.k, G);
-            A.gz[at] = g.f == 0.f || g.k == 0.f ? 0.f : G * (before - A.x[at]) * (g.f * g.k);
-            q = times(g.f, G);
+        for (long t = 0; t < A.L.length; t += U, at += U * step) {
+            float z[U], x[U], gh[U], before[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+                if (t + i < A.L.length) {
+                    z[i] = A.z[at + i * step]; x[i] = A.x[at + i * step]; gh[i] = A.gh[at + i * step];
+                    before[i] = t + i + 1 < A.L.length ? A.h[at + (i + 1) * step] : h0;
+                }
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+                if (t + i < A.L.length) {
+                    const Gate g = gate(z[i]);
+                    const float G = gh[i] + q;
+                    float gz;
+                    A.gx[at + i * step] = grads(g, G, before[i], x[i], gz);
+                    A.gz[at + i * step] = gz;
+                    q = times(g.f, G);
+                }
         }
         if (A.gh0) A.gh0[l] = q;
     }
+}
+
+// ---------------------------------------------------------------- the choice
+enum Way { WALK, ACROSS, ALONG };
+constexpr int kSteps = 32, kStepsBwd = 16;      // of a wave across
+struct Split {
+    Way way;
+    int waves;              // of a workgroup
+    long groups, pieces;    // across: groups of 64 lines, pieces of a line; along: tiles
+    int tile;               // along: steps of one
+    bool chained;
+};
+
+Split lines_split(const Lines& L, bool backward)
+{
+    Split S = {};
+    const long lines = L.outer * L.inner;
+    if (L.inner == 1) {
+        S.way = ALONG;
+        S.waves = kAlongWaves;
+        S.tile = S.waves * kWaveSteps;
+        const long steps = L.outer * L.length, whole = L.length <= S.tile ? S.tile / L.length * L.length : 0;
+        S.chained = 4 * whole < 3 * S.tile;
+        if (!S.chained) S.tile = (int)whole;
+        S.pieces = (steps + S.tile - 1) / S.tile;
+        S.groups = 1;
+        S.chained = S.chained && S.pieces > 1;
+        return S;
+    }
+    const int steps = backward ? kStepsBwd : kSteps;
+    if (lines >= 1L << 17 || L.length <= steps / 2) return S;
+    S.way = ACROSS;
+    S.waves = (int)std::min((L.length + steps - 1) / steps, (long)kMostWaves);
+    S.pieces = (L.length + S.waves * steps - 1) / (S.waves * steps);
+    if (S.pieces > 1) {
+        S.waves = 8;
+        S.pieces = (L.length + S.waves * steps - 1) / (S.waves * steps);
+    }
+    S.groups = (lines + 63) / 64;
+    S.chained = S.pieces > 1;
+    return S;
+}
+
+// Records of pieces and of their groups
+size_t runs_of(const Split& S) { return (size_t)S.pieces * (S.way == ACROSS ? 64 * S.groups : 1); }
+size_t states_of(const Split& S) { return S.way == ACROSS ? (size_t)(S.pieces / kAcrossGroup) * 64 * S.groups : S.pieces / kAlongGroup; }
+size_t split_bytes(const Split& S) { return S.chained ? 256 + sizeof(unsigned long) * (runs_of(S) + states_of(S)) : 0; }
+
+int begin_lines(const Split& S, void* ws, Chain* C, hipStream_t s)
+{
+    *C = Chain{};
+    if (!S.chained) return ZNN_OK;
+    unsigned long* const runs = (unsigned long*)((char*)ws + 256);
+    *C = Chain{(unsigned*)ws, runs, runs + runs_of(S)};
+    const long records = (long)(runs_of(S) + states_of(S));
+    ZNN_LAUNCH("recurrence pieces", s, k_lines_begin, dim3((unsigned)std::min((records + 255) / 256, 2048L)), dim3(256), 0, *C, records);
+    return check_launch("recurrence pieces");
+}
+
+unsigned walk_groups(const Lines& L) { return (unsigned)std::min((L.outer * L.inner + 255) / 256, 1L << 20); }
+Along along(const Lines& L, const Split& S, const Chain& C)
+{
+    return Along{L.outer * L.length, S.tile, make_fastdiv((unsigned)std::min(L.length, (long)kFarOff)), C};
+}
+
+int lines_fwd(const LinesFwd& A, void* ws, hipStream_t s)
+{
+    const Split S = lines_split(A.L, false);
+    Chain C;
+    const int rc = begin_lines(S, ws, &C, s);
+    if (rc != ZNN_OK) return rc;
+    const dim3 grid((unsigned)(S.groups * S.pieces)), block(64 * S.waves);
+    if (S.way == ALONG) ZNN_LAUNCH("recurrence forward", s, k_lines_along, grid, block, 0, A, along(A.L, S, C));
+    else if (S.way == ACROSS)
+        ZNN_LAUNCH("recurrence forward", s, k_lines_across<kSteps>, grid, block, 0, A, Across{(unsigned)S.groups, (unsigned)S.pieces, S.waves, C});
+    else ZNN_LAUNCH("recurrence forward", s, k_lines_walk<8>, dim3(walk_groups(A.L)), dim3(256), 0, A);
+    return check_launch("recurrence forward");
+}
+
+int lines_bwd(const LinesBwd& A, void* ws, hipStream_t s)
+{
+    const Split S = lines_split(A.L, true);
+    Chain C;
+    const int rc = begin_lines(S, ws, &C, s);
+    if (rc != ZNN_OK) return rc;
+    const dim3 grid((unsigned)(S.groups * S.pieces)), block(64 * S.waves);
+    if (S.way == ALONG) ZNN_LAUNCH("recurrence backward", s, k_lines_along_bwd, grid, block, 0, A, along(A.L, S, C));
+    else if (S.way == ACROSS)
+        ZNN_LAUNCH("recurrence backward", s, k_lines_across_bwd<kStepsBwd>, grid, block, 0, A, Across{(unsigned)S.groups, (unsigned)S.pieces, S.waves, C});
+    else ZNN_LAUNCH("recurrence backward", s, k_lines_walk_bwd<4>, dim3(walk_groups(A.L)), dim3(256), 0, A);
+    return check_launch("recurrence backward");
 }
 
 int check_lines(int64_t outer, int64_t length, int64_t inner)
@@ -67,7 +619,7 @@ int check_lines(int64_t outer, int64_t length, int64_t inner)
     return ZNN_OK;
 }
 
-size_t lines_workspace(const Lines&) { return 0; }
+size_t lines_workspace(const Lines& L) { return std::max(split_bytes(lines_split(L, false)), split_bytes(lines_split(L, true))); }
 
 int check_lines_workspace(const Lines& L, const void* ws, size_t ws_bytes)
 {
@@ -91,7 +643,7 @@ int znn_recurrence_workspace_bytes(int64_t outer, int64_t length, int64_t inner,
     int rc = check_lines(outer, length, inner);
     if (rc != ZNN_OK) return rc;
     if (!bytes) return fail(ZNN_EINVAL, "NULL argument");
-    *bytes = lines_workspace(Lines{(long)outer, (long)length, (long)inner, 0});
+    *bytes = lines_workspace(Lines{(long)outer, (long)length, (long)inner});
     return ZNN_OK;
 }
 
@@ -101,12 +653,10 @@ int znn_recurrence_fwd(int64_t outer, int64_t length, int64_t inner, int32_t rev
     int rc = check_lines(outer, length, inner);
     if (rc != ZNN_OK) return rc;
     if (!z || !x || !h) return fail(ZNN_EINVAL, "NULL argument");
-    const LinesFwd A = {{(long)outer, (long)length, (long)inner, reverse != 0}, z, x, h0, h};
+    const LinesFwd A = {{(long)outer, (long)length, (long)inner}, reverse != 0, z, x, h0, h};
     rc = check_lines_workspace(A.L, ws, ws_bytes);
     if (rc != ZNN_OK) return rc;
-    const hipStream_t s = (hipStream_t)stream;
-    ZNN_LAUNCH("recurrence forward", s, k_lines_fwd, dim3((unsigned)std::min((outer * inner + 255) / 256, (int64_t)1 << 20)), dim3(256), 0, A);
-    return check_launch("recurrence forward");
+    return lines_fwd(A, ws, (hipStream_t)stream);
 }
 
 int znn_recurrence_bwd(int64_t outer, int64_t length, int64_t inner, int32_t reverse, const float* gh, const float* z, const float* x,
@@ -115,12 +665,10 @@ int znn_recurrence_bwd(int64_t outer, int64_t length, int64_t inner, int32_t rev
     int rc = check_lines(outer, length, inner);
     if (rc != ZNN_OK) return rc;
     if (!gh || !z || !x || !h || !gz || !gx) return fail(ZNN_EINVAL, "NULL argument");
-    const LinesBwd A = {{(long)outer, (long)length, (long)inner, reverse != 0}, gh, z, x, h, h0, gz, gx, gh0};
+    const LinesBwd A = {{(long)outer, (long)length, (long)inner}, reverse == 0, gh, z, x, h, h0, gz, gx, gh0};
     rc = check_lines_workspace(A.L, ws, ws_bytes);
     if (rc != ZNN_OK) return rc;
-    const hipStream_t s = (hipStream_t)stream;
-    ZNN_LAUNCH("recurrence backward", s, k_lines_bwd, dim3((unsigned)std::min((outer * inner + 255) / 256, (int64_t)1 << 20)), dim3(256), 0, A);
-    return check_launch("recurrence backward");
+    return lines_bwd(A, ws, (hipStream_t)stream);
 }
 
 }  // extern "C"
