@@ -42,15 +42,16 @@ __device__ __forceinline__ float after(const Run& r, float state) { return times
 
 // ---------------------------------------------------------------- pieces of a line that wait for each other
 // A line too long for one workgroup is cut into pieces, and a workgroup takes a piece where its ticket says: the pieces before it have been taken by
-// workgroups that run already.  Each piece leaves what it makes of a state as soon as it has seen its own steps, for those behind it in its group of pieces,
-// and the last piece of a group leaves the state after the group.  The state before a piece follows from the state after the group before and from what the
-// pieces before it in its own group make of that, joined in one order: results do not depend on who came first.  A record is one word of 64 bits, so that
-// nothing has to be ordered with it; `kPending` is no factor (a factor is in 0 .. 1).  Everything is read once and written once; two launches that
-// read the operands twice would move 20 instead of 12 bytes an element forward, 32 instead of 24 backward.
+// workgroups that run already.  Each piece leaves what it makes of a state as soon as it has seen its own steps; the last piece of a group of pieces
+// leaves what the group does, and the last piece of a group of groups leaves the state after it.  The state before a piece follows from the last such state, the
+// groups since then and the pieces since the last of those, joined in one order: results do not depend on who came first, and pieces wait for a
+// state to be handed on once in a group of groups only.  A record is one word of 64 bits, so that nothing has to be ordered with it; `kPending` is no
+// factor (a factor is in 0 .. 1).  Everything is read once and written once; two launches that read the operands twice would move 20 instead of 12
+// bytes an element forward, 32 instead of 24 backward.
 constexpr unsigned kPending = 0xffffffffu;
 constexpr int kPatience = 1 << 22;      // looks at a record: far more than any wait takes; then the state is NaN instead of a launch that never ends
 
-struct Chain { unsigned* ticket; unsigned long *runs, *states; };   // ticket NULL: no piece waits for another
+struct Chain { unsigned* ticket; unsigned long *runs, *groups, *states; };   // ticket NULL: no piece waits for another
 
 __global__ void __launch_bounds__(256) k_lines_begin(Chain C, long records)
 {
@@ -86,65 +87,76 @@ __device__ __forceinline__ Run await(const unsigned long* at, unsigned long w)
 }
 
 // ---------------------------------------------------------------- across: a lane a line
-// Lanes are neighbouring lines, so that a step of 64 lines is one or a few runs of memory.  A wave holds P steps of its lines in registers, the
-// waves of a workgroup follow each other, W P steps in all; what the waves make of a state goes through shared memory.
+// Lanes are neighbouring lines, so that a step of 64 lines is one or a few runs of memory.  A wave holds P steps of its lines in registers.  Of the
+// waves of a workgroup `beside` lie side by side and `waves` follow each other; what they make of a state goes through shared memory.
 
-constexpr int kMostWaves = 16;
+constexpr int kMostWaves = 8;
 
-struct Across { unsigned groups, pieces; int waves; Chain chain; };     // groups of 64 lines, pieces of a line
+struct Across { unsigned groups, pieces; int waves, beside; Chain chain; };     // groups of 64 * beside lines, pieces of a line
 
-constexpr int kAcrossGroup = 16;        // pieces of a group
+constexpr int kAcrossGroup = 16;        // pieces of a group, groups of a group of groups
+
+// What `count` records from `at` on, `row` apart, make of a state.
+__device__ __forceinline__ Run join_records(const unsigned long* at, long row, int count)
+{
+    unsigned long w[kAcrossGroup];
+#pragma unroll
+    for (int i = 0; i < kAcrossGroup; ++i) w[i] = i < count ? look(at + i * row) : 0ul;
+    Run seen = {1.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kAcrossGroup; ++i)
+        if (i < count) seen = then(seen, await(at + i * row, w[i]));
+    return seen;
+}
 
 // The state before this wave's steps.  All waves of the workgroup call it with what their steps make of a state.
-__device__ __forceinline__ float state_before(const Run& mine, const Across& T, unsigned piece, long line, float first)
+__device__ __forceinline__ float state_before(const Run& mine, const Across& T, unsigned piece, long line, int after_waves, float first)
 {
-    __shared__ Run runs[kMostWaves][64];
-    __shared__ float states[64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ Run runs[kMostWaves][64], pieces[kMostWaves][64];
+    __shared__ float states[kMostWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, side = wave - after_waves * T.beside;
     float state = first;
     if (T.waves > 1 || T.pieces > 1) {
         runs[wave][lane] = mine;
         __syncthreads();
     }
     if (T.pieces > 1) {
-        if (wave == 0) {
-            Run all = mine;
-            for (int w = 1; w < T.waves; ++w) all = then(all, runs[w][lane]);
-            // lines behind the last one have records of their own
-            const long row = (long)T.groups * 64;
-            const unsigned group = piece / kAcrossGroup, at = piece % kAcrossGroup;
-            unsigned long* const here = T.chain.runs + piece * row + line;
-            const bool last = piece + 1 == T.pieces;
-            if (at + 1 < kAcrossGroup && !last) leave(here, all);
-            unsigned long w[kAcrossGroup];
-            const unsigned long* const before = T.chain.states + ((long)group - 1) * row + line;
-            const unsigned long s = group ? look(before) : 0ul;
-#pragma unroll
-            for (int i = 0; i < kAcrossGroup; ++i) w[i] = i < (int)at ? look(here - ((int)at - i) * row) : 0ul;
-            Run seen = {1.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < kAcrossGroup; ++i)
-                if (i < (int)at) seen = then(seen, await(here - ((int)at - i) * row, w[i]));
-            all = then(seen, all);
-            if (group) state = await(before, s).b;
-            if (at + 1 == kAcrossGroup && !last) leave(T.chain.states + (long)group * row + line, Run{0.f, after(all, state)});
-            states[lane] = after(seen, state);
+        // lines behind the last one have records of their own
+        const long row = (long)T.groups * 64 * T.beside;
+        const unsigned group = piece / kAcrossGroup, at = piece % kAcrossGroup, far = group / kAcrossGroup, group_at = group % kAcrossGroup;
+        const bool last = piece + 1 == T.pieces;
+        Run all = mine;
+        if (after_waves == 0) {
+            for (int w = 1; w < T.waves; ++w) all = then(all, runs[w * T.beside + side][lane]);
+            if (at + 1 < kAcrossGroup && !last) leave(T.chain.runs + piece * row + line, all);
+            const Run seen = join_records(T.chain.runs + (piece - at) * row + line, row, (int)at);
+            if (at + 1 == kAcrossGroup && group_at + 1 < kAcrossGroup && !last) leave(T.chain.groups + group * row + line, then(seen, all));
+            pieces[side][lane] = seen;
+        } else if (after_waves == 1) {
+            const Run seen = join_records(T.chain.groups + (group - group_at) * row + line, row, (int)group_at);
+            if (far) {
+                const unsigned long* const before = T.chain.states + (far - 1) * row + line;
+                state = await(before, look(before)).b;
+            }
+            states[side][lane] = after(seen, state);
         }
         __syncthreads();
-        state = states[lane];
+        state = after(pieces[side][lane], states[side][lane]);
+        if (after_waves == 0 && at + 1 == kAcrossGroup && group_at + 1 == kAcrossGroup && !last)
+            leave(T.chain.states + far * row + line, Run{0.f, after(all, state)});
     }
-    for (int w = 0; w < wave; ++w) state = after(runs[w][lane], state);
+    for (int w = 0; w < after_waves; ++w) state = after(runs[w * T.beside + side][lane], state);
     return state;
 }
 
 template <int P>
-__global__ void __launch_bounds__(1024) k_lines_across(LinesFwd A, Across T)
+__global__ void __launch_bounds__(64 * kMostWaves) k_lines_across(LinesFwd A, Across T)
 {
     const unsigned ticket = take_ticket(T.chain), piece = ticket / T.groups, group = ticket - piece * T.groups;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long lines = A.L.outer * A.L.inner, line = group * 64L + lane, l = line < lines ? line : lines - 1;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, later = wave / T.beside, side = wave - later * T.beside;
+    const long lines = A.L.outer * A.L.inner, line = (group * (long)T.beside + side) * 64 + lane, l = line < lines ? line : lines - 1;
     const long o = l / A.L.inner, step = A.mirror ? -A.L.inner : A.L.inner;
-    const long t0 = ((long)piece * T.waves + wave) * P, left = A.L.length - t0;
+    const long t0 = ((long)piece * T.waves + later) * P, left = A.L.length - t0;
     const int n = left > P ? P : left > 0 ? (int)left : 0;       // uniform in a wave
     const long at = (o * A.L.length + (A.mirror ? A.L.length - 1 - t0 : t0)) * A.L.inner + (l - o * A.L.inner);
     float f[P], b[P];
@@ -161,7 +173,7 @@ __global__ void __launch_bounds__(1024) k_lines_across(LinesFwd A, Across T)
             b[i] = times(g.k, b[i]);
             mine = then(mine, Run{f[i], b[i]});
         }
-    float h = state_before(mine, T, piece, line, A.h0 ? A.h0[l] : 0.f);
+    float h = state_before(mine, T, piece, line, later, A.h0 ? A.h0[l] : 0.f);
     if (line >= lines) return;
     float* ph = A.h + at;
 #pragma unroll
@@ -177,13 +189,13 @@ __device__ __forceinline__ float grads(const Gate& g, float G, float before, flo
 }
 
 template <int P>
-__global__ void __launch_bounds__(1024) k_lines_across_bwd(LinesBwd A, Across T)
+__global__ void __launch_bounds__(64 * kMostWaves) k_lines_across_bwd(LinesBwd A, Across T)
 {
     const unsigned ticket = take_ticket(T.chain), piece = ticket / T.groups, group = ticket - piece * T.groups;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long lines = A.L.outer * A.L.inner, line = group * 64L + lane, l = line < lines ? line : lines - 1;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, later = wave / T.beside, side = wave - later * T.beside;
+    const long lines = A.L.outer * A.L.inner, line = (group * (long)T.beside + side) * 64 + lane, l = line < lines ? line : lines - 1;
     const long o = l / A.L.inner, step = A.mirror ? -A.L.inner : A.L.inner;
-    const long t0 = ((long)piece * T.waves + wave) * P, left = A.L.length - t0;
+    const long t0 = ((long)piece * T.waves + later) * P, left = A.L.length - t0;
     const int n = left > P ? P : left > 0 ? (int)left : 0;
     const long at = (o * A.L.length + (A.mirror ? A.L.length - 1 - t0 : t0)) * A.L.inner + (l - o * A.L.inner);
     float z[P], gh[P], x[P], before[P];
@@ -202,7 +214,7 @@ __global__ void __launch_bounds__(1024) k_lines_across_bwd(LinesBwd A, Across T)
             const float f = gate(z[i]).f;
             mine = then(mine, Run{f, times(f, gh[i])});
         }
-    float q = state_before(mine, T, piece, line, 0.f);
+    float q = state_before(mine, T, piece, line, later, 0.f);
     if (line >= lines) return;
     float *qx = A.gx + at, *qz = A.gz + at;
 #pragma unroll
@@ -218,10 +230,10 @@ __global__ void __launch_bounds__(1024) k_lines_across_bwd(LinesBwd A, Across T)
 
 // ---------------------------------------------------------------- along: lanes follow a line
 // Lines along the fastest extent lie one behind the other, so that the array is one line of outer * length steps in which a line begins every
-// `length` steps: a step whose gate takes nothing of the state before it.  A lane holds quads of four neighbouring steps, a wave kQuads rows of
-// 64 quads, one after the other; the waves of a workgroup follow each other.
+// `length` steps: a step whose gate takes nothing of the state before it.  A lane holds quads of four neighbouring steps, a wave Q rows of 64
+// quads, one after the other; the W waves of a workgroup follow each other.
 
-constexpr int kQuads = 4, kWaveSteps = 256 * kQuads, kAlongWaves = 4, kFarOff = 1 << 30;
+constexpr int kFarOff = 1 << 30;
 typedef float floatu4 __attribute__((ext_vector_type(4), aligned(4)));      // lines begin at any element
 
 // steps in all and of a workgroup; min(length, kFarOff)
@@ -315,60 +327,67 @@ __device__ __forceinline__ Run scan_lanes(const Run& mine, Run& before)
     return Run{last_lane(r.a), last_lane(r.b)};
 }
 
-constexpr int kAlongGroup = 64;         // pieces of a group: a lane a record
+constexpr int kAlongGroup = 64;         // pieces of a group, groups of a group of groups: a lane a record
+
+// What `count` records from `at` on make of a state.
+__device__ __forceinline__ Run join_records(const unsigned long* at, int count)
+{
+    const int lane = threadIdx.x & 63;
+    const Run r = scan_lanes(lane < count ? await(at + lane, look(at + lane)) : Run{1.f, 0.f});
+    return Run{last_lane(r.a), last_lane(r.b)};
+}
 
 // The state before this wave's steps.
-__device__ __forceinline__ float state_before(const Run& mine, const Along& T, const Tile& S, unsigned number)
+template <int W>
+__device__ __forceinline__ float state_before(const Run& mine, const Along& T, unsigned number)
 {
-    __shared__ Run runs[kMostWaves];
-    __shared__ float shared_state;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    __shared__ Run runs[W], pieces;
+    __shared__ float state_of_groups;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (lane == 0) runs[wave] = mine;
     __syncthreads();
     float state = 0.f;
     if (T.chain.ticket) {
+        const unsigned group = number / kAlongGroup, at = number % kAlongGroup, far = group / kAlongGroup, group_at = group % kAlongGroup;
+        Run all = mine;
         if (wave == 0) {
-            Run all = mine;
-            for (int w = 1; w < waves; ++w) all = then(all, runs[w]);
-            const unsigned group = number / kAlongGroup, at = number % kAlongGroup;
-            const bool leaves = at + 1 == kAlongGroup && number + 1 < gridDim.x;
+            for (int w = 1; w < W; ++w) all = then(all, runs[w]);
             if (lane == 0 && at + 1 < kAlongGroup) leave(T.chain.runs + number, all);
-            // nothing reaches a tile that begins with a line
-            if (!S.begins) {
-                const unsigned long* const from = T.chain.runs + (number - at + lane);
-                const Run r = scan_lanes(lane < (int)at ? await(from, look(from)) : Run{1.f, 0.f});
-                const Run seen = {last_lane(r.a), last_lane(r.b)};
-                if (seen.a != 0.f && group) {
-                    const unsigned long* const before = T.chain.states + (group - 1);
-                    state = await(before, look(before)).b;
-                }
-                state = after(seen, state);
+            const Run seen = join_records(T.chain.runs + (number - at), (int)at);
+            if (lane == 0 && at + 1 == kAlongGroup && group_at + 1 < kAlongGroup) leave(T.chain.groups + group, then(seen, all));
+            if (lane == 0) pieces = seen;
+        } else if (wave == 1) {
+            const Run seen = join_records(T.chain.groups + (group - group_at), (int)group_at);
+            if (seen.a != 0.f && far) {
+                const unsigned long* const before = T.chain.states + (far - 1);
+                state = await(before, look(before)).b;
             }
-            if (lane == 0 && leaves) leave(T.chain.states + group, Run{0.f, after(all, state)});
-            if (lane == 0) shared_state = state;
+            if (lane == 0) state_of_groups = after(seen, state);
         }
         __syncthreads();
-        state = shared_state;
+        state = after(pieces, state_of_groups);
+        if (threadIdx.x == 0 && at + 1 == kAlongGroup && group_at + 1 == kAlongGroup) leave(T.chain.states + far, Run{0.f, after(all, state)});
     }
     for (int w = 0; w < wave; ++w) state = after(runs[w], state);
     return state;
 }
 
-__global__ void __launch_bounds__(64 * kAlongWaves) k_lines_along(LinesFwd A, Along T)
+template <int Q, int W>
+__global__ void __launch_bounds__(64 * W) k_lines_along(LinesFwd A, Along T)
 {
     const unsigned number = take_ticket(T.chain);
     const Tile S = tile_of(A.L, T, number);
-    const int off0 = (threadIdx.x >> 6) * kWaveSteps + (threadIdx.x & 63) * 4;
-    float f[kQuads][4], b[kQuads][4];
+    const int off0 = (threadIdx.x >> 6) * (256 * Q) + (threadIdx.x & 63) * 4;
+    float f[Q][4], b[Q][4];
 #pragma unroll
-    for (int q = 0; q < kQuads; ++q) {
+    for (int q = 0; q < Q; ++q) {
         const int off = off0 + q * 256;
         load_steps(f[q], A.z, S.first + off, S.count - off, A.mirror, T.steps - 1);
         load_steps(b[q], A.x, S.first + off, S.count - off, A.mirror, T.steps - 1);
     }
-    Run mine = {1.f, 0.f}, before[kQuads];
+    Run mine = {1.f, 0.f}, before[Q];
 #pragma unroll
-    for (int q = 0; q < kQuads; ++q) {
+    for (int q = 0; q < Q; ++q) {
         const int off = off0 + q * 256;
         Run4 R = place_in_line(S, T.line, off);
         Run r = {1.f, 0.f};
@@ -388,9 +407,9 @@ __global__ void __launch_bounds__(64 * kAlongWaves) k_lines_along(LinesFwd A, Al
         before[q] = then(mine, before[q]);
         mine = then(mine, all);
     }
-    const float first = state_before(mine, T, S, number);
+    const float first = state_before<W>(mine, T, number);
 #pragma unroll
-    for (int q = 0; q < kQuads; ++q) {
+    for (int q = 0; q < Q; ++q) {
         const int off = off0 + q * 256;
         float h = after(before[q], first);
 #pragma unroll
@@ -399,15 +418,16 @@ __global__ void __launch_bounds__(64 * kAlongWaves) k_lines_along(LinesFwd A, Al
     }
 }
 
-__global__ void __launch_bounds__(64 * kAlongWaves) k_lines_along_bwd(LinesBwd A, Along T)
+template <int Q, int W>
+__global__ void __launch_bounds__(64 * W) k_lines_along_bwd(LinesBwd A, Along T)
 {
     const unsigned number = take_ticket(T.chain);
     const Tile S = tile_of(A.L, T, number);
-    const int off0 = (threadIdx.x >> 6) * kWaveSteps + (threadIdx.x & 63) * 4;
+    const int off0 = (threadIdx.x >> 6) * (256 * Q) + (threadIdx.x & 63) * 4;
     const long last = T.steps - 1;
-    float z[kQuads][4], gh[kQuads][4], x[kQuads][4], h[kQuads][4];
+    float z[Q][4], gh[Q][4], x[Q][4], h[Q][4];
 #pragma unroll
-    for (int q = 0; q < kQuads; ++q) {
+    for (int q = 0; q < Q; ++q) {
         const int off = off0 + q * 256;
         load_steps(z[q], A.z, S.first + off, S.count - off, A.mirror, last);
         load_steps(gh[q], A.gh, S.first + off, S.count - off, A.mirror, last);
@@ -416,9 +436,9 @@ __global__ void __launch_bounds__(64 * kAlongWaves) k_lines_along_bwd(LinesBwd A
         const long e = S.first + off + 1;
         load_steps(h[q], A.h, e, off >= S.count ? 0 : T.steps - e < 4 ? (int)(T.steps - e) : 4, A.mirror, last);
     }
-    Run mine = {1.f, 0.f}, before[kQuads];
+    Run mine = {1.f, 0.f}, before[Q];
 #pragma unroll
-    for (int q = 0; q < kQuads; ++q) {
+    for (int q = 0; q < Q; ++q) {
         const int off = off0 + q * 256;
         Run4 R = place_in_line(S, T.line, off);
         Run r = {1.f, 0.f};
@@ -432,9 +452,9 @@ __global__ void __launch_bounds__(64 * kAlongWaves) k_lines_along_bwd(LinesBwd A
         before[q] = then(mine, before[q]);
         mine = then(mine, all);
     }
-    const float first = state_before(mine, T, S, number);
+    const float first = state_before<W>(mine, T, number);
 #pragma unroll
-    for (int q = 0; q < kQuads; ++q) {
+    for (int q = 0; q < Q; ++q) {
         const int off = off0 + q * 256, most = S.count - off;
         Run4 R = place_in_line(S, T.line, off);
         float state = after(before[q], first);
@@ -469,19 +489,20 @@ __global__ void __launch_bounds__(256) k_lines_walk(LinesFwd A)
     const long lines = A.L.outer * A.L.inner, step = A.mirror ? -A.L.inner : A.L.inner;
     for (long l = blockIdx.x * 256L + threadIdx.x; l < lines; l += gridDim.x * 256L) {
         const long o = l / A.L.inner;
-        long at = (o * A.L.length + (A.mirror ? A.L.length - 1 : 0)) * A.L.inner + (l - o * A.L.inner);
+        const long at = (o * A.L.length + (A.mirror ? A.L.length - 1 : 0)) * A.L.inner + (l - o * A.L.inner);
         float h = A.h0 ? A.h0[l] : 0.f;
-        for (long t = 0; t < A.L.length; t += U, at += U * step) {
+        const float *pz = A.z + at, *px = A.x + at;
+        float* ph = A.h + at;
+        for (long left = A.L.length; left > 0; left -= U) {
             float z[U], x[U];
 #pragma unroll
-            for (int i = 0; i < U; ++i)
-                if (t + i < A.L.length) { z[i] = A.z[at + i * step]; x[i] = A.x[at + i * step]; }
+            for (int i = 0; i < U; ++i, pz += step, px += step)
+                if (i < left) { z[i] = *pz; x[i] = *px; }
 #pragma unroll
-            for (int i = 0; i < U; ++i)
-                if (t + i < A.L.length) {
+            for (int i = 0; i < U; ++i, ph += step)
+                if (i < left) {
                     const Gate g = gate(z[i]);
-                    h = times(g.f, h) + times(g.k, x[i]);
-                    A.h[at + i * step] = h;
+                    *ph = h = times(g.f, h) + times(g.k, x[i]);
                 }
         }
     }
@@ -493,25 +514,25 @@ __global__ void __launch_bounds__(256) k_lines_walk_bwd(LinesBwd A)
     const long lines = A.L.outer * A.L.inner, step = A.mirror ? -A.L.inner : A.L.inner;
     for (long l = blockIdx.x * 256L + threadIdx.x; l < lines; l += gridDim.x * 256L) {
         const long o = l / A.L.inner;
-        long at = (o * A.L.length + (A.mirror ? A.L.length - 1 : 0)) * A.L.inner + (l - o * A.L.inner);
+        const long at = (o * A.L.length + (A.mirror ? A.L.length - 1 : 0)) * A.L.inner + (l - o * A.L.inner);
         const float h0 = A.h0 ? A.h0[l] : 0.f;
         float q = 0.f;
-        for (long t = 0; t < A.L.length; t += U, at += U * step) {
+        const float *pz = A.z + at, *px = A.x + at, *pg = A.gh + at, *ph = A.h + at + step;
+        float *qx = A.gx + at, *qz = A.gz + at;
+        for (long left = A.L.length; left > 0; left -= U) {
             float z[U], x[U], gh[U], before[U];
 #pragma unroll
-            for (int i = 0; i < U; ++i)
-                if (t + i < A.L.length) {
-                    z[i] = A.z[at + i * step]; x[i] = A.x[at + i * step]; gh[i] = A.gh[at + i * step];
-                    before[i] = t + i + 1 < A.L.length ? A.h[at + (i + 1) * step] : h0;
+            for (int i = 0; i < U; ++i, pz += step, px += step, pg += step, ph += step)
+                if (i < left) {
+                    z[i] = *pz; x[i] = *px; gh[i] = *pg;
+                    before[i] = i + 1 < left ? *ph : h0;
                 }
 #pragma unroll
-            for (int i = 0; i < U; ++i)
-                if (t + i < A.L.length) {
+            for (int i = 0; i < U; ++i, qx += step, qz += step)
+                if (i < left) {
                     const Gate g = gate(z[i]);
                     const float G = gh[i] + q;
-                    float gz;
-                    A.gx[at + i * step] = grads(g, G, before[i], x[i], gz);
-                    A.gz[at + i * step] = gz;
+                    *qx = grads(g, G, before[i], x[i], *qz);
                     q = times(g.f, G);
                 }
         }
@@ -524,9 +545,9 @@ enum Way { WALK, ACROSS, ALONG };
 constexpr int kSteps = 32, kStepsBwd = 16;      // of a wave across
 struct Split {
     Way way;
-    int waves;              // of a workgroup
-    long groups, pieces;    // across: groups of 64 lines, pieces of a line; along: tiles
-    int tile;               // along: steps of one
+    int waves, beside;      // of a workgroup: one after another, side by side
+    long groups, pieces;    // across: groups of lines, pieces of a line; along: tiles
+    int quads, tile;        // along: rows of a wave, steps of a tile
     bool chained;
 };
 
@@ -535,12 +556,32 @@ Split lines_split(const Lines& L, bool backward)
     Split S = {};
     const long lines = L.outer * L.inner;
     if (L.inner == 1) {
+        const long steps = L.outer * L.length;
         S.way = ALONG;
-        S.waves = kAlongWaves;
-        S.tile = S.waves * kWaveSteps;
-        const long steps = L.outer * L.length, whole = L.length <= S.tile ? S.tile / L.length * L.length : 0;
-        S.chained = 4 * whole < 3 * S.tile;
-        if (!S.chained) S.tile = (int)whole;
+        S.beside = 1;
+        // Whole lines in a tile where they fill it, so that no tile waits for another, in the smaller one where that does: 144 000 lines of 60
+        // forward 24.6 us in tiles of 512, 27.7 of 2048; backward 44.9 and 48.6.
+        S.chained = true;
+        for (int small = 1; small >= 0 && S.chained; --small) {
+            S.quads = small ? 1 : 2;
+            S.waves = small ? 2 : 4;
+            const long most = 256 * S.quads * S.waves, whole = most / L.length * L.length;
+            if (4 * whole >= 3 * most) {
+                S.chained = false;
+                S.tile = (int)whole;
+            }
+        }
+        // Else large tiles, as tickets are handed out one every 13 to 17 ns; those of 8192 and 4096 steps leave room for two workgroups and more on a unit, which
+        // pays where there are many: 4 lines of 10^6 forward 21.8 us with 16 384, 25.6 with 8192, backward 35.5 and 45; 64 lines 277 and 239, 478 and 434.
+        if (S.chained) {
+            S.quads = 4;
+            S.waves = 16;
+            if (steps > 1L << 23) {
+                S.waves = 8;
+                if (backward) S.quads = 2;
+            }
+            S.tile = 256 * S.quads * S.waves;
+        }
         S.pieces = (steps + S.tile - 1) / S.tile;
         S.groups = 1;
         S.chained = S.chained && S.pieces > 1;
@@ -549,29 +590,32 @@ Split lines_split(const Lines& L, bool backward)
     const int steps = backward ? kStepsBwd : kSteps;
     if (lines >= 1L << 17 || L.length <= steps / 2) return S;
     S.way = ACROSS;
-    S.waves = (int)std::min((L.length + steps - 1) / steps, (long)kMostWaves);
+    S.beside = lines > 1024 ? 2 : 1;
+    S.waves = (int)std::min((L.length + steps - 1) / steps, (long)(kMostWaves / S.beside));
+    if (L.length > S.waves * steps) S.waves = kMostWaves / S.beside;
     S.pieces = (L.length + S.waves * steps - 1) / (S.waves * steps);
-    if (S.pieces > 1) {
-        S.waves = 8;
-        S.pieces = (L.length + S.waves * steps - 1) / (S.waves * steps);
-    }
-    S.groups = (lines + 63) / 64;
+    S.groups = (lines + 64 * S.beside - 1) / (64 * S.beside);
     S.chained = S.pieces > 1;
     return S;
 }
 
-// Records of pieces and of their groups
-size_t runs_of(const Split& S) { return (size_t)S.pieces * (S.way == ACROSS ? 64 * S.groups : 1); }
-size_t states_of(const Split& S) { return S.way == ACROSS ? (size_t)(S.pieces / kAcrossGroup) * 64 * S.groups : S.pieces / kAlongGroup; }
-size_t split_bytes(const Split& S) { return S.chained ? 256 + sizeof(unsigned long) * (runs_of(S) + states_of(S)) : 0; }
+// Records of pieces, groups of them and groups of these
+struct Records { size_t runs, groups, states; size_t all() const { return runs + groups + states; } };
+Records records_of(const Split& S)
+{
+    const size_t row = S.way == ACROSS ? (size_t)S.groups * 64 * S.beside : 1, group = S.way == ACROSS ? kAcrossGroup : kAlongGroup;
+    return Records{S.pieces * row, S.pieces / group * row, S.pieces / (group * group) * row};
+}
+size_t split_bytes(const Split& S) { return S.chained ? 256 + sizeof(unsigned long) * records_of(S).all() : 0; }
 
 int begin_lines(const Split& S, void* ws, Chain* C, hipStream_t s)
 {
     *C = Chain{};
     if (!S.chained) return ZNN_OK;
     unsigned long* const runs = (unsigned long*)((char*)ws + 256);
-    *C = Chain{(unsigned*)ws, runs, runs + runs_of(S)};
-    const long records = (long)(runs_of(S) + states_of(S));
+    const Records R = records_of(S);
+    *C = Chain{(unsigned*)ws, runs, runs + R.runs, runs + R.runs + R.groups};
+    const long records = (long)R.all();
     ZNN_LAUNCH("recurrence pieces", s, k_lines_begin, dim3((unsigned)std::min((records + 255) / 256, 2048L)), dim3(256), 0, *C, records);
     return check_launch("recurrence pieces");
 }
@@ -588,10 +632,15 @@ int lines_fwd(const LinesFwd& A, void* ws, hipStream_t s)
     Chain C;
     const int rc = begin_lines(S, ws, &C, s);
     if (rc != ZNN_OK) return rc;
-    const dim3 grid((unsigned)(S.groups * S.pieces)), block(64 * S.waves);
-    if (S.way == ALONG) ZNN_LAUNCH("recurrence forward", s, k_lines_along, grid, block, 0, A, along(A.L, S, C));
-    else if (S.way == ACROSS)
-        ZNN_LAUNCH("recurrence forward", s, k_lines_across<kSteps>, grid, block, 0, A, Across{(unsigned)S.groups, (unsigned)S.pieces, S.waves, C});
+    const dim3 grid((unsigned)(S.groups * S.pieces)), block(64 * S.waves * S.beside);
+    if (S.way == ALONG) {
+        const Along T = along(A.L, S, C);
+        if (S.waves == 2) ZNN_LAUNCH("recurrence forward", s, (k_lines_along<1, 2>), grid, block, 0, A, T);
+        else if (S.waves == 4) ZNN_LAUNCH("recurrence forward", s, (k_lines_along<2, 4>), grid, block, 0, A, T);
+        else if (S.waves == 8) ZNN_LAUNCH("recurrence forward", s, (k_lines_along<4, 8>), grid, block, 0, A, T);
+        else ZNN_LAUNCH("recurrence forward", s, (k_lines_along<4, 16>), grid, block, 0, A, T);
+    } else if (S.way == ACROSS)
+        ZNN_LAUNCH("recurrence forward", s, k_lines_across<kSteps>, grid, block, 0, A, Across{(unsigned)S.groups, (unsigned)S.pieces, S.waves, S.beside, C});
     else ZNN_LAUNCH("recurrence forward", s, k_lines_walk<8>, dim3(walk_groups(A.L)), dim3(256), 0, A);
     return check_launch("recurrence forward");
 }
@@ -602,10 +651,15 @@ int lines_bwd(const LinesBwd& A, void* ws, hipStream_t s)
     Chain C;
     const int rc = begin_lines(S, ws, &C, s);
     if (rc != ZNN_OK) return rc;
-    const dim3 grid((unsigned)(S.groups * S.pieces)), block(64 * S.waves);
-    if (S.way == ALONG) ZNN_LAUNCH("recurrence backward", s, k_lines_along_bwd, grid, block, 0, A, along(A.L, S, C));
-    else if (S.way == ACROSS)
-        ZNN_LAUNCH("recurrence backward", s, k_lines_across_bwd<kStepsBwd>, grid, block, 0, A, Across{(unsigned)S.groups, (unsigned)S.pieces, S.waves, C});
+    const dim3 grid((unsigned)(S.groups * S.pieces)), block(64 * S.waves * S.beside);
+    if (S.way == ALONG) {
+        const Along T = along(A.L, S, C);
+        if (S.waves == 2) ZNN_LAUNCH("recurrence backward", s, (k_lines_along_bwd<1, 2>), grid, block, 0, A, T);
+        else if (S.waves == 4) ZNN_LAUNCH("recurrence backward", s, (k_lines_along_bwd<2, 4>), grid, block, 0, A, T);
+        else if (S.waves == 8) ZNN_LAUNCH("recurrence backward", s, (k_lines_along_bwd<2, 8>), grid, block, 0, A, T);
+        else ZNN_LAUNCH("recurrence backward", s, (k_lines_along_bwd<4, 16>), grid, block, 0, A, T);
+    } else if (S.way == ACROSS)
+        ZNN_LAUNCH("recurrence backward", s, k_lines_across_bwd<kStepsBwd>, grid, block, 0, A, Across{(unsigned)S.groups, (unsigned)S.pieces, S.waves, S.beside, C});
     else ZNN_LAUNCH("recurrence backward", s, k_lines_walk_bwd<4>, dim3(walk_groups(A.L)), dim3(256), 0, A);
     return check_launch("recurrence backward");
 }
@@ -614,7 +668,7 @@ int check_lines(int64_t outer, int64_t length, int64_t inner)
 {
     if (outer < 1 || length < 1 || inner < 1) return fail(ZNN_EINVAL, "extents must be >= 1");
     constexpr int64_t most = 1LL << 34;
-    if (outer > most || length > most || inner > most || (double)outer * length * inner > 1099511627776.0)
+    if (outer > most || length > most || inner > most || (double)outer * length * inner > 274877906944.0)
         return fail(ZNN_EUNSUPPORTED, "lines of %lld x %lld x %lld elements are too large", (long long)outer, (long long)length, (long long)inner);
     return ZNN_OK;
 }

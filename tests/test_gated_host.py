@@ -50,7 +50,7 @@ def test_line_extents(name):
         for v in (0, -1):
             assert call(name, **{e: v}) == znn.ZNN_EINVAL
         assert call(name, **{e: (1 << 34) + 1}) == znn.ZNN_EUNSUPPORTED
-    assert call(name, outer=1 << 20, length=1 << 20, inner=2) == znn.ZNN_EUNSUPPORTED
+    assert call(name, outer=1 << 19, length=1 << 19, inner=2) == znn.ZNN_EUNSUPPORTED
 
 
 def need_of(name, shape):

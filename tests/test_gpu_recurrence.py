@@ -212,3 +212,52 @@ def test_gradients_against_differences():
             d = (value(*(t + e * w for t, w in zip(arrays, way))) - value(*(t - e * w for t, w in zip(arrays, way)))) / (2 * e)
             terms = np.abs(grads[which] * way[which]).sum()
             assert abs(d - (grads[which] * way[which]).sum()) <= 1e-5 * terms + 1e-9
+
+
+# lines of more pieces than a group of groups holds: along the fastest extent, across few lines and across many
+@pytest.mark.parametrize("shape", [(1, 34000003, 1), (2, 17000001, 1), (1, 70001, 2), (1, 33001, 1100), (3, 140000, 5)])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_states_are_handed_on_over_the_longest_lines(shape, reverse):
+    """Gates are wide open but for a few steps, the same in all lines, where half of the state goes: everything in between is exact."""
+    outer, length, inner = shape
+    r = np.random.default_rng(61)
+    steps = np.unique(np.concatenate([r.integers(0, length, 40), [0, 1, length - 1, length // 2]]))
+    order = steps[::-1] if reverse else steps
+    at = torch.from_numpy(steps.copy()).cuda()
+    xs = r.normal(size=(outer, len(steps), inner)).astype(np.float32)
+    gs = r.normal(size=(outer, len(steps), inner)).astype(np.float32)
+    h0 = r.normal(size=(outer, inner)).astype(np.float32)
+    z = torch.full(shape, float("inf"), device="cuda:0")
+    z[:, at] = 0
+    x = torch.full(shape, float("nan"), device="cuda:0")
+    x[:, at] = dev(xs)
+    h = znn.recurrence_fwd(z, x, dev(h0), 1, reverse)
+    state, want = h0.astype(np.float64), torch.empty(shape, device="cuda:0")
+    ends = list(order[1:]) + [None]
+    if reverse:
+        want[:, order[0] + 1:] = dev(h0)[:, None]
+    else:
+        want[:, :order[0]] = dev(h0)[:, None]
+    befores = {}
+    for t, e in zip(order, ends):
+        i = int(np.searchsorted(steps, t))
+        befores[t] = state
+        state = 0.5 * state + 0.5 * xs[:, i]
+        piece = slice(None if e is None else e + 1, t + 1) if reverse else slice(t, e)
+        want[:, piece] = dev(state)[:, None]
+    tol = 2 * len(steps) * gated.HALF * 8
+    assert float((h - want).abs().max()) <= tol
+    del want
+    gh = torch.zeros(shape, device="cuda:0")
+    gh[:, at] = dev(gs)
+    gz, gx, gh0 = znn.recurrence_bwd(gh, z, x, h, dev(h0), 1, reverse)
+    q = np.zeros((outer, inner))
+    for t in order[::-1]:
+        i = int(np.searchsorted(steps, t))
+        g = q + gs[:, i]
+        assert np.abs(host(gx[:, t]) - 0.5 * g).max() <= 2 * tol
+        assert np.abs(host(gz[:, t]) - g * (befores[t] - xs[:, i]) * 0.25).max() <= 8 * tol
+        q = 0.5 * g
+    assert np.abs(host(gh0) - q).max() <= 2 * tol
+    gz[:, at], gx[:, at] = 0, 0
+    assert not bool(gz.any()) and not bool(gx.any())
