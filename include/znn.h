@@ -343,7 +343,8 @@ int  znn_residual_norm_bwd(int64_t rows, int64_t cols, int32_t axis, double p, c
  * Sums are taken in fp32 in an order that follows from the extents alone: results repeat themselves to the bit.
  * Functions at infinity are their limits (SiLU and GELU are 0 at minus infinity); the rectifier is 0 at NaN, as its transfer function is.
  * The calls take a workspace of znn_gated_workspace_bytes for their pass (ZNN_PASS_FWD or ZNN_PASS_BWD; 256-byte aligned; may be
- * NULL if that is 0).  ZNN_EUNSUPPORTED: more than 2^20 features on either side, or more than 2^31 - 1 positions.
+ * NULL if that is 0).  ZNN_EUNSUPPORTED: more than 2^20 features on either side, more than 2^31 - 1 positions, or
+ * more than 2^38 elements of an array.
  */
 typedef enum znn_gate_fn {
     ZNN_GATE_RECTIFY  = 0,   /* max(u, 0)                       */

@@ -29,100 +29,306 @@ __device__ __forceinline__ Gated gate_fn(int fn, float u)
     return Gated{u > 0.f ? u * s : finite * s, fmaf(finite, s * t, s)};
 }
 
-// Strides of an array [features][positions]: images, or rows of features.
-struct Place { long feature, position; };
-Place place(int axis, long features, long positions) { return axis ? Place{1, features} : Place{positions, 1}; }
+// ---------------------------------------------------------------- products of matrices
+// C[i][j] = sum over k of A[i][k] B[j][k] on the fp32 matrix cores, rows j of C contiguous.  A workgroup of WI x WJ waves makes a tile of
+// 32 WI AI x 32 WJ AJ results, a wave AI x AJ of 32 x 32.  Both operands go through shared memory as [row][kDepth] in quads along k, whatever way they lie
+// in memory; while one step is multiplied the next one's loads are in flight.  Quads of a row change places by the row's number: 16 lanes that
+// read a quad of 16 rows, and 8 that write one of rows four apart, touch different banks.
+// v_mfma_f32_32x32x2_f32 takes k = lane / 32; which k that stands for is free as long as both operands agree: lanes below 32 take the first
+// quad of eight k, the others the second one, so that a quad feeds four instructions.
 
-struct Operand { const float* p; long outer, k; };     // element (i, k) at p + i outer + k k
-struct Product { Operand A, B; long M, N, K; };
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatu4 __attribute__((ext_vector_type(4), aligned(4)));      // rows begin at any element
 
-constexpr int kTile = 64, kDepth = 16;
-struct Tiles { float a[2][kDepth][kTile + 4], b[kDepth][kTile + 4]; };
+constexpr int kDepth = 32;
 
-__device__ __forceinline__ void stage(float (&t)[kDepth][kTile + 4], const Operand& O, long first, long rows, long k0, long K)
+// Element (row, k) of an operand at p + row * ld + k (ALONG_K) or at p + k * ld + row.
+struct Operand { const float* p; long ld; };
+
+__device__ __forceinline__ int quad_place(int row, int quad) { return row * kDepth + ((quad ^ (row >> 1 & 7) ^ (row >> 4 & 1)) << 2); }
+
+// A tile's row in the operand.  Halves: 32 rows of the first half lie beside the same rows of the second one, `half` rows on.
+template <bool HALVES>
+__device__ __forceinline__ long source_row(long first, int row, long rows, long half)
 {
-    for (int e = threadIdx.x; e < kTile * kDepth; e += 256) {
-        const int r = O.k == 1 ? e / kDepth : e % kTile, k = O.k == 1 ? e % kDepth : e / kTile;
-        t[k][r] = first + r < rows && k0 + k < K ? O.p[(first + r) * O.outer + (k0 + k) * O.k] : 0.f;
-    }
+    const long r = first + (HALVES ? (row >> 6) * 32 + (row & 31) : row);
+    return (r < rows ? r : rows - 1) + (HALVES && (row & 32) ? half : 0);
 }
 
-template <int HALVES>
-__device__ __forceinline__ void tile_product(Tiles& S, float (&acc)[HALVES][4][4], const Product& P, long half, long m0, long n0)
-{
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    for (long k0 = 0; k0 < P.K; k0 += kDepth) {
-        __syncthreads();
-        for (int h = 0; h < HALVES; ++h) stage(S.a[h], Operand{P.A.p + h * half, P.A.outer, P.A.k}, m0, P.M, k0, P.K);
-        stage(S.b, P.B, n0, P.N, k0, P.K);
-        __syncthreads();
-        for (int k = 0; k < kDepth; ++k)
-            for (int h = 0; h < HALVES; ++h)
-                for (int i = 0; i < 4; ++i)
-                    for (int j = 0; j < 4; ++j) acc[h][i][j] = fmaf(S.a[h][k][ty * 4 + i], S.b[k][tx * 4 + j], acc[h][i][j]);
-    }
-}
+// R rows from `first` on (of `rows`), kDepth k from k0 on (k < K; 0 behind), on their way into shared memory.
+template <int R, int THREADS, bool ALONG_K, bool HALVES>
+struct Stage {
+    static constexpr int kPieces = (R * kDepth / 4 + THREADS - 1) / THREADS;        // quads of a thread
+    static constexpr int kBlocks = (R * kDepth / 16 + THREADS - 1) / THREADS;       // or blocks of 4 x 4
+    floatx4 v[ALONG_K ? kPieces : 4 * kBlocks];
 
-struct GatedFwd { Product P; long half; int fn; const float* bias; float *y, *kept; Place to; };
-
-__global__ void __launch_bounds__(256) k_gated_fwd(GatedFwd G)
-{
-    __shared__ Tiles S;
-    const long m0 = (long)blockIdx.y * kTile, n0 = (long)blockIdx.x * kTile;
-    float acc[2][4][4] = {};
-    tile_product<2>(S, acc, G.P, G.half, m0, n0);
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const long m = m0 + threadIdx.x / 16 * 4 + i, n = n0 + threadIdx.x % 16 * 4 + j;
-            if (m >= G.P.M || n >= G.P.N) continue;
-            const float u = acc[0][i][j] + (G.bias ? G.bias[m] : 0.f), v = acc[1][i][j] + (G.bias ? G.bias[G.P.M + m] : 0.f);
-            const bool rows = G.to.feature == 1;
-            G.y[m * G.to.feature + n * G.to.position] = gate_fn(G.fn, u).a * v;
-            if (G.kept) {
-                const long at = m * G.to.feature + n * G.to.position * (rows ? 2 : 1);
-                G.kept[at] = u;
-                G.kept[at + G.P.M * G.to.feature] = v;
+    __device__ __forceinline__ void load(const Operand& O, long first, long rows, long half, long k0, long K)
+    {
+        if (ALONG_K) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int e = threadIdx.x + i * THREADS, row = e / (kDepth / 4), quad = e % (kDepth / 4);
+                if (R * kDepth / 4 % THREADS && row >= R) break;
+                const long k = k0 + quad * 4;
+                const float* p = O.p + source_row<HALVES>(first, row, rows, half) * O.ld + k;
+                if (k0 + kDepth <= K) v[i] = *(const floatu4*)p;
+                else
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) v[i][c] = k + c < K ? p[c] : 0.f;
+            }
+        } else {
+            const bool whole = k0 + kDepth <= K && first + R <= rows;
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i) {
+                const int e = threadIdx.x + i * THREADS, row = e % (R / 4) * 4, quad = e / (R / 4);
+                if (R * kDepth / 16 % THREADS && quad >= kDepth / 4) break;
+                const long r = first + row, k = k0 + quad * 4;
+                const float* p = O.p + k * O.ld + r;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if (whole) v[4 * i + c] = *(const floatu4*)(p + c * O.ld);
+                    else
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[4 * i + c][j] = k + c < K && r + j < rows ? p[c * O.ld + j] : 0.f;
+                }
             }
         }
-}
-
-struct Product1 { Product P; float* c; long cm, cn; };
-__global__ void __launch_bounds__(256) k_product(Product1 G)
-{
-    __shared__ Tiles S;
-    const long m0 = (long)blockIdx.y * kTile, n0 = (long)blockIdx.x * kTile;
-    float acc[1][4][4] = {};
-    tile_product<1>(S, acc, G.P, 0, m0, n0);
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const long m = m0 + threadIdx.x / 16 * 4 + i, n = n0 + threadIdx.x % 16 * 4 + j;
-            if (m < G.P.M && n < G.P.N) G.c[m * G.cm + n * G.cn] = acc[0][i][j];
+    }
+    __device__ __forceinline__ void store(float* lds) const
+    {
+        if (ALONG_K) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int e = threadIdx.x + i * THREADS, row = e / (kDepth / 4), quad = e % (kDepth / 4);
+                if (R * kDepth / 4 % THREADS && row >= R) break;
+                *(floatx4*)(lds + quad_place(row, quad)) = v[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i) {
+                const int e = threadIdx.x + i * THREADS, row = e % (R / 4) * 4, quad = e / (R / 4);
+                if (R * kDepth / 16 % THREADS && quad >= kDepth / 4) break;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *(floatx4*)(lds + quad_place(row + j, quad)) = floatx4{v[4 * i][j], v[4 * i + 1][j], v[4 * i + 2][j], v[4 * i + 3][j]};
+            }
         }
-}
-
-// [du; dv] from gy and the kept [u; v], in the layout of the kept.
-__global__ void __launch_bounds__(256) k_gated_grads(int fn, long features, long positions, int rows, const float* gy, const float* kept, float* g)
-{
-    const long count = features * positions, step = rows ? features : count;
-    for (long e = blockIdx.x * 256L + threadIdx.x; e < count; e += gridDim.x * 256L) {
-        const long at = rows ? e + e / features * features : e;
-        const Gated a = gate_fn(fn, kept[at]);
-        g[at] = gy[e] * kept[at + step] * a.d;
-        g[at + step] = gy[e] * a.a;
     }
-}
+};
 
-__global__ void __launch_bounds__(256) k_gated_bias(long positions, Place at, const float* g, float* gb)
+enum Halves { NO_HALVES, HALVES_I, HALVES_J };
+template <int WI_, int WJ_, int AI_, int AJ_> struct Waves {
+    static constexpr int WI = WI_, WJ = WJ_, AI = AI_, AJ = AJ_, kThreads = 64 * WI * WJ, TI = 32 * WI * AI, TJ = 32 * WJ * AJ;
+};
+
+struct Matrices { Operand A, B; long rows_i, rows_j, half, k0, K; };     // rows that there are (of a half); the sum goes over k0 <= k < K
+
+template <class W, bool A_ALONG, bool B_ALONG, Halves H>
+__device__ __forceinline__ void tile_product(floatx16 (&acc)[W::AI][W::AJ], const Matrices& M, long i0, long j0)
 {
-    __shared__ float part[256];
-    float s = 0.f;
-    for (long n = threadIdx.x; n < positions; n += 256) s += g[blockIdx.x * at.feature + n * at.position];
-    part[threadIdx.x] = s;
-    for (int w = 128; w > 0; w /= 2) {
+    __shared__ float lds[2][(W::TI + W::TJ) * kDepth];
+    Stage<W::TI, W::kThreads, A_ALONG, H == HALVES_I> a;
+    Stage<W::TJ, W::kThreads, B_ALONG, H == HALVES_J> b;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 31, side = lane >> 5;
+    const int wi = wave / W::WJ * (32 * W::AI) + row, wj = W::TI + wave % W::WJ * (32 * W::AJ) + row;
+#pragma unroll
+    for (int x = 0; x < W::AI; ++x)
+#pragma unroll
+        for (int y = 0; y < W::AJ; ++y)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[x][y][r] = 0.f;
+    a.load(M.A, i0, M.rows_i, M.half, M.k0, M.K);
+    b.load(M.B, j0, M.rows_j, M.half, M.k0, M.K);
+    a.store(lds[0]);
+    b.store(lds[0] + W::TI * kDepth);
+    __syncthreads();
+    int buffer = 0;
+    for (long k = M.k0; k < M.K; k += kDepth) {
+        const bool more = k + kDepth < M.K;
+        if (more) {
+            a.load(M.A, i0, M.rows_i, M.half, k + kDepth, M.K);
+            b.load(M.B, j0, M.rows_j, M.half, k + kDepth, M.K);
+        }
+        const float* const from = lds[buffer];
+#pragma unroll
+        for (int q = 0; q < kDepth / 8; ++q) {
+            floatx4 u[W::AI], v[W::AJ];
+#pragma unroll
+            for (int x = 0; x < W::AI; ++x) u[x] = *(const floatx4*)(from + quad_place(wi + 32 * x, 2 * q + side));
+#pragma unroll
+            for (int y = 0; y < W::AJ; ++y) v[y] = *(const floatx4*)(from + W::TI * kDepth + quad_place(wj - W::TI + 32 * y, 2 * q + side));
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int x = 0; x < W::AI; ++x)
+#pragma unroll
+                    for (int y = 0; y < W::AJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x2f32(u[x][s], v[y][s], acc[x][y], 0, 0, 0);
+        }
+        if (more) {
+            buffer ^= 1;
+            a.store(lds[buffer]);
+            b.store(lds[buffer] + W::TI * kDepth);
+        }
         __syncthreads();
-        if ((int)threadIdx.x < w) part[threadIdx.x] += part[threadIdx.x + w];
     }
-    if (threadIdx.x == 0) gb[blockIdx.x] = part[0];
+}
+
+// Register r of a 32 x 32 result belongs to this row and to column lane % 32.
+__device__ __forceinline__ int result_row(int r) { return r / 4 * 8 + (threadIdx.x >> 5 & 1) * 4 + r % 4; }
+
+// Tiles in the order of their numbers: those of one XCD (number mod 8 as workgroups are dealt) are neighbours, eight rows of tiles at a time.
+struct Tiles { unsigned ni, nj, count; };
+struct TilePlace { unsigned i, j; };
+__device__ __forceinline__ TilePlace tile_place(const Tiles& T, unsigned number)
+{
+    const unsigned each = T.count / 8, rest = T.count % 8, xcd = number % 8, nth = number / 8;
+    const unsigned t = xcd * each + (xcd < rest ? xcd : rest) + nth;
+    const unsigned band = t / (8 * T.nj), first = band * 8, high = T.ni - first < 8 ? T.ni - first : 8, in = t - first * T.nj;
+    return TilePlace{first + in % high, in / high};
+}
+
+struct GatedFwd { Matrices M; Tiles T; int fn, fo; const float* bias; float *y, *kept; long ld; };      // rows of y are ld elements apart
+
+// AXIS 0: i = features (halves), j = positions.  AXIS 1: i = positions, j = features (halves); rows of `kept` hold both halves.
+template <class W, int AXIS>
+__global__ void __launch_bounds__(W::kThreads) k_gated_fwd(GatedFwd G)
+{
+    const TilePlace P = tile_place(G.T, blockIdx.x);
+    const long i0 = (long)P.i * (AXIS ? W::TI : W::TI / 2), j0 = (long)P.j * (AXIS ? W::TJ / 2 : W::TJ);
+    floatx16 acc[W::AI][W::AJ];
+    tile_product<W, true, AXIS == 1, AXIS ? HALVES_J : HALVES_I>(acc, G.M, i0, j0);
+    const int wave = threadIdx.x >> 6, wi = wave / W::WJ, wj = wave % W::WJ, column = threadIdx.x & 31;
+    static_assert(AXIS ? W::AJ == 2 : W::AI == 2, "a wave holds both halves");
+#pragma unroll
+    for (int n = 0; n < (AXIS ? W::AI : W::AJ); ++n) {
+        const floatx16 &us = AXIS ? acc[n][0] : acc[0][n], &vs = AXIS ? acc[n][1] : acc[1][n];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const long i = i0 + (AXIS ? wi * (32 * W::AI) + 32 * n : wi * 32) + result_row(r);
+            const long j = j0 + (AXIS ? wj * 32 : wj * (32 * W::AJ) + 32 * n) + column, m = AXIS ? j : i;
+            if (i >= G.M.rows_i || j >= G.M.rows_j) continue;
+            const float u = us[r] + (G.bias ? G.bias[m] : 0.f), v = vs[r] + (G.bias ? G.bias[G.fo + m] : 0.f);
+            G.y[i * G.ld + j] = gate_fn(G.fn, u).a * v;
+            if (G.kept) {
+                float* const at = G.kept + i * (AXIS ? 2 * G.ld : G.ld) + j;
+                at[0] = u;
+                at[AXIS ? G.ld : G.fo * G.ld] = v;
+            }
+        }
+    }
+}
+
+// A product, or with several shares of the sum over k (`span` of it each) partial ones, one behind the other.
+struct Product { Matrices M; Tiles T; float* c; long span; };
+template <class W, bool A_ALONG, bool B_ALONG>
+__global__ void __launch_bounds__(W::kThreads) k_product(Product G)
+{
+    const TilePlace P = tile_place(G.T, blockIdx.x);
+    const long i0 = (long)P.i * W::TI, j0 = (long)P.j * W::TJ;
+    Matrices M = G.M;
+    M.k0 = blockIdx.y * G.span;
+    if (M.k0 + G.span < M.K) M.K = M.k0 + G.span;
+    floatx16 acc[W::AI][W::AJ];
+    tile_product<W, A_ALONG, B_ALONG, NO_HALVES>(acc, M, i0, j0);
+    float* const c = G.c + blockIdx.y * (M.rows_i * M.rows_j);
+    const int wave = threadIdx.x >> 6, column = threadIdx.x & 31;
+#pragma unroll
+    for (int x = 0; x < W::AI; ++x)
+#pragma unroll
+        for (int y = 0; y < W::AJ; ++y)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const long i = i0 + wave / W::WJ * (32 * W::AI) + 32 * x + result_row(r), j = j0 + wave % W::WJ * (32 * W::AJ) + 32 * y + column;
+                if (i < M.rows_i && j < M.rows_j) c[i * M.rows_j + j] = acc[x][y][r];
+            }
+}
+
+// The sum of shares: every sixteenth by one wave, then these in their order.
+__global__ void __launch_bounds__(1024) k_sum_shares(long count, int shares, const float* parts, float* out)
+{
+    __shared__ float part[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (long first = blockIdx.x * 64L; first < count; first += gridDim.x * 64L) {
+        const long e = first + lane;
+        float s = 0.f;
+        if (e < count) {
+            int n = wave;
+            for (; n + 48 < shares; n += 64) {
+                float v[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] = parts[(n + 16 * c) * count + e];
+                s += (v[0] + v[1]) + (v[2] + v[3]);
+            }
+            for (; n < shares; n += 16) s += parts[n * count + e];
+        }
+        part[wave][lane] = s;
+        __syncthreads();
+        if (wave == 0 && e < count) {
+#pragma unroll
+            for (int w = 1; w < 16; ++w) s += part[w][lane];
+            out[e] = s;
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------- gradients of both halves
+// [du; dv] from gy and the kept [u; v], in the layout of the kept, and their sums over `span` positions for the biases.
+
+struct Grads { int fn; long fo, positions, span; const float *gy, *kept; float *g, *sums; };      // sums [share][2 f'], or NULL
+
+// images: a workgroup a share of one map
+__global__ void __launch_bounds__(256) k_gated_grads_maps(Grads G)
+{
+    __shared__ float part[2][4];
+    const long m = blockIdx.x, first = blockIdx.y * G.span, end = first + G.span < G.positions ? first + G.span : G.positions;
+    const long at = m * G.positions, other = G.fo * G.positions;
+    float su = 0.f, sv = 0.f;
+    for (long n = first + threadIdx.x; n < end; n += 256) {
+        const Gated a = gate_fn(G.fn, G.kept[at + n]);
+        const float gy = G.gy[at + n], du = gy * G.kept[at + other + n] * a.d, dv = gy * a.a;
+        G.g[at + n] = du;
+        G.g[at + other + n] = dv;
+        su += du;
+        sv += dv;
+    }
+    if (!G.sums) return;
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) { su += __shfl_xor(su, d); sv += __shfl_xor(sv, d); }
+    if ((threadIdx.x & 63) == 0) { part[0][threadIdx.x >> 6] = su; part[1][threadIdx.x >> 6] = sv; }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        const float* p = part[threadIdx.x];
+        G.sums[blockIdx.y * 2 * G.fo + threadIdx.x * G.fo + m] = p[0] + p[1] + p[2] + p[3];
+    }
+}
+
+// rows of features: a workgroup a share of 64 columns, four rows at a time
+__global__ void __launch_bounds__(256) k_gated_grads_rows(Grads G)
+{
+    __shared__ float part[2][4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long m = blockIdx.x * 64L + lane, first = blockIdx.y * G.span, end = first + G.span < G.positions ? first + G.span : G.positions;
+    float su = 0.f, sv = 0.f;
+    if (m < G.fo)
+        for (long n = first + wave; n < end; n += 4) {
+            const long at = n * 2 * G.fo + m;
+            const Gated a = gate_fn(G.fn, G.kept[at]);
+            const float gy = G.gy[n * G.fo + m], du = gy * G.kept[at + G.fo] * a.d, dv = gy * a.a;
+            G.g[at] = du;
+            G.g[at + G.fo] = dv;
+            su += du;
+            sv += dv;
+        }
+    if (!G.sums) return;
+    part[0][wave][lane] = su;
+    part[1][wave][lane] = sv;
+    __syncthreads();
+    if (wave < 2 && m < G.fo) {
+        const float* p = part[wave][0] + lane;
+        G.sums[blockIdx.y * 2 * G.fo + wave * G.fo + m] = p[0] + p[64] + p[128] + p[192];
+    }
 }
 
 struct Shape { int f, fo, axis; long positions; };
@@ -133,10 +339,125 @@ int check_gated(int32_t fan_in, int32_t fan_out, int64_t positions, int32_t axis
     if (axis != 0 && axis != 1) return fail(ZNN_EINVAL, "axis must be 0 (images) or 1 (rows of features)");
     if (fan_in > 1 << 20 || fan_out > 1 << 20 || positions > 2147483647LL)
         return fail(ZNN_EUNSUPPORTED, "a gated unit of %d to %d features over %lld positions is too large", fan_in, fan_out, (long long)positions);
+    // numbers of tiles have 31 bits
+    if ((double)std::max(fan_in, fan_out) * positions > 274877906944.0)
+        return fail(ZNN_EUNSUPPORTED, "arrays of %d features at %lld positions are too large", (int)std::max(fan_in, fan_out), (long long)positions);
     return ZNN_OK;
 }
 
-size_t gated_workspace(const Shape& S, bool backward) { return backward ? sizeof(float) * 2 * S.fo * S.positions : 0; }
+// ---------------------------------------------------------------- tiles, shares, launches
+typedef Waves<2, 2, 2, 2> Large;        // 128 x 128
+typedef Waves<1, 4, 2, 1> Wide;         // 64 x 128
+typedef Waves<4, 1, 1, 2> Tall;         // 128 x 64
+
+// Tiles of a product and into how many shares its sum goes, so that there are workgroups for the chip.
+struct Layout { bool large; Tiles T; int shares; long span; };
+constexpr long kUnits = 256, kMostShares = 512, kLeastSpan = 8 * kDepth;
+Tiles tiles_of(long i, long j, long ti, long tj)
+{
+    const long ni = (i + ti - 1) / ti, nj = (j + tj - 1) / tj;
+    return Tiles{(unsigned)ni, (unsigned)nj, (unsigned)(ni * nj)};
+}
+Layout product_layout(long I, long J, long K)
+{
+    Layout L = {};
+    const Tiles large = tiles_of(I, J, Large::TI, Large::TJ);
+    L.large = I > 64 && large.count >= 2 * kUnits;
+    L.T = L.large ? large : tiles_of(I, J, Wide::TI, Wide::TJ);
+    L.shares = (int)std::max(1L, std::min({kMostShares, 4 * kUnits / (long)L.T.count, K / kLeastSpan}));
+    L.span = (K / kDepth + L.shares) / L.shares * kDepth;
+    L.shares = (int)((K + L.span - 1) / L.span);
+    return L;
+}
+size_t product_bytes(const Layout& L, long I, long J) { return L.shares > 1 ? align256(sizeof(float) * L.shares * I * J) : 0; }
+
+template <class W, bool A_ALONG, bool B_ALONG>
+void launch_tiles(const Product& P, const Layout& L, hipStream_t s)
+{
+    ZNN_LAUNCH("gated unit product", s, (k_product<W, A_ALONG, B_ALONG>), dim3(L.T.count, (unsigned)L.shares), dim3(W::kThreads), 0, P);
+}
+// c [I][J] = sum over k of A B; `parts` holds product_bytes
+template <bool A_ALONG, bool B_ALONG>
+int product(const Operand& A, const Operand& B, long I, long J, long K, float* c, float* parts, hipStream_t s)
+{
+    const Layout L = product_layout(I, J, K);
+    const Product P = {{A, B, I, J, 0, 0, K}, L.T, L.shares > 1 ? parts : c, L.span};
+    if (L.large) launch_tiles<Large, A_ALONG, B_ALONG>(P, L, s);
+    else launch_tiles<Wide, A_ALONG, B_ALONG>(P, L, s);
+    if (L.shares > 1)
+        ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3((unsigned)std::min((I * J + 63) / 64, 1L << 20)), dim3(1024), 0, I * J, L.shares,
+                   (const float*)parts, c);
+    return check_launch("gated unit product");
+}
+
+// Shares of the biases' sums
+struct BiasShares { int count; long span; };
+BiasShares bias_shares(const Shape& S)
+{
+    const long across = S.axis ? (S.fo + 63) / 64 : S.fo, least = S.axis ? 32 : 1024;
+    const long count = std::max(1L, std::min({8 * kUnits / across + 1, (S.positions + least - 1) / least, 1L << 15}));
+    const long span = (S.positions + count - 1) / count;
+    return BiasShares{(int)((S.positions + span - 1) / span), span};
+}
+
+struct Scratch { size_t g, sums, parts, all; };     // offsets
+Scratch backward_scratch(const Shape& S)
+{
+    const long both = 2L * S.fo, n = S.positions;
+    Scratch W = {};
+    W.sums = align256(sizeof(float) * both * n);
+    W.parts = W.sums + align256(sizeof(float) * both * bias_shares(S).count);
+    const size_t gx = S.axis ? product_bytes(product_layout(n, S.f, both), n, S.f) : product_bytes(product_layout(S.f, n, both), S.f, n);
+    W.all = W.parts + std::max(gx, product_bytes(product_layout(both, S.f, n), both, S.f));
+    return W;
+}
+size_t gated_workspace(const Shape& S, bool backward) { return backward ? backward_scratch(S).all : 0; }
+
+template <class W, int AXIS>
+void launch_fwd(GatedFwd G, hipStream_t s)
+{
+    G.T = AXIS ? tiles_of(G.M.rows_i, G.M.rows_j, W::TI, W::TJ / 2) : tiles_of(G.M.rows_i, G.M.rows_j, W::TI / 2, W::TJ);
+    ZNN_LAUNCH("gated unit forward", s, (k_gated_fwd<W, AXIS>), dim3(G.T.count), dim3(W::kThreads), 0, G);
+}
+
+int gated_fwd(const Shape& S, int fn, const float* x, const float* w, const float* b, float* y, float* kept, hipStream_t s)
+{
+    const Operand weights = {w, S.f};
+    const long half = S.fo;
+    const bool large = tiles_of(S.fo, S.positions, 64, 128).count >= 2 * kUnits;
+    if (S.axis) {
+        const GatedFwd G = {{{x, S.f}, weights, S.positions, S.fo, half, 0, S.f}, Tiles{}, fn, S.fo, b, y, kept, S.fo};
+        if (large) launch_fwd<Large, 1>(G, s);
+        else launch_fwd<Tall, 1>(G, s);
+    } else {
+        const GatedFwd G = {{weights, {x, S.positions}, S.fo, S.positions, half, 0, S.f}, Tiles{}, fn, S.fo, b, y, kept, S.positions};
+        if (large) launch_fwd<Large, 0>(G, s);
+        else launch_fwd<Wide, 0>(G, s);
+    }
+    return check_launch("gated unit forward");
+}
+
+int gated_bwd(const Shape& S, int fn, const float* gy, const float* x, const float* w, const float* kept, float* gx, float* gw, float* gb,
+              char* ws, hipStream_t s)
+{
+    const Scratch W = backward_scratch(S);
+    const BiasShares bias = bias_shares(S);
+    float *const g = (float*)ws, *const sums = (float*)(ws + W.sums), *const parts = (float*)(ws + W.parts);
+    const long both = 2L * S.fo, n = S.positions;
+    const Grads G = {fn, S.fo, n, bias.span, gy, kept, g, gb ? (bias.count > 1 ? sums : gb) : nullptr};
+    if (S.axis) ZNN_LAUNCH("gated unit gradients", s, k_gated_grads_rows, dim3((unsigned)((S.fo + 63) / 64), (unsigned)bias.count), dim3(256), 0, G);
+    else ZNN_LAUNCH("gated unit gradients", s, k_gated_grads_maps, dim3((unsigned)S.fo, (unsigned)bias.count), dim3(256), 0, G);
+    if (gb && bias.count > 1)
+        ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3((unsigned)((both + 63) / 64)), dim3(1024), 0, both, bias.count, (const float*)sums, gb);
+    int rc = check_launch("gated unit gradients");
+    if (rc != ZNN_OK) return rc;
+    if (S.axis) {
+        if (gx) rc = product<true, false>({g, both}, {w, S.f}, n, S.f, both, gx, parts, s);
+        return rc != ZNN_OK ? rc : product<false, false>({g, both}, {x, S.f}, both, S.f, n, gw, parts, s);
+    }
+    if (gx) rc = product<false, false>({w, S.f}, {g, n}, S.f, n, both, gx, parts, s);
+    return rc != ZNN_OK ? rc : product<true, true>({g, n}, {x, n}, both, S.f, n, gw, parts, s);
+}
 
 int check_gated_call(int32_t fn, const Shape& S, bool backward, const void* ws, size_t ws_bytes)
 {
@@ -148,8 +469,6 @@ int check_gated_call(int32_t fn, const Shape& S, bool backward, const void* ws, 
     if (ws_bytes < need) return fail(ZNN_EWORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, need);
     return ZNN_OK;
 }
-
-dim3 tiles_of(long M, long N) { return dim3((unsigned)((N + kTile - 1) / kTile), (unsigned)((M + kTile - 1) / kTile)); }
 
 }  // namespace
 }  // namespace znn
@@ -177,11 +496,7 @@ int znn_gated_fwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t positions
     const Shape S = {fan_in, fan_out, axis, (long)positions};
     rc = check_gated_call(fn, S, false, ws, ws_bytes);
     if (rc != ZNN_OK) return rc;
-    const Place in = place(axis, S.f, S.positions);
-    const GatedFwd G = {{{w, S.f, 1}, {x, in.position, in.feature}, S.fo, S.positions, S.f}, (long)S.fo * S.f, fn, b, y, kept,
-                        place(axis, S.fo, S.positions)};
-    ZNN_LAUNCH("gated unit forward", (hipStream_t)stream, k_gated_fwd, tiles_of(S.fo, S.positions), dim3(256), 0, G);
-    return check_launch("gated unit forward");
+    return gated_fwd(S, fn, x, w, b, y, kept, (hipStream_t)stream);
 }
 
 int znn_gated_bwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t positions, int32_t axis, const float* gy, const float* x,
@@ -193,20 +508,7 @@ int znn_gated_bwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t positions
     const Shape S = {fan_in, fan_out, axis, (long)positions};
     rc = check_gated_call(fn, S, true, ws, ws_bytes);
     if (rc != ZNN_OK) return rc;
-    const hipStream_t s = (hipStream_t)stream;
-    float* const g = (float*)ws;
-    const Place in = place(axis, S.f, S.positions), both = place(axis, 2L * S.fo, S.positions);
-    const long work = (long)S.fo * S.positions;
-    ZNN_LAUNCH("gated unit gradients", s, k_gated_grads, dim3((unsigned)std::min((work + 255) / 256, 1L << 20)), dim3(256), 0, fn, (long)S.fo,
-               S.positions, axis, gy, kept, g);
-    if (gx) {
-        const Product1 P = {{{w, 1, S.f}, {g, both.position, both.feature}, S.f, S.positions, 2L * S.fo}, gx, in.feature, in.position};
-        ZNN_LAUNCH("gated unit backward", s, k_product, tiles_of(S.f, S.positions), dim3(256), 0, P);
-    }
-    const Product1 P = {{{g, both.feature, both.position}, {x, in.feature, in.position}, 2L * S.fo, S.f, S.positions}, gw, S.f, 1};
-    ZNN_LAUNCH("gated unit weights", s, k_product, tiles_of(2L * S.fo, S.f), dim3(256), 0, P);
-    if (gb) ZNN_LAUNCH("gated unit bias", s, k_gated_bias, dim3(2 * S.fo), dim3(256), 0, S.positions, both, (const float*)g, gb);
-    return check_launch("gated unit backward");
+    return gated_bwd(S, fn, gy, x, w, kept, gx, gw, gb, (char*)ws, (hipStream_t)stream);
 }
 
 }  // extern "C"

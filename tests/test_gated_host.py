@@ -40,6 +40,8 @@ def test_gated_extents(name):
         assert call(name, axis=axis) == znn.ZNN_EINVAL
     for fn in (-1, 5):
         assert call(name, fn=fn) == znn.ZNN_EINVAL
+    assert call(name, fan_in=1 << 10, positions=(1 << 28) + 1) == znn.ZNN_EUNSUPPORTED
+    assert call(name, fan_out=1 << 10, positions=(1 << 28) + 1) == znn.ZNN_EUNSUPPORTED
     for e, v in (("fan_in", (1 << 20) + 1), ("fan_out", (1 << 20) + 1), ("positions", 1 << 31)):
         assert call(name, **{e: v}) == znn.ZNN_EUNSUPPORTED
 
