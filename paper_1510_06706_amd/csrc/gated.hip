@@ -1,5 +1,5 @@
 // Gated unit y = fn(W x + b) (V x + c) and its Jacobian.
-#include "znn_internal.h"
+#include "split_parts.h"
 
 #include <algorithm>
 
@@ -38,7 +38,10 @@ __device__ __forceinline__ Gated gate_fn(int fn, float u)
 // quad of eight k, the others the second one, so that a quad feeds four instructions.
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
+using split::bf16x8;
+using split::floatx4;
+using split::uintx4;
+typedef float floatu2 __attribute__((ext_vector_type(2), aligned(4)));
 typedef float floatu4 __attribute__((ext_vector_type(4), aligned(4)));      // rows begin at any element
 
 constexpr int kDepth = 32;
@@ -188,6 +191,148 @@ __device__ __forceinline__ TilePlace tile_place(const Tiles& T, unsigned number)
     return TilePlace{first + in % high, in / high};
 }
 
+// ---------------------------------------------------------------- the same on the bf16 matrix cores
+// Operands as three bf16 parts each (split_parts.h), six products of a step of 32 k: the work of the fp32 instruction in 96 clocks of 256.
+// A workgroup of four waves makes a tile of 128 x 128 results, a wave 64 x 64 of them as 4 x 4 tiles of 16 x 16.  Values are taken apart on their way into shared
+// memory, [part][row][32 k] of 49 KB, of which a unit holds two workgroups': while one multiplies, the other one's step is taken apart.
+// Results lie with their rows (the instruction's first operand) along j, so that a lane has four neighbours of a row of C.
+
+constexpr int kSplitTile = 128, kPlane = kSplitTile * kDepth * 2;       // bytes of a part of one operand
+
+// Octet of eight k of a row: 16 lanes read one octet of 16 rows, and take all banks.
+__device__ __forceinline__ int octet_place(int row, int octet) { return row * 64 + ((octet ^ (row >> 2 & 3)) << 4); }
+
+template <bool ALONG_K, bool HALVES>
+struct SplitStage {
+    float v[2][8];          // ALONG_K: two rows 64 apart, else two neighbours
+
+    __device__ __forceinline__ void load(const Operand& O, long first, long rows, long half, long k0, long K)
+    {
+        if (ALONG_K) {
+            const long k = k0 + threadIdx.x % 4 * 8;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float* p = O.p + source_row<HALVES>(first, threadIdx.x / 4 + 64 * i, rows, half) * O.ld + k;
+                if (k0 + kDepth <= K) {
+                    *(floatx4*)v[i] = *(const floatu4*)p;
+                    *(floatx4*)(v[i] + 4) = *(const floatu4*)(p + 4);
+                } else
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) v[i][c] = k + c < K ? p[c] : 0.f;
+            }
+        } else {
+            const long r = first + threadIdx.x % 64 * 2, k = k0 + threadIdx.x / 64 * 8;
+            const float* p = O.p + k * O.ld + r;
+            const bool whole = k0 + kDepth <= K && first + kSplitTile <= rows;
+#pragma unroll
+            for (int c = 0; c < 8; ++c, p += O.ld) {
+                if (whole) {
+                    const floatu2 two = *(const floatu2*)p;
+                    v[0][c] = two[0];
+                    v[1][c] = two[1];
+                } else {
+                    v[0][c] = k + c < K && r < rows ? p[0] : 0.f;
+                    v[1][c] = k + c < K && r + 1 < rows ? p[1] : 0.f;
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void store(char* lds, float scale)
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = ALONG_K ? threadIdx.x / 4 + 64 * i : threadIdx.x % 64 * 2 + i, octet = ALONG_K ? threadIdx.x % 4 : threadIdx.x / 64;
+            char* const at = lds + octet_place(row, octet);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[i][c] *= scale;
+#pragma unroll
+            for (int part = 0; part < 3; ++part) *(uintx4*)(at + part * kPlane) = split::take_part8(v[i]);
+        }
+    }
+};
+
+// acc[x][y]: rows i = 16 x + lane % 16 and columns j = 16 y + lane / 16 * 4 + 0 .. 3 of the wave's 64 x 64
+template <bool A_ALONG, bool B_ALONG, Halves H>
+__device__ __forceinline__ void split_product(floatx4 (&acc)[4][4], const Matrices& M, long i0, long j0)
+{
+    __shared__ __attribute__((aligned(16))) char lds[6 * kPlane];
+    SplitStage<A_ALONG, H == HALVES_I> a;
+    SplitStage<B_ALONG, H == HALVES_J> b;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, octet = lane >> 4;
+    const int wi = wave / 2 * 64 + row, wj = wave % 2 * 64 + row;
+    char *const lds_a = lds, *const lds_b = lds + 3 * kPlane;
+    const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+    floatx4 t[2][4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        t[1][x] = zero;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) acc[x][y] = zero;
+    }
+    a.load(M.A, i0, M.rows_i, M.half, M.k0, M.K);
+    b.load(M.B, j0, M.rows_j, M.half, M.k0, M.K);
+    float sign = 1.f;
+    for (long k = M.k0; k < M.K; k += kDepth) {
+        a.store(lds_a, sign * split::kScale);
+        b.store(lds_b, split::kScale);
+        __syncthreads();
+        if (k + kDepth < M.K) {
+            a.load(M.A, i0, M.rows_i, M.half, k + kDepth, M.K);
+            b.load(M.B, j0, M.rows_j, M.half, k + kDepth, M.K);
+        }
+        bf16x8 v[4][3];
+        uintx4 u[2][3];
+#pragma unroll
+        for (int part = 0; part < 3; ++part) u[0][part] = *(const uintx4*)(lds_a + part * kPlane + octet_place(wi, octet));
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int part = 0; part < 3; ++part)
+                v[y][part] = __builtin_bit_cast(bf16x8, *(const uintx4*)(lds_b + part * kPlane + octet_place(wj + 16 * y, octet)));
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            // the products of the row before are added meanwhile, and the next row's operand is requested
+            floatx4* add[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) add[y] = &acc[x ? x - 1 : 3][y];
+            split::products<4, 0, true>(t[x & 1], v, u[x & 1], t[~x & 1], x ? sign : -sign, add, [&](int slot) {
+                if (x < 3 && slot < 3) u[~x & 1][slot] = *(const uintx4*)(lds_a + slot * kPlane + octet_place(wi + 16 * (x + 1), octet));
+            });
+        }
+        sign = -sign;
+        __syncthreads();
+    }
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+        split::add_signed<0>(acc[3][y], t[1][y], -sign);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) acc[x][y] *= split::kUnscale;
+    }
+}
+
+// A result that is not finite is taken again from memory: parts of infinite operands are no numbers, and sums are 2^32 too large until they are done.
+__device__ __noinline__ float again(const float* a, long step_a, const float* b, long step_b, long count)
+{
+    float s = 0.f;
+    for (long k = 0; k < count; ++k, a += step_a, b += step_b) s = fmaf(*a, *b, s);
+    return s;
+}
+template <bool A_ALONG, bool B_ALONG>
+__device__ __forceinline__ float again(const Matrices& M, long row_a, long row_b)
+{
+    const long step_a = A_ALONG ? 1 : M.A.ld, step_b = B_ALONG ? 1 : M.B.ld;
+    return again(M.A.p + row_a * (A_ALONG ? M.A.ld : 1) + M.k0 * step_a, step_a, M.B.p + row_b * (B_ALONG ? M.B.ld : 1) + M.k0 * step_b, step_b, M.K - M.k0);
+}
+__device__ __forceinline__ void store4(float* p, const floatx4& v, int most)
+{
+    if (most == 4) *(floatu4*)p = v;
+    else
+#pragma unroll
+        for (int r = 0; r < 3; ++r)
+            if (r < most) p[r] = v[r];
+}
+__device__ __forceinline__ bool finite(float v) { return fabsf(v) <= split::kLargest; }
+
 struct GatedFwd { Matrices M; Tiles T; int fn, fo; const float* bias; float *y, *kept; long ld; };      // rows of y are ld elements apart
 
 // AXIS 0: i = features (halves), j = positions.  AXIS 1: i = positions, j = features (halves); rows of `kept` hold both halves.
@@ -219,6 +364,45 @@ __global__ void __launch_bounds__(W::kThreads) k_gated_fwd(GatedFwd G)
     }
 }
 
+template <int AXIS>
+__global__ void __launch_bounds__(256, 2) k_gated_fwd_split(GatedFwd G)
+{
+    const TilePlace P = tile_place(G.T, blockIdx.x);
+    const long i0 = (long)P.i * (AXIS ? kSplitTile : kSplitTile / 2), j0 = (long)P.j * (AXIS ? kSplitTile / 2 : kSplitTile);
+    floatx4 acc[4][4];
+    split_product<true, AXIS == 1, AXIS ? HALVES_J : HALVES_I>(acc, G.M, i0, j0);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // halves are 32 of a wave's 64 rows or columns apart
+#pragma unroll
+    for (int x = 0; x < (AXIS ? 4 : 2); ++x)
+#pragma unroll
+        for (int y = 0; y < (AXIS ? 2 : 4); ++y) {
+            const long i = i0 + wave / 2 * (AXIS ? 64 : 32) + 16 * x + (lane & 15), j = j0 + wave % 2 * (AXIS ? 32 : 64) + 16 * y + (lane >> 4) * 4;
+            if (i >= G.M.rows_i || j >= G.M.rows_j) continue;
+            const int most = G.M.rows_j - j < 4 ? (int)(G.M.rows_j - j) : 4;
+            floatx4 u = acc[x][y], v = AXIS ? acc[x][(y + 2) & 3] : acc[(x + 2) & 3][y], out;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const long m = AXIS ? j + r : i, other = AXIS ? i : j + r;
+                if (r < most) {
+                    if (!finite(u[r])) u[r] = AXIS ? again<true, true>(G.M, other, m) : again<true, false>(G.M, m, other);
+                    if (!finite(v[r])) v[r] = AXIS ? again<true, true>(G.M, other, m + G.fo) : again<true, false>(G.M, m + G.fo, other);
+                    if (G.bias) {
+                        u[r] += G.bias[m];
+                        v[r] += G.bias[G.fo + m];
+                    }
+                }
+                out[r] = gate_fn(G.fn, u[r]).a * v[r];
+            }
+            store4(G.y + i * G.ld + j, out, most);
+            if (G.kept) {
+                float* const at = G.kept + i * (AXIS ? 2 * G.ld : G.ld) + j;
+                store4(at, u, most);
+                store4(at + (AXIS ? G.ld : G.fo * G.ld), v, most);
+            }
+        }
+}
+
 // A product, or with several shares of the sum over k (`span` of it each) partial ones, one behind the other.
 struct Product { Matrices M; Tiles T; float* c; long span; };
 template <class W, bool A_ALONG, bool B_ALONG>
@@ -242,6 +426,32 @@ __global__ void __launch_bounds__(W::kThreads) k_product(Product G)
                 const long i = i0 + wave / W::WJ * (32 * W::AI) + 32 * x + result_row(r), j = j0 + wave % W::WJ * (32 * W::AJ) + 32 * y + column;
                 if (i < M.rows_i && j < M.rows_j) c[i * M.rows_j + j] = acc[x][y][r];
             }
+}
+
+template <bool A_ALONG, bool B_ALONG>
+__global__ void __launch_bounds__(256, 2) k_product_split(Product G)
+{
+    const TilePlace P = tile_place(G.T, blockIdx.x);
+    const long i0 = (long)P.i * kSplitTile, j0 = (long)P.j * kSplitTile;
+    Matrices M = G.M;
+    M.k0 = blockIdx.y * G.span;
+    if (M.k0 + G.span < M.K) M.K = M.k0 + G.span;
+    floatx4 acc[4][4];
+    split_product<A_ALONG, B_ALONG, NO_HALVES>(acc, M, i0, j0);
+    float* const c = G.c + blockIdx.y * (M.rows_i * M.rows_j);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const long i = i0 + wave / 2 * 64 + 16 * x + (lane & 15), j = j0 + wave % 2 * 64 + 16 * y + (lane >> 4) * 4;
+            if (i >= M.rows_i || j >= M.rows_j) continue;
+            const int most = M.rows_j - j < 4 ? (int)(M.rows_j - j) : 4;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (r < most && !finite(acc[x][y][r])) acc[x][y][r] = again<A_ALONG, B_ALONG>(M, i, j + r);
+            store4(c + i * M.rows_j + j, acc[x][y], most);
+        }
 }
 
 // The sum of shares: every sixteenth by one wave, then these in their order.
@@ -346,7 +556,6 @@ int check_gated(int32_t fan_in, int32_t fan_out, int64_t positions, int32_t axis
 }
 
 // ---------------------------------------------------------------- tiles, shares, launches
-typedef Waves<2, 2, 2, 2> Large;        // 128 x 128
 typedef Waves<1, 4, 2, 1> Wide;         // 64 x 128
 typedef Waves<4, 1, 1, 2> Tall;         // 128 x 64
 
@@ -361,7 +570,7 @@ Tiles tiles_of(long i, long j, long ti, long tj)
 Layout product_layout(long I, long J, long K)
 {
     Layout L = {};
-    const Tiles large = tiles_of(I, J, Large::TI, Large::TJ);
+    const Tiles large = tiles_of(I, J, kSplitTile, kSplitTile);
     L.large = I > 64 && large.count >= 2 * kUnits;
     L.T = L.large ? large : tiles_of(I, J, Wide::TI, Wide::TJ);
     L.shares = (int)std::max(1L, std::min({kMostShares, 4 * kUnits / (long)L.T.count, K / kLeastSpan}));
@@ -371,19 +580,15 @@ Layout product_layout(long I, long J, long K)
 }
 size_t product_bytes(const Layout& L, long I, long J) { return L.shares > 1 ? align256(sizeof(float) * L.shares * I * J) : 0; }
 
-template <class W, bool A_ALONG, bool B_ALONG>
-void launch_tiles(const Product& P, const Layout& L, hipStream_t s)
-{
-    ZNN_LAUNCH("gated unit product", s, (k_product<W, A_ALONG, B_ALONG>), dim3(L.T.count, (unsigned)L.shares), dim3(W::kThreads), 0, P);
-}
 // c [I][J] = sum over k of A B; `parts` holds product_bytes
 template <bool A_ALONG, bool B_ALONG>
 int product(const Operand& A, const Operand& B, long I, long J, long K, float* c, float* parts, hipStream_t s)
 {
     const Layout L = product_layout(I, J, K);
     const Product P = {{A, B, I, J, 0, 0, K}, L.T, L.shares > 1 ? parts : c, L.span};
-    if (L.large) launch_tiles<Large, A_ALONG, B_ALONG>(P, L, s);
-    else launch_tiles<Wide, A_ALONG, B_ALONG>(P, L, s);
+    const dim3 grid(L.T.count, (unsigned)L.shares);
+    if (L.large) ZNN_LAUNCH("gated unit product", s, (k_product_split<A_ALONG, B_ALONG>), grid, dim3(256), 0, P);
+    else ZNN_LAUNCH("gated unit product", s, (k_product<Wide, A_ALONG, B_ALONG>), grid, dim3(Wide::kThreads), 0, P);
     if (L.shares > 1)
         ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3((unsigned)std::min((I * J + 63) / 64, 1L << 20)), dim3(1024), 0, I * J, L.shares,
                    (const float*)parts, c);
@@ -420,6 +625,14 @@ void launch_fwd(GatedFwd G, hipStream_t s)
     ZNN_LAUNCH("gated unit forward", s, (k_gated_fwd<W, AXIS>), dim3(G.T.count), dim3(W::kThreads), 0, G);
 }
 
+template <int AXIS>
+void launch_fwd_split(GatedFwd G, hipStream_t s)
+{
+    constexpr long tile = kSplitTile;
+    G.T = AXIS ? tiles_of(G.M.rows_i, G.M.rows_j, tile, tile / 2) : tiles_of(G.M.rows_i, G.M.rows_j, tile / 2, tile);
+    ZNN_LAUNCH("gated unit forward", s, k_gated_fwd_split<AXIS>, dim3(G.T.count), dim3(256), 0, G);
+}
+
 int gated_fwd(const Shape& S, int fn, const float* x, const float* w, const float* b, float* y, float* kept, hipStream_t s)
 {
     const Operand weights = {w, S.f};
@@ -427,11 +640,11 @@ int gated_fwd(const Shape& S, int fn, const float* x, const float* w, const floa
     const bool large = tiles_of(S.fo, S.positions, 64, 128).count >= 2 * kUnits;
     if (S.axis) {
         const GatedFwd G = {{{x, S.f}, weights, S.positions, S.fo, half, 0, S.f}, Tiles{}, fn, S.fo, b, y, kept, S.fo};
-        if (large) launch_fwd<Large, 1>(G, s);
+        if (large) launch_fwd_split<1>(G, s);
         else launch_fwd<Tall, 1>(G, s);
     } else {
         const GatedFwd G = {{weights, {x, S.positions}, S.fo, S.positions, half, 0, S.f}, Tiles{}, fn, S.fo, b, y, kept, S.positions};
-        if (large) launch_fwd<Large, 0>(G, s);
+        if (large) launch_fwd_split<0>(G, s);
         else launch_fwd<Wide, 0>(G, s);
     }
     return check_launch("gated unit forward");
