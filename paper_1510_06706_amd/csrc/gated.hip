@@ -2,6 +2,7 @@
 #include "split_parts.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace znn {
 namespace {
@@ -193,115 +194,198 @@ __device__ __forceinline__ TilePlace tile_place(const Tiles& T, unsigned number)
 
 // ---------------------------------------------------------------- the same on the bf16 matrix cores
 // Operands as three bf16 parts each (split_parts.h), six products of a step of 32 k: the work of the fp32 instruction in 96 clocks of 256.
-// A workgroup of four waves makes a tile of 128 x 128 results, a wave 64 x 64 of them as 4 x 4 tiles of 16 x 16.  Values are taken apart on their way into shared
-// memory, [part][row][32 k] of 49 KB, of which a unit holds two workgroups': while one multiplies, the other one's step is taken apart.
+// A workgroup of WI x 2 waves makes a tile of 64 WI x 128 results, a wave 64 x 64 of them as 4 x 4 tiles of 16 x 16.  Values are taken apart on their way into
+// shared memory, [part][row][32 k], of which there are two: while one step is multiplied, the next one is taken apart between its instructions, a
+// pair of values at a time, and the loads of the one behind it are issued as soon as registers are free for them.
 // Results lie with their rows (the instruction's first operand) along j, so that a lane has four neighbours of a row of C.
 
-constexpr int kSplitTile = 128, kPlane = kSplitTile * kDepth * 2;       // bytes of a part of one operand
+constexpr int kSplitColumns = 128, kSplitWaves = 4;     // rows of waves
 
 // Octet of eight k of a row: 16 lanes read one octet of 16 rows, and take all banks.
 __device__ __forceinline__ int octet_place(int row, int octet) { return row * 64 + ((octet ^ (row >> 2 & 3)) << 4); }
 
-template <bool ALONG_K, bool HALVES>
+// The octets of an operand that a thread moves: one row each (ALONG_K), or one or two neighbouring rows of one octet.
+template <int R, int THREADS, bool ALONG_K, bool HALVES>
 struct SplitStage {
-    float v[2][8];          // ALONG_K: two rows 64 apart, else two neighbours
+    static constexpr int kUnits = R * 4 / THREADS, kPart = R * 64;      // bytes of a part
+    static_assert(kUnits == 1 || kUnits == 2, "one or two octets of a thread");
+    float v[kUnits][8];
+    unsigned w[4];
+    const float* p[kUnits];         // ALONG_K: the thread's next octets
+    const float* base;              // else: row `first` of the next step's first k of this wave's octet
+    unsigned at;                    // and this thread's row behind it
 
-    __device__ __forceinline__ void load(const Operand& O, long first, long rows, long half, long k0, long K)
+    __device__ __forceinline__ static int octet() { return ALONG_K ? threadIdx.x % 4 : __builtin_amdgcn_readfirstlane(threadIdx.x / (THREADS / 4)); }
+    __device__ __forceinline__ static int row(int unit)
     {
-        if (ALONG_K) {
-            const long k = k0 + threadIdx.x % 4 * 8;
+        return ALONG_K ? threadIdx.x / 4 + THREADS / 4 * unit : threadIdx.x % (THREADS / 4) * kUnits + unit;
+    }
+    __device__ __forceinline__ void begin(const Operand& O, long first, long rows, long half, long k0)
+    {
+        if (ALONG_K)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float* p = O.p + source_row<HALVES>(first, threadIdx.x / 4 + 64 * i, rows, half) * O.ld + k;
-                if (k0 + kDepth <= K) {
-                    *(floatx4*)v[i] = *(const floatu4*)p;
-                    *(floatx4*)(v[i] + 4) = *(const floatu4*)(p + 4);
-                } else
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) v[i][c] = k + c < K ? p[c] : 0.f;
-            }
-        } else {
-            const long r = first + threadIdx.x % 64 * 2, k = k0 + threadIdx.x / 64 * 8;
-            const float* p = O.p + k * O.ld + r;
-            const bool whole = k0 + kDepth <= K && first + kSplitTile <= rows;
-#pragma unroll
-            for (int c = 0; c < 8; ++c, p += O.ld) {
-                if (whole) {
-                    const floatu2 two = *(const floatu2*)p;
-                    v[0][c] = two[0];
-                    v[1][c] = two[1];
-                } else {
-                    v[0][c] = k + c < K && r < rows ? p[0] : 0.f;
-                    v[1][c] = k + c < K && r + 1 < rows ? p[1] : 0.f;
-                }
-            }
+            for (int u = 0; u < kUnits; ++u) p[u] = O.p + source_row<HALVES>(first, row(u), rows, half) * O.ld + k0 + octet() * 8;
+        else {
+            base = O.p + (k0 + octet() * 8) * O.ld + first;
+            at = row(0);
         }
     }
-    __device__ __forceinline__ void store(char* lds, float scale)
+    // steps that are there as a whole
+    __device__ __forceinline__ void load(int unit, const Operand& O)
     {
+        if (ALONG_K) {
+            *(floatx4*)v[unit] = *(const floatu4*)p[unit];
+            *(floatx4*)(v[unit] + 4) = *(const floatu4*)(p[unit] + 4);
+            p[unit] += kDepth;
+        } else if (unit == kUnits - 1) {
+            const float* q = base;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = ALONG_K ? threadIdx.x / 4 + 64 * i : threadIdx.x % 64 * 2 + i, octet = ALONG_K ? threadIdx.x % 4 : threadIdx.x / 64;
-            char* const at = lds + octet_place(row, octet);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) v[i][c] *= scale;
-#pragma unroll
-            for (int part = 0; part < 3; ++part) *(uintx4*)(at + part * kPlane) = split::take_part8(v[i]);
+            for (int c = 0; c < 8; ++c, q += O.ld) {
+                if (kUnits == 2) {
+                    const floatu2 two = *(const floatu2*)(q + at);
+                    v[0][c] = two[0];
+                    v[kUnits - 1][c] = two[1];
+                } else v[0][c] = q[at];
+            }
+            base += kDepth * O.ld;
         }
+    }
+    __device__ __forceinline__ bool whole(long first, long rows) const { return ALONG_K || first + R <= rows; }
+    // any step: `left` k are there of the operand from its first one on
+    __device__ __forceinline__ void load_some(const Operand& O, long first, long rows, long left)
+    {
+        const int most = (int)(left < kDepth ? left : kDepth) - octet() * 8;
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const float* const q = ALONG_K ? p[u] : base + at + u;
+            const bool there = ALONG_K || first + row(u) < rows;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[u][c] = there && c < most ? q[ALONG_K ? c : c * O.ld] : 0.f;
+            if (ALONG_K) p[u] += kDepth;
+        }
+        if (!ALONG_K) base += kDepth * O.ld;
+    }
+    // twelve pieces of work a unit
+    __device__ __forceinline__ void take(char* lds, int piece, float scale)
+    {
+        const int unit = piece / 12, part = piece % 12 / 4, pair = piece % 4;
+        float &x = v[unit][2 * pair], &y = v[unit][2 * pair + 1];
+        if (part == 0) { x *= scale; y *= scale; }
+        w[pair] = split::take_part(x, y);
+        if (pair == 3) *(uintx4*)(lds + part * kPart + octet_place(row(unit), octet())) = uintx4{w[0], w[1], w[2], w[3]};
     }
 };
 
-// acc[x][y]: rows i = 16 x + lane % 16 and columns j = 16 y + lane / 16 * 4 + 0 .. 3 of the wave's 64 x 64
-template <bool A_ALONG, bool B_ALONG, Halves H>
+// Six products of a step, from zero, smallest first, of one operand (u) with four (v); meanwhile acc += sign before, which are the products before,
+// and request(slot), slot = 0 .. 23, between any two instructions.  ROWS_V: the results' rows are v's.
+template <bool ROWS_V, class Request>
+__device__ __forceinline__ void products(floatx4 (&t)[4], const bf16x8 (&v)[4][3], const uintx4 (&u)[3], const floatx4 (&before)[4], float sign,
+                                         floatx4 (&acc)[4], Request request)
+{
+    constexpr int of_v[6] = {0, 2, 1, 0, 1, 0}, of_u[6] = {2, 0, 1, 1, 0, 0};
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int g = 0; g < 6; ++g)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const bf16x8 one = __builtin_bit_cast(bf16x8, u[of_u[g]]);
+            const floatx4 c = g ? t[y] : floatx4{0.f, 0.f, 0.f, 0.f};
+            t[y] = ROWS_V ? split::mfma(v[y][of_v[g]], one, c) : split::mfma(one, v[y][of_v[g]], c);
+            request(g * 4 + y);
+            if (g >= 1 && g <= 4) acc[y][g - 1] = fmaf(before[y][g - 1], sign, acc[y][g - 1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+}
+
+// acc[x][y], of the wave's 64 x 64: rows i = 16 x + lane % 16 and columns j = 16 y + lane / 16 * 4 + 0 .. 3, or (TURNED) rows
+// i = 16 x + lane / 16 * 4 + 0 .. 3 and columns j = 16 y + lane % 16
+template <int WI, bool A_ALONG, bool B_ALONG, Halves H, bool TURNED>
 __device__ __forceinline__ void split_product(floatx4 (&acc)[4][4], const Matrices& M, long i0, long j0)
 {
-    __shared__ __attribute__((aligned(16))) char lds[6 * kPlane];
-    SplitStage<A_ALONG, H == HALVES_I> a;
-    SplitStage<B_ALONG, H == HALVES_J> b;
+    typedef SplitStage<64 * WI, 128 * WI, A_ALONG, H == HALVES_I> StageA;
+    typedef SplitStage<kSplitColumns, 128 * WI, B_ALONG, H == HALVES_J> StageB;
+    constexpr int kBytes = 3 * (StageA::kPart + StageB::kPart), kPieces = 12 * (StageA::kUnits + StageB::kUnits);
+    __shared__ __attribute__((aligned(16))) char lds[2 * kBytes];
+    StageA a;
+    StageB b;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, octet = lane >> 4;
-    const int wi = wave / 2 * 64 + row, wj = wave % 2 * 64 + row;
-    char *const lds_a = lds, *const lds_b = lds + 3 * kPlane;
-    const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+    const int from_a = octet_place(wave / 2 * 64 + row, octet), from_b = 3 * StageA::kPart + octet_place(wave % 2 * 64 + row, octet);
     floatx4 t[2][4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-        t[1][x] = zero;
+        t[1][x] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int y = 0; y < 4; ++y) acc[x][y] = zero;
+        for (int y = 0; y < 4; ++y) acc[x][y] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
-    a.load(M.A, i0, M.rows_i, M.half, M.k0, M.K);
-    b.load(M.B, j0, M.rows_j, M.half, M.k0, M.K);
-    float sign = 1.f;
-    for (long k = M.k0; k < M.K; k += kDepth) {
-        a.store(lds_a, sign * split::kScale);
-        b.store(lds_b, split::kScale);
-        __syncthreads();
-        if (k + kDepth < M.K) {
-            a.load(M.A, i0, M.rows_i, M.half, k + kDepth, M.K);
-            b.load(M.B, j0, M.rows_j, M.half, k + kDepth, M.K);
+    const long steps = (M.K - M.k0 + kDepth - 1) / kDepth;
+    // steps from there on are loaded by parts
+    const long plain = a.whole(i0, M.rows_i) && b.whole(j0, M.rows_j) ? (M.K - M.k0) / kDepth : 0;
+    auto load = [&](long step) {
+        if (step < plain) {
+#pragma unroll
+            for (int u = 0; u < StageA::kUnits; ++u) a.load(u, M.A);
+#pragma unroll
+            for (int u = 0; u < StageB::kUnits; ++u) b.load(u, M.B);
+        } else if (step < steps) {
+            a.load_some(M.A, i0, M.rows_i, M.K - M.k0 - step * kDepth);
+            b.load_some(M.B, j0, M.rows_j, M.K - M.k0 - step * kDepth);
         }
+    };
+    auto take = [&](char* to, int piece, float sign) {
+        if (piece < 12 * StageA::kUnits) a.take(to, piece, sign * split::kScale);
+        else b.take(to + 3 * StageA::kPart, piece - 12 * StageA::kUnits, split::kScale);
+    };
+    a.begin(M.A, i0, M.rows_i, M.half, M.k0);
+    b.begin(M.B, j0, M.rows_j, M.half, M.k0);
+    load(0);
+#pragma unroll
+    for (int n = 0; n < kPieces; ++n) take(lds, n, 1.f);
+    load(1);
+    __syncthreads();
+    float sign = 1.f;
+    // One step: its products, and between them the next one taken apart (TAKES) and the loads of the one behind that (LOADS).
+    auto step = [&](auto takes, auto loads, const char* here, char* next) {
         bf16x8 v[4][3];
         uintx4 u[2][3];
 #pragma unroll
-        for (int part = 0; part < 3; ++part) u[0][part] = *(const uintx4*)(lds_a + part * kPlane + octet_place(wi, octet));
+        for (int part = 0; part < 3; ++part) u[0][part] = *(const uintx4*)(here + part * StageA::kPart + from_a);
 #pragma unroll
         for (int y = 0; y < 4; ++y)
 #pragma unroll
             for (int part = 0; part < 3; ++part)
-                v[y][part] = __builtin_bit_cast(bf16x8, *(const uintx4*)(lds_b + part * kPlane + octet_place(wj + 16 * y, octet)));
+                v[y][part] = __builtin_bit_cast(bf16x8, *(const uintx4*)(here + part * StageB::kPart + from_b + 1024 * y));
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-            // the products of the row before are added meanwhile, and the next row's operand is requested
-            floatx4* add[4];
-#pragma unroll
-            for (int y = 0; y < 4; ++y) add[y] = &acc[x ? x - 1 : 3][y];
-            split::products<4, 0, true>(t[x & 1], v, u[x & 1], t[~x & 1], x ? sign : -sign, add, [&](int slot) {
-                if (x < 3 && slot < 3) u[~x & 1][slot] = *(const uintx4*)(lds_a + slot * kPlane + octet_place(wi + 16 * (x + 1), octet));
+            products<!TURNED>(t[x & 1], v, u[x & 1], t[~x & 1], x ? sign : -sign, acc[x ? x - 1 : 3], [&](int slot) {
+                if (x < 3 && slot < 3) u[~x & 1][slot] = *(const uintx4*)(here + slot * StageA::kPart + from_a + 1024 * (x + 1));
+                constexpr int kFirst = 6, kEach = (96 - kFirst) / kPieces;
+                const int n = x * 24 + slot - kFirst, piece = n / kEach;
+                if (takes.value && n >= 0 && n % kEach == 0 && piece < kPieces) {
+                    take(next, piece, -sign);
+                    if (loads.value && piece % 12 == 11) {
+                        if (piece < 12 * StageA::kUnits) a.load(piece / 12, M.A);
+                        else b.load(piece / 12 - StageA::kUnits, M.B);
+                    }
+                }
             });
         }
         sign = -sign;
+    };
+    typedef std::integral_constant<bool, true> Yes;
+    typedef std::integral_constant<bool, false> No;
+    long n = 0;
+    auto here = [&] { return lds + (n & 1) * kBytes; };
+    auto next = [&] { return lds + (~n & 1) * kBytes; };
+    for (; n + 2 < plain; ++n) {
+        step(Yes{}, Yes{}, here(), next());
         __syncthreads();
     }
+    for (; n + 1 < steps; ++n) {
+        step(Yes{}, No{}, here(), next());
+        load(n + 2);
+        __syncthreads();
+    }
+    step(No{}, No{}, here(), next());
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
         split::add_signed<0>(acc[3][y], t[1][y], -sign);
@@ -330,6 +414,16 @@ __device__ __forceinline__ void store4(float* p, const floatx4& v, int most)
 #pragma unroll
         for (int r = 0; r < 3; ++r)
             if (r < most) p[r] = v[r];
+}
+__device__ __forceinline__ floatx4 load4(const float* p, int most)
+{
+    floatx4 v = {0.f, 0.f, 0.f, 0.f};
+    if (most == 4) v = *(const floatu4*)p;
+    else
+#pragma unroll
+        for (int r = 0; r < 3; ++r)
+            if (r < most) v[r] = p[r];
+    return v;
 }
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) <= split::kLargest; }
 
@@ -364,13 +458,13 @@ __global__ void __launch_bounds__(W::kThreads) k_gated_fwd(GatedFwd G)
     }
 }
 
-template <int AXIS>
-__global__ void __launch_bounds__(256, 2) k_gated_fwd_split(GatedFwd G)
+template <int WI, int AXIS>
+__global__ void __launch_bounds__(128 * WI, WI / 2) k_gated_fwd_split(GatedFwd G)
 {
     const TilePlace P = tile_place(G.T, blockIdx.x);
-    const long i0 = (long)P.i * (AXIS ? kSplitTile : kSplitTile / 2), j0 = (long)P.j * (AXIS ? kSplitTile / 2 : kSplitTile);
+    const long i0 = (long)P.i * (AXIS ? 64 * WI : 32 * WI), j0 = (long)P.j * (AXIS ? kSplitColumns / 2 : kSplitColumns);
     floatx4 acc[4][4];
-    split_product<true, AXIS == 1, AXIS ? HALVES_J : HALVES_I>(acc, G.M, i0, j0);
+    split_product<WI, true, AXIS == 1, AXIS ? HALVES_J : HALVES_I, false>(acc, G.M, i0, j0);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     // halves are 32 of a wave's 64 rows or columns apart
 #pragma unroll
@@ -428,30 +522,50 @@ __global__ void __launch_bounds__(W::kThreads) k_product(Product G)
             }
 }
 
-template <bool A_ALONG, bool B_ALONG>
-__global__ void __launch_bounds__(256, 2) k_product_split(Product G)
+// TURNED: c [j][i]
+template <int WI, bool A_ALONG, bool B_ALONG, bool TURNED>
+__global__ void __launch_bounds__(128 * WI, WI / 2) k_product_split(Product G)
 {
     const TilePlace P = tile_place(G.T, blockIdx.x);
-    const long i0 = (long)P.i * kSplitTile, j0 = (long)P.j * kSplitTile;
+    const long i0 = (long)P.i * (64 * WI), j0 = (long)P.j * kSplitColumns;
     Matrices M = G.M;
     M.k0 = blockIdx.y * G.span;
     if (M.k0 + G.span < M.K) M.K = M.k0 + G.span;
     floatx4 acc[4][4];
-    split_product<A_ALONG, B_ALONG, NO_HALVES>(acc, M, i0, j0);
+    split_product<WI, A_ALONG, B_ALONG, NO_HALVES, TURNED>(acc, M, i0, j0);
     float* const c = G.c + blockIdx.y * (M.rows_i * M.rows_j);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, one = lane & 15, four = (lane >> 4) * 4;
+    const long ld = TURNED ? M.rows_i : M.rows_j;
 #pragma unroll
     for (int x = 0; x < 4; ++x)
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-            const long i = i0 + wave / 2 * 64 + 16 * x + (lane & 15), j = j0 + wave % 2 * 64 + 16 * y + (lane >> 4) * 4;
+            const long i = i0 + wave / 2 * 64 + 16 * x + (TURNED ? four : one), j = j0 + wave % 2 * 64 + 16 * y + (TURNED ? one : four);
             if (i >= M.rows_i || j >= M.rows_j) continue;
-            const int most = M.rows_j - j < 4 ? (int)(M.rows_j - j) : 4;
+            const long left = TURNED ? M.rows_i - i : M.rows_j - j;
+            const int most = left < 4 ? (int)left : 4;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                if (r < most && !finite(acc[x][y][r])) acc[x][y][r] = again<A_ALONG, B_ALONG>(M, i, j + r);
-            store4(c + i * M.rows_j + j, acc[x][y], most);
+                if (r < most && !finite(acc[x][y][r])) acc[x][y][r] = again<A_ALONG, B_ALONG>(M, TURNED ? i + r : i, TURNED ? j : j + r);
+            store4(TURNED ? c + j * ld + i : c + i * ld + j, acc[x][y], most);
         }
+}
+
+// The sum of a few shares, in their order, four elements a thread.
+__global__ void __launch_bounds__(256) k_sum_few(long count, int shares, const float* parts, float* out)
+{
+    const long quads = count / 4;
+    for (long q = blockIdx.x * 256L + threadIdx.x; q < quads; q += gridDim.x * 256L) {
+        floatx4 s = *(const floatu4*)(parts + 4 * q);
+        for (int n = 1; n < shares; ++n) s += *(const floatu4*)(parts + n * count + 4 * q);
+        *(floatu4*)(out + 4 * q) = s;
+    }
+    if (blockIdx.x == 0 && threadIdx.x < count - 4 * quads) {
+        const long e = 4 * quads + threadIdx.x;
+        float s = parts[e];
+        for (int n = 1; n < shares; ++n) s += parts[n * count + e];
+        out[e] = s;
+    }
 }
 
 // The sum of shares: every sixteenth by one wave, then these in their order.
@@ -488,20 +602,26 @@ __global__ void __launch_bounds__(1024) k_sum_shares(long count, int shares, con
 
 struct Grads { int fn; long fo, positions, span; const float *gy, *kept; float *g, *sums; };      // sums [share][2 f'], or NULL
 
-// images: a workgroup a share of one map
+// images: a workgroup a share of one map, four neighbours a thread
 __global__ void __launch_bounds__(256) k_gated_grads_maps(Grads G)
 {
     __shared__ float part[2][4];
     const long m = blockIdx.x, first = blockIdx.y * G.span, end = first + G.span < G.positions ? first + G.span : G.positions;
     const long at = m * G.positions, other = G.fo * G.positions;
     float su = 0.f, sv = 0.f;
-    for (long n = first + threadIdx.x; n < end; n += 256) {
-        const Gated a = gate_fn(G.fn, G.kept[at + n]);
-        const float gy = G.gy[at + n], du = gy * G.kept[at + other + n] * a.d, dv = gy * a.a;
-        G.g[at + n] = du;
-        G.g[at + other + n] = dv;
-        su += du;
-        sv += dv;
+    for (long n = first + threadIdx.x * 4L; n < end; n += 1024) {
+        const int most = end - n < 4 ? (int)(end - n) : 4;
+        const floatx4 u = load4(G.kept + at + n, most), v = load4(G.kept + at + other + n, most), gy = load4(G.gy + at + n, most);
+        floatx4 du, dv;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const Gated a = gate_fn(G.fn, u[c]);
+            du[c] = gy[c] * v[c] * a.d;
+            dv[c] = gy[c] * a.a;
+            if (c < most) { su += du[c]; sv += dv[c]; }
+        }
+        store4(G.g + at + n, du, most);
+        store4(G.g + at + other + n, dv, most);
     }
     if (!G.sums) return;
 #pragma unroll
@@ -514,20 +634,27 @@ __global__ void __launch_bounds__(256) k_gated_grads_maps(Grads G)
     }
 }
 
-// rows of features: a workgroup a share of 64 columns, four rows at a time
+// rows of features: a workgroup a share of 256 columns, four a thread, four rows at a time
 __global__ void __launch_bounds__(256) k_gated_grads_rows(Grads G)
 {
-    __shared__ float part[2][4][64];
+    __shared__ floatx4 part[2][4][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long m = blockIdx.x * 64L + lane, first = blockIdx.y * G.span, end = first + G.span < G.positions ? first + G.span : G.positions;
-    float su = 0.f, sv = 0.f;
-    if (m < G.fo)
+    const long m = blockIdx.x * 256L + lane * 4, first = blockIdx.y * G.span, end = first + G.span < G.positions ? first + G.span : G.positions;
+    const int most = G.fo - m < 4 ? G.fo > m ? (int)(G.fo - m) : 0 : 4;
+    floatx4 su = {0.f, 0.f, 0.f, 0.f}, sv = su;
+    if (most)
         for (long n = first + wave; n < end; n += 4) {
             const long at = n * 2 * G.fo + m;
-            const Gated a = gate_fn(G.fn, G.kept[at]);
-            const float gy = G.gy[n * G.fo + m], du = gy * G.kept[at + G.fo] * a.d, dv = gy * a.a;
-            G.g[at] = du;
-            G.g[at + G.fo] = dv;
+            const floatx4 u = load4(G.kept + at, most), v = load4(G.kept + at + G.fo, most), gy = load4(G.gy + n * G.fo + m, most);
+            floatx4 du, dv;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const Gated a = gate_fn(G.fn, u[c]);
+                du[c] = gy[c] * v[c] * a.d;
+                dv[c] = gy[c] * a.a;
+            }
+            store4(G.g + at, du, most);
+            store4(G.g + at + G.fo, dv, most);
             su += du;
             sv += dv;
         }
@@ -535,9 +662,9 @@ __global__ void __launch_bounds__(256) k_gated_grads_rows(Grads G)
     part[0][wave][lane] = su;
     part[1][wave][lane] = sv;
     __syncthreads();
-    if (wave < 2 && m < G.fo) {
-        const float* p = part[wave][0] + lane;
-        G.sums[blockIdx.y * 2 * G.fo + wave * G.fo + m] = p[0] + p[64] + p[128] + p[192];
+    if (wave < 2 && most) {
+        const floatx4* p = part[wave][0] + lane;
+        store4(G.sums + blockIdx.y * 2 * G.fo + wave * G.fo + m, (p[0] + p[64]) + (p[128] + p[192]), most);
     }
 }
 
@@ -559,24 +686,47 @@ int check_gated(int32_t fan_in, int32_t fan_out, int64_t positions, int32_t axis
 typedef Waves<1, 4, 2, 1> Wide;         // 64 x 128
 typedef Waves<4, 1, 1, 2> Tall;         // 128 x 64
 
-// Tiles of a product and into how many shares its sum goes, so that there are workgroups for the chip.
-struct Layout { bool large; Tiles T; int shares; long span; };
+// Tiles of a product and into how many shares its sum goes, by what it is expected to take: a unit takes 2.6 us for a step of 32 k of a tile of 256 x 128 on the
+// bf16 matrix cores (205 TFLOP/s in all), and 1.3 us for one of 64 x 128 on the fp32 ones (100 TFLOP/s), which take three tiles side by side; sums of
+// shares move their bytes at 4 TB/s and a launch takes 3 us.
+enum Kind { FP32, SPLIT, SPLIT_TURNED };
+struct Layout { Kind kind; Tiles T; int shares; long span; double us; };
 constexpr long kUnits = 256, kMostShares = 512, kLeastSpan = 8 * kDepth;
 Tiles tiles_of(long i, long j, long ti, long tj)
 {
     const long ni = (i + ti - 1) / ti, nj = (j + tj - 1) / tj;
     return Tiles{(unsigned)ni, (unsigned)nj, (unsigned)(ni * nj)};
 }
+Layout layout_of(Kind kind, const Tiles& T, long I, long J, long K, bool shares)
+{
+    const long beside = kind == FP32 ? 3 * kUnits : kUnits;
+    Layout best = {};
+    for (long wanted = 1; wanted <= (shares ? kMostShares : 1); wanted = wanted < 4 ? wanted + 1 : wanted + wanted / 4) {
+        if (wanted > 1 && K / wanted < kLeastSpan) break;
+        Layout L = {kind, T, 1, (K + kDepth - 1) / kDepth * kDepth, 0.0};
+        if (wanted > 1) {
+            L.span = (K + wanted * kDepth - 1) / (wanted * kDepth) * kDepth;
+            L.shares = (int)((K + L.span - 1) / L.span);
+        }
+        const long tiles = T.count * (long)L.shares, rounds = (tiles + beside - 1) / beside, last = tiles - (rounds - 1) * beside;
+        const double steps = (double)(L.span / kDepth), step = kind == FP32 ? 1.3 : 2.6;
+        // tiles of the last round that stand alone on their unit take less than three side by side do
+        const double tall = kind == FP32 ? 3.0 * (rounds - 1) + (last > 2 * kUnits ? 3.0 : last > kUnits ? 2.0 : 1.2) : rounds;
+        L.us = tall * (steps * step + (kind == FP32 ? 2.0 : 5.0));
+        if (L.shares > 1) L.us += 3.0 + 1e-6 * I * J * 2 * L.shares;
+        if (wanted == 1 || L.us < best.us) best = L;
+    }
+    return best;
+}
 Layout product_layout(long I, long J, long K)
 {
-    Layout L = {};
-    const Tiles large = tiles_of(I, J, kSplitTile, kSplitTile);
-    L.large = I > 64 && large.count >= 2 * kUnits;
-    L.T = L.large ? large : tiles_of(I, J, Wide::TI, Wide::TJ);
-    L.shares = (int)std::max(1L, std::min({kMostShares, 4 * kUnits / (long)L.T.count, K / kLeastSpan}));
-    L.span = (K / kDepth + L.shares) / L.shares * kDepth;
-    L.shares = (int)((K + L.span - 1) / L.span);
-    return L;
+    Layout best = layout_of(FP32, tiles_of(I, J, Wide::TI, Wide::TJ), I, J, K, true);
+    for (Kind kind : {SPLIT, SPLIT_TURNED}) {
+        const Tiles T = kind == SPLIT ? tiles_of(I, J, 64 * kSplitWaves, kSplitColumns) : tiles_of(J, I, 64 * kSplitWaves, kSplitColumns);
+        const Layout L = layout_of(kind, T, I, J, K, true);
+        if (L.us < best.us) best = L;
+    }
+    return best;
 }
 size_t product_bytes(const Layout& L, long I, long J) { return L.shares > 1 ? align256(sizeof(float) * L.shares * I * J) : 0; }
 
@@ -585,12 +735,19 @@ template <bool A_ALONG, bool B_ALONG>
 int product(const Operand& A, const Operand& B, long I, long J, long K, float* c, float* parts, hipStream_t s)
 {
     const Layout L = product_layout(I, J, K);
-    const Product P = {{A, B, I, J, 0, 0, K}, L.T, L.shares > 1 ? parts : c, L.span};
-    const dim3 grid(L.T.count, (unsigned)L.shares);
-    if (L.large) ZNN_LAUNCH("gated unit product", s, (k_product_split<A_ALONG, B_ALONG>), grid, dim3(256), 0, P);
-    else ZNN_LAUNCH("gated unit product", s, (k_product<Wide, A_ALONG, B_ALONG>), grid, dim3(Wide::kThreads), 0, P);
-    if (L.shares > 1)
-        ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3((unsigned)std::min((I * J + 63) / 64, 1L << 20)), dim3(1024), 0, I * J, L.shares,
+    Product P = {{A, B, I, J, 0, 0, K}, L.T, L.shares > 1 ? parts : c, L.span};
+    const dim3 grid(L.T.count, (unsigned)L.shares), wide(128 * kSplitWaves);
+    if (L.kind == SPLIT) ZNN_LAUNCH("gated unit product", s, (k_product_split<kSplitWaves, A_ALONG, B_ALONG, false>), grid, wide, 0, P);
+    else if (L.kind == SPLIT_TURNED) {
+        P.M = Matrices{B, A, J, I, 0, 0, K};
+        ZNN_LAUNCH("gated unit product", s, (k_product_split<kSplitWaves, B_ALONG, A_ALONG, true>), grid, wide, 0, P);
+    } else ZNN_LAUNCH("gated unit product", s, (k_product<Wide, A_ALONG, B_ALONG>), grid, dim3(Wide::kThreads), 0, P);
+    const long count = I * J;
+    if (L.shares > 16)
+        ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3((unsigned)std::min((count + 63) / 64, 1L << 20)), dim3(1024), 0, count, L.shares,
+                   (const float*)parts, c);
+    else if (L.shares > 1)
+        ZNN_LAUNCH("gated unit shares", s, k_sum_few, dim3((unsigned)std::min((count + 1023) / 1024, 1L << 20)), dim3(256), 0, count, L.shares,
                    (const float*)parts, c);
     return check_launch("gated unit product");
 }
@@ -599,9 +756,9 @@ int product(const Operand& A, const Operand& B, long I, long J, long K, float* c
 struct BiasShares { int count; long span; };
 BiasShares bias_shares(const Shape& S)
 {
-    const long across = S.axis ? (S.fo + 63) / 64 : S.fo, least = S.axis ? 32 : 1024;
+    const long across = S.axis ? (S.fo + 255) / 256 : S.fo, least = S.axis ? 32 : 1024;
     const long count = std::max(1L, std::min({8 * kUnits / across + 1, (S.positions + least - 1) / least, 1L << 15}));
-    const long span = (S.positions + count - 1) / count;
+    const long span = ((S.positions + count - 1) / count + 31) / 32 * 32;
     return BiasShares{(int)((S.positions + span - 1) / span), span};
 }
 
@@ -628,16 +785,17 @@ void launch_fwd(GatedFwd G, hipStream_t s)
 template <int AXIS>
 void launch_fwd_split(GatedFwd G, hipStream_t s)
 {
-    constexpr long tile = kSplitTile;
-    G.T = AXIS ? tiles_of(G.M.rows_i, G.M.rows_j, tile, tile / 2) : tiles_of(G.M.rows_i, G.M.rows_j, tile / 2, tile);
-    ZNN_LAUNCH("gated unit forward", s, k_gated_fwd_split<AXIS>, dim3(G.T.count), dim3(256), 0, G);
+    G.T = AXIS ? tiles_of(G.M.rows_i, G.M.rows_j, 64 * kSplitWaves, kSplitColumns / 2) : tiles_of(G.M.rows_i, G.M.rows_j, 32 * kSplitWaves, kSplitColumns);
+    ZNN_LAUNCH("gated unit forward", s, (k_gated_fwd_split<kSplitWaves, AXIS>), dim3(G.T.count), dim3(128 * kSplitWaves), 0, G);
 }
 
 int gated_fwd(const Shape& S, int fn, const float* x, const float* w, const float* b, float* y, float* kept, hipStream_t s)
 {
     const Operand weights = {w, S.f};
     const long half = S.fo;
-    const bool large = tiles_of(S.fo, S.positions, 64, 128).count >= 2 * kUnits;
+    const long I = S.axis ? S.positions : 2 * half, J = S.axis ? 2 * half : S.positions;
+    const bool large = layout_of(SPLIT, tiles_of(I, J, 64 * kSplitWaves, kSplitColumns), I, J, S.f, false).us <
+                       layout_of(FP32, S.axis ? tiles_of(I, J, Tall::TI, Tall::TJ) : tiles_of(I, J, Wide::TI, Wide::TJ), I, J, S.f, false).us;
     if (S.axis) {
         const GatedFwd G = {{{x, S.f}, weights, S.positions, S.fo, half, 0, S.f}, Tiles{}, fn, S.fo, b, y, kept, S.fo};
         if (large) launch_fwd_split<1>(G, s);
@@ -658,7 +816,7 @@ int gated_bwd(const Shape& S, int fn, const float* gy, const float* x, const flo
     float *const g = (float*)ws, *const sums = (float*)(ws + W.sums), *const parts = (float*)(ws + W.parts);
     const long both = 2L * S.fo, n = S.positions;
     const Grads G = {fn, S.fo, n, bias.span, gy, kept, g, gb ? (bias.count > 1 ? sums : gb) : nullptr};
-    if (S.axis) ZNN_LAUNCH("gated unit gradients", s, k_gated_grads_rows, dim3((unsigned)((S.fo + 63) / 64), (unsigned)bias.count), dim3(256), 0, G);
+    if (S.axis) ZNN_LAUNCH("gated unit gradients", s, k_gated_grads_rows, dim3((unsigned)((S.fo + 255) / 256), (unsigned)bias.count), dim3(256), 0, G);
     else ZNN_LAUNCH("gated unit gradients", s, k_gated_grads_maps, dim3((unsigned)S.fo, (unsigned)bias.count), dim3(256), 0, G);
     if (gb && bias.count > 1)
         ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3((unsigned)((both + 63) / 64)), dim3(1024), 0, both, bias.count, (const float*)sums, gb);

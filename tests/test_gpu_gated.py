@@ -69,6 +69,19 @@ def test_shapes(f, fo, n, axis):
     check(f, fo, n, axis, fn)
 
 
+# enough tiles for the bf16 matrix cores, in one or all of the products: one step of k and less, whole steps, steps cut short, ragged tiles
+LARGE = [(130, 70, 40001), (20, 200, 40000), (32, 64, 70016), (33, 130, 33000), (64, 65, 66000), (95, 96, 45001), (1500, 2800, 300), (1024, 2816, 64),
+         (300, 3001, 1025), (1281, 1792, 1100)]
+
+
+@pytest.mark.parametrize("axis", [0, 1])
+@pytest.mark.parametrize("f,fo,n", LARGE)
+def test_large_shapes(f, fo, n, axis):
+    fn = FNS[(f + fo + n) % 5]
+    print("case", f, fo, n, axis, fn, flush=True)
+    check(f, fo, n, axis, fn)
+
+
 @pytest.mark.parametrize("axis", [0, 1])
 @pytest.mark.parametrize("fn", FNS)
 @pytest.mark.parametrize("f,fo,n", [(24, 40, 200), (96, 30, 1), (65, 129, 700)])
@@ -118,7 +131,7 @@ def test_gates_far_out_and_not_finite(fn, axis, n):
 
 
 @pytest.mark.parametrize("axis", [0, 1])
-@pytest.mark.parametrize("f,fo,n", [(40, 30, 1), (40, 30, 200), (200, 140, 500)])
+@pytest.mark.parametrize("f,fo,n", [(40, 30, 1), (40, 30, 200), (200, 140, 500), (70, 66, 66001)])
 def test_operands_that_are_not_finite_or_at_the_ends_of_the_range(f, fo, n, axis):
     """An infinity or NaN reaches what it is a term of, and nothing else; sums of the largest and smallest numbers are those of fp32."""
     x, w, b, gy = operands(f, fo, n, 17)
@@ -150,7 +163,7 @@ def test_operands_that_are_not_finite_or_at_the_ends_of_the_range(f, fo, n, axis
 
 
 @pytest.mark.parametrize("axis", [0, 1])
-@pytest.mark.parametrize("f,fo,n", [(33, 21, 1), (40, 24, 6), (33, 21, 150), (64, 64, 256), (130, 70, 301)])
+@pytest.mark.parametrize("f,fo,n", [(33, 21, 1), (40, 24, 6), (33, 21, 150), (64, 64, 256), (130, 70, 301), (130, 130, 33001), (1281, 1793, 130)])
 def test_arrays_on_no_boundary_and_nothing_beside_them(f, fo, n, axis):
     x, w, b, gy = operands(f, fo, n, 19)
     base = [dev(lay(x, axis)), dev(w), dev(b), dev(lay(gy, axis))]
