@@ -497,6 +497,74 @@ __global__ void __launch_bounds__(128 * WI, WI / 2) k_gated_fwd_split(GatedFwd G
         }
 }
 
+// ---------------------------------------------------------------- few positions
+// Every weight is read for a few products only, so that their bytes are all there is: a wave takes one feature, lanes quads of its two rows of weights, and N
+// positions at once.
+
+__device__ __forceinline__ float sum_lanes(float v)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
+    return v;
+}
+
+struct GatedFew { const float *x, *w, *bias; float *y, *kept; int fn, f, fo; long positions, feature, position; };   // strides of x
+
+template <int N, int AXIS>
+__global__ void __launch_bounds__(256) k_gated_few(GatedFew G)
+{
+    const int lane = threadIdx.x & 63, m = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (m >= G.fo) return;
+    const long n0 = blockIdx.y * N;
+    const float *const wu = G.w + (long)m * G.f, *const wv = wu + (long)G.fo * G.f;
+    float u[N], v[N];
+#pragma unroll
+    for (int p = 0; p < N; ++p) u[p] = v[p] = 0.f;
+#pragma unroll 4
+    for (int k = lane * 4; k < G.f; k += 256) {
+        const int most = G.f - k < 4 ? G.f - k : 4;
+        const floatx4 a = load4(wu + k, most), b = load4(wv + k, most);
+        floatx4 x[N];
+        if (AXIS)
+#pragma unroll
+            for (int p = 0; p < N; ++p) x[p] = load4(G.x + (n0 + p < G.positions ? n0 + p : G.positions - 1) * G.position + k, most);
+        else
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const float* const at = G.x + (k + (c < most ? c : 0)) * G.feature + n0;
+#pragma unroll
+                for (int q = 0; q < (N + 3) / 4; ++q) {
+                    const long left = G.positions - n0 - 4 * q;
+                    const floatx4 some = N < 4 ? floatx4{at[0], left > 1 ? at[N - 1] : 0.f, 0.f, 0.f} : load4(at + 4 * q, left < 0 ? 0 : left < 4 ? (int)left : 4);
+#pragma unroll
+                    for (int p = 4 * q; p < 4 * q + 4 && p < N; ++p) x[p][c] = some[p & 3];
+                }
+            }
+#pragma unroll
+        for (int p = 0; p < N; ++p)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                // weights behind the last one are zeros, x there a number of its own
+                u[p] = c < most ? fmaf(a[c], x[p][c], u[p]) : u[p];
+                v[p] = c < most ? fmaf(b[c], x[p][c], v[p]) : v[p];
+            }
+    }
+    float mine_u = 0.f, mine_v = 0.f;       // of position `lane`
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+        const float su = sum_lanes(u[p]), sv = sum_lanes(v[p]);
+        if (lane == p) { mine_u = su; mine_v = sv; }
+    }
+    const long n = n0 + lane;
+    if (lane >= N || n >= G.positions) return;
+    if (G.bias) { mine_u += G.bias[m]; mine_v += G.bias[G.fo + m]; }
+    G.y[AXIS ? n * G.fo + m : m * G.positions + n] = gate_fn(G.fn, mine_u).a * mine_v;
+    if (G.kept) {
+        G.kept[AXIS ? n * 2 * G.fo + m : m * G.positions + n] = mine_u;
+        G.kept[AXIS ? n * 2 * G.fo + G.fo + m : (G.fo + (long)m) * G.positions + n] = mine_v;
+    }
+}
+
 // A product, or with several shares of the sum over k (`span` of it each) partial ones, one behind the other.
 struct Product { Matrices M; Tiles T; float* c; long span; };
 template <class W, bool A_ALONG, bool B_ALONG>
@@ -691,7 +759,7 @@ typedef Waves<4, 1, 1, 2> Tall;         // 128 x 64
 // shares move their bytes at 4 TB/s and a launch takes 3 us.
 enum Kind { FP32, SPLIT, SPLIT_TURNED };
 struct Layout { Kind kind; Tiles T; int shares; long span; double us; };
-constexpr long kUnits = 256, kMostShares = 512, kLeastSpan = 8 * kDepth;
+constexpr long kFewPositions = 32, kUnits = 256, kMostShares = 512, kLeastSpan = 8 * kDepth;
 Tiles tiles_of(long i, long j, long ti, long tj)
 {
     const long ni = (i + ti - 1) / ti, nj = (j + tj - 1) / tj;
@@ -789,8 +857,24 @@ void launch_fwd_split(GatedFwd G, hipStream_t s)
     ZNN_LAUNCH("gated unit forward", s, (k_gated_fwd_split<kSplitWaves, AXIS>), dim3(G.T.count), dim3(128 * kSplitWaves), 0, G);
 }
 
+template <int N>
+void launch_few(const GatedFew& G, int axis, hipStream_t s)
+{
+    const dim3 grid((unsigned)((G.fo + 3) / 4), (unsigned)((G.positions + N - 1) / N));
+    if (axis) ZNN_LAUNCH("gated unit forward", s, (k_gated_few<N, 1>), grid, dim3(256), 0, G);
+    else ZNN_LAUNCH("gated unit forward", s, (k_gated_few<N, 0>), grid, dim3(256), 0, G);
+}
+
 int gated_fwd(const Shape& S, int fn, const float* x, const float* w, const float* b, float* y, float* kept, hipStream_t s)
 {
+    if (S.positions <= kFewPositions) {
+        const GatedFew G = {x, w, b, y, kept, fn, S.f, S.fo, S.positions, S.axis ? 1 : S.positions, S.axis ? S.f : 1};
+        if (S.positions == 1) launch_few<1>(G, S.axis, s);
+        else if (S.positions == 2) launch_few<2>(G, S.axis, s);
+        else if (S.positions <= 4) launch_few<4>(G, S.axis, s);
+        else launch_few<8>(G, S.axis, s);
+        return check_launch("gated unit forward");
+    }
     const Operand weights = {w, S.f};
     const long half = S.fo;
     const long I = S.axis ? S.positions : 2 * half, J = S.axis ? 2 * half : S.positions;

@@ -56,7 +56,8 @@ def check(f, fo, n, axis, fn, seed=3, bias=True, kept=True):
 
 
 # single features and positions, one position of many features, few positions, odd numbers around the extents of tiles, many positions of few maps
-SHAPES = [(1, 1, 1), (5, 3, 1), (1024, 500, 1), (1001, 77, 1), (130, 40, 2), (257, 33, 3), (64, 65, 4), (100, 31, 5), (515, 70, 8), (48, 64, 9), (33, 20, 17),
+SHAPES = [(1, 1, 1), (5, 3, 1), (1024, 500, 1), (1001, 77, 1), (130, 40, 2), (257, 33, 3), (64, 65, 4), (100, 31, 5), (515, 70, 8), (48, 64, 9), (33, 20, 17), (1023, 9, 7), (270, 66, 32),
+          (259, 5, 33),
           (70, 50, 31), (16, 16, 16), (31, 33, 63), (32, 32, 64), (33, 31, 65), (40, 80, 1728), (127, 129, 130), (128, 128, 128), (129, 127, 257),
           (3, 2, 4099), (2, 5, 10007), (120, 240, 1000), (17, 9, 20011), (300, 5, 777), (5, 300, 776), (260, 515, 300), (1, 64, 515), (64, 1, 515)]
 
