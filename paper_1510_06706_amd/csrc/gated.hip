@@ -1,4 +1,5 @@
 // Gated unit y = fn(W x + b) (V x + c) and its Jacobian.
+#include "gate.h"
 #include "split_parts.h"
 
 #include <algorithm>
@@ -11,23 +12,36 @@ struct Gated { float a, d; };       // fn(u) and its derivative
 
 constexpr float kLargestFloat = 3.402823466e38f;
 
-// fn by its number; every branch is uniform.  Values at infinity are limits: an infinite u times a factor of 0 would not be.
-__device__ __forceinline__ Gated gate_fn(int fn, float u)
+// Values at infinity are limits: an infinite u times a factor of 0 would not be.
+template <int FN>
+__device__ __forceinline__ Gated gate_fn(float u)
 {
-    if (fn == ZNN_GATE_RECTIFY) return Gated{u > 0.f ? u : 0.f, u > 0.f ? 1.f : 0.f};
-    if (fn == ZNN_GATE_TANH) {
-        const float t = tanhf(u), e = expf(-2.f * fabsf(u)), r = 1.f / (1.f + e);
-        return Gated{t, 4.f * e * r * r};           // 1 - t^2 without its cancellation
+    if (FN == ZNN_GATE_RECTIFY) return Gated{u > 0.f ? u : 0.f, u > 0.f ? 1.f : 0.f};
+    if (FN == ZNN_GATE_TANH) {
+        const Gate g = gate(2.f * u);
+        return Gated{tanhf(u), 4.f * g.f * g.k};            // 1 - tanh^2 without its cancellation
     }
-    const float finite = u > kLargestFloat ? kLargestFloat : u < -kLargestFloat ? -kLargestFloat : u;
-    if (fn == ZNN_GATE_GELU) {
+    const float finite = __builtin_amdgcn_fmed3f(u, -kLargestFloat, kLargestFloat);
+    if (FN == ZNN_GATE_GELU) {
         const float p = 0.5f * erfcf(-0.707106781f * finite);
         return Gated{u > 0.f ? u * p : finite * p, fmaf(finite, 0.398942280f * expf(-0.5f * finite * finite), p)};
     }
-    const float e = expf(-fabsf(u)), large = 1.f / (1.f + e), small = e * large;
-    const float s = u < 0.f ? small : large, t = u < 0.f ? large : small;
-    if (fn == ZNN_GATE_LOGISTIC) return Gated{s, s * t};
-    return Gated{u > 0.f ? u * s : finite * s, fmaf(finite, s * t, s)};
+    const Gate g = gate(u);
+    if (FN == ZNN_GATE_LOGISTIC) return Gated{g.f, g.f * g.k};
+    return Gated{u > 0.f ? u * g.f : finite * g.f, fmaf(finite, g.f * g.k, g.f)};
+}
+
+// f with the function's number as a constant
+template <class F>
+__device__ __forceinline__ void with_fn(int fn, F f)
+{
+    switch (fn) {
+        case ZNN_GATE_RECTIFY: return f(std::integral_constant<int, ZNN_GATE_RECTIFY>{});
+        case ZNN_GATE_LOGISTIC: return f(std::integral_constant<int, ZNN_GATE_LOGISTIC>{});
+        case ZNN_GATE_TANH: return f(std::integral_constant<int, ZNN_GATE_TANH>{});
+        case ZNN_GATE_SILU: return f(std::integral_constant<int, ZNN_GATE_SILU>{});
+        default: return f(std::integral_constant<int, ZNN_GATE_GELU>{});
+    }
 }
 
 // ---------------------------------------------------------------- products of matrices
@@ -427,6 +441,91 @@ __device__ __forceinline__ floatx4 load4(const float* p, int most)
 }
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) <= split::kLargest; }
 
+template <int C> __device__ __forceinline__ void store_some(float* p, const float (&v)[C], int most)
+{
+    typedef float vector __attribute__((ext_vector_type(C), aligned(4)));
+    if (most == C) {
+        vector q;
+#pragma unroll
+        for (int c = 0; c < C; ++c) q[c] = v[c];
+        *(vector*)p = q;
+    } else
+#pragma unroll
+        for (int c = 0; c < C - 1; ++c)
+            if (c < most) p[c] = v[c];
+}
+
+struct Element { long feature, position; };
+
+// What the split products leave of a gated unit: C neighbours of N groups, finished together.  place(g): feature and position of a group's first one;
+// dots(feature, position, u, v) takes both sums again; at(g): where the group lies in y and in kept (and how far apart its halves), and how many are there.
+struct Spot { long y, kept; int most; };
+template <int N, int C, int AXIS, class Place, class Again, class At>
+__device__ __forceinline__ void finish(int fn, const float* bias, int fo, long half, float* y, float* kept, float (&u)[N][C], float (&v)[N][C], Place place, Again dots, At at)
+{
+    // 0 times any number is 0 but for infinities and NaN
+    float test = 0.f;
+#pragma unroll
+    for (int g = 0; g < N; ++g) {
+        const int most = at(g).most;
+#pragma unroll
+        for (int c = 0; c < C; ++c) test = c < most ? fmaf(v[g][c], 0.f, fmaf(u[g][c], 0.f, test)) : test;
+        if (bias && most > 0) {
+            const float* const b = bias + place(g).feature;
+            if (AXIS) {
+                const floatx4 bu = load4(b, most), bv = load4(b + fo, most);
+#pragma unroll
+                for (int c = 0; c < C; ++c) { u[g][c] += bu[c & 3]; v[g][c] += bv[c & 3]; }
+            } else {
+                const float bu = *b, bv = b[fo];
+#pragma unroll
+                for (int c = 0; c < C; ++c) { u[g][c] += bu; v[g][c] += bv; }
+            }
+        }
+    }
+    float out[N][C];
+    with_fn(fn, [&](auto number) {
+#pragma unroll
+        for (int g = 0; g < N; ++g)
+#pragma unroll
+            for (int c = 0; c < C; ++c) out[g][c] = gate_fn<number.value>(u[g][c]).a * v[g][c];
+    });
+    unsigned bad_u = 0, bad_v = 0;
+#pragma unroll
+    for (int g = 0; g < N; ++g) {
+        const Spot s = at(g);
+        if (s.most <= 0) continue;
+        store_some(y + s.y, out[g], s.most);
+        if (kept) {
+            store_some(kept + s.kept, u[g], s.most);
+            store_some(kept + s.kept + half, v[g], s.most);
+        }
+        if (test != 0.f)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (c < s.most) {
+                    bad_u |= (unsigned)!finite(u[g][c]) << (C * g + c);
+                    bad_v |= (unsigned)!finite(v[g][c]) << (C * g + c);
+                }
+    }
+#pragma unroll 1
+    for (unsigned e = 0; e < N * C && (bad_u | bad_v) >> e; ++e) {
+        if (!((bad_u | bad_v) >> e & 1)) continue;
+        const Element p = place(e / C);
+        const Spot s = at(e / C);
+        const long c = e % C, feature = p.feature + (AXIS ? c : 0);
+        float a, b;
+        dots(feature, p.position + (AXIS ? 0 : c), a, b);
+        if (bias) {
+            a += bias[feature];
+            b += bias[fo + feature];
+        }
+        with_fn(fn, [&](auto number) { y[s.y + c] = gate_fn<number.value>(a).a * b; });
+        if (kept && (bad_u >> e & 1)) kept[s.kept + c] = a;
+        if (kept && (bad_v >> e & 1)) kept[s.kept + half + c] = b;
+    }
+}
+
 struct GatedFwd { Matrices M; Tiles T; int fn, fo; const float* bias; float *y, *kept; long ld; };      // rows of y are ld elements apart
 
 // AXIS 0: i = features (halves), j = positions.  AXIS 1: i = positions, j = features (halves); rows of `kept` hold both halves.
@@ -441,18 +540,30 @@ __global__ void __launch_bounds__(W::kThreads) k_gated_fwd(GatedFwd G)
     static_assert(AXIS ? W::AJ == 2 : W::AI == 2, "a wave holds both halves");
 #pragma unroll
     for (int n = 0; n < (AXIS ? W::AI : W::AJ); ++n) {
-        const floatx16 &us = AXIS ? acc[n][0] : acc[0][n], &vs = AXIS ? acc[n][1] : acc[1][n];
+        floatx16 &us = AXIS ? acc[n][0] : acc[0][n], &vs = AXIS ? acc[n][1] : acc[1][n];
+        const long first = i0 + (AXIS ? wi * (32 * W::AI) + 32 * n : wi * 32), j = j0 + (AXIS ? wj * 32 : wj * (32 * W::AJ) + 32 * n) + column;
+        if (j >= G.M.rows_j) continue;
+        if (G.bias)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const long i = first + result_row(r), m = AXIS ? j : i < G.M.rows_i ? i : G.M.rows_i - 1;
+                us[r] += G.bias[m];
+                vs[r] += G.bias[G.fo + m];
+            }
+        floatx16 y;
+        with_fn(G.fn, [&](auto fn) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) y[r] = gate_fn<fn.value>(us[r]).a * vs[r];
+        });
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const long i = i0 + (AXIS ? wi * (32 * W::AI) + 32 * n : wi * 32) + result_row(r);
-            const long j = j0 + (AXIS ? wj * 32 : wj * (32 * W::AJ) + 32 * n) + column, m = AXIS ? j : i;
-            if (i >= G.M.rows_i || j >= G.M.rows_j) continue;
-            const float u = us[r] + (G.bias ? G.bias[m] : 0.f), v = vs[r] + (G.bias ? G.bias[G.fo + m] : 0.f);
-            G.y[i * G.ld + j] = gate_fn(G.fn, u).a * v;
+            const long i = first + result_row(r);
+            if (i >= G.M.rows_i) continue;
+            G.y[i * G.ld + j] = y[r];
             if (G.kept) {
                 float* const at = G.kept + i * (AXIS ? 2 * G.ld : G.ld) + j;
-                at[0] = u;
-                at[AXIS ? G.ld : G.fo * G.ld] = v;
+                at[0] = us[r];
+                at[AXIS ? G.ld : G.fo * G.ld] = vs[r];
             }
         }
     }
@@ -468,33 +579,26 @@ __global__ void __launch_bounds__(128 * WI, WI / 2) k_gated_fwd_split(GatedFwd G
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     // halves are 32 of a wave's 64 rows or columns apart
 #pragma unroll
-    for (int x = 0; x < (AXIS ? 4 : 2); ++x)
+    for (int x = 0; x < (AXIS ? 4 : 2); ++x) {
+        constexpr int N = AXIS ? 2 : 4;
+        const long i = i0 + wave / 2 * (AXIS ? 64 : 32) + 16 * x + (lane & 15), j = j0 + wave % 2 * (AXIS ? 32 : 64) + (lane >> 4) * 4;
+        if (i >= G.M.rows_i) continue;
+        float u[N][4], v[N][4];
 #pragma unroll
-        for (int y = 0; y < (AXIS ? 2 : 4); ++y) {
-            const long i = i0 + wave / 2 * (AXIS ? 64 : 32) + 16 * x + (lane & 15), j = j0 + wave % 2 * (AXIS ? 32 : 64) + 16 * y + (lane >> 4) * 4;
-            if (i >= G.M.rows_i || j >= G.M.rows_j) continue;
-            const int most = G.M.rows_j - j < 4 ? (int)(G.M.rows_j - j) : 4;
-            floatx4 u = acc[x][y], v = AXIS ? acc[x][(y + 2) & 3] : acc[(x + 2) & 3][y], out;
+        for (int y = 0; y < N; ++y)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const long m = AXIS ? j + r : i, other = AXIS ? i : j + r;
-                if (r < most) {
-                    if (!finite(u[r])) u[r] = AXIS ? again<true, true>(G.M, other, m) : again<true, false>(G.M, m, other);
-                    if (!finite(v[r])) v[r] = AXIS ? again<true, true>(G.M, other, m + G.fo) : again<true, false>(G.M, m + G.fo, other);
-                    if (G.bias) {
-                        u[r] += G.bias[m];
-                        v[r] += G.bias[G.fo + m];
-                    }
-                }
-                out[r] = gate_fn(G.fn, u[r]).a * v[r];
-            }
-            store4(G.y + i * G.ld + j, out, most);
-            if (G.kept) {
-                float* const at = G.kept + i * (AXIS ? 2 * G.ld : G.ld) + j;
-                store4(at, u, most);
-                store4(at + (AXIS ? G.ld : G.fo * G.ld), v, most);
-            }
-        }
+            for (int r = 0; r < 4; ++r) { u[y][r] = acc[x][y][r]; v[y][r] = AXIS ? acc[x][(y + 2) & 3][r] : acc[(x + 2) & 3][y][r]; }
+        finish<N, 4, AXIS>(G.fn, G.bias, G.fo, AXIS ? G.ld : G.fo * G.ld, G.y, G.kept, u, v,
+            [&](int y) { return AXIS ? Element{j + 16 * y, i} : Element{i, j + 16 * y}; },
+            [&](long m, long n, float& a, float& b) {
+                a = AXIS ? again<true, true>(G.M, n, m) : again<true, false>(G.M, m, n);
+                b = AXIS ? again<true, true>(G.M, n, m + G.fo) : again<true, false>(G.M, m + G.fo, n);
+            },
+            [&](int y) {
+                const long left = G.M.rows_j - j - 16 * y;
+                return Spot{i * G.ld + j + 16 * y, i * (AXIS ? 2 * G.ld : G.ld) + j + 16 * y, left < 4 ? (int)(left < 0 ? 0 : left) : 4};
+            });
+    }
 }
 
 // ---------------------------------------------------------------- few positions
@@ -558,10 +662,160 @@ __global__ void __launch_bounds__(256) k_gated_few(GatedFew G)
     const long n = n0 + lane;
     if (lane >= N || n >= G.positions) return;
     if (G.bias) { mine_u += G.bias[m]; mine_v += G.bias[G.fo + m]; }
-    G.y[AXIS ? n * G.fo + m : m * G.positions + n] = gate_fn(G.fn, mine_u).a * mine_v;
+    with_fn(G.fn, [&](auto fn) { G.y[AXIS ? n * G.fo + m : m * G.positions + n] = gate_fn<fn.value>(mine_u).a * mine_v; });
     if (G.kept) {
         G.kept[AXIS ? n * 2 * G.fo + m : m * G.positions + n] = mine_u;
         G.kept[AXIS ? n * 2 * G.fo + G.fo + m : (G.fo + (long)m) * G.positions + n] = mine_v;
+    }
+}
+
+// ---------------------------------------------------------------- few features in, many positions
+// Up to 128 features of a position are taken apart once and stay in registers, 16 P positions a wave; weights, taken apart beforehand, pass through
+// shared memory, 16 features (both halves) at a time, and every wave multiplies all of them.  Nothing of x is read or taken apart twice, and a step's results are
+// finished while the other workgroup of the unit multiplies.
+
+// Weights in the order they are read: [16 features][half][step of 32 k][part][lane] of 16 bytes.  Every second step has its sign changed.
+constexpr int kNarrowSteps = 4;
+constexpr long narrow_bytes(int steps) { return 2L * steps * 3 * 1024; }      // of 16 features
+
+__global__ void __launch_bounds__(256) k_pack_gated(const float* w, int f, int fo, int steps, char* packed)
+{
+    const long t = blockIdx.x * 256L + threadIdx.x, groups = (fo + 15) / 16;
+    const int lane = (int)(t & 63);
+    const long piece = t >> 6, step = piece % steps, half = piece / steps % 2, group = piece / steps / 2;
+    if (group >= groups) return;
+    const long m = group * 16 + (lane & 15);
+    const float* const from = w + (half * fo + (m < fo ? m : fo - 1)) * f;
+    float v[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        const int k = (int)step * kDepth + (lane >> 4) * 8 + c;
+        v[c] = k < f ? from[k] * (step & 1 ? -split::kScale : split::kScale) : 0.f;
+    }
+#pragma unroll
+    for (int part = 0; part < 3; ++part) *(uintx4*)(packed + (piece * 3 + part) * 1024 + lane * 16) = split::take_part8(v);
+}
+
+struct GatedNarrow { const float *x, *w, *bias; const char* packed; float *y, *kept; int fn, f, fo, groups; long positions; };   // groups of 16 features a workgroup
+
+template <int STEPS, int P, int AXIS>
+__global__ void __launch_bounds__(256, 2) k_gated_narrow(GatedNarrow G)
+{
+    constexpr int kBytes = (int)narrow_bytes(STEPS);
+    __shared__ __attribute__((aligned(16))) char lds[2][kBytes];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, one = lane & 15, octet = lane >> 4;
+    const long n0 = ((long)blockIdx.x * 4 + wave) * (16 * P);
+    const int first = blockIdx.y * G.groups, all = (G.fo + 15) / 16, groups = all - first < G.groups ? all - first : G.groups;
+    const char* from = G.packed + (long)first * kBytes + threadIdx.x * 16;
+    auto fetch = [&](char* to) {
+#pragma unroll
+        for (int i = 0; i < kBytes / 4096; ++i)
+            __builtin_amdgcn_global_load_lds((split::global_ptr)(from + i * 4096), (split::lds_ptr)(to + i * 4096 + wave * 1024), 16, 0, 0);
+        if (kBytes % 4096 && wave * 1024 < kBytes % 4096)
+            __builtin_amdgcn_global_load_lds((split::global_ptr)(from + kBytes / 4096 * 4096), (split::lds_ptr)(to + kBytes / 4096 * 4096 + wave * 1024), 16, 0, 0);
+        from += kBytes;
+    };
+    fetch(lds[0]);
+    // images: a lane's P positions lie side by side, so that 16 lanes read and write whole lines; rows of features: 16 positions apart
+    bf16x8 x[P][STEPS][3];
+    const long mine = n0 + (AXIS ? one : P * one);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        const int k = s * kDepth + octet * 8;
+        float all[P][8];
+        if (!AXIS) {
+            typedef float vector __attribute__((ext_vector_type(P), aligned(4)));
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const float* const at = G.x + (k + c < G.f ? k + c : 0) * G.positions;
+                if (n0 + 16 * P <= G.positions) {
+                    const vector some = *(const vector*)(at + mine);
+#pragma unroll
+                    for (int p = 0; p < P; ++p) all[p][c] = some[p];
+                } else
+#pragma unroll
+                    for (int p = 0; p < P; ++p) all[p][c] = at[mine + p < G.positions ? mine + p : G.positions - 1];
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const long n = mine + 16 * p < G.positions ? mine + 16 * p : G.positions - 1;
+            float v[8];
+            if (AXIS) {
+                const float* const at = G.x + n * G.f + k;
+                if ((s + 1) * kDepth <= G.f) {
+                    *(floatx4*)v = *(const floatu4*)at;
+                    *(floatx4*)(v + 4) = *(const floatu4*)(at + 4);
+                } else
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) v[c] = k + c < G.f ? at[c] : 0.f;
+            } else
+#pragma unroll
+                for (int c = 0; c < 8; ++c) v[c] = k + c < G.f ? all[p][c] : 0.f;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] *= split::kScale;
+#pragma unroll
+            for (int part = 0; part < 3; ++part) x[p][s][part] = __builtin_bit_cast(bf16x8, split::take_part8(v));
+        }
+    }
+    __syncthreads();
+    for (int g = 0; g < groups; ++g) {
+        const char* const here = lds[g & 1] + lane * 16;
+        constexpr int of_w[6] = {0, 2, 1, 0, 1, 0}, of_x[6] = {2, 0, 1, 1, 0, 0};
+        if (g + 1 < groups) fetch(lds[~g & 1]);
+        floatx4 acc[2][P], t[2][2][P];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            bf16x8 w[2][3];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int part = 0; part < 3; ++part) w[h][part] = __builtin_bit_cast(bf16x8, *(const uintx4*)(here + ((h * STEPS + s) * 3 + part) * 1024));
+#pragma unroll
+            for (int q = 0; q < 6; ++q)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        const floatx4 c = q ? t[s & 1][h][p] : floatx4{0.f, 0.f, 0.f, 0.f};
+                        t[s & 1][h][p] = split::mfma(w[h][of_w[q]], x[p][s][of_x[q]], c);
+                    }
+            // a step's products are added once they are done, beside the next one's
+            if (s)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int p = 0; p < P; ++p) acc[h][p] = s == 1 ? t[0][h][p] : s & 1 ? acc[h][p] + t[0][h][p] : acc[h][p] - t[1][h][p];
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                if (STEPS == 1) acc[h][p] = t[0][h][p];
+                else if (STEPS & 1) acc[h][p] += t[0][h][p];
+                else acc[h][p] -= t[1][h][p];
+                acc[h][p] *= split::kUnscale;
+            }
+        __syncthreads();
+        // a lane has four features of its P positions
+        const long m = (first + g) * 16 + octet * 4, ld = AXIS ? G.fo : G.positions;
+        constexpr int N = AXIS ? P : 4, C = AXIS ? 4 : P;
+        float u[N][C], v[N][C];
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { u[AXIS ? p : r][AXIS ? r : p] = acc[0][p][r]; v[AXIS ? p : r][AXIS ? r : p] = acc[1][p][r]; }
+        finish<N, C, AXIS>(G.fn, G.bias, G.fo, AXIS ? ld : G.fo * ld, G.y, G.kept, u, v,
+            [&](int i) { return AXIS ? Element{m, mine + 16 * i} : Element{m + i, mine}; },
+            [&](long feature, long at, float& a, float& b) {
+                const float *const xs = AXIS ? G.x + at * G.f : G.x + at, *const ws = G.w + feature * G.f;
+                a = again(ws, 1, xs, AXIS ? 1 : G.positions, G.f);
+                b = again(ws + (long)G.fo * G.f, 1, xs, AXIS ? 1 : G.positions, G.f);
+            },
+            [&](int i) {
+                const long row = AXIS ? mine + 16 * i : m + i, column = AXIS ? m : mine, left = row < (AXIS ? G.positions : G.fo) ? ld - column : 0;
+                return Spot{row * ld + column, AXIS ? 2 * row * ld + column : row * ld + column, left < C ? (int)(left < 0 ? 0 : left) : C};
+            });
     }
 }
 
@@ -670,6 +924,18 @@ __global__ void __launch_bounds__(1024) k_sum_shares(long count, int shares, con
 
 struct Grads { int fn; long fo, positions, span; const float *gy, *kept; float *g, *sums; };      // sums [share][2 f'], or NULL
 
+__device__ __forceinline__ void gradients(int fn, const floatx4& u, const floatx4& v, const floatx4& gy, floatx4& du, floatx4& dv)
+{
+    with_fn(fn, [&](auto number) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const Gated a = gate_fn<number.value>(u[c]);
+            du[c] = gy[c] * v[c] * a.d;
+            dv[c] = gy[c] * a.a;
+        }
+    });
+}
+
 // images: a workgroup a share of one map, four neighbours a thread
 __global__ void __launch_bounds__(256) k_gated_grads_maps(Grads G)
 {
@@ -681,13 +947,10 @@ __global__ void __launch_bounds__(256) k_gated_grads_maps(Grads G)
         const int most = end - n < 4 ? (int)(end - n) : 4;
         const floatx4 u = load4(G.kept + at + n, most), v = load4(G.kept + at + other + n, most), gy = load4(G.gy + at + n, most);
         floatx4 du, dv;
+        gradients(G.fn, u, v, gy, du, dv);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const Gated a = gate_fn(G.fn, u[c]);
-            du[c] = gy[c] * v[c] * a.d;
-            dv[c] = gy[c] * a.a;
+        for (int c = 0; c < 4; ++c)
             if (c < most) { su += du[c]; sv += dv[c]; }
-        }
         store4(G.g + at + n, du, most);
         store4(G.g + at + other + n, dv, most);
     }
@@ -715,12 +978,7 @@ __global__ void __launch_bounds__(256) k_gated_grads_rows(Grads G)
             const long at = n * 2 * G.fo + m;
             const floatx4 u = load4(G.kept + at, most), v = load4(G.kept + at + G.fo, most), gy = load4(G.gy + n * G.fo + m, most);
             floatx4 du, dv;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const Gated a = gate_fn(G.fn, u[c]);
-                du[c] = gy[c] * v[c] * a.d;
-                dv[c] = gy[c] * a.a;
-            }
+            gradients(G.fn, u, v, gy, du, dv);
             store4(G.g + at, du, most);
             store4(G.g + at + G.fo, dv, most);
             su += du;
@@ -759,7 +1017,7 @@ typedef Waves<4, 1, 1, 2> Tall;         // 128 x 64
 // shares move their bytes at 4 TB/s and a launch takes 3 us.
 enum Kind { FP32, SPLIT, SPLIT_TURNED };
 struct Layout { Kind kind; Tiles T; int shares; long span; double us; };
-constexpr long kFewPositions = 32, kUnits = 256, kMostShares = 512, kLeastSpan = 8 * kDepth;
+constexpr long kFewPositions = 32, kNarrowLeast = 8192, kUnits = 256, kMostShares = 512, kLeastSpan = 8 * kDepth;
 Tiles tiles_of(long i, long j, long ti, long tj)
 {
     const long ni = (i + ti - 1) / ti, nj = (j + tj - 1) / tj;
@@ -830,6 +1088,11 @@ BiasShares bias_shares(const Shape& S)
     return BiasShares{(int)((S.positions + span - 1) / span), span};
 }
 
+// Few features in: taken apart in registers where enough positions keep the chip busy.
+constexpr int narrow_steps(int f) { return f <= kNarrowSteps * kDepth ? (f + kDepth - 1) / kDepth : 0; }
+bool takes_narrow(const Shape& S) { return narrow_steps(S.f) && S.positions >= kNarrowLeast; }
+size_t narrow_scratch(const Shape& S) { return align256((size_t)narrow_bytes(narrow_steps(S.f)) * ((S.fo + 15) / 16)); }
+
 struct Scratch { size_t g, sums, parts, all; };     // offsets
 Scratch backward_scratch(const Shape& S)
 {
@@ -841,7 +1104,7 @@ Scratch backward_scratch(const Shape& S)
     W.all = W.parts + std::max(gx, product_bytes(product_layout(both, S.f, n), both, S.f));
     return W;
 }
-size_t gated_workspace(const Shape& S, bool backward) { return backward ? backward_scratch(S).all : 0; }
+size_t gated_workspace(const Shape& S, bool backward) { return backward ? backward_scratch(S).all : takes_narrow(S) ? narrow_scratch(S) : 0; }
 
 template <class W, int AXIS>
 void launch_fwd(GatedFwd G, hipStream_t s)
@@ -865,8 +1128,32 @@ void launch_few(const GatedFew& G, int axis, hipStream_t s)
     else ZNN_LAUNCH("gated unit forward", s, (k_gated_few<N, 0>), grid, dim3(256), 0, G);
 }
 
-int gated_fwd(const Shape& S, int fn, const float* x, const float* w, const float* b, float* y, float* kept, hipStream_t s)
+template <int STEPS, int P>
+void launch_narrow(const GatedNarrow& G, int axis, hipStream_t s)
 {
+    const long blocks = (G.positions + 64 * P - 1) / (64 * P), all = (G.fo + 15) / 16;
+    GatedNarrow A = G;
+    // features over several workgroups where positions alone are too few for two of them on every unit
+    const long parts = std::min(all, std::max(1L, 2 * kUnits / blocks));
+    A.groups = (int)((all + parts - 1) / parts);
+    const dim3 grid((unsigned)blocks, (unsigned)((all + A.groups - 1) / A.groups));
+    if (axis) ZNN_LAUNCH("gated unit forward", s, (k_gated_narrow<STEPS, P, 1>), grid, dim3(256), 0, A);
+    else ZNN_LAUNCH("gated unit forward", s, (k_gated_narrow<STEPS, P, 0>), grid, dim3(256), 0, A);
+}
+
+int gated_fwd(const Shape& S, int fn, const float* x, const float* w, const float* b, float* y, float* kept, char* ws, hipStream_t s)
+{
+    if (takes_narrow(S)) {
+        const int steps = narrow_steps(S.f);
+        const long threads = (S.fo + 15) / 16 * 2L * steps * 64;
+        ZNN_LAUNCH("gated unit weights", s, k_pack_gated, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, w, S.f, S.fo, steps, ws);
+        const GatedNarrow G = {x, w, b, ws, y, kept, fn, S.f, S.fo, 0, S.positions};
+        if (steps == 1) launch_narrow<1, 4>(G, S.axis, s);
+        else if (steps == 2) launch_narrow<2, 4>(G, S.axis, s);
+        else if (steps == 3) launch_narrow<3, 2>(G, S.axis, s);
+        else launch_narrow<4, 2>(G, S.axis, s);
+        return check_launch("gated unit forward");
+    }
     if (S.positions <= kFewPositions) {
         const GatedFew G = {x, w, b, y, kept, fn, S.f, S.fo, S.positions, S.axis ? 1 : S.positions, S.axis ? S.f : 1};
         if (S.positions == 1) launch_few<1>(G, S.axis, s);
@@ -951,7 +1238,7 @@ int znn_gated_fwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t positions
     const Shape S = {fan_in, fan_out, axis, (long)positions};
     rc = check_gated_call(fn, S, false, ws, ws_bytes);
     if (rc != ZNN_OK) return rc;
-    return gated_fwd(S, fn, x, w, b, y, kept, (hipStream_t)stream);
+    return gated_fwd(S, fn, x, w, b, y, kept, (char*)ws, (hipStream_t)stream);
 }
 
 int znn_gated_bwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t positions, int32_t axis, const float* gy, const float* x,
