@@ -18,8 +18,15 @@ __device__ __forceinline__ Gated gate_fn(float u)
 {
     if (FN == ZNN_GATE_RECTIFY) return Gated{u > 0.f ? u : 0.f, u > 0.f ? 1.f : 0.f};
     if (FN == ZNN_GATE_TANH) {
+        // f - k of the logistic function at 2 u; below 0.35, where that would lose digits, the series of tanh, whose next term is below 2^-26 there
         const Gate g = gate(2.f * u);
-        return Gated{tanhf(u), 4.f * g.f * g.k};            // 1 - tanh^2 without its cancellation
+        const float s = u * u;
+        float p = fmaf(s, 21844.f / 6081075.f, -1382.f / 155925.f);
+        p = fmaf(s, p, 62.f / 2835.f);
+        p = fmaf(s, p, -17.f / 315.f);
+        p = fmaf(s, p, 2.f / 15.f);
+        p = fmaf(s, p, -1.f / 3.f);
+        return Gated{fabsf(u) < 0.35f ? fmaf(u * s, p, u) : g.f - g.k, 4.f * g.f * g.k};       // 1 - tanh^2 without its cancellation
     }
     const float finite = __builtin_amdgcn_fmed3f(u, -kLargestFloat, kLargestFloat);
     if (FN == ZNN_GATE_GELU) {
@@ -994,6 +1001,366 @@ __global__ void __launch_bounds__(256) k_gated_grads_rows(Grads G)
     }
 }
 
+// ---------------------------------------------------------------- backward with few features in
+// Over many positions the bytes count, and du and dv, which would be written and read twice, are made where they are used, once for each of the two products.
+
+struct GatedBack { const float *gy, *x, *w, *kept; int fn, f, fo; long positions; };
+
+// gy, u and v of four features from m on (of fo) and C positions
+template <int C> struct Raw { float gy[4][C], u[4][C], v[4][C]; };
+
+// Sums taken again where they came out as no numbers: of gx, and of gw.
+template <int AXIS> __device__ __forceinline__ void gradient_of(const GatedBack& G, long m, long n, float& du, float& dv)
+{
+    const long at = AXIS ? n * G.fo + m : m * G.positions + n, kept = AXIS ? n * 2 * G.fo + m : at, half = AXIS ? G.fo : G.fo * G.positions;
+    const float gy = G.gy[at], v = G.kept[kept + half], u = G.kept[kept];
+    with_fn(G.fn, [&](auto fn) {
+        const Gated a = gate_fn<fn.value>(u);
+        du = gy * v * a.d;
+        dv = gy * a.a;
+    });
+}
+template <int AXIS> __device__ __noinline__ float gx_again(const GatedBack& G, long i, long n)
+{
+    float s = 0.f, du, dv;
+    for (long m = 0; m < G.fo; ++m) {
+        gradient_of<AXIS>(G, m, n, du, dv);
+        s = fmaf(G.w[(G.fo + m) * G.f + i], dv, fmaf(G.w[m * G.f + i], du, s));
+    }
+    return s;
+}
+template <int AXIS> __device__ __noinline__ float gw_again(const GatedBack& G, long m, int half, long j, long first, long end)
+{
+    float s = 0.f, du, dv;
+    for (long n = first; n < end; ++n) {
+        gradient_of<AXIS>(G, m, n, du, dv);
+        s = fmaf(half ? dv : du, G.x[AXIS ? n * G.f + j : j * G.positions + n], s);
+    }
+    return s;
+}
+
+// Weights as the gradient of x reads them: [16 features][16 inputs][part][lane]; eight k are four features of W and the same of V.
+__global__ void __launch_bounds__(256) k_pack_gated_back(const float* w, int f, int fo, int tiles, char* packed)
+{
+    const long t = blockIdx.x * 256L + threadIdx.x, groups = (fo + 15) / 16;
+    const int lane = (int)(t & 63);
+    const long piece = t >> 6, tile = piece % tiles, group = piece / tiles;
+    if (group >= groups) return;
+    const long i = tile * 16 + (lane & 15), m = group * 16 + (lane >> 4) * 4;
+    float v[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        const long row = m + (c & 3);
+        v[c] = row < fo && i < f ? w[((c >> 2) * (long)fo + row) * f + i] * (group & 1 ? -split::kScale : split::kScale) : 0.f;
+    }
+#pragma unroll
+    for (int part = 0; part < 3; ++part) *(uintx4*)(packed + (piece * 3 + part) * 1024 + lane * 16) = split::take_part8(v);
+}
+
+// gx: a wave takes 32 positions and all TILES x 16 inputs, workgroups of four waves walk over the positions.  While 16 features are multiplied, the
+// next ones' gy, u and v are on their way into registers and their weights into shared memory.
+template <int TILES, int AXIS>
+__global__ void __launch_bounds__(256, 2) k_gated_gx(GatedBack G, const char* packed, float* gx)
+{
+    constexpr int P = 2, kBytes = TILES * 3 * 1024;
+    __shared__ __attribute__((aligned(16))) char lds[2][kBytes];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, one = lane & 15, octet = lane >> 4;
+    const int groups = (G.fo + 15) / 16;
+    const long tiles = (G.positions + 64 * P - 1) / (64 * P), half = AXIS ? G.fo : G.fo * G.positions;
+    auto fetch = [&](int group, char* to) {
+        const char* const from = packed + (long)group * kBytes;
+#pragma unroll
+        for (int i = 0; i < (kBytes + 4095) / 4096; ++i)
+            if (i * 4096 + wave * 1024 < kBytes)
+                __builtin_amdgcn_global_load_lds((split::global_ptr)(from + i * 4096 + threadIdx.x * 16), (split::lds_ptr)(to + i * 4096 + wave * 1024), 16, 0, 0);
+    };
+    Raw<P> raw;
+    auto load = [&](long tile, int group) {
+        const long n0 = (tile * 4 + wave) * (16 * P);
+        const int m = group * 16 + octet * 4;
+        if (AXIS) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const long want = n0 + one + 16 * p, n = want < G.positions ? want : G.positions - 1;
+                const float *const gy = G.gy + n * G.fo, *const u = G.kept + n * 2 * G.fo, *const v = u + G.fo;
+                if (group * 16 + 16 <= G.fo) {
+                    const floatx4 a = *(const floatu4*)(gy + m), b = *(const floatu4*)(u + m), c = *(const floatu4*)(v + m);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) { raw.gy[r][p] = a[r]; raw.u[r][p] = b[r]; raw.v[r][p] = c[r]; }
+                } else
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int row = m + r < G.fo ? m + r : G.fo - 1;
+                        raw.gy[r][p] = gy[row]; raw.u[r][p] = u[row]; raw.v[r][p] = v[row];
+                    }
+            }
+        } else
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const long at = (m + r < G.fo ? m + r : G.fo - 1) * G.positions, n = n0 + P * one;
+                if (n0 + 16 * P <= G.positions) {
+                    const floatu2 a = *(const floatu2*)(G.gy + at + n), b = *(const floatu2*)(G.kept + at + n), c = *(const floatu2*)(G.kept + half + at + n);
+#pragma unroll
+                    for (int p = 0; p < P; ++p) { raw.gy[r][p] = a[p]; raw.u[r][p] = b[p]; raw.v[r][p] = c[p]; }
+                } else
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        const long place = at + (n + p < G.positions ? n + p : G.positions - 1);
+                        raw.gy[r][p] = G.gy[place]; raw.u[r][p] = G.kept[place]; raw.v[r][p] = G.kept[half + place];
+                    }
+            }
+    };
+    const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+    fetch(0, lds[0]);
+    load(blockIdx.x, 0);
+    __syncthreads();
+    int buffer = 0;
+    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        floatx4 acc[TILES][P];
+#pragma unroll
+        for (int y = 0; y < TILES; ++y)
+#pragma unroll
+            for (int p = 0; p < P; ++p) acc[y][p] = zero;
+        for (int group = 0; group < groups; ++group) {
+            const char* const here = lds[buffer] + lane * 16;
+            buffer ^= 1;
+            const bool last = group + 1 == groups;
+            if (!last || tile + gridDim.x < tiles) fetch(last ? 0 : group + 1, lds[buffer]);
+            float g[P][8];
+            with_fn(G.fn, [&](auto fn) {
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const Gated a = gate_fn<fn.value>(raw.u[r][p]);
+                        const bool there = group * 16 + octet * 4 + r < G.fo;
+                        g[p][r] = there ? raw.gy[r][p] * raw.v[r][p] * a.d * split::kScale : 0.f;
+                        g[p][r + 4] = there ? raw.gy[r][p] * a.a * split::kScale : 0.f;
+                    }
+            });
+            if (!last || tile + gridDim.x < tiles) load(last ? tile + gridDim.x : tile, last ? 0 : group + 1);
+            bf16x8 x[P][3];
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int part = 0; part < 3; ++part) x[p][part] = __builtin_bit_cast(bf16x8, split::take_part8(g[p]));
+            const float sign = group & 1 ? -1.f : 1.f;
+            constexpr int of_w[6] = {0, 2, 1, 0, 1, 0}, of_x[6] = {2, 0, 1, 1, 0, 0};
+            floatx4 t[2][P];
+#pragma unroll
+            for (int y = 0; y < TILES; ++y) {
+                bf16x8 w[3];
+#pragma unroll
+                for (int part = 0; part < 3; ++part) w[part] = __builtin_bit_cast(bf16x8, *(const uintx4*)(here + (y * 3 + part) * 1024));
+#pragma unroll
+                for (int q = 0; q < 6; ++q)
+#pragma unroll
+                    for (int p = 0; p < P; ++p) t[y & 1][p] = split::mfma(w[of_w[q]], x[p][of_x[q]], q ? t[y & 1][p] : zero);
+                if (y)
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[y - 1][p][r] = fmaf(t[~y & 1][p][r], sign, acc[y - 1][p][r]);
+            }
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[TILES - 1][p][r] = fmaf(t[(TILES - 1) & 1][p][r], sign, acc[TILES - 1][p][r]);
+            __syncthreads();
+        }
+        // a lane has four inputs of its P positions
+        const long mine = (tile * 4 + wave) * (16 * P) + (AXIS ? one : P * one);
+        float test = 0.f;
+#pragma unroll
+        for (int y = 0; y < TILES; ++y) {
+            const long i = y * 16 + octet * 4;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                acc[y][p] *= split::kUnscale;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) test = fmaf(acc[y][p][r], 0.f, test);
+            }
+            if (AXIS) {
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const long n = mine + 16 * p;
+                    if (n < G.positions && i < G.f) store4(gx + n * G.f + i, acc[y][p], G.f - i < 4 ? (int)(G.f - i) : 4);
+                }
+            } else
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float out[2] = {acc[y][0][r], acc[y][1][r]};
+                    const long left = G.positions - mine;
+                    if (i + r < G.f && left > 0) store_some(gx + (i + r) * G.positions + mine, out, left < P ? (int)left : P);
+                }
+        }
+        if (test != 0.f) {
+            unsigned long bad = 0;
+#pragma unroll
+            for (int y = 0; y < TILES; ++y)
+#pragma unroll
+                for (int e = 0; e < 4 * P; ++e) bad |= (unsigned long)!finite(acc[y][e >> 2][e & 3]) << (y * 4 * P + e);
+#pragma unroll 1
+            for (int e = 0; e < 4 * P * TILES; ++e) {
+                const long i = e / (4 * P) * 16 + octet * 4 + (e & 3), n = mine + (e >> 2) % P * (AXIS ? 16 : 1);
+                if ((bad >> e & 1) && i < G.f && n < G.positions) gx[AXIS ? n * G.f + i : i * G.positions + n] = gx_again<AXIS>(G, i, n);
+            }
+        }
+    }
+}
+
+constexpr int kBackWaves = 4;       // of a workgroup: with three on a SIMD
+
+// gw and gb: a wave takes 16 features (both halves) and all TILES x 16 inputs, workgroups a share of the positions, 32 at a time; x is taken apart by all
+// waves for all of them.
+template <int TILES, int AXIS>
+__global__ void __launch_bounds__(64 * kBackWaves, 3) k_gated_gw(GatedBack G, long span, int waves, float* parts, float* sums)
+{
+    constexpr int kBytes = TILES * 3 * 1024;
+    __shared__ __attribute__((aligned(16))) char lds[2][kBytes];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, one = lane & 15, octet = lane >> 4, threads = waves * 64;
+    const long m = ((long)blockIdx.y * waves + wave) * 16 + one, half = AXIS ? G.fo : G.fo * G.positions;
+    const long row = m < G.fo ? m : G.fo - 1, first = blockIdx.x * span, end = first + span < G.positions ? first + span : G.positions;
+    const bool works = ((long)blockIdx.y * waves + wave) * 16 < G.fo;      // else it moves x alone; uniform
+    // octets of x that this thread moves, at most two
+    auto unit_row = [&](int u) { return AXIS ? u % (TILES * 16) : u / 4; };
+    auto unit_octet = [&](int u) { return AXIS ? u / (TILES * 16) : u % 4; };
+    float xs[2][8], gy[8], u[8], v[8];
+    auto load = [&](long n0) {
+        const bool whole = n0 + kDepth <= end;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int unit = threadIdx.x + c * threads;
+            if (unit >= TILES * 64) break;
+            const int j = unit_row(unit);
+            const long n = n0 + unit_octet(unit) * 8;
+            const float* const at = AXIS ? G.x + n * G.f + (j < G.f ? j : G.f - 1) : G.x + (j < G.f ? j : G.f - 1) * G.positions + n;
+            if (!AXIS && whole) {
+                *(floatx4*)xs[c] = *(const floatu4*)at;
+                *(floatx4*)(xs[c] + 4) = *(const floatu4*)(at + 4);
+            } else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) xs[c][e] = n + e < end ? at[AXIS ? e * (long)G.f : e] : 0.f;
+        }
+        if (!works) return;
+        const long n = n0 + octet * 8;
+        if (!AXIS && whole) {
+            const long at = row * G.positions + n;
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) {
+                *(floatx4*)(gy + e) = *(const floatu4*)(G.gy + at + e);
+                *(floatx4*)(u + e) = *(const floatu4*)(G.kept + at + e);
+                *(floatx4*)(v + e) = *(const floatu4*)(G.kept + half + at + e);
+            }
+        } else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const long k = n + e < end ? n + e : end - 1;
+                gy[e] = G.gy[AXIS ? k * G.fo + row : row * G.positions + k];
+                const long at = AXIS ? k * 2 * G.fo + row : row * G.positions + k;
+                u[e] = G.kept[at];
+                v[e] = G.kept[half + at];
+            }
+    };
+    auto store = [&](char* to) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int unit = threadIdx.x + c * threads;
+            if (unit >= TILES * 64) break;
+            const int j = unit_row(unit);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) xs[c][e] *= split::kScale;
+#pragma unroll
+            for (int part = 0; part < 3; ++part)
+                *(uintx4*)(to + ((j >> 4) * 3 + part) * 1024 + (unit_octet(unit) * 16 + (j & 15)) * 16) = split::take_part8(xs[c]);
+        }
+    };
+    const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+    floatx4 acc[TILES][2];
+#pragma unroll
+    for (int y = 0; y < TILES; ++y) acc[y][0] = acc[y][1] = zero;
+    float su = 0.f, sv = 0.f, sign = 1.f;
+    load(first);
+    store(lds[0]);
+    __syncthreads();
+    int buffer = 0;
+    for (long n0 = first; n0 < end; n0 += kDepth, sign = -sign) {
+        const char* const here = lds[buffer] + lane * 16;
+        buffer ^= 1;
+        float g[2][8];
+        if (works)
+            with_fn(G.fn, [&](auto fn) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const Gated a = gate_fn<fn.value>(u[e]);
+                    const bool there = n0 + octet * 8 + e < end;
+                    const float du = there ? gy[e] * v[e] * a.d : 0.f, dv = there ? gy[e] * a.a : 0.f;
+                    su += du;
+                    sv += dv;
+                    g[0][e] = du * (sign * split::kScale);
+                    g[1][e] = dv * (sign * split::kScale);
+                }
+            });
+        const bool more = n0 + kDepth < end;
+        if (more) load(n0 + kDepth);
+        if (works) {
+            bf16x8 a[2][3];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int part = 0; part < 3; ++part) a[h][part] = __builtin_bit_cast(bf16x8, split::take_part8(g[h]));
+            constexpr int of_a[6] = {0, 2, 1, 0, 1, 0}, of_x[6] = {2, 0, 1, 1, 0, 0};
+            floatx4 t[2][2];
+#pragma unroll
+            for (int y = 0; y < TILES; ++y) {
+                bf16x8 x[3];
+#pragma unroll
+                for (int part = 0; part < 3; ++part) x[part] = __builtin_bit_cast(bf16x8, *(const uintx4*)(here + (y * 3 + part) * 1024));
+#pragma unroll
+                for (int q = 0; q < 6; ++q)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) t[y & 1][h] = split::mfma(x[of_x[q]], a[h][of_a[q]], q ? t[y & 1][h] : zero);
+                if (y)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[y - 1][h][r] = fmaf(t[~y & 1][h][r], sign, acc[y - 1][h][r]);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[TILES - 1][h][r] = fmaf(t[(TILES - 1) & 1][h][r], sign, acc[TILES - 1][h][r]);
+        }
+        if (more) store(lds[buffer]);
+        __syncthreads();
+    }
+    if (!works) return;
+    su += __shfl_xor(su, 16);
+    sv += __shfl_xor(sv, 16);
+    su += __shfl_xor(su, 32);
+    sv += __shfl_xor(sv, 32);
+    if (sums && octet == 0 && m < G.fo) {
+        sums[blockIdx.x * 2L * G.fo + m] = su;
+        sums[blockIdx.x * 2L * G.fo + G.fo + m] = sv;
+    }
+    if (m >= G.fo) return;
+    // a lane has four inputs of its feature
+    float* const out = parts + blockIdx.x * 2L * G.fo * G.f + m * G.f;
+#pragma unroll
+    for (int y = 0; y < TILES; ++y)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const long j = y * 16 + octet * 4;
+            if (j >= G.f) continue;
+            const int most = G.f - j < 4 ? (int)(G.f - j) : 4;
+            floatx4 s = acc[y][h] * split::kUnscale;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (r < most && !finite(s[r])) s[r] = gw_again<AXIS>(G, m, h, j + r, first, end);
+            store4(out + h * (long)G.fo * G.f + j, s, most);
+        }
+}
+
 struct Shape { int f, fo, axis; long positions; };
 
 int check_gated(int32_t fan_in, int32_t fan_out, int64_t positions, int32_t axis)
@@ -1017,7 +1384,7 @@ typedef Waves<4, 1, 1, 2> Tall;         // 128 x 64
 // shares move their bytes at 4 TB/s and a launch takes 3 us.
 enum Kind { FP32, SPLIT, SPLIT_TURNED };
 struct Layout { Kind kind; Tiles T; int shares; long span; double us; };
-constexpr long kFewPositions = 32, kNarrowLeast = 8192, kUnits = 256, kMostShares = 512, kLeastSpan = 8 * kDepth;
+constexpr long kFewPositions = 32, kUnits = 256, kMostShares = 512, kLeastSpan = 8 * kDepth;
 Tiles tiles_of(long i, long j, long ti, long tj)
 {
     const long ni = (i + ti - 1) / ti, nj = (j + tj - 1) / tj;
@@ -1056,6 +1423,12 @@ Layout product_layout(long I, long J, long K)
 }
 size_t product_bytes(const Layout& L, long I, long J) { return L.shares > 1 ? align256(sizeof(float) * L.shares * I * J) : 0; }
 
+void sum_shares(long count, int shares, const float* parts, float* out, hipStream_t s)
+{
+    if (shares > 16) ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3((unsigned)std::min((count + 63) / 64, 1L << 20)), dim3(1024), 0, count, shares, parts, out);
+    else ZNN_LAUNCH("gated unit shares", s, k_sum_few, dim3((unsigned)std::min((count + 1023) / 1024, 1L << 20)), dim3(256), 0, count, shares, parts, out);
+}
+
 // c [I][J] = sum over k of A B; `parts` holds product_bytes
 template <bool A_ALONG, bool B_ALONG>
 int product(const Operand& A, const Operand& B, long I, long J, long K, float* c, float* parts, hipStream_t s)
@@ -1068,13 +1441,7 @@ int product(const Operand& A, const Operand& B, long I, long J, long K, float* c
         P.M = Matrices{B, A, J, I, 0, 0, K};
         ZNN_LAUNCH("gated unit product", s, (k_product_split<kSplitWaves, B_ALONG, A_ALONG, true>), grid, wide, 0, P);
     } else ZNN_LAUNCH("gated unit product", s, (k_product<Wide, A_ALONG, B_ALONG>), grid, dim3(Wide::kThreads), 0, P);
-    const long count = I * J;
-    if (L.shares > 16)
-        ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3((unsigned)std::min((count + 63) / 64, 1L << 20)), dim3(1024), 0, count, L.shares,
-                   (const float*)parts, c);
-    else if (L.shares > 1)
-        ZNN_LAUNCH("gated unit shares", s, k_sum_few, dim3((unsigned)std::min((count + 1023) / 1024, 1L << 20)), dim3(256), 0, count, L.shares,
-                   (const float*)parts, c);
+    if (L.shares > 1) sum_shares(I * J, L.shares, parts, c, s);
     return check_launch("gated unit product");
 }
 
@@ -1088,9 +1455,37 @@ BiasShares bias_shares(const Shape& S)
     return BiasShares{(int)((S.positions + span - 1) / span), span};
 }
 
+// Backward with du and dv made where they are used.  us, so and by products of all of du and dv: maps 10 -> 20 at 4000 positions 35.4 and 33.9, at 12 000
+// 31.8 and 36.7, at 300 000 88.6 and 124; 40 -> 80 at 12 000 49.2 and 54.1, at 300 000 263 and 292; 64 -> 128 at 36 000 83.5 and 82.3, at 100 000 137
+// and 165; rows of 40 -> 80 at 12 000 49.2 and 70.4, at 300 000 265 and 406.  128 inputs take registers that more waves would need: 859 and 804 at 300 000.
+bool takes_narrow_back(const Shape& S)
+{
+    return S.f <= 64 && S.positions >= 8192 && (S.axis || S.f <= 48 || S.positions >= 65536);
+}
 // Few features in: taken apart in registers where enough positions keep the chip busy.
 constexpr int narrow_steps(int f) { return f <= kNarrowSteps * kDepth ? (f + kDepth - 1) / kDepth : 0; }
-bool takes_narrow(const Shape& S) { return narrow_steps(S.f) && S.positions >= kNarrowLeast; }
+bool takes_narrow(const Shape& S)
+{
+    // us, in registers and by tiles: maps 40 -> 80 at 12 000 positions 17.1 and 13.1 (weights are taken apart by a launch of their own), at 36 000 20.5 and 23.5, at
+    // 100 000 33.1 and 57.8; 100 -> 200 at 12 000 22.4 and 26.1; rows of 128 -> 256 at 100 000 156 and 142
+    return narrow_steps(S.f) && S.positions >= 8192 && S.positions * S.f >= 1L << 20 && (!S.axis || S.f < 128);
+}
+// Backward: shares of the positions, workgroups of up to kBackWaves waves of 16 features each
+struct NarrowBack { int tiles, waves, shares; unsigned groups; long span; };
+NarrowBack narrow_back(const Shape& S)
+{
+    NarrowBack N = {};
+    if (!takes_narrow_back(S)) return N;
+    const int tiles = (S.f + 15) / 16, features = (S.fo + 15) / 16;
+    N.tiles = tiles;
+    N.groups = (unsigned)((features + kBackWaves - 1) / kBackWaves);
+    N.waves = std::max((int)((features + N.groups - 1) / N.groups), (N.tiles + 1) / 2);
+    const long wanted = std::max(1L, 8 * kUnits / ((long)N.groups * N.waves)), steps = (S.positions + kDepth - 1) / kDepth;
+    const long each = std::max(8L, (steps + wanted - 1) / wanted);
+    N.span = each * kDepth;
+    N.shares = (int)((S.positions + N.span - 1) / N.span);
+    return N;
+}
 size_t narrow_scratch(const Shape& S) { return align256((size_t)narrow_bytes(narrow_steps(S.f)) * ((S.fo + 15) / 16)); }
 
 struct Scratch { size_t g, sums, parts, all; };     // offsets
@@ -1098,6 +1493,12 @@ Scratch backward_scratch(const Shape& S)
 {
     const long both = 2L * S.fo, n = S.positions;
     Scratch W = {};
+    if (const NarrowBack N = narrow_back(S); N.tiles) {
+        W.sums = align256(sizeof(float) * both * S.f * N.shares);                               // behind the shares of gw
+        W.parts = W.sums + align256(sizeof(float) * both * N.shares);                           // packed weights
+        W.all = W.parts + align256((size_t)N.tiles * 3 * 1024 * ((S.fo + 15) / 16));
+        return W;
+    }
     W.sums = align256(sizeof(float) * both * n);
     W.parts = W.sums + align256(sizeof(float) * both * bias_shares(S).count);
     const size_t gx = S.axis ? product_bytes(product_layout(n, S.f, both), n, S.f) : product_bytes(product_layout(S.f, n, both), S.f, n);
@@ -1179,18 +1580,53 @@ int gated_fwd(const Shape& S, int fn, const float* x, const float* w, const floa
     return check_launch("gated unit forward");
 }
 
+template <int TILES, int AXIS>
+void launch_narrow_back(const GatedBack& G, const NarrowBack& N, float* gx, const char* packed, float* parts, float* sums, hipStream_t s)
+{
+    if (gx) {
+        const long tiles = (G.positions + 127) / 128;
+        ZNN_LAUNCH("gated unit backward", s, (k_gated_gx<TILES, AXIS>), dim3((unsigned)std::min(tiles, 2 * kUnits)), dim3(256), 0, G, packed, gx);
+    }
+    ZNN_LAUNCH("gated unit weights", s, (k_gated_gw<TILES, AXIS>), dim3((unsigned)N.shares, N.groups), dim3(64 * N.waves), 0, G, N.span, N.waves, parts, sums);
+}
+
+template <int AXIS>
+int gated_bwd_narrow(const GatedBack& G, const NarrowBack& N, const Scratch& W, float* gx, float* gw, float* gb, char* ws, hipStream_t s)
+{
+    char* const packed = ws + W.parts;
+    float *const parts = N.shares > 1 ? (float*)ws : gw, *const sums = gb ? N.shares > 1 ? (float*)(ws + W.sums) : gb : nullptr;
+    if (gx) {
+        const long threads = (G.fo + 15) / 16 * (long)N.tiles * 64;
+        ZNN_LAUNCH("gated unit packing", s, k_pack_gated_back, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, G.w, G.f, G.fo, N.tiles, packed);
+    }
+    switch (N.tiles) {
+        case 1: launch_narrow_back<1, AXIS>(G, N, gx, packed, parts, sums, s); break;
+        case 2: launch_narrow_back<2, AXIS>(G, N, gx, packed, parts, sums, s); break;
+        case 3: launch_narrow_back<3, AXIS>(G, N, gx, packed, parts, sums, s); break;
+        default: launch_narrow_back<4, AXIS>(G, N, gx, packed, parts, sums, s);
+    }
+    if (N.shares > 1) {
+        sum_shares(2L * G.fo * G.f, N.shares, parts, gw, s);
+        if (gb) sum_shares(2L * G.fo, N.shares, sums, gb, s);
+    }
+    return check_launch("gated unit backward");
+}
+
 int gated_bwd(const Shape& S, int fn, const float* gy, const float* x, const float* w, const float* kept, float* gx, float* gw, float* gb,
               char* ws, hipStream_t s)
 {
     const Scratch W = backward_scratch(S);
+    if (const NarrowBack N = narrow_back(S); N.tiles) {
+        const GatedBack G = {gy, x, w, kept, fn, S.f, S.fo, S.positions};
+        return S.axis ? gated_bwd_narrow<1>(G, N, W, gx, gw, gb, ws, s) : gated_bwd_narrow<0>(G, N, W, gx, gw, gb, ws, s);
+    }
     const BiasShares bias = bias_shares(S);
     float *const g = (float*)ws, *const sums = (float*)(ws + W.sums), *const parts = (float*)(ws + W.parts);
     const long both = 2L * S.fo, n = S.positions;
     const Grads G = {fn, S.fo, n, bias.span, gy, kept, g, gb ? (bias.count > 1 ? sums : gb) : nullptr};
     if (S.axis) ZNN_LAUNCH("gated unit gradients", s, k_gated_grads_rows, dim3((unsigned)((S.fo + 255) / 256), (unsigned)bias.count), dim3(256), 0, G);
     else ZNN_LAUNCH("gated unit gradients", s, k_gated_grads_maps, dim3((unsigned)S.fo, (unsigned)bias.count), dim3(256), 0, G);
-    if (gb && bias.count > 1)
-        ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3((unsigned)((both + 63) / 64)), dim3(1024), 0, both, bias.count, (const float*)sums, gb);
+    if (gb && bias.count > 1) sum_shares(both, bias.count, sums, gb, s);
     int rc = check_launch("gated unit gradients");
     if (rc != ZNN_OK) return rc;
     if (S.axis) {

@@ -72,7 +72,7 @@ def test_shapes(f, fo, n, axis):
 
 # enough tiles for the bf16 matrix cores, in one or all of the products: one step of k and less, whole steps, steps cut short, ragged tiles
 LARGE = [(130, 70, 40001), (20, 200, 40000), (32, 64, 70016), (33, 130, 33000), (64, 65, 66000), (95, 96, 45001), (1500, 2800, 300), (1024, 2816, 64),
-         (300, 3001, 1025), (1281, 1792, 1100)]
+         (300, 3001, 1025), (1281, 1792, 1100), (127, 33, 9001), (128, 260, 9003), (50, 17, 30001), (81, 16, 13009), (16, 15, 66001), (3, 2, 350003)]
 
 
 @pytest.mark.parametrize("axis", [0, 1])
@@ -132,7 +132,7 @@ def test_gates_far_out_and_not_finite(fn, axis, n):
 
 
 @pytest.mark.parametrize("axis", [0, 1])
-@pytest.mark.parametrize("f,fo,n", [(40, 30, 1), (40, 30, 200), (200, 140, 500), (70, 66, 66001)])
+@pytest.mark.parametrize("f,fo,n", [(40, 30, 1), (40, 30, 200), (200, 140, 500), (70, 66, 66001), (140, 66, 66001)])
 def test_operands_that_are_not_finite_or_at_the_ends_of_the_range(f, fo, n, axis):
     """An infinity or NaN reaches what it is a term of, and nothing else; sums of the largest and smallest numbers are those of fp32."""
     x, w, b, gy = operands(f, fo, n, 17)
@@ -164,7 +164,46 @@ def test_operands_that_are_not_finite_or_at_the_ends_of_the_range(f, fo, n, axis
 
 
 @pytest.mark.parametrize("axis", [0, 1])
-@pytest.mark.parametrize("f,fo,n", [(33, 21, 1), (40, 24, 6), (33, 21, 150), (64, 64, 256), (130, 70, 301), (130, 130, 33001), (1281, 1793, 130)])
+@pytest.mark.parametrize("f,fo,n", [(33, 21, 5), (40, 30, 200), (70, 66, 33001), (140, 66, 66001), (1281, 1793, 130)])
+def test_gradients_of_operands_that_are_not_finite(f, fo, n, axis):
+    """An infinity or NaN in one operand reaches the gradients whose sums it is a term of, and no others."""
+    x, w, b, gy = operands(f, fo, n, 21)
+    _, both, _, _ = gated.gated_fwd(x, w, b, "silu")
+    both = both.astype(np.float32)
+
+    def grads(x, w, both, gy):
+        got = znn.gated_bwd(dev(lay(gy, axis)), dev(lay(x, axis)), dev(w), dev(lay(both, axis)), "silu", axis)
+        return lay(host(got[0]), axis), host(got[1]), host(got[2])
+
+    clean = grads(x, w, both, gy)
+    p, m = n // 2, fo // 2
+    for bad in (np.inf, np.nan, 3e38):
+        g2 = gy.copy()
+        g2[m, p] = bad
+        gx, gw, gb = grads(x, w, both, g2)
+        others = np.arange(n) != p
+        assert np.array_equal(gx[:, others], clean[0][:, others])
+        rows = np.ones(2 * fo, bool)
+        rows[[m, fo + m]] = False
+        assert np.array_equal(gw[rows], clean[1][rows]) and np.array_equal(gb[rows], clean[2][rows])
+        with np.errstate(invalid="ignore", over="ignore"):
+            wants, _ = gated.gated_bwd(g2, x, w, both, "silu")
+            for got, want in zip((gx[:, p], gw[[m, fo + m]], gb[[m, fo + m]]), (wants[0][:, p], wants[1][[m, fo + m]], wants[2][[m, fo + m]])):
+                want = want.astype(np.float32)
+                assert np.array_equal(np.isnan(got), np.isnan(want))
+                same = np.isinf(want)
+                assert np.array_equal(got[same], want[same])
+        x2 = x.copy()
+        x2[f // 3, p] = bad
+        gx, gw, gb = grads(x2, w, both, gy)
+        columns = np.arange(f) != f // 3
+        assert np.array_equal(gx, clean[0]) and np.array_equal(gb, clean[2]) and np.array_equal(gw[:, columns], clean[1][:, columns])
+        if not np.isfinite(bad):
+            assert not np.isfinite(gw[:, f // 3]).any()
+
+
+@pytest.mark.parametrize("axis", [0, 1])
+@pytest.mark.parametrize("f,fo,n", [(33, 21, 1), (40, 24, 6), (33, 21, 150), (64, 64, 256), (130, 70, 301), (130, 130, 33001), (1281, 1793, 130), (45, 70, 33001), (100, 20, 11003)])
 def test_arrays_on_no_boundary_and_nothing_beside_them(f, fo, n, axis):
     x, w, b, gy = operands(f, fo, n, 19)
     base = [dev(lay(x, axis)), dev(w), dev(b), dev(lay(gy, axis))]
