@@ -54,8 +54,8 @@ __device__ __forceinline__ void with_fn(int fn, F f)
 // ---------------------------------------------------------------- products of matrices
 // C[i][j] = sum over k of A[i][k] B[j][k] on the fp32 matrix cores, rows j of C contiguous.  A workgroup of WI x WJ waves makes a tile of
 // 32 WI AI x 32 WJ AJ results, a wave AI x AJ of 32 x 32.  Both operands go through shared memory as [row][kDepth] in quads along k, whatever way they lie
-// in memory; while one step is multiplied the next one's loads are in flight.  Quads of a row change places by the row's number: 16 lanes that
-// read a quad of 16 rows, and 8 that write one of rows four apart, touch different banks.
+// in memory; while one step is multiplied the next one's loads are in flight.  Quads of a row change places by the row's number: eight lanes, a
+// clock's worth, that read a quad of eight rows or write one of rows four apart touch different banks.
 // v_mfma_f32_32x32x2_f32 takes k = lane / 32; which k that stands for is free as long as both operands agree: lanes below 32 take the first
 // quad of eight k, the others the second one, so that a quad feeds four instructions.
 
@@ -71,7 +71,7 @@ constexpr int kDepth = 32;
 // Element (row, k) of an operand at p + row * ld + k (ALONG_K) or at p + k * ld + row.
 struct Operand { const float* p; long ld; };
 
-__device__ __forceinline__ int quad_place(int row, int quad) { return row * kDepth + ((quad ^ (row >> 1 & 7) ^ (row >> 4 & 1)) << 2); }
+__device__ __forceinline__ int quad_place(int row, int quad) { return row * kDepth + ((quad ^ (row & 7) ^ (row >> 3 & 3)) << 2); }
 
 // A tile's row in the operand.  Halves: 32 rows of the first half lie beside the same rows of the second one, `half` rows on.
 template <bool HALVES>
@@ -222,8 +222,8 @@ __device__ __forceinline__ TilePlace tile_place(const Tiles& T, unsigned number)
 
 constexpr int kSplitColumns = 128, kSplitWaves = 4;     // rows of waves
 
-// Octet of eight k of a row: 16 lanes read one octet of 16 rows, and take all banks.
-__device__ __forceinline__ int octet_place(int row, int octet) { return row * 64 + ((octet ^ (row >> 2 & 3)) << 4); }
+// Octet of eight k of a row: eight lanes, a clock's worth, read one octet of eight rows, and take different banks.
+__device__ __forceinline__ int octet_place(int row, int octet) { return row * 64 + ((octet ^ (row >> 1 & 3)) << 4); }
 
 // The octets of an operand that a thread moves: one row each (ALONG_K), or one or two neighbouring rows of one octet.
 template <int R, int THREADS, bool ALONG_K, bool HALVES>
@@ -476,7 +476,7 @@ __device__ __forceinline__ void finish(int fn, const float* bias, int fo, long h
     for (int g = 0; g < N; ++g) {
         const int most = at(g).most;
 #pragma unroll
-        for (int c = 0; c < C; ++c) test = c < most ? fmaf(v[g][c], 0.f, fmaf(u[g][c], 0.f, test)) : test;
+        for (int c = 0; c < C; ++c) test = fmaf(v[g][c], 0.f, fmaf(u[g][c], 0.f, test));
         if (bias && most > 0) {
             const float* const b = bias + place(g).feature;
             if (AXIS) {
@@ -880,49 +880,48 @@ __global__ void __launch_bounds__(128 * WI, WI / 2) k_product_split(Product G)
         }
 }
 
-// The sum of a few shares, in their order, four elements a thread.
-__global__ void __launch_bounds__(256) k_sum_few(long count, int shares, const float* parts, float* out)
-{
-    const long quads = count / 4;
-    for (long q = blockIdx.x * 256L + threadIdx.x; q < quads; q += gridDim.x * 256L) {
-        floatx4 s = *(const floatu4*)(parts + 4 * q);
-        for (int n = 1; n < shares; ++n) s += *(const floatu4*)(parts + n * count + 4 * q);
-        *(floatu4*)(out + 4 * q) = s;
-    }
-    if (blockIdx.x == 0 && threadIdx.x < count - 4 * quads) {
-        const long e = 4 * quads + threadIdx.x;
-        float s = parts[e];
-        for (int n = 1; n < shares; ++n) s += parts[n * count + e];
-        out[e] = s;
-    }
-}
+// Sums of shares that several launches have left, in one: a workgroup takes `each` elements of one of them.  A few shares are added in their order, four
+// neighbours a thread; of many, every sixteenth by one wave, and then these in their order.
+struct SharedSum { const float* parts; float* out; long count; int shares; unsigned first; };     // first workgroup
+struct SharedSums { SharedSum of[3]; int n; };
+constexpr int kFewShares = 16;
+constexpr long elements_of(int shares) { return shares > kFewShares ? 64 : 4096; }
 
-// The sum of shares: every sixteenth by one wave, then these in their order.
-__global__ void __launch_bounds__(1024) k_sum_shares(long count, int shares, const float* parts, float* out)
+__global__ void __launch_bounds__(1024) k_sum_shares(SharedSums A)
 {
     __shared__ float part[16][64];
+    int which = 0;
+    while (which + 1 < A.n && blockIdx.x >= A.of[which + 1].first) ++which;       // uniform
+    const SharedSum S = A.of[which];
+    const long block = blockIdx.x - S.first;
+    if (S.shares <= kFewShares) {
+        const long e = block * 4096 + threadIdx.x * 4;
+        if (e >= S.count) return;
+        const int most = S.count - e < 4 ? (int)(S.count - e) : 4;
+        floatx4 s = load4(S.parts + e, most);
+        for (int n = 1; n < S.shares; ++n) s += load4(S.parts + n * S.count + e, most);
+        store4(S.out + e, s, most);
+        return;
+    }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (long first = blockIdx.x * 64L; first < count; first += gridDim.x * 64L) {
-        const long e = first + lane;
-        float s = 0.f;
-        if (e < count) {
-            int n = wave;
-            for (; n + 48 < shares; n += 64) {
-                float v[4];
+    const long e = block * 64 + lane;
+    float s = 0.f;
+    if (e < S.count) {
+        int n = wave;
+        for (; n + 48 < S.shares; n += 64) {
+            float v[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] = parts[(n + 16 * c) * count + e];
-                s += (v[0] + v[1]) + (v[2] + v[3]);
-            }
-            for (; n < shares; n += 16) s += parts[n * count + e];
+            for (int c = 0; c < 4; ++c) v[c] = S.parts[(n + 16 * c) * S.count + e];
+            s += (v[0] + v[1]) + (v[2] + v[3]);
         }
-        part[wave][lane] = s;
-        __syncthreads();
-        if (wave == 0 && e < count) {
+        for (; n < S.shares; n += 16) s += S.parts[n * S.count + e];
+    }
+    part[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && e < S.count) {
 #pragma unroll
-            for (int w = 1; w < 16; ++w) s += part[w][lane];
-            out[e] = s;
-        }
-        __syncthreads();
+        for (int w = 1; w < 16; ++w) s += part[w][lane];
+        S.out[e] = s;
     }
 }
 
@@ -1039,10 +1038,11 @@ template <int AXIS> __device__ __noinline__ float gw_again(const GatedBack& G, l
     return s;
 }
 
-// Weights as the gradient of x reads them: [16 features][16 inputs][part][lane]; eight k are four features of W and the same of V.
-__global__ void __launch_bounds__(256) k_pack_gated_back(const float* w, int f, int fo, int tiles, char* packed)
+// Weights as the gradient of x reads them: [16 features][16 inputs][part][lane]; eight k are four features of W and the same of V.  Thread t of those of
+// one lane each.
+__device__ __forceinline__ void pack_back(const float* w, int f, int fo, int tiles, long t, char* packed)
 {
-    const long t = blockIdx.x * 256L + threadIdx.x, groups = (fo + 15) / 16;
+    const long groups = (fo + 15) / 16;
     const int lane = (int)(t & 63);
     const long piece = t >> 6, tile = piece % tiles, group = piece / tiles;
     if (group >= groups) return;
@@ -1212,10 +1212,14 @@ __global__ void __launch_bounds__(256, 2) k_gated_gx(GatedBack G, const char* pa
 constexpr int kBackWaves = 4;       // of a workgroup: with three on a SIMD
 
 // gw and gb: a wave takes 16 features (both halves) and all TILES x 16 inputs, workgroups a share of the positions, 32 at a time; x is taken apart by all
-// waves for all of them.
+// waves for all of them.  Workgroups behind the shares pack the weights for k_gated_gx, which comes next.
 template <int TILES, int AXIS>
-__global__ void __launch_bounds__(64 * kBackWaves, 3) k_gated_gw(GatedBack G, long span, int waves, float* parts, float* sums)
+__global__ void __launch_bounds__(64 * kBackWaves, 3) k_gated_gw(GatedBack G, long span, int shares, int waves, float* parts, float* sums, char* packed)
 {
+    if ((int)blockIdx.x >= shares) {
+        pack_back(G.w, G.f, G.fo, TILES, ((long)(blockIdx.x - shares) * gridDim.y + blockIdx.y) * waves * 64 + threadIdx.x, packed);
+        return;
+    }
     constexpr int kBytes = TILES * 3 * 1024;
     __shared__ __attribute__((aligned(16))) char lds[2][kBytes];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, one = lane & 15, octet = lane >> 4, threads = waves * 64;
@@ -1423,15 +1427,26 @@ Layout product_layout(long I, long J, long K)
 }
 size_t product_bytes(const Layout& L, long I, long J) { return L.shares > 1 ? align256(sizeof(float) * L.shares * I * J) : 0; }
 
-void sum_shares(long count, int shares, const float* parts, float* out, hipStream_t s)
+void add_shares(SharedSums& A, const float* parts, float* out, long count, int shares)
 {
-    if (shares > 16) ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3((unsigned)std::min((count + 63) / 64, 1L << 20)), dim3(1024), 0, count, shares, parts, out);
-    else ZNN_LAUNCH("gated unit shares", s, k_sum_few, dim3((unsigned)std::min((count + 1023) / 1024, 1L << 20)), dim3(256), 0, count, shares, parts, out);
+    if (shares <= 1) return;
+    unsigned first = 0;
+    if (A.n) {
+        const SharedSum& last = A.of[A.n - 1];
+        first = last.first + (unsigned)((last.count + elements_of(last.shares) - 1) / elements_of(last.shares));
+    }
+    A.of[A.n++] = SharedSum{parts, out, count, shares, first};
 }
-
-// c [I][J] = sum over k of A B; `parts` holds product_bytes
+void sum_shares(const SharedSums& A, hipStream_t s)
+{
+    if (!A.n) return;
+    const SharedSum& last = A.of[A.n - 1];
+    const unsigned blocks = last.first + (unsigned)((last.count + elements_of(last.shares) - 1) / elements_of(last.shares));
+    ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3(blocks), dim3(1024), 0, A);
+}
+// c [I][J] = sum over k of A B, once `sums` are taken; `parts` holds product_bytes
 template <bool A_ALONG, bool B_ALONG>
-int product(const Operand& A, const Operand& B, long I, long J, long K, float* c, float* parts, hipStream_t s)
+int product(const Operand& A, const Operand& B, long I, long J, long K, float* c, float* parts, SharedSums& sums, hipStream_t s)
 {
     const Layout L = product_layout(I, J, K);
     Product P = {{A, B, I, J, 0, 0, K}, L.T, L.shares > 1 ? parts : c, L.span};
@@ -1441,7 +1456,7 @@ int product(const Operand& A, const Operand& B, long I, long J, long K, float* c
         P.M = Matrices{B, A, J, I, 0, 0, K};
         ZNN_LAUNCH("gated unit product", s, (k_product_split<kSplitWaves, B_ALONG, A_ALONG, true>), grid, wide, 0, P);
     } else ZNN_LAUNCH("gated unit product", s, (k_product<Wide, A_ALONG, B_ALONG>), grid, dim3(Wide::kThreads), 0, P);
-    if (L.shares > 1) sum_shares(I * J, L.shares, parts, c, s);
+    add_shares(sums, parts, c, I * J, L.shares);
     return check_launch("gated unit product");
 }
 
@@ -1488,7 +1503,7 @@ NarrowBack narrow_back(const Shape& S)
 }
 size_t narrow_scratch(const Shape& S) { return align256((size_t)narrow_bytes(narrow_steps(S.f)) * ((S.fo + 15) / 16)); }
 
-struct Scratch { size_t g, sums, parts, all; };     // offsets
+struct Scratch { size_t sums, parts, more, all; };     // offsets
 Scratch backward_scratch(const Shape& S)
 {
     const long both = 2L * S.fo, n = S.positions;
@@ -1501,8 +1516,8 @@ Scratch backward_scratch(const Shape& S)
     }
     W.sums = align256(sizeof(float) * both * n);
     W.parts = W.sums + align256(sizeof(float) * both * bias_shares(S).count);
-    const size_t gx = S.axis ? product_bytes(product_layout(n, S.f, both), n, S.f) : product_bytes(product_layout(S.f, n, both), S.f, n);
-    W.all = W.parts + std::max(gx, product_bytes(product_layout(both, S.f, n), both, S.f));
+    W.more = W.parts + (S.axis ? product_bytes(product_layout(n, S.f, both), n, S.f) : product_bytes(product_layout(S.f, n, both), S.f, n));
+    W.all = W.more + product_bytes(product_layout(both, S.f, n), both, S.f);
     return W;
 }
 size_t gated_workspace(const Shape& S, bool backward) { return backward ? backward_scratch(S).all : takes_narrow(S) ? narrow_scratch(S) : 0; }
@@ -1581,13 +1596,16 @@ int gated_fwd(const Shape& S, int fn, const float* x, const float* w, const floa
 }
 
 template <int TILES, int AXIS>
-void launch_narrow_back(const GatedBack& G, const NarrowBack& N, float* gx, const char* packed, float* parts, float* sums, hipStream_t s)
+void launch_narrow_back(const GatedBack& G, const NarrowBack& N, float* gx, char* packed, float* parts, float* sums, hipStream_t s)
 {
-    if (gx) {
-        const long tiles = (G.positions + 127) / 128;
-        ZNN_LAUNCH("gated unit backward", s, (k_gated_gx<TILES, AXIS>), dim3((unsigned)std::min(tiles, 2 * kUnits)), dim3(256), 0, G, packed, gx);
-    }
-    ZNN_LAUNCH("gated unit weights", s, (k_gated_gw<TILES, AXIS>), dim3((unsigned)N.shares, N.groups), dim3(64 * N.waves), 0, G, N.span, N.waves, parts, sums);
+    const long threads = (G.fo + 15) / 16 * (long)TILES * 64, each = (long)N.groups * N.waves * 64;
+    const unsigned packers = gx ? (unsigned)((threads + each - 1) / each) : 0;
+    ZNN_LAUNCH("gated unit weights", s, (k_gated_gw<TILES, AXIS>), dim3((unsigned)N.shares + packers, N.groups), dim3(64 * N.waves), 0, G, N.span, N.shares,
+               N.waves, parts, sums, packed);
+    // three workgroups stay on a unit: 40 -> 80 maps of 61 x 58 x 63 68 us, 80 with two of them, 75 with one tile a workgroup
+    if (gx)
+        ZNN_LAUNCH("gated unit backward", s, (k_gated_gx<TILES, AXIS>), dim3((unsigned)std::min((G.positions + 127) / 128, 3 * kUnits)), dim3(256), 0, G,
+                   (const char*)packed, gx);
 }
 
 template <int AXIS>
@@ -1595,20 +1613,16 @@ int gated_bwd_narrow(const GatedBack& G, const NarrowBack& N, const Scratch& W, 
 {
     char* const packed = ws + W.parts;
     float *const parts = N.shares > 1 ? (float*)ws : gw, *const sums = gb ? N.shares > 1 ? (float*)(ws + W.sums) : gb : nullptr;
-    if (gx) {
-        const long threads = (G.fo + 15) / 16 * (long)N.tiles * 64;
-        ZNN_LAUNCH("gated unit packing", s, k_pack_gated_back, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, G.w, G.f, G.fo, N.tiles, packed);
-    }
     switch (N.tiles) {
         case 1: launch_narrow_back<1, AXIS>(G, N, gx, packed, parts, sums, s); break;
         case 2: launch_narrow_back<2, AXIS>(G, N, gx, packed, parts, sums, s); break;
         case 3: launch_narrow_back<3, AXIS>(G, N, gx, packed, parts, sums, s); break;
         default: launch_narrow_back<4, AXIS>(G, N, gx, packed, parts, sums, s);
     }
-    if (N.shares > 1) {
-        sum_shares(2L * G.fo * G.f, N.shares, parts, gw, s);
-        if (gb) sum_shares(2L * G.fo, N.shares, sums, gb, s);
-    }
+    SharedSums A = {};
+    add_shares(A, parts, gw, 2L * G.fo * G.f, N.shares);
+    if (gb) add_shares(A, sums, gb, 2L * G.fo, N.shares);
+    sum_shares(A, s);
     return check_launch("gated unit backward");
 }
 
@@ -1626,15 +1640,21 @@ int gated_bwd(const Shape& S, int fn, const float* gy, const float* x, const flo
     const Grads G = {fn, S.fo, n, bias.span, gy, kept, g, gb ? (bias.count > 1 ? sums : gb) : nullptr};
     if (S.axis) ZNN_LAUNCH("gated unit gradients", s, k_gated_grads_rows, dim3((unsigned)((S.fo + 255) / 256), (unsigned)bias.count), dim3(256), 0, G);
     else ZNN_LAUNCH("gated unit gradients", s, k_gated_grads_maps, dim3((unsigned)S.fo, (unsigned)bias.count), dim3(256), 0, G);
-    if (gb && bias.count > 1) sum_shares(both, bias.count, sums, gb, s);
     int rc = check_launch("gated unit gradients");
     if (rc != ZNN_OK) return rc;
+    float* const more = (float*)(ws + W.more);
+    SharedSums A = {};
+    if (gb) add_shares(A, sums, gb, both, bias.count);
     if (S.axis) {
-        if (gx) rc = product<true, false>({g, both}, {w, S.f}, n, S.f, both, gx, parts, s);
-        return rc != ZNN_OK ? rc : product<false, false>({g, both}, {x, S.f}, both, S.f, n, gw, parts, s);
+        if (gx) rc = product<true, false>({g, both}, {w, S.f}, n, S.f, both, gx, parts, A, s);
+        if (rc == ZNN_OK) rc = product<false, false>({g, both}, {x, S.f}, both, S.f, n, gw, more, A, s);
+    } else {
+        if (gx) rc = product<false, false>({w, S.f}, {g, n}, S.f, n, both, gx, parts, A, s);
+        if (rc == ZNN_OK) rc = product<true, true>({g, n}, {x, n}, both, S.f, n, gw, more, A, s);
     }
-    if (gx) rc = product<false, false>({w, S.f}, {g, n}, S.f, n, both, gx, parts, s);
-    return rc != ZNN_OK ? rc : product<true, true>({g, n}, {x, n}, both, S.f, n, gw, parts, s);
+    if (rc != ZNN_OK) return rc;
+    sum_shares(A, s);
+    return check_launch("gated unit shares");
 }
 
 int check_gated_call(int32_t fn, const Shape& S, bool backward, const void* ws, size_t ws_bytes)
