@@ -365,8 +365,8 @@ int  znn_gated_bwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t position
  * for every line of an array [outer][length][inner], t its place along the middle extent: along any axis of images (outer = maps
  * and slower axes, inner = faster axes), along the steps of [batch][step][feature].  `reverse` != 0 takes the steps from the last to the
  * first.  h0 [outer][inner] is the state before the first step taken (NULL: zeros), so that one step of a running sequence is a call of length 1.
- *   A gate that is shut (z = -inf, or so low that f_t is below 2^-126) forgets the state whatever it holds: a line may hold several
- * sequences one after another.  One that is wide open (z = inf, 1 - f_t below 2^-126) keeps the state whatever x_t holds: padding.
+ *   A gate that is shut (z = -inf, or anything below -104: f_t is 0) forgets the state whatever it holds: a line may hold several
+ * sequences one after another.  One that is wide open (z = inf, or anything above 104) keeps the state whatever x_t holds: padding.
  * znn_recurrence_bwd : from gh, the gradient of every h_t, with G_t = gh_t + f_(t+1) G_(t+1):
  *     gz = G_t (h_(t-1) - x_t) f_t (1 - f_t),  gx = G_t (1 - f_t),  gh0 = f_1 G_1 (may be NULL),
  *   0 where a factor f_t or 1 - f_t is 0, whatever the others hold.

@@ -8,7 +8,6 @@ from __future__ import annotations
 
 import ctypes
 import functools
-import math
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -632,31 +631,43 @@ def _take_workspace(like, need):
 
 
 def _operands(*tensors):
-    """Device pointers of fp32 tensors (None -> NULL), which have to live on the current device: the call runs on a stream of it."""
-    pointers = [_ptr(t, torch.float32) for t in tensors]
-    device = torch.cuda.current_device()
+    """(device pointers of fp32 tensors, None -> NULL, handle of the current stream).  Tensors have to live on the current device: the
+    call runs on a stream of it."""
+    pointers = []
     for t in tensors:
-        if t is not None and t.get_device() != device:
+        if t is None:
+            pointers.append(None)
+            continue
+        if not (t.is_cuda and t.dtype is torch.float32 and t.is_contiguous()):
+            _ptr(t, torch.float32)          # says what is wrong
+        if not pointers:
+            device = torch._C._cuda_getDevice()
+        if t.get_device() != device:
             raise ValueError("tensor lives on device %d, the current one is %d" % (t.get_device(), device))
-    return pointers
+        pointers.append(t.data_ptr())
+    return pointers, torch._C._cuda_getCurrentRawStream(device)
 
 
 def _gate_number(fn):
-    if fn not in GATE_FNS:
+    number = GATE_FNS.get(fn)
+    if number is None:
         raise ValueError("a gate function is one of %s, got %r" % (", ".join(GATE_FNS), fn))
-    return GATE_FNS[fn]
+    return number
 
 
 def _gated_extents(x, w, axis):
     """(f, f', positions) of x with its features along ``axis`` and w [2 f', f], which may have axes of extent 1 behind these."""
-    if axis not in (0, 1):
+    if axis != 0 and axis != 1:
         raise ValueError("axis must be 0 or 1, got %r" % (axis,))
-    if x.dim() < 1 or x.numel() < 1:
-        raise ValueError("expected an array of features, got %s" % (tuple(x.shape),))
-    f = x.shape[0] if axis == 0 else x.shape[-1]
-    if w.dim() < 2 or w.shape[1] != f or w.shape[0] % 2 or w.numel() != w.shape[0] * f:
-        raise ValueError("expected weights [2 f', %d], got %s" % (f, tuple(w.shape)))
-    return f, w.shape[0] // 2, x.numel() // f
+    shape, ws, count = x.shape, w.shape, x.numel()
+    if not shape or count < 1:
+        raise ValueError("expected an array of features, got %s" % (tuple(shape),))
+    f = shape[-axis]
+    if len(ws) < 2 or ws[1] != f or ws[0] % 2 or w.numel() != ws[0] * f:
+        raise ValueError("expected weights [2 f', %d], got %s" % (f, tuple(ws)))
+    if f >> 31 or ws[0] >> 31:          # ctypes would cut them off
+        raise ValueError("%d to %d features are too many" % (f, ws[0] // 2))
+    return f, ws[0] // 2, count // f
 
 
 def _gated_like(x, axis, features):
@@ -685,11 +696,11 @@ def gated_fwd(x, w, b=None, fn="silu", axis=0, kept=True, stream=None):
     f, fo, positions = _gated_extents(x, w, axis)
     if b is not None and b.numel() != 2 * fo:
         raise ValueError("expected %d biases, got %d" % (2 * fo, b.numel()))
-    operands = _operands(x, w, b)
+    operands, on = _operands(x, w, b)
     y = _gated_like(x, axis, fo)
     both = _gated_like(x, axis, 2 * fo) if kept else None
     ws, at, need = _take_workspace(x, gated_workspace_bytes(f, fo, positions, axis, ZNN_PASS_FWD))
-    _check(lib().znn_gated_fwd(number, f, fo, positions, axis, *operands, y.data_ptr(), _ptr(both), at, need, _stream_ptr()))
+    _check(lib().znn_gated_fwd(number, f, fo, positions, axis, *operands, y.data_ptr(), both.data_ptr() if kept else None, at, need, on))
     return y, both
 
 
@@ -703,23 +714,30 @@ def gated_bwd(gy, x, w, kept, fn="silu", axis=0, bias=True, need_gx=True, stream
     outer = (lambda n: (n,) + x.shape[1:]) if axis == 0 else (lambda n: x.shape[:-1] + (n,))
     _expect_shape(gy, outer(fo), "a gradient")
     _expect_shape(kept, outer(2 * fo), "kept values")
-    operands = _operands(gy, x, w, kept)
+    operands, on = _operands(gy, x, w, kept)
     gx, gw = torch.empty_like(x) if need_gx else None, torch.empty_like(w)
     gb = w.new_empty(2 * fo) if bias else None
     ws, at, need = _take_workspace(x, gated_workspace_bytes(f, fo, positions, axis, ZNN_PASS_BWD))
-    _check(lib().znn_gated_bwd(number, f, fo, positions, axis, *operands, _ptr(gx), gw.data_ptr(), _ptr(gb), at, need, _stream_ptr()))
+    _check(lib().znn_gated_bwd(number, f, fo, positions, axis, *operands, _ptr(gx), gw.data_ptr(), _ptr(gb), at, need, on))
     return gx, gw, gb
 
 
-def _line_extents(z, dim, *others):
-    """(outer, length, inner) of the lines along a dimension."""
-    if not -z.dim() <= dim < z.dim():
-        raise ValueError("an array of %d dimensions has no dimension %r" % (z.dim(), dim))
-    if z.numel() < 1:
-        raise ValueError("expected an array of lines, got %s" % (tuple(z.shape),))
+def _line_extents(z, dim, h0, *others):
+    """(outer, length, inner) of the lines along a dimension; h0 has a state for each of them, or is None."""
+    shape = z.shape
+    if not -len(shape) <= dim < len(shape):
+        raise ValueError("an array of %d dimensions has no dimension %r" % (len(shape), dim))
+    count = z.numel()
+    if count < 1:
+        raise ValueError("expected an array of lines, got %s" % (tuple(shape),))
     _same_shape(z, *others)
-    dim %= z.dim()
-    return math.prod(z.shape[:dim]), z.shape[dim], math.prod(z.shape[dim + 1:])
+    dim %= len(shape)
+    if h0 is not None and h0.shape != shape[:dim] + shape[dim + 1:]:
+        raise ValueError("expected one state for every line along dimension %d of %s, got %s" % (dim, tuple(shape), tuple(h0.shape)))
+    outer = 1
+    for n in shape[:dim]:
+        outer *= n
+    return outer, shape[dim], count // (outer * shape[dim])
 
 
 @functools.lru_cache(maxsize=1024)
@@ -729,23 +747,17 @@ def recurrence_workspace_bytes(outer, length, inner):
     return b.value
 
 
-def _check_state(h0, z, dim):
-    if h0 is not None and h0.shape != z.shape[:dim % z.dim()] + z.shape[dim % z.dim() + 1:]:
-        raise ValueError("expected one state for every line along dimension %d of %s, got %s" % (dim, tuple(z.shape), tuple(h0.shape)))
-
-
 def recurrence_fwd(z, x, h0=None, dim=-1, reverse=False, out=None, stream=None):
     """h with h_t = f_t h_(t-1) + (1 - f_t) x_t, f = logistic(z), along a dimension, from the state h0 (the shape without that
     dimension; None: zeros).  One step of a running sequence is a call on one step, with the last state as h0."""
     if stream is not None:          # what is made belongs to the stream that works on it
         with torch.cuda.stream(stream):
             return recurrence_fwd(z, x, h0, dim, reverse, out)
-    outer, length, inner = _line_extents(z, dim, x, out)
-    _check_state(h0, z, dim)
-    operands = _operands(z, x, h0, out)[:3]
+    outer, length, inner = _line_extents(z, dim, h0, x, out)
+    (zp, xp, sp, _), on = _operands(z, x, h0, out)
     h = torch.empty_like(z) if out is None else out
     ws, at, need = _take_workspace(z, recurrence_workspace_bytes(outer, length, inner))
-    _check(lib().znn_recurrence_fwd(outer, length, inner, bool(reverse), *operands, h.data_ptr(), at, need, _stream_ptr()))
+    _check(lib().znn_recurrence_fwd(outer, length, inner, bool(reverse), zp, xp, sp, h.data_ptr(), at, need, on))
     return h
 
 
@@ -754,15 +766,13 @@ def recurrence_bwd(gh, z, x, h, h0=None, dim=-1, reverse=False, gz=None, gx=None
     if stream is not None:          # what is made belongs to the stream that works on it
         with torch.cuda.stream(stream):
             return recurrence_bwd(gh, z, x, h, h0, dim, reverse, gz, gx)
-    outer, length, inner = _line_extents(z, dim, gh, x, h, gz, gx)
-    _check_state(h0, z, dim)
-    operands = _operands(gh, z, x, h, h0, gz, gx)[:5]
+    outer, length, inner = _line_extents(z, dim, h0, gh, x, h, gz, gx)
+    operands, on = _operands(gh, z, x, h, h0, gz, gx)
     gz = torch.empty_like(z) if gz is None else gz
     gx = torch.empty_like(x) if gx is None else gx
     gh0 = None if h0 is None else torch.empty_like(h0)
     ws, at, need = _take_workspace(z, recurrence_workspace_bytes(outer, length, inner))
-    _check(lib().znn_recurrence_bwd(outer, length, inner, bool(reverse), *operands, gz.data_ptr(), gx.data_ptr(), _ptr(gh0), at, need,
-                                    _stream_ptr()))
+    _check(lib().znn_recurrence_bwd(outer, length, inner, bool(reverse), *operands[:5], gz.data_ptr(), gx.data_ptr(), _ptr(gh0), at, need, on))
     return gz, gx, gh0
 
 

@@ -1038,6 +1038,41 @@ template <int AXIS> __device__ __noinline__ float gw_again(const GatedBack& G, l
     return s;
 }
 
+// Forward from shares of [u; v], where tiles alone are too few for the chip: their sum, the biases and the gate.
+struct GatedJoin { const float* parts; int shares, fn, rows; long fo, positions; const float* bias; float *y, *kept; };
+__global__ void __launch_bounds__(256) k_gated_join(GatedJoin G)
+{
+    // quads of neighbours: of features (rows), or of positions
+    const long line = G.rows ? G.fo : G.positions, quads = (line + 3) / 4, lines = G.rows ? G.positions : G.fo, both = 2 * G.fo * G.positions;
+    for (long q = blockIdx.x * 256L + threadIdx.x; q < lines * quads; q += gridDim.x * 256L) {
+        const long l = q / quads, c = (q - l * quads) * 4, at = G.rows ? 2 * l * line + c : l * line + c, other = at + (G.rows ? G.fo : G.fo * G.positions);
+        const int most = line - c < 4 ? (int)(line - c) : 4;
+        floatx4 u = load4(G.parts + at, most), v = load4(G.parts + other, most), out;
+        for (int n = 1; n < G.shares; ++n) {
+            u += load4(G.parts + n * both + at, most);
+            v += load4(G.parts + n * both + other, most);
+        }
+        if (G.bias) {
+            if (G.rows) {
+                u += load4(G.bias + c, most);
+                v += load4(G.bias + G.fo + c, most);
+            } else {
+                u += G.bias[l];
+                v += G.bias[G.fo + l];
+            }
+        }
+        with_fn(G.fn, [&](auto number) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) out[r] = gate_fn<number.value>(u[r]).a * v[r];
+        });
+        store4(G.y + l * line + c, out, most);
+        if (G.kept) {
+            store4(G.kept + at, u, most);
+            store4(G.kept + other, v, most);
+        }
+    }
+}
+
 // Weights as the gradient of x reads them: [16 features][16 inputs][part][lane]; eight k are four features of W and the same of V.  Thread t of those of
 // one lane each.
 __device__ __forceinline__ void pack_back(const float* w, int f, int fo, int tiles, long t, char* packed)
@@ -1388,7 +1423,7 @@ typedef Waves<4, 1, 1, 2> Tall;         // 128 x 64
 // shares move their bytes at 4 TB/s and a launch takes 3 us.
 enum Kind { FP32, SPLIT, SPLIT_TURNED };
 struct Layout { Kind kind; Tiles T; int shares; long span; double us; };
-constexpr long kFewPositions = 32, kUnits = 256, kMostShares = 512, kLeastSpan = 8 * kDepth;
+constexpr long kFewPositions = 32, kUnits = 256, kMostShares = 512, kLeastSpan = kDepth;
 Tiles tiles_of(long i, long j, long ti, long tj)
 {
     const long ni = (i + ti - 1) / ti, nj = (j + tj - 1) / tj;
@@ -1444,18 +1479,46 @@ void sum_shares(const SharedSums& A, hipStream_t s)
     const unsigned blocks = last.first + (unsigned)((last.count + elements_of(last.shares) - 1) / elements_of(last.shares));
     ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3(blocks), dim3(1024), 0, A);
 }
-// c [I][J] = sum over k of A B, once `sums` are taken; `parts` holds product_bytes
-template <bool A_ALONG, bool B_ALONG>
-int product(const Operand& A, const Operand& B, long I, long J, long K, float* c, float* parts, SharedSums& sums, hipStream_t s)
+// How the forward pass of more than a few positions and features goes: tiles that hold both halves, or shares of all [u; v] joined by a launch behind them.
+struct Forward { bool split, joined; Layout shares; };
+Forward forward_of(const Shape& S)
 {
-    const Layout L = product_layout(I, J, K);
-    Product P = {{A, B, I, J, 0, 0, K}, L.T, L.shares > 1 ? parts : c, L.span};
+    const long I = S.axis ? S.positions : 2L * S.fo, J = S.axis ? 2L * S.fo : S.positions;
+    const Layout split = layout_of(SPLIT, tiles_of(I, J, 64 * kSplitWaves, kSplitColumns), I, J, S.f, false);
+    const Layout fp32 = layout_of(FP32, S.axis ? tiles_of(I, J, Tall::TI, Tall::TJ) : tiles_of(I, J, Wide::TI, Wide::TJ), I, J, S.f, false);
+    Forward F = {split.us < fp32.us, false, {}};
+    const double best = F.split ? split.us : fp32.us;
+    // the launch behind: 3 us, and all shares once more.  64 rows of 1024 -> 4096 49 us by tiles and 24 so, 200 rows 53 and 38
+    if (best > 15.0) {
+        F.shares = product_layout(I, J, S.f);
+        F.joined = F.shares.us + 3.0 + 1e-6 * I * J < best;
+    }
+    return F;
+}
+size_t forward_bytes(const Shape& S)
+{
+    const Forward F = forward_of(S);
+    return F.joined ? align256(sizeof(float) * F.shares.shares * 2 * S.fo * S.positions) : 0;
+}
+
+// Shares of c [I][J] = sum over k of A B in `parts`, or all of it in c
+template <bool A_ALONG, bool B_ALONG>
+void product_shares(const Layout& L, const Operand& A, const Operand& B, long I, long J, long K, float* c, hipStream_t s)
+{
+    Product P = {{A, B, I, J, 0, 0, K}, L.T, c, L.span};
     const dim3 grid(L.T.count, (unsigned)L.shares), wide(128 * kSplitWaves);
     if (L.kind == SPLIT) ZNN_LAUNCH("gated unit product", s, (k_product_split<kSplitWaves, A_ALONG, B_ALONG, false>), grid, wide, 0, P);
     else if (L.kind == SPLIT_TURNED) {
         P.M = Matrices{B, A, J, I, 0, 0, K};
         ZNN_LAUNCH("gated unit product", s, (k_product_split<kSplitWaves, B_ALONG, A_ALONG, true>), grid, wide, 0, P);
     } else ZNN_LAUNCH("gated unit product", s, (k_product<Wide, A_ALONG, B_ALONG>), grid, dim3(Wide::kThreads), 0, P);
+}
+// c [I][J] = sum over k of A B, once `sums` are taken; `parts` holds product_bytes
+template <bool A_ALONG, bool B_ALONG>
+int product(const Operand& A, const Operand& B, long I, long J, long K, float* c, float* parts, SharedSums& sums, hipStream_t s)
+{
+    const Layout L = product_layout(I, J, K);
+    product_shares<A_ALONG, B_ALONG>(L, A, B, I, J, K, L.shares > 1 ? parts : c, s);
     add_shares(sums, parts, c, I * J, L.shares);
     return check_launch("gated unit product");
 }
@@ -1520,7 +1583,7 @@ Scratch backward_scratch(const Shape& S)
     W.all = W.more + product_bytes(product_layout(both, S.f, n), both, S.f);
     return W;
 }
-size_t gated_workspace(const Shape& S, bool backward) { return backward ? backward_scratch(S).all : takes_narrow(S) ? narrow_scratch(S) : 0; }
+size_t gated_workspace(const Shape& S, bool backward) { return backward ? backward_scratch(S).all : takes_narrow(S) ? narrow_scratch(S) : S.positions <= kFewPositions ? 0 : forward_bytes(S); }
 
 template <class W, int AXIS>
 void launch_fwd(GatedFwd G, hipStream_t s)
@@ -1580,16 +1643,24 @@ int gated_fwd(const Shape& S, int fn, const float* x, const float* w, const floa
     }
     const Operand weights = {w, S.f};
     const long half = S.fo;
-    const long I = S.axis ? S.positions : 2 * half, J = S.axis ? 2 * half : S.positions;
-    const bool large = layout_of(SPLIT, tiles_of(I, J, 64 * kSplitWaves, kSplitColumns), I, J, S.f, false).us <
-                       layout_of(FP32, S.axis ? tiles_of(I, J, Tall::TI, Tall::TJ) : tiles_of(I, J, Wide::TI, Wide::TJ), I, J, S.f, false).us;
+    const Forward F = forward_of(S);
+    if (F.joined) {
+        float* const parts = (float*)ws;
+        const long n = S.positions;
+        if (S.axis) product_shares<true, true>(F.shares, {x, S.f}, weights, n, 2 * half, S.f, parts, s);
+        else product_shares<true, false>(F.shares, weights, {x, n}, 2 * half, n, S.f, parts, s);
+        const GatedJoin G = {parts, F.shares.shares, fn, S.axis, half, n, b, y, kept};
+        const long quads = S.axis ? n * ((half + 3) / 4) : half * ((n + 3) / 4);
+        ZNN_LAUNCH("gated unit join", s, k_gated_join, dim3((unsigned)std::min((quads + 255) / 256, 1L << 20)), dim3(256), 0, G);
+        return check_launch("gated unit forward");
+    }
     if (S.axis) {
         const GatedFwd G = {{{x, S.f}, weights, S.positions, S.fo, half, 0, S.f}, Tiles{}, fn, S.fo, b, y, kept, S.fo};
-        if (large) launch_fwd_split<1>(G, s);
+        if (F.split) launch_fwd_split<1>(G, s);
         else launch_fwd<Tall, 1>(G, s);
     } else {
         const GatedFwd G = {{weights, {x, S.positions}, S.fo, S.positions, half, 0, S.f}, Tiles{}, fn, S.fo, b, y, kept, S.positions};
-        if (large) launch_fwd_split<0>(G, s);
+        if (F.split) launch_fwd_split<0>(G, s);
         else launch_fwd<Wide, 0>(G, s);
     }
     return check_launch("gated unit forward");
