@@ -88,6 +88,33 @@ def test_sequences_in_a_line(shape, reverse):
         check(z, x, gh, h0, reverse)
 
 
+@pytest.mark.parametrize("shape", [(3, 7000, 1), (1, 9000, 64), (200000, 9, 2), (5000, 60, 1)])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_gates_that_are_no_numbers(shape, reverse):
+    """Make their own state and those behind it, to the next shut gate, no numbers, and nothing else."""
+    z, x, gh, h0 = operands(shape, 21)
+    r = np.random.default_rng(22)
+    z[r.random(shape) < 0.002] = np.nan
+    z[r.random(shape) < 0.02] = -np.inf
+    with np.errstate(invalid="ignore"):
+        check(z, x, gh, h0, reverse)
+
+
+def test_many_lines_beyond_32_bits():
+    """2^31 elements and more: the last lines are those of a call on them alone."""
+    shape = (24, 900, 110000)
+    gen = torch.Generator(device="cuda:0").manual_seed(3)
+    z, x, gh = (torch.randn(shape, generator=gen, device="cuda:0") for _ in range(3))
+    h0 = torch.randn((24, 110000), generator=gen, device="cuda:0")
+    h = znn.recurrence_fwd(z, x, h0, 1)
+    part = [t[22:].contiguous() for t in (z, x, h0, gh)]
+    some = znn.recurrence_fwd(part[0], part[1], part[2], 1)
+    assert torch.equal(h[22:], some)
+    gz, gx, gh0 = znn.recurrence_bwd(gh, z, x, h, h0, 1)
+    want = znn.recurrence_bwd(part[3], part[0], part[1], some, part[2], 1)
+    assert torch.equal(gz[22:], want[0]) and torch.equal(gx[22:], want[1]) and torch.equal(gh0[22:], want[2])
+
+
 @pytest.mark.parametrize("shape", [(3, 20000, 1), (1, 9000, 64)])
 def test_a_state_that_is_not_finite_stays_until_a_gate_is_shut(shape):
     """Also where the product of the gates since then has left the range of fp32, in whatever piece of the line."""
@@ -215,7 +242,8 @@ def test_gradients_against_differences():
 
 
 # lines of more pieces than a group of groups holds: along the fastest extent, across few lines and across many
-@pytest.mark.parametrize("shape", [(1, 34000003, 1), (2, 17000001, 1), (1, 70001, 2), (1, 33001, 1100), (3, 140000, 5)])
+# (the last two hold more than 2^31 elements)
+@pytest.mark.parametrize("shape", [(1, 34000003, 1), (2, 17000001, 1), (1, 70001, 2), (1, 33001, 1100), (3, 140000, 5), (3, 750000001, 1), (1, 1048581, 2100)])
 @pytest.mark.parametrize("reverse", [False, True])
 def test_states_are_handed_on_over_the_longest_lines(shape, reverse):
     """Gates are wide open but for a few steps, the same in all lines, where half of the state goes: everything in between is exact."""
