@@ -35,7 +35,7 @@ __device__ __forceinline__ Gated gate_fn(float u)
     }
     const Gate g = gate(u);
     if (FN == ZNN_GATE_LOGISTIC) return Gated{g.f, g.f * g.k};
-    return Gated{u > 0.f ? u * g.f : finite * g.f, fmaf(finite, g.f * g.k, g.f)};
+    return Gated{fmaxf(u, -kLargestFloat) * g.f, fmaf(finite, g.f * g.k, g.f)};      // NaN comes from g
 }
 
 // f with the function's number as a constant
@@ -297,9 +297,9 @@ struct SplitStage {
     }
 };
 
-// Six products of a step, from zero, smallest first, of one operand (u) with four (v); meanwhile acc += sign before, which are the products before,
-// and request(slot), slot = 0 .. 23, between any two instructions.  ROWS_V: the results' rows are v's.
-template <bool ROWS_V, class Request>
+// Six products of a step, from zero, smallest first, of one operand (u) with those of four (v) from FROM to TO; meanwhile acc += sign before, which are the
+// products before, and request(slot), slot = 0, 1 .., between any two instructions.  ROWS_V: the results' rows are v's.
+template <bool ROWS_V, int FROM, int TO, class Request>
 __device__ __forceinline__ void products(floatx4 (&t)[4], const bf16x8 (&v)[4][3], const uintx4 (&u)[3], const floatx4 (&before)[4], float sign,
                                          floatx4 (&acc)[4], Request request)
 {
@@ -308,11 +308,11 @@ __device__ __forceinline__ void products(floatx4 (&t)[4], const bf16x8 (&v)[4][3
 #pragma unroll
     for (int g = 0; g < 6; ++g)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
+        for (int y = FROM; y < TO; ++y) {
             const bf16x8 one = __builtin_bit_cast(bf16x8, u[of_u[g]]);
             const floatx4 c = g ? t[y] : floatx4{0.f, 0.f, 0.f, 0.f};
             t[y] = ROWS_V ? split::mfma(v[y][of_v[g]], one, c) : split::mfma(one, v[y][of_v[g]], c);
-            request(g * 4 + y);
+            request(g * (TO - FROM) + y - FROM);
             if (g >= 1 && g <= 4) acc[y][g - 1] = fmaf(before[y][g - 1], sign, acc[y][g - 1]);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -370,26 +370,32 @@ __device__ __forceinline__ void split_product(floatx4 (&acc)[4][4], const Matric
         uintx4 u[2][3];
 #pragma unroll
         for (int part = 0; part < 3; ++part) u[0][part] = *(const uintx4*)(here + part * StageA::kPart + from_a);
+        auto fetch = [&](int y, int part) {
+            v[y][part] = __builtin_bit_cast(bf16x8, *(const uintx4*)(here + part * StageB::kPart + from_b + 1024 * y));
+        };
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
-#pragma unroll
-            for (int part = 0; part < 3; ++part)
-                v[y][part] = __builtin_bit_cast(bf16x8, *(const uintx4*)(here + part * StageB::kPart + from_b + 1024 * y));
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            products<!TURNED>(t[x & 1], v, u[x & 1], t[~x & 1], x ? sign : -sign, acc[x ? x - 1 : 3], [&](int slot) {
-                if (x < 3 && slot < 3) u[~x & 1][slot] = *(const uintx4*)(here + slot * StageA::kPart + from_a + 1024 * (x + 1));
-                constexpr int kFirst = 6, kEach = (96 - kFirst) / kPieces;
-                const int n = x * 24 + slot - kFirst, piece = n / kEach;
-                if (takes.value && n >= 0 && n % kEach == 0 && piece < kPieces) {
-                    take(next, piece, -sign);
-                    if (loads.value && piece % 12 == 11) {
-                        if (piece < 12 * StageA::kUnits) a.load(piece / 12, M.A);
-                        else b.load(piece / 12 - StageA::kUnits, M.B);
-                    }
+        for (int n = 0; n < 6; ++n) fetch(n / 3, n % 3);
+        // what is done between the instructions of a step, n = 0 .. 95 of them
+        auto between = [&](int n) {
+            constexpr int kFirst = 12, kEach = (96 - kFirst) / kPieces;
+            const int x = n / 24, slot = n % 24;
+            if (n < 6) fetch(2 + n / 3, n % 3);
+            if (x < 3 && slot >= 6 && slot < 9) u[~x & 1][slot - 6] = *(const uintx4*)(here + (slot - 6) * StageA::kPart + from_a + 1024 * (x + 1));
+            const int piece = (n - kFirst) / kEach;
+            if (takes.value && n >= kFirst && (n - kFirst) % kEach == 0 && piece < kPieces) {
+                take(next, piece, -sign);
+                if (loads.value && piece % 12 == 11) {
+                    if (piece < 12 * StageA::kUnits) a.load(piece / 12, M.A);
+                    else b.load(piece / 12 - StageA::kUnits, M.B);
                 }
-            });
-        }
+            }
+        };
+        // two columns first: all waves read their operands behind the barrier, and two need fewer of them
+        products<!TURNED, 0, 2>(t[0], v, u[0], t[1], -sign, acc[3], [&](int slot) { between(slot); });
+        products<!TURNED, 2, 4>(t[0], v, u[0], t[1], -sign, acc[3], [&](int slot) { between(12 + slot); });
+#pragma unroll
+        for (int x = 1; x < 4; ++x)
+            products<!TURNED, 0, 4>(t[x & 1], v, u[x & 1], t[~x & 1], sign, acc[x - 1], [&](int slot) { between(24 * x + slot); });
         sign = -sign;
     };
     typedef std::integral_constant<bool, true> Yes;
