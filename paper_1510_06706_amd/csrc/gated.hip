@@ -3,6 +3,7 @@
 #include "split_parts.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace znn {
@@ -1431,10 +1432,11 @@ typedef Waves<4, 1, 1, 2> Tall;         // 128 x 64
 
 // Tiles of a product and into how many shares its sum goes, by what it is expected to take: a unit takes 2.6 us for a step of 32 k of a tile of 256 x 128 on the
 // bf16 matrix cores (205 TFLOP/s in all), and 1.3 us for one of 64 x 128 on the fp32 ones (100 TFLOP/s), which take three tiles side by side; sums of
-// shares move their bytes at 4 TB/s and a launch takes 3 us.
+// shares move their bytes at 4 TB/s and a launch takes 3 us.  Sums of more than 2^16 terms (2048 additions one after another) go into shares whatever they
+// cost, as far as there are shares.
 enum Kind { FP32, SPLIT, SPLIT_TURNED };
 struct Layout { Kind kind; Tiles T; int shares; long span; double us; };
-constexpr long kFewPositions = 32, kUnits = 256, kMostShares = 512, kLeastSpan = kDepth;
+constexpr long kFewPositions = 32, kUnits = 256, kMostShares = 512, kLeastSpan = kDepth, kMostSpan = 1L << 16;
 Tiles tiles_of(long i, long j, long ti, long tj)
 {
     const long ni = (i + ti - 1) / ti, nj = (j + tj - 1) / tj;
@@ -1444,7 +1446,8 @@ Layout layout_of(Kind kind, const Tiles& T, long I, long J, long K, bool shares)
 {
     const long beside = kind == FP32 ? 3 * kUnits : kUnits;
     Layout best = {};
-    for (long wanted = 1; wanted <= (shares ? kMostShares : 1); wanted = wanted < 4 ? wanted + 1 : wanted + wanted / 4) {
+    best.us = HUGE_VAL;
+    for (long wanted = 1; wanted <= (shares ? kMostShares : 1); wanted = wanted < 4 ? wanted + 1 : wanted < kMostShares ? std::min(kMostShares, wanted + wanted / 4) : kMostShares + 1) {
         if (wanted > 1 && K / wanted < kLeastSpan) break;
         Layout L = {kind, T, 1, (K + kDepth - 1) / kDepth * kDepth, 0.0};
         if (wanted > 1) {
@@ -1457,7 +1460,8 @@ Layout layout_of(Kind kind, const Tiles& T, long I, long J, long K, bool shares)
         const double tall = kind == FP32 ? 3.0 * (rounds - 1) + (last > 2 * kUnits ? 3.0 : last > kUnits ? 2.0 : 1.2) : rounds;
         L.us = tall * (steps * step + (kind == FP32 ? 2.0 : 5.0));
         if (L.shares > 1) L.us += 3.0 + 1e-6 * I * J * 2 * L.shares;
-        if (wanted == 1 || L.us < best.us) best = L;
+        if (L.span > kMostSpan && shares && wanted < kMostShares) L.us *= 1e6 * L.span / kMostSpan;
+        if (L.us < best.us) best = L;
     }
     return best;
 }
@@ -1490,26 +1494,36 @@ void sum_shares(const SharedSums& A, hipStream_t s)
     const unsigned blocks = last.first + (unsigned)((last.count + elements_of(last.shares) - 1) / elements_of(last.shares));
     ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3(blocks), dim3(1024), 0, A);
 }
-// How the forward pass of more than a few positions and features goes: tiles that hold both halves, or shares of all [u; v] joined by a launch behind them.
-struct Forward { bool split, joined; Layout shares; };
+// Few features in: taken apart in registers where enough positions keep the chip busy.
+constexpr int narrow_steps(int f) { return f <= kNarrowSteps * kDepth ? (f + kDepth - 1) / kDepth : 0; }
+bool takes_narrow(const Shape& S)
+{
+    // us, in registers and by tiles: maps 40 -> 80 at 12 000 positions 17.1 and 13.1 (weights are taken apart by a launch of their own), at 36 000 20.5 and 23.5, at
+    // 100 000 33.1 and 57.8; 100 -> 200 at 12 000 22.4 and 26.1; rows of 128 -> 256 at 100 000 156 and 142
+    return narrow_steps(S.f) && S.positions >= 8192 && S.positions * S.f >= 1L << 20 && (!S.axis || S.f < 128);
+}
+// How the forward pass goes, and its workspace: a few positions, few features, tiles that hold both halves, or shares of all [u; v] joined by a launch behind
+// them.
+struct Forward { bool few, narrow, split, joined; Layout shares; size_t bytes; };
 Forward forward_of(const Shape& S)
 {
+    Forward F = {};
+    F.narrow = takes_narrow(S);
+    F.few = !F.narrow && S.positions <= kFewPositions;
+    if (F.narrow) F.bytes = align256((size_t)narrow_bytes(narrow_steps(S.f)) * ((S.fo + 15) / 16));
+    if (F.narrow || F.few) return F;
     const long I = S.axis ? S.positions : 2L * S.fo, J = S.axis ? 2L * S.fo : S.positions;
     const Layout split = layout_of(SPLIT, tiles_of(I, J, 64 * kSplitWaves, kSplitColumns), I, J, S.f, false);
     const Layout fp32 = layout_of(FP32, S.axis ? tiles_of(I, J, Tall::TI, Tall::TJ) : tiles_of(I, J, Wide::TI, Wide::TJ), I, J, S.f, false);
-    Forward F = {split.us < fp32.us, false, {}};
+    F.split = split.us < fp32.us;
     const double best = F.split ? split.us : fp32.us;
     // the launch behind: 3 us, and all shares once more.  64 rows of 1024 -> 4096 49 us by tiles and 24 so, 200 rows 53 and 38
     if (best > 15.0) {
         F.shares = product_layout(I, J, S.f);
         F.joined = F.shares.us + 3.0 + 1e-6 * I * J < best;
+        if (F.joined) F.bytes = align256(sizeof(float) * F.shares.shares * I * J);
     }
     return F;
-}
-size_t forward_bytes(const Shape& S)
-{
-    const Forward F = forward_of(S);
-    return F.joined ? align256(sizeof(float) * F.shares.shares * 2 * S.fo * S.positions) : 0;
 }
 
 // Shares of c [I][J] = sum over k of A B in `parts`, or all of it in c
@@ -1526,9 +1540,8 @@ void product_shares(const Layout& L, const Operand& A, const Operand& B, long I,
 }
 // c [I][J] = sum over k of A B, once `sums` are taken; `parts` holds product_bytes
 template <bool A_ALONG, bool B_ALONG>
-int product(const Operand& A, const Operand& B, long I, long J, long K, float* c, float* parts, SharedSums& sums, hipStream_t s)
+int product(const Layout& L, const Operand& A, const Operand& B, long I, long J, long K, float* c, float* parts, SharedSums& sums, hipStream_t s)
 {
-    const Layout L = product_layout(I, J, K);
     product_shares<A_ALONG, B_ALONG>(L, A, B, I, J, K, L.shares > 1 ? parts : c, s);
     add_shares(sums, parts, c, I * J, L.shares);
     return check_launch("gated unit product");
@@ -1551,14 +1564,6 @@ bool takes_narrow_back(const Shape& S)
 {
     return S.f <= 64 && S.positions >= 8192 && (S.axis || S.f <= 48 || S.positions >= 65536);
 }
-// Few features in: taken apart in registers where enough positions keep the chip busy.
-constexpr int narrow_steps(int f) { return f <= kNarrowSteps * kDepth ? (f + kDepth - 1) / kDepth : 0; }
-bool takes_narrow(const Shape& S)
-{
-    // us, in registers and by tiles: maps 40 -> 80 at 12 000 positions 17.1 and 13.1 (weights are taken apart by a launch of their own), at 36 000 20.5 and 23.5, at
-    // 100 000 33.1 and 57.8; 100 -> 200 at 12 000 22.4 and 26.1; rows of 128 -> 256 at 100 000 156 and 142
-    return narrow_steps(S.f) && S.positions >= 8192 && S.positions * S.f >= 1L << 20 && (!S.axis || S.f < 128);
-}
 // Backward: shares of the positions, workgroups of up to kBackWaves waves of 16 features each
 struct NarrowBack { int tiles, waves, shares; unsigned groups; long span; };
 NarrowBack narrow_back(const Shape& S)
@@ -1576,26 +1581,34 @@ NarrowBack narrow_back(const Shape& S)
     N.shares = (int)((S.positions + N.span - 1) / N.span);
     return N;
 }
-size_t narrow_scratch(const Shape& S) { return align256((size_t)narrow_bytes(narrow_steps(S.f)) * ((S.fo + 15) / 16)); }
-
-struct Scratch { size_t sums, parts, more, all; };     // offsets
-Scratch backward_scratch(const Shape& S)
+// How the backward pass goes, and where things lie in its workspace.
+struct Backward {
+    NarrowBack narrow;              // tiles 0: du and dv are stored
+    Layout gx, gw;
+    BiasShares bias;
+    size_t sums, parts, more, bytes;
+};
+Backward backward_of(const Shape& S)
 {
     const long both = 2L * S.fo, n = S.positions;
-    Scratch W = {};
-    if (const NarrowBack N = narrow_back(S); N.tiles) {
-        W.sums = align256(sizeof(float) * both * S.f * N.shares);                               // behind the shares of gw
-        W.parts = W.sums + align256(sizeof(float) * both * N.shares);                           // packed weights
-        W.all = W.parts + align256((size_t)N.tiles * 3 * 1024 * ((S.fo + 15) / 16));
-        return W;
+    Backward B = {};
+    B.narrow = narrow_back(S);
+    if (B.narrow.tiles) {
+        B.sums = align256(sizeof(float) * both * S.f * B.narrow.shares);                        // behind the shares of gw
+        B.parts = B.sums + align256(sizeof(float) * both * B.narrow.shares);                    // packed weights
+        B.bytes = B.parts + align256((size_t)B.narrow.tiles * 3 * 1024 * ((S.fo + 15) / 16));
+        return B;
     }
-    W.sums = align256(sizeof(float) * both * n);
-    W.parts = W.sums + align256(sizeof(float) * both * bias_shares(S).count);
-    W.more = W.parts + (S.axis ? product_bytes(product_layout(n, S.f, both), n, S.f) : product_bytes(product_layout(S.f, n, both), S.f, n));
-    W.all = W.more + product_bytes(product_layout(both, S.f, n), both, S.f);
-    return W;
+    const long I = S.axis ? n : S.f, J = S.axis ? S.f : n;
+    B.gx = product_layout(I, J, both);
+    B.gw = product_layout(both, S.f, n);
+    B.bias = bias_shares(S);
+    B.sums = align256(sizeof(float) * both * n);
+    B.parts = B.sums + align256(sizeof(float) * both * B.bias.count);
+    B.more = B.parts + product_bytes(B.gx, I, J);
+    B.bytes = B.more + product_bytes(B.gw, both, S.f);
+    return B;
 }
-size_t gated_workspace(const Shape& S, bool backward) { return backward ? backward_scratch(S).all : takes_narrow(S) ? narrow_scratch(S) : S.positions <= kFewPositions ? 0 : forward_bytes(S); }
 
 template <class W, int AXIS>
 void launch_fwd(GatedFwd G, hipStream_t s)
@@ -1632,9 +1645,9 @@ void launch_narrow(const GatedNarrow& G, int axis, hipStream_t s)
     else ZNN_LAUNCH("gated unit forward", s, (k_gated_narrow<STEPS, P, 0>), grid, dim3(256), 0, A);
 }
 
-int gated_fwd(const Shape& S, int fn, const float* x, const float* w, const float* b, float* y, float* kept, char* ws, hipStream_t s)
+int gated_fwd(const Shape& S, const Forward& F, int fn, const float* x, const float* w, const float* b, float* y, float* kept, char* ws, hipStream_t s)
 {
-    if (takes_narrow(S)) {
+    if (F.narrow) {
         const int steps = narrow_steps(S.f);
         const long threads = (S.fo + 15) / 16 * 2L * steps * 64;
         ZNN_LAUNCH("gated unit weights", s, k_pack_gated, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, w, S.f, S.fo, steps, ws);
@@ -1645,7 +1658,7 @@ int gated_fwd(const Shape& S, int fn, const float* x, const float* w, const floa
         else launch_narrow<4, 2>(G, S.axis, s);
         return check_launch("gated unit forward");
     }
-    if (S.positions <= kFewPositions) {
+    if (F.few) {
         const GatedFew G = {x, w, b, y, kept, fn, S.f, S.fo, S.positions, S.axis ? 1 : S.positions, S.axis ? S.f : 1};
         if (S.positions == 1) launch_few<1>(G, S.axis, s);
         else if (S.positions == 2) launch_few<2>(G, S.axis, s);
@@ -1655,7 +1668,6 @@ int gated_fwd(const Shape& S, int fn, const float* x, const float* w, const floa
     }
     const Operand weights = {w, S.f};
     const long half = S.fo;
-    const Forward F = forward_of(S);
     if (F.joined) {
         float* const parts = (float*)ws;
         const long n = S.positions;
@@ -1692,10 +1704,11 @@ void launch_narrow_back(const GatedBack& G, const NarrowBack& N, float* gx, char
 }
 
 template <int AXIS>
-int gated_bwd_narrow(const GatedBack& G, const NarrowBack& N, const Scratch& W, float* gx, float* gw, float* gb, char* ws, hipStream_t s)
+int gated_bwd_narrow(const GatedBack& G, const Backward& B, float* gx, float* gw, float* gb, char* ws, hipStream_t s)
 {
-    char* const packed = ws + W.parts;
-    float *const parts = N.shares > 1 ? (float*)ws : gw, *const sums = gb ? N.shares > 1 ? (float*)(ws + W.sums) : gb : nullptr;
+    const NarrowBack& N = B.narrow;
+    char* const packed = ws + B.parts;
+    float *const parts = N.shares > 1 ? (float*)ws : gw, *const sums = gb ? N.shares > 1 ? (float*)(ws + B.sums) : gb : nullptr;
     switch (N.tiles) {
         case 1: launch_narrow_back<1, AXIS>(G, N, gx, packed, parts, sums, s); break;
         case 2: launch_narrow_back<2, AXIS>(G, N, gx, packed, parts, sums, s); break;
@@ -1709,41 +1722,38 @@ int gated_bwd_narrow(const GatedBack& G, const NarrowBack& N, const Scratch& W, 
     return check_launch("gated unit backward");
 }
 
-int gated_bwd(const Shape& S, int fn, const float* gy, const float* x, const float* w, const float* kept, float* gx, float* gw, float* gb,
-              char* ws, hipStream_t s)
+int gated_bwd(const Shape& S, const Backward& B, int fn, const float* gy, const float* x, const float* w, const float* kept, float* gx, float* gw,
+              float* gb, char* ws, hipStream_t s)
 {
-    const Scratch W = backward_scratch(S);
-    if (const NarrowBack N = narrow_back(S); N.tiles) {
+    if (B.narrow.tiles) {
         const GatedBack G = {gy, x, w, kept, fn, S.f, S.fo, S.positions};
-        return S.axis ? gated_bwd_narrow<1>(G, N, W, gx, gw, gb, ws, s) : gated_bwd_narrow<0>(G, N, W, gx, gw, gb, ws, s);
+        return S.axis ? gated_bwd_narrow<1>(G, B, gx, gw, gb, ws, s) : gated_bwd_narrow<0>(G, B, gx, gw, gb, ws, s);
     }
-    const BiasShares bias = bias_shares(S);
-    float *const g = (float*)ws, *const sums = (float*)(ws + W.sums), *const parts = (float*)(ws + W.parts);
+    const BiasShares& bias = B.bias;
+    float *const g = (float*)ws, *const sums = (float*)(ws + B.sums), *const parts = (float*)(ws + B.parts), *const more = (float*)(ws + B.more);
     const long both = 2L * S.fo, n = S.positions;
     const Grads G = {fn, S.fo, n, bias.span, gy, kept, g, gb ? (bias.count > 1 ? sums : gb) : nullptr};
     if (S.axis) ZNN_LAUNCH("gated unit gradients", s, k_gated_grads_rows, dim3((unsigned)((S.fo + 255) / 256), (unsigned)bias.count), dim3(256), 0, G);
     else ZNN_LAUNCH("gated unit gradients", s, k_gated_grads_maps, dim3((unsigned)S.fo, (unsigned)bias.count), dim3(256), 0, G);
     int rc = check_launch("gated unit gradients");
     if (rc != ZNN_OK) return rc;
-    float* const more = (float*)(ws + W.more);
     SharedSums A = {};
     if (gb) add_shares(A, sums, gb, both, bias.count);
     if (S.axis) {
-        if (gx) rc = product<true, false>({g, both}, {w, S.f}, n, S.f, both, gx, parts, A, s);
-        if (rc == ZNN_OK) rc = product<false, false>({g, both}, {x, S.f}, both, S.f, n, gw, more, A, s);
+        if (gx) rc = product<true, false>(B.gx, {g, both}, {w, S.f}, n, S.f, both, gx, parts, A, s);
+        if (rc == ZNN_OK) rc = product<false, false>(B.gw, {g, both}, {x, S.f}, both, S.f, n, gw, more, A, s);
     } else {
-        if (gx) rc = product<false, false>({w, S.f}, {g, n}, S.f, n, both, gx, parts, A, s);
-        if (rc == ZNN_OK) rc = product<true, true>({g, n}, {x, n}, both, S.f, n, gw, more, A, s);
+        if (gx) rc = product<false, false>(B.gx, {w, S.f}, {g, n}, S.f, n, both, gx, parts, A, s);
+        if (rc == ZNN_OK) rc = product<true, true>(B.gw, {g, n}, {x, n}, both, S.f, n, gw, more, A, s);
     }
     if (rc != ZNN_OK) return rc;
     sum_shares(A, s);
     return check_launch("gated unit shares");
 }
 
-int check_gated_call(int32_t fn, const Shape& S, bool backward, const void* ws, size_t ws_bytes)
+int check_gated_call(int32_t fn, size_t need, const void* ws, size_t ws_bytes)
 {
     if (fn < ZNN_GATE_RECTIFY || fn > ZNN_GATE_GELU) return fail(ZNN_EINVAL, "unknown gate function %d", fn);
-    const size_t need = gated_workspace(S, backward);
     if (!need) return ZNN_OK;
     if (!ws) return fail(ZNN_EWORKSPACE, "workspace is NULL but %zu bytes are needed", need);
     if ((uintptr_t)ws & 255) return fail(ZNN_EWORKSPACE, "workspace is not 256-byte aligned");
@@ -1764,7 +1774,8 @@ int znn_gated_workspace_bytes(int32_t fan_in, int32_t fan_out, int64_t positions
     if (rc != ZNN_OK) return rc;
     if (pass != ZNN_PASS_FWD && pass != ZNN_PASS_BWD) return fail(ZNN_EINVAL, "pass must be forward or backward");
     if (!bytes) return fail(ZNN_EINVAL, "NULL argument");
-    *bytes = gated_workspace(Shape{fan_in, fan_out, axis, (long)positions}, pass == ZNN_PASS_BWD);
+    const Shape S = {fan_in, fan_out, axis, (long)positions};
+    *bytes = pass == ZNN_PASS_BWD ? backward_of(S).bytes : forward_of(S).bytes;
     return ZNN_OK;
 }
 
@@ -1775,9 +1786,10 @@ int znn_gated_fwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t positions
     if (rc != ZNN_OK) return rc;
     if (!x || !w || !y) return fail(ZNN_EINVAL, "NULL argument");
     const Shape S = {fan_in, fan_out, axis, (long)positions};
-    rc = check_gated_call(fn, S, false, ws, ws_bytes);
+    const Forward F = forward_of(S);
+    rc = check_gated_call(fn, F.bytes, ws, ws_bytes);
     if (rc != ZNN_OK) return rc;
-    return gated_fwd(S, fn, x, w, b, y, kept, (char*)ws, (hipStream_t)stream);
+    return gated_fwd(S, F, fn, x, w, b, y, kept, (char*)ws, (hipStream_t)stream);
 }
 
 int znn_gated_bwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t positions, int32_t axis, const float* gy, const float* x,
@@ -1787,9 +1799,10 @@ int znn_gated_bwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t positions
     if (rc != ZNN_OK) return rc;
     if (!gy || !x || !w || !kept || !gw) return fail(ZNN_EINVAL, "NULL argument");
     const Shape S = {fan_in, fan_out, axis, (long)positions};
-    rc = check_gated_call(fn, S, true, ws, ws_bytes);
+    const Backward B = backward_of(S);
+    rc = check_gated_call(fn, B.bytes, ws, ws_bytes);
     if (rc != ZNN_OK) return rc;
-    return gated_bwd(S, fn, gy, x, w, kept, gx, gw, gb, (char*)ws, (hipStream_t)stream);
+    return gated_bwd(S, B, fn, gy, x, w, kept, gx, gw, gb, (char*)ws, (hipStream_t)stream);
 }
 
 }  // extern "C"
