@@ -237,7 +237,7 @@ struct SplitStage {
     unsigned w[4];
     const float* p[kUnits];         // ALONG_K: the thread's next octets
     const float* base;              // else: row `first` of the next step's first k of this wave's octet
-    unsigned at;                    // and this thread's row behind it
+    unsigned at;                    // and this thread's (first) row behind it: rows behind the last one are not moved, several threads move the last ones
 
     __device__ __forceinline__ static int octet() { return ALONG_K ? threadIdx.x % 4 : __builtin_amdgcn_readfirstlane(threadIdx.x / (THREADS / 4)); }
     __device__ __forceinline__ static int row(int unit)
@@ -251,7 +251,8 @@ struct SplitStage {
             for (int u = 0; u < kUnits; ++u) p[u] = O.p + source_row<HALVES>(first, row(u), rows, half) * O.ld + k0 + octet() * 8;
         else {
             base = O.p + (k0 + octet() * 8) * O.ld + first;
-            at = row(0);
+            const long left = rows - first, r = row(0), most = left < kUnits ? 0 : left - kUnits;
+            at = (unsigned)(r < most ? r : most);
         }
     }
     // steps that are there as a whole
@@ -274,7 +275,7 @@ struct SplitStage {
             base += kDepth * O.ld;
         }
     }
-    __device__ __forceinline__ bool whole(long first, long rows) const { return ALONG_K || first + R <= rows; }
+    __device__ __forceinline__ static bool whole(long first, long rows) { return ALONG_K || first + kUnits <= rows; }
     // any step: `left` k are there of the operand from its first one on
     __device__ __forceinline__ void load_some(const Operand& O, long first, long rows, long left)
     {
@@ -282,7 +283,7 @@ struct SplitStage {
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const float* const q = ALONG_K ? p[u] : base + at + u;
-            const bool there = ALONG_K || first + row(u) < rows;
+            const bool there = ALONG_K || first + at + u < rows;
 #pragma unroll
             for (int c = 0; c < 8; ++c) v[u][c] = there && c < most ? q[ALONG_K ? c : c * O.ld] : 0.f;
             if (ALONG_K) p[u] += kDepth;
@@ -296,7 +297,7 @@ struct SplitStage {
         float &x = v[unit][2 * pair], &y = v[unit][2 * pair + 1];
         if (part == 0) { x *= scale; y *= scale; }
         w[pair] = split::take_part(x, y);
-        if (pair == 3) *(uintx4*)(lds + part * kPart + octet_place(row(unit), octet())) = uintx4{w[0], w[1], w[2], w[3]};
+        if (pair == 3) *(uintx4*)(lds + part * kPart + octet_place(ALONG_K ? row(unit) : at + unit, octet())) = uintx4{w[0], w[1], w[2], w[3]};
     }
 };
 
