@@ -721,7 +721,7 @@ __global__ void __launch_bounds__(256, 2) k_gated_narrow(GatedNarrow G)
 {
     constexpr int kBytes = (int)narrow_bytes(STEPS);
     __shared__ __attribute__((aligned(16))) char lds[2][kBytes];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, one = lane & 15, octet = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), one = lane & 15, octet = lane >> 4;
     const long n0 = ((long)blockIdx.x * 4 + wave) * (16 * P);
     const int first = blockIdx.y * G.groups, all = (G.fo + 15) / 16, groups = all - first < G.groups ? all - first : G.groups;
     const char* from = G.packed + (long)first * kBytes + threadIdx.x * 16;
@@ -1270,7 +1270,7 @@ __global__ void __launch_bounds__(64 * kBackWaves, 3) k_gated_gw(GatedBack G, lo
     }
     constexpr int kBytes = TILES * 3 * 1024;
     __shared__ __attribute__((aligned(16))) char lds[2][kBytes];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, one = lane & 15, octet = lane >> 4, threads = waves * 64;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), one = lane & 15, octet = lane >> 4, threads = waves * 64;
     const long m = ((long)blockIdx.y * waves + wave) * 16 + one, half = AXIS ? G.fo : G.fo * G.positions;
     const long row = m < G.fo ? m : G.fo - 1, first = blockIdx.x * span, end = first + span < G.positions ? first + span : G.positions;
     const bool works = ((long)blockIdx.y * waves + wave) * 16 < G.fo;      // else it moves x alone; uniform
