@@ -740,6 +740,14 @@ def _line_extents(z, dim, h0, *others):
     return outer, shape[dim], count // (outer * shape[dim])
 
 
+def _expect_apart(results, operands):
+    """Pieces of a line are read and written side by side: a result that shares memory with anything else would be read half changed."""
+    spans = [(t.data_ptr(), t.data_ptr() + 4 * t.numel()) for t in results + operands if t is not None]
+    for i, (first, end) in enumerate(spans[:sum(t is not None for t in results)]):
+        if any(first < other_end and other < end for other, other_end in spans[i + 1:]):
+            raise ValueError("a result needs memory of its own")
+
+
 @functools.lru_cache(maxsize=1024)
 def recurrence_workspace_bytes(outer, length, inner):
     b = ctypes.c_size_t(0)
@@ -749,11 +757,14 @@ def recurrence_workspace_bytes(outer, length, inner):
 
 def recurrence_fwd(z, x, h0=None, dim=-1, reverse=False, out=None, stream=None):
     """h with h_t = f_t h_(t-1) + (1 - f_t) x_t, f = logistic(z), along a dimension, from the state h0 (the shape without that
-    dimension; None: zeros).  One step of a running sequence is a call on one step, with the last state as h0."""
+    dimension; None: zeros).  One step of a running sequence is a call on one step, with the last state as h0.  ``out`` (optional) receives h, in
+    memory of its own."""
     if stream is not None:          # what is made belongs to the stream that works on it
         with torch.cuda.stream(stream):
             return recurrence_fwd(z, x, h0, dim, reverse, out)
     outer, length, inner = _line_extents(z, dim, h0, x, out)
+    if out is not None:
+        _expect_apart((out,), (z, x, h0))
     (zp, xp, sp, _), on = _operands(z, x, h0, out)
     h = torch.empty_like(z) if out is None else out
     ws, at, need = _take_workspace(z, recurrence_workspace_bytes(outer, length, inner))
@@ -762,11 +773,14 @@ def recurrence_fwd(z, x, h0=None, dim=-1, reverse=False, out=None, stream=None):
 
 
 def recurrence_bwd(gh, z, x, h, h0=None, dim=-1, reverse=False, gz=None, gx=None, stream=None):
-    """(gz, gx, gh0) from the gradient of every h and the forward pass's operands and result; gh0 is None without h0."""
+    """(gz, gx, gh0) from the gradient of every h and the forward pass's operands and result; gh0 is None without h0.  ``gz`` and ``gx``
+    (optional) receive these, in memory of their own."""
     if stream is not None:          # what is made belongs to the stream that works on it
         with torch.cuda.stream(stream):
             return recurrence_bwd(gh, z, x, h, h0, dim, reverse, gz, gx)
     outer, length, inner = _line_extents(z, dim, h0, gh, x, h, gz, gx)
+    if gz is not None or gx is not None:
+        _expect_apart((gz, gx), (gh, z, x, h, h0))
     operands, on = _operands(gh, z, x, h, h0, gz, gx)
     gz = torch.empty_like(z) if gz is None else gz
     gx = torch.empty_like(x) if gx is None else gx

@@ -113,3 +113,25 @@ def test_gated_arguments(refused, match):
 def test_line_arguments(refused, match):
     with pytest.raises(ValueError, match=match):
         refused()
+
+
+# lines are cut into pieces that are worked on side by side: nothing may be written over what another piece reads
+STATES, ROWS = torch.zeros(40), torch.zeros(9, 5)
+
+
+@pytest.mark.parametrize("refused", [
+    lambda: znn.recurrence_fwd(X, X, out=X), lambda: znn.recurrence_fwd(ROWS[:4], torch.zeros(4, 5), out=ROWS[3:7]),
+    lambda: znn.recurrence_fwd(X, X, STATES[:4], out=STATES[2:22].view(4, 5)), lambda: znn.recurrence_bwd(X, X, X, X, gz=X),
+    lambda: znn.recurrence_bwd(X, X, X, X, gx=X), lambda: znn.recurrence_bwd(X, X, X, X, gz=ROWS[:4], gx=ROWS[3:7]),
+    lambda: znn.recurrence_bwd(X, X, X, ROWS[:4], gx=ROWS[1:5])])
+def test_results_that_share_memory_are_refused(refused):
+    with pytest.raises(ValueError, match="memory of its own"):
+        refused()
+
+
+def test_results_side_by_side_are_not():
+    a, b = ROWS[:4], ROWS[4:8]
+    with pytest.raises(ValueError, match="GPU"):        # as far as that
+        znn.recurrence_fwd(X, X, out=a)
+    with pytest.raises(ValueError, match="GPU"):
+        znn.recurrence_bwd(X, X, X, X, gz=a, gx=b)
