@@ -549,9 +549,9 @@ Split lines_split(const Lines& L, bool backward)
         S.way = ALONG;
         S.beside = 1;
         // Whole lines in a tile where they fill it, so that no tile waits for another, in the smaller one where that does: 144 000 lines of 60
-        // forward 24.6 us in tiles of 512, 27.7 of 2048; backward 44.9 and 48.6.
+        // forward 24.6 us in tiles of 512, 27.7 of 2048; backward 44.9 and 48.6.  A launch has fewer than 2^32 threads, and these take three or four steps each.
         S.chained = true;
-        for (int small = 1; small >= 0 && S.chained; --small) {
+        for (int small = steps < 1L << 33; small >= 0 && S.chained; --small) {
             S.quads = small ? 1 : 2;
             S.waves = small ? 2 : 4;
             const long most = 256 * S.quads * S.waves, whole = most / L.length * L.length;

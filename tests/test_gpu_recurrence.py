@@ -289,3 +289,34 @@ def test_states_are_handed_on_over_the_longest_lines(shape, reverse):
     assert np.abs(host(gh0) - q).max() <= 2 * tol
     gz[:, at], gx[:, at] = 0, 0
     assert not bool(gz.any()) and not bool(gx.any())
+
+
+# more steps than a launch of the smaller tiles has threads for, in short lines that are all alike but for some at either end and in the middle
+@pytest.mark.parametrize("length", [1, 500])
+def test_more_short_lines_than_threads(length):
+    lines = (1 << 34) // length         # an extent has no more
+    print("case", lines, length, flush=True)
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 10 * lines * length:
+        pytest.skip("not enough memory")
+    z = torch.full((lines, length), 0.75, device="cuda:0")
+    some = [0, 1, lines // 2, lines - 2, lines - 1]
+    for n in some:
+        z[n] = torch.linspace(-2, 2, length, device="cuda:0") + 0.01 * (n % 7)
+    h = znn.recurrence_fwd(z, z)
+    for n in some:
+        line = host(z[n])[None, :, None]
+        want, bound = gated.recurrence_fwd(line, line)
+        compare(host(h[n])[None, :, None], want, bound, n)
+    line = np.full((1, length, 1), 0.75)
+    want, bound = (torch.from_numpy(t[0, :, 0]).to("cuda:0") for t in gated.recurrence_fwd(line, line))
+    rows = (1 << 26) // length
+    for first in range(0, lines, rows):
+        last = min(lines, first + rows)
+        wrong = ((h[first:last].double() - want).abs() > bound).any(1)
+        for n in some:
+            if first <= n < last:
+                wrong[n - first] = False
+        assert not bool(wrong.any()), first
+    del z, h
+    torch.cuda.empty_cache()
