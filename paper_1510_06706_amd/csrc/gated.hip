@@ -891,12 +891,14 @@ __global__ void __launch_bounds__(128 * WI, WI / 2) k_product_split(Product G)
         }
 }
 
-// Sums of shares that several launches have left, in one: a workgroup takes `each` elements of one of them.  A few shares are added in their order, four
-// neighbours a thread; of many, every sixteenth by one wave, and then these in their order.
+// Sums of shares that several launches have left, in one.  A few shares, or those of many elements, are added in their order, four neighbours a
+// thread; of many shares every sixteenth by one wave, and then these in their order.  That takes sixteen threads an element, where a launch has fewer than 2^32.
 struct SharedSum { const float* parts; float* out; long count; int shares; unsigned first; };     // first workgroup
 struct SharedSums { SharedSum of[3]; int n; };
 constexpr int kFewShares = 16;
-constexpr long elements_of(int shares) { return shares > kFewShares ? 64 : 4096; }
+__host__ __device__ constexpr bool in_order(const SharedSum& S) { return S.shares <= kFewShares || S.count >= 1L << 24; }
+// workgroups
+unsigned blocks_of(const SharedSum& S) { return (unsigned)((S.count + (in_order(S) ? 4095 : 63)) / (in_order(S) ? 4096 : 64)); }
 
 __global__ void __launch_bounds__(1024) k_sum_shares(SharedSums A)
 {
@@ -905,7 +907,7 @@ __global__ void __launch_bounds__(1024) k_sum_shares(SharedSums A)
     while (which + 1 < A.n && blockIdx.x >= A.of[which + 1].first) ++which;       // uniform
     const SharedSum S = A.of[which];
     const long block = blockIdx.x - S.first;
-    if (S.shares <= kFewShares) {
+    if (in_order(S)) {
         const long e = block * 4096 + threadIdx.x * 4;
         if (e >= S.count) return;
         const int most = S.count - e < 4 ? (int)(S.count - e) : 4;
@@ -1481,19 +1483,14 @@ size_t product_bytes(const Layout& L, long I, long J) { return L.shares > 1 ? al
 void add_shares(SharedSums& A, const float* parts, float* out, long count, int shares)
 {
     if (shares <= 1) return;
-    unsigned first = 0;
-    if (A.n) {
-        const SharedSum& last = A.of[A.n - 1];
-        first = last.first + (unsigned)((last.count + elements_of(last.shares) - 1) / elements_of(last.shares));
-    }
+    const unsigned first = A.n ? A.of[A.n - 1].first + blocks_of(A.of[A.n - 1]) : 0;
     A.of[A.n++] = SharedSum{parts, out, count, shares, first};
 }
 void sum_shares(const SharedSums& A, hipStream_t s)
 {
     if (!A.n) return;
     const SharedSum& last = A.of[A.n - 1];
-    const unsigned blocks = last.first + (unsigned)((last.count + elements_of(last.shares) - 1) / elements_of(last.shares));
-    ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3(blocks), dim3(1024), 0, A);
+    ZNN_LAUNCH("gated unit shares", s, k_sum_shares, dim3(last.first + blocks_of(last)), dim3(1024), 0, A);
 }
 // Few features in: taken apart in registers where enough positions keep the chip busy.
 constexpr int narrow_steps(int f) { return f <= kNarrowSteps * kDepth ? (f + kDepth - 1) / kDepth : 0; }

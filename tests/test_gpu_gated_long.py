@@ -51,3 +51,24 @@ def test_last_positions_and_sums_over_all(f, fo, n, axis):
     bound = (16 + gated._sum_bound(n)) * gated.HALF
     assert bool(((gw.double() - sums[0]).abs() <= bound * sums[2]).all())
     assert bool(((gb.double() - sums[1]).abs() <= bound * sums[3]).all())
+
+
+# shares of a sum over more than 17 * 2^16 positions, of 2^24 elements
+def test_gradients_of_many_weights_over_many_positions():
+    f, fo, n = 2048, 4096, 17 * 65536 + 1
+    gen = torch.Generator(device="cuda:0").manual_seed(6)
+    x, kept, gy = (torch.randn((n, k), generator=gen, device="cuda:0") for k in (f, 2 * fo, fo))
+    w = torch.randn((2 * fo, f), generator=gen, device="cuda:0")
+    _, gw, gb = znn.gated_bwd(gy, x, w, kept, "silu", 1, need_gx=False)
+    some = torch.tensor([0, 1, 777, fo - 1], device="cuda:0")
+    k, v, g = kept[:, some].double(), kept[:, some + fo].double(), gy[:, some].double()
+    a, d = silu(k)
+    sums, sizes = torch.zeros((8, f), dtype=torch.float64, device="cuda:0"), torch.zeros((8, f), dtype=torch.float64, device="cuda:0")
+    grad, size = torch.cat([g * v * d, g * a], 1), torch.cat([(g * v).abs() * (d.abs() + 1), g.abs() * (a.abs() + k.abs().clamp(max=1))], 1)
+    for first in range(0, n, 1 << 18):
+        part = x[first:first + (1 << 18)].double()
+        sums += grad[first:first + (1 << 18)].t() @ part
+        sizes += size[first:first + (1 << 18)].t() @ part.abs()
+    bound, rows = (16 + gated._sum_bound(n)) * gated.HALF, torch.cat([some, some + fo])
+    assert bool(((gw[rows].double() - sums).abs() <= bound * sizes).all())
+    assert bool(((gb[rows].double() - grad.sum(0)).abs() <= bound * size.sum(0)).all())
