@@ -1306,14 +1306,23 @@ __global__ void __launch_bounds__(64 * kBackWaves, 3) k_gated_gw(GatedBack G, lo
                 *(floatx4*)(u + e) = *(const floatu4*)(G.kept + at + e);
                 *(floatx4*)(v + e) = *(const floatu4*)(G.kept + half + at + e);
             }
+        } else if (whole) {
+            const float *const ys = G.gy + n * G.fo + row, *const us = G.kept + n * 2 * G.fo + row;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                gy[e] = ys[e * (long)G.fo];
+                u[e] = us[e * 2L * G.fo];
+                v[e] = us[e * 2L * G.fo + half];
+            }
         } else
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const long k = n + e < end ? n + e : end - 1;
-                gy[e] = G.gy[AXIS ? k * G.fo + row : row * G.positions + k];
-                const long at = AXIS ? k * 2 * G.fo + row : row * G.positions + k;
-                u[e] = G.kept[at];
-                v[e] = G.kept[half + at];
+                // positions behind the last one: zeros, whose gradients are zeros
+                const bool there = n + e < end;
+                const long k = there ? n + e : end - 1, at = AXIS ? k * 2 * G.fo + row : row * G.positions + k;
+                gy[e] = there ? G.gy[AXIS ? k * G.fo + row : row * G.positions + k] : 0.f;
+                u[e] = there ? G.kept[at] : 0.f;
+                v[e] = there ? G.kept[half + at] : 0.f;
             }
     };
     auto store = [&](char* to) {
@@ -1347,8 +1356,7 @@ __global__ void __launch_bounds__(64 * kBackWaves, 3) k_gated_gw(GatedBack G, lo
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const Gated a = gate_fn<fn.value>(u[e]);
-                    const bool there = n0 + octet * 8 + e < end;
-                    const float du = there ? gy[e] * v[e] * a.d : 0.f, dv = there ? gy[e] * a.a : 0.f;
+                    const float du = gy[e] * v[e] * a.d, dv = gy[e] * a.a;
                     su += du;
                     sv += dv;
                     g[0][e] = du * (sign * split::kScale);
@@ -1555,9 +1563,10 @@ BiasShares bias_shares(const Shape& S)
     return BiasShares{(int)((S.positions + span - 1) / span), span};
 }
 
-// Backward with du and dv made where they are used.  us, so and by products of all of du and dv: maps 10 -> 20 at 4000 positions 35.4 and 33.9, at 12 000
-// 31.8 and 36.7, at 300 000 88.6 and 124; 40 -> 80 at 12 000 49.2 and 54.1, at 300 000 263 and 292; 64 -> 128 at 36 000 83.5 and 82.3, at 100 000 137
-// and 165; rows of 40 -> 80 at 12 000 49.2 and 70.4, at 300 000 265 and 406.  128 inputs take registers that more waves would need: 859 and 804 at 300 000.
+// Backward with du and dv made where they are used.  us, so and by products of all of du and dv: maps 10 -> 20 at 4000 positions 29.7 and 23.6, at 12 000
+// 26.7 and 23.8, at 300 000 75.7 and 120; 40 -> 80 at 4000 42.1 and 25.7, at 12 000 43.1 and 46.2, at 300 000 232 and 299; 64 -> 128 at 36 000 75.6 and 73.9, at
+// 100 000 122 and 146; rows of 40 -> 80 at 4000 42.4 and 29.2, at 12 000 40.9 and 50.2, at 300 000 226 and 332; of 64 -> 128 at 12 000 53.0 and 54.6.  128 inputs take
+// registers that more waves would need: 859 and 804 at 300 000.
 bool takes_narrow_back(const Shape& S)
 {
     return S.f <= 64 && S.positions >= 8192 && (S.axis || S.f <= 48 || S.positions >= 65536);
