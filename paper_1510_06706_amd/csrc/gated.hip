@@ -31,7 +31,7 @@ __device__ __forceinline__ Gated gate_fn(float u)
     }
     const float finite = __builtin_amdgcn_fmed3f(u, -kLargestFloat, kLargestFloat);
     if (FN == ZNN_GATE_GELU) {
-        const float p = 0.5f * erfcf(-0.707106781f * finite);
+        const float p = 0.5f * erfcf(-0.707106781f * u);       // NaN comes from here: `finite` has a number in its place
         return Gated{u > 0.f ? u * p : finite * p, fmaf(finite, 0.398942280f * expf(-0.5f * finite * finite), p)};
     }
     const Gate g = gate(u);
