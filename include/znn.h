@@ -370,8 +370,8 @@ int  znn_gated_bwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t position
  * znn_recurrence_bwd : from gh, the gradient of every h_t, with G_t = gh_t + f_(t+1) G_(t+1):
  *     gz = G_t (h_(t-1) - x_t) f_t (1 - f_t),  gx = G_t (1 - f_t),  gh0 = f_1 G_1 (may be NULL),
  *   0 where a factor f_t or 1 - f_t is 0, whatever the others hold.
- * A line is taken in pieces that follow from the extents alone: results repeat themselves to the bit.  Where the gates since a step have multiplied to
- * less than 2^-126, what is left of the state that they met is known to 2^-149 of its size then.
+ * A line is taken in pieces that follow from the extents alone: results repeat themselves to the bit.  Where a factor f_t or 1 - f_t, or what the gates since a
+ * step have multiplied to, is less than 2^-126, what is left of the operand or state that it met is known to 2^-149 of its size then.
  * The calls take a workspace of znn_recurrence_workspace_bytes (256-byte aligned; may be NULL if that is 0).
  * ZNN_EUNSUPPORTED: more than 2^34 elements along an extent, or more than 2^38 in all.
  */
