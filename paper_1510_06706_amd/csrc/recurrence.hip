@@ -168,10 +168,13 @@ __global__ void __launch_bounds__(64 * kMostWaves) k_lines_across(LinesFwd A, Ac
         if (i < n) *ph = h = times(f[i], h) + b[i];
 }
 
-// What flows backwards is q_t = f_t G_t with G_t = gh_t + q_(t+1): the factors of a step are its own.
+// What flows backwards is q_t = f_t G_t with G_t = gh_t + q_(t+1): the factors of a step are its own.  Of G and the difference the larger one is multiplied by f (1 - f)
+// first: their product may leave the range where gz does not.
 __device__ __forceinline__ float grads(const Gate& g, float G, float before, float x, float& gz)
 {
-    gz = g.f == 0.f || g.k == 0.f ? 0.f : G * (before - x) * (g.f * g.k);
+    const float d = before - x;
+    const bool swap = fabsf(G) > fabsf(d);
+    gz = g.f == 0.f || g.k == 0.f ? 0.f : (swap ? G : d) * (g.f * g.k) * (swap ? d : G);
     return times(g.k, G);
 }
 
