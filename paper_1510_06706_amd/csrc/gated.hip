@@ -9,7 +9,8 @@
 namespace znn {
 namespace {
 
-struct Gated { float a, d; };       // fn(u) and its derivative
+// fn(u) and its derivative.  That is 1.13 at most, so du = gy (v d) takes it first: gy v may leave the range where du does not, and is no number times a d of 0 then.
+struct Gated { float a, d; };
 
 constexpr float kLargestFloat = 3.402823466e38f;
 
@@ -949,7 +950,7 @@ __device__ __forceinline__ void gradients(int fn, const floatx4& u, const floatx
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const Gated a = gate_fn<number.value>(u[c]);
-            du[c] = gy[c] * v[c] * a.d;
+            du[c] = gy[c] * (v[c] * a.d);
             dv[c] = gy[c] * a.a;
         }
     });
@@ -1028,7 +1029,7 @@ template <int AXIS> __device__ __forceinline__ void gradient_of(const GatedBack&
     const float gy = G.gy[at], v = G.kept[kept + half], u = G.kept[kept];
     with_fn(G.fn, [&](auto fn) {
         const Gated a = gate_fn<fn.value>(u);
-        du = gy * v * a.d;
+        du = gy * (v * a.d);
         dv = gy * a.a;
     });
 }
@@ -1183,7 +1184,7 @@ __global__ void __launch_bounds__(256, 2) k_gated_gx(GatedBack G, const char* pa
                     for (int r = 0; r < 4; ++r) {
                         const Gated a = gate_fn<fn.value>(raw.u[r][p]);
                         const bool there = group * 16 + octet * 4 + r < G.fo;
-                        g[p][r] = there ? raw.gy[r][p] * raw.v[r][p] * a.d * split::kScale : 0.f;
+                        g[p][r] = there ? raw.gy[r][p] * (raw.v[r][p] * a.d) * split::kScale : 0.f;
                         g[p][r + 4] = there ? raw.gy[r][p] * a.a * split::kScale : 0.f;
                     }
             });
@@ -1356,7 +1357,7 @@ __global__ void __launch_bounds__(64 * kBackWaves, 3) k_gated_gw(GatedBack G, lo
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const Gated a = gate_fn<fn.value>(u[e]);
-                    const float du = gy[e] * v[e] * a.d, dv = gy[e] * a.a;
+                    const float du = gy[e] * (v[e] * a.d), dv = gy[e] * a.a;
                     su += du;
                     sv += dv;
                     g[0][e] = du * (sign * split::kScale);
