@@ -552,9 +552,10 @@ Split lines_split(const Lines& L, bool backward)
         S.way = ALONG;
         S.beside = 1;
         // Whole lines in a tile where they fill it, so that no tile waits for another, in the smaller one where that does: 144 000 lines of 60
-        // forward 24.6 us in tiles of 512, 27.7 of 2048; backward 44.9 and 48.6.  A launch has fewer than 2^32 threads, and these take three or four steps each.
+        // forward 24.6 us in tiles of 512, 27.7 of 2048; backward 44.9 and 48.6.  A launch has fewer than 2^32 threads, and these take three or four steps each, six to
+        // eight in the larger tiles.
         S.chained = true;
-        for (int small = steps < 1L << 33; small >= 0 && S.chained; --small) {
+        for (int small = steps < 1L << 33; small >= 0 && S.chained && steps <= 1L << 34; --small) {
             S.quads = small ? 1 : 2;
             S.waves = small ? 2 : 4;
             const long most = 256 * S.quads * S.waves, whole = most / L.length * L.length;
@@ -618,22 +619,34 @@ Along along(const Lines& L, const Split& S, const Chain& C)
     return Along{L.outer * L.length, S.tile, make_fastdiv((unsigned)std::min(L.length, (long)kFarOff)), C};
 }
 
+// launch(grid, block) for all workgroups of a split.  A launch has fewer than 2^32 threads; pieces of lines may need more, as lines across fill up to whole waves
+// (2^31 steps of two lines are 2^32 threads): the next launch goes on where the tickets of the last one end.
+template <class Launch>
+void for_all_pieces(const Split& S, Launch launch)
+{
+    const dim3 block(64 * S.waves * S.beside);
+    const long all = S.groups * S.pieces, most = S.chained ? (1L << 31) / block.x : all;
+    for (long first = 0; first < all; first += most) launch(dim3((unsigned)std::min(all - first, most)), block);
+}
+
 int lines_fwd(const LinesFwd& A, void* ws, hipStream_t s)
 {
     const Split S = lines_split(A.L, false);
     Chain C;
     const int rc = begin_lines(S, ws, &C, s);
     if (rc != ZNN_OK) return rc;
-    const dim3 grid((unsigned)(S.groups * S.pieces)), block(64 * S.waves * S.beside);
     if (S.way == ALONG) {
         const Along T = along(A.L, S, C);
-        if (S.waves == 2) ZNN_LAUNCH("recurrence forward", s, (k_lines_along<1, 2>), grid, block, 0, A, T);
-        else if (S.waves == 4) ZNN_LAUNCH("recurrence forward", s, (k_lines_along<2, 4>), grid, block, 0, A, T);
-        else if (S.waves == 8) ZNN_LAUNCH("recurrence forward", s, (k_lines_along<4, 8>), grid, block, 0, A, T);
-        else ZNN_LAUNCH("recurrence forward", s, (k_lines_along<4, 16>), grid, block, 0, A, T);
-    } else if (S.way == ACROSS)
-        ZNN_LAUNCH("recurrence forward", s, k_lines_across<kSteps>, grid, block, 0, A, Across{(unsigned)S.groups, (unsigned)S.pieces, S.waves, S.beside, C});
-    else ZNN_LAUNCH("recurrence forward", s, k_lines_walk<8>, dim3(walk_groups(A.L)), dim3(256), 0, A);
+        for_all_pieces(S, [&](dim3 grid, dim3 block) {
+            if (S.waves == 2) ZNN_LAUNCH("recurrence forward", s, (k_lines_along<1, 2>), grid, block, 0, A, T);
+            else if (S.waves == 4) ZNN_LAUNCH("recurrence forward", s, (k_lines_along<2, 4>), grid, block, 0, A, T);
+            else if (S.waves == 8) ZNN_LAUNCH("recurrence forward", s, (k_lines_along<4, 8>), grid, block, 0, A, T);
+            else ZNN_LAUNCH("recurrence forward", s, (k_lines_along<4, 16>), grid, block, 0, A, T);
+        });
+    } else if (S.way == ACROSS) {
+        const Across T = {(unsigned)S.groups, (unsigned)S.pieces, S.waves, S.beside, C};
+        for_all_pieces(S, [&](dim3 grid, dim3 block) { ZNN_LAUNCH("recurrence forward", s, k_lines_across<kSteps>, grid, block, 0, A, T); });
+    } else ZNN_LAUNCH("recurrence forward", s, k_lines_walk<8>, dim3(walk_groups(A.L)), dim3(256), 0, A);
     return check_launch("recurrence forward");
 }
 
@@ -643,16 +656,18 @@ int lines_bwd(const LinesBwd& A, void* ws, hipStream_t s)
     Chain C;
     const int rc = begin_lines(S, ws, &C, s);
     if (rc != ZNN_OK) return rc;
-    const dim3 grid((unsigned)(S.groups * S.pieces)), block(64 * S.waves * S.beside);
     if (S.way == ALONG) {
         const Along T = along(A.L, S, C);
-        if (S.waves == 2) ZNN_LAUNCH("recurrence backward", s, (k_lines_along_bwd<1, 2>), grid, block, 0, A, T);
-        else if (S.waves == 4) ZNN_LAUNCH("recurrence backward", s, (k_lines_along_bwd<2, 4>), grid, block, 0, A, T);
-        else if (S.waves == 8) ZNN_LAUNCH("recurrence backward", s, (k_lines_along_bwd<2, 8>), grid, block, 0, A, T);
-        else ZNN_LAUNCH("recurrence backward", s, (k_lines_along_bwd<4, 16>), grid, block, 0, A, T);
-    } else if (S.way == ACROSS)
-        ZNN_LAUNCH("recurrence backward", s, k_lines_across_bwd<kStepsBwd>, grid, block, 0, A, Across{(unsigned)S.groups, (unsigned)S.pieces, S.waves, S.beside, C});
-    else ZNN_LAUNCH("recurrence backward", s, k_lines_walk_bwd<4>, dim3(walk_groups(A.L)), dim3(256), 0, A);
+        for_all_pieces(S, [&](dim3 grid, dim3 block) {
+            if (S.waves == 2) ZNN_LAUNCH("recurrence backward", s, (k_lines_along_bwd<1, 2>), grid, block, 0, A, T);
+            else if (S.waves == 4) ZNN_LAUNCH("recurrence backward", s, (k_lines_along_bwd<2, 4>), grid, block, 0, A, T);
+            else if (S.waves == 8) ZNN_LAUNCH("recurrence backward", s, (k_lines_along_bwd<2, 8>), grid, block, 0, A, T);
+            else ZNN_LAUNCH("recurrence backward", s, (k_lines_along_bwd<4, 16>), grid, block, 0, A, T);
+        });
+    } else if (S.way == ACROSS) {
+        const Across T = {(unsigned)S.groups, (unsigned)S.pieces, S.waves, S.beside, C};
+        for_all_pieces(S, [&](dim3 grid, dim3 block) { ZNN_LAUNCH("recurrence backward", s, k_lines_across_bwd<kStepsBwd>, grid, block, 0, A, T); });
+    } else ZNN_LAUNCH("recurrence backward", s, k_lines_walk_bwd<4>, dim3(walk_groups(A.L)), dim3(256), 0, A);
     return check_launch("recurrence backward");
 }
 
