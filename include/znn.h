@@ -342,6 +342,7 @@ int  znn_residual_norm_bwd(int64_t rows, int64_t cols, int32_t axis, double p, c
  *   gx may be NULL where nothing reads it, gb where there is no bias.
  * Sums are taken in fp32 in an order that follows from the extents alone: results repeat themselves to the bit.
  * Functions at infinity are their limits (SiLU and GELU are 0 at minus infinity); the rectifier is 0 at NaN, as its transfer function is.
+ * A result that shares memory with an operand or another result is refused with ZNN_EINVAL.
  * The calls take a workspace of znn_gated_workspace_bytes for their pass (ZNN_PASS_FWD or ZNN_PASS_BWD; 256-byte aligned; may be
  * NULL if that is 0).  ZNN_EUNSUPPORTED: more than 2^20 features on either side, more than 2^31 - 1 positions, or
  * more than 2^38 elements of an array.
@@ -372,6 +373,8 @@ int  znn_gated_bwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t position
  *   0 where a factor f_t or 1 - f_t is 0, whatever the others hold.
  * A line is taken in pieces that follow from the extents alone: results repeat themselves to the bit.  Where a factor f_t or 1 - f_t, or what the gates since a
  * step have multiplied to, is less than 2^-126, what is left of the operand or state that it met is known to 2^-149 of its size then.
+ * A result that shares memory with an operand (a state among them) or another result is refused with ZNN_EINVAL: pieces of a line are read and written side by
+ * side.
  * The calls take a workspace of znn_recurrence_workspace_bytes (256-byte aligned; may be NULL if that is 0).
  * ZNN_EUNSUPPORTED: more than 2^34 elements along an extent, or more than 2^38 in all.
  */

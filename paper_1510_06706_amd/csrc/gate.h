@@ -1,7 +1,9 @@
-// The logistic function of a gate, for the gated recurrence and the gated unit.
+// What the gated recurrence and the gated unit share: the logistic function of a gate, and the check that results have memory of their own.
 #pragma once
 
 #include "znn_internal.h"
+
+#include <initializer_list>
 
 namespace znn {
 
@@ -17,6 +19,24 @@ __device__ __forceinline__ Gate gate(float z)
     const float r = fmaf(m, -1.92596299e-8f, fmaf(m, -1.44269502f, -n)), e = __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(r), (int)n);
     const float d = 1.f + e, guess = __builtin_amdgcn_rcpf(d), large = fmaf(fmaf(-d, guess, 1.f), guess, guess), small = e * large;
     return z < 0.f ? Gate{small, large} : Gate{large, small};
+}
+
+// Results are written while operands are read, by other workgroups among them: one that shares memory with an operand or another result would change it
+// on the way.  Arrays that are not there are NULL.
+struct Span { const void* first; int64_t floats; };
+inline int check_apart(std::initializer_list<Span> results, std::initializer_list<Span> operands)
+{
+    auto share = [](const Span& a, const Span& b) {
+        const uintptr_t p = (uintptr_t)a.first, q = (uintptr_t)b.first;
+        return p && q && p < q + 4 * (uintptr_t)b.floats && q < p + 4 * (uintptr_t)a.floats;
+    };
+    for (const Span* r = results.begin(); r != results.end(); ++r) {
+        for (const Span* other = r + 1; other != results.end(); ++other)
+            if (share(*r, *other)) return fail(ZNN_EINVAL, "two results share memory");
+        for (const Span& o : operands)
+            if (share(*r, o)) return fail(ZNN_EINVAL, "a result shares memory with an operand");
+    }
+    return ZNN_OK;
 }
 
 }  // namespace znn

@@ -1796,6 +1796,8 @@ int znn_gated_fwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t positions
     const Shape S = {fan_in, fan_out, axis, (long)positions};
     const Forward F = forward_of(S);
     rc = check_gated_call(fn, F.bytes, ws, ws_bytes);
+    const int64_t f = fan_in, both = 2LL * fan_out;
+    if (rc == ZNN_OK) rc = check_apart({{y, fan_out * positions}, {kept, both * positions}}, {{x, f * positions}, {w, both * f}, {b, both}});
     if (rc != ZNN_OK) return rc;
     return gated_fwd(S, F, fn, x, w, b, y, kept, (char*)ws, (hipStream_t)stream);
 }
@@ -1809,6 +1811,10 @@ int znn_gated_bwd(int32_t fn, int32_t fan_in, int32_t fan_out, int64_t positions
     const Shape S = {fan_in, fan_out, axis, (long)positions};
     const Backward B = backward_of(S);
     rc = check_gated_call(fn, B.bytes, ws, ws_bytes);
+    const int64_t f = fan_in, both = 2LL * fan_out;
+    if (rc == ZNN_OK)
+        rc = check_apart({{gx, f * positions}, {gw, both * f}, {gb, both}},
+                         {{gy, fan_out * positions}, {x, f * positions}, {w, both * f}, {kept, both * positions}});
     if (rc != ZNN_OK) return rc;
     return gated_bwd(S, B, fn, gy, x, w, kept, gx, gw, gb, (char*)ws, (hipStream_t)stream);
 }

@@ -716,6 +716,8 @@ int znn_recurrence_fwd(int64_t outer, int64_t length, int64_t inner, int32_t rev
     if (!z || !x || !h) return fail(ZNN_EINVAL, "NULL argument");
     const LinesFwd A = {{(long)outer, (long)length, (long)inner}, reverse != 0, z, x, h0, h};
     rc = check_lines_workspace(A.L, ws, ws_bytes);
+    const int64_t lines = outer * inner, all = lines * length;
+    if (rc == ZNN_OK) rc = check_apart({{h, all}}, {{z, all}, {x, all}, {h0, lines}});
     if (rc != ZNN_OK) return rc;
     return lines_fwd(A, ws, (hipStream_t)stream);
 }
@@ -728,6 +730,8 @@ int znn_recurrence_bwd(int64_t outer, int64_t length, int64_t inner, int32_t rev
     if (!gh || !z || !x || !h || !gz || !gx) return fail(ZNN_EINVAL, "NULL argument");
     const LinesBwd A = {{(long)outer, (long)length, (long)inner}, reverse == 0, gh, z, x, h, h0, gz, gx, gh0};
     rc = check_lines_workspace(A.L, ws, ws_bytes);
+    const int64_t lines = outer * inner, all = lines * length;
+    if (rc == ZNN_OK) rc = check_apart({{gz, all}, {gx, all}, {gh0, lines}}, {{gh, all}, {z, all}, {x, all}, {h, all}, {h0, lines}});
     if (rc != ZNN_OK) return rc;
     return lines_bwd(A, ws, (hipStream_t)stream);
 }
