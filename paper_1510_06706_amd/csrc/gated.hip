@@ -968,9 +968,12 @@ __global__ void __launch_bounds__(256) k_gated_grads_maps(Grads G)
         const floatx4 u = load4(G.kept + at + n, most), v = load4(G.kept + at + other + n, most), gy = load4(G.gy + at + n, most);
         floatx4 du, dv;
         gradients(G.fn, u, v, gy, du, dv);
+        float tu = 0.f, tv = 0.f;
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-            if (c < most) { su += du[c]; sv += dv[c]; }
+            if (c < most) { tu += du[c]; tv += dv[c]; }
+        su += tu;
+        sv += tv;
         store4(G.g + at + n, du, most);
         store4(G.g + at + other + n, dv, most);
     }
@@ -1354,15 +1357,18 @@ __global__ void __launch_bounds__(64 * kBackWaves, 3) k_gated_gw(GatedBack G, lo
         float g[2][8];
         if (works)
             with_fn(G.fn, [&](auto fn) {
+                float tu = 0.f, tv = 0.f;       // a step by itself: chains of 8, and of one number a step (span / 32 at most 2048)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const Gated a = gate_fn<fn.value>(u[e]);
                     const float du = gy[e] * (v[e] * a.d), dv = gy[e] * a.a;
-                    su += du;
-                    sv += dv;
+                    tu += du;
+                    tv += dv;
                     g[0][e] = du * (sign * split::kScale);
                     g[1][e] = dv * (sign * split::kScale);
                 }
+                su += tu;
+                sv += tv;
             });
         const bool more = n0 + kDepth < end;
         if (more) load(n0 + kDepth);
@@ -1554,12 +1560,14 @@ int product(const Layout& L, const Operand& A, const Operand& B, long I, long J,
     return check_launch("gated unit product");
 }
 
-// Shares of the biases' sums
+// Shares of the biases' sums.  A thread adds up 1024 numbers one after another, each of one position (rows, up to 2^28 of them) or four (images), and no more: roundings of
+// terms that are alike do not cancel.
 struct BiasShares { int count; long span; };
 BiasShares bias_shares(const Shape& S)
 {
-    const long across = S.axis ? (S.fo + 255) / 256 : S.fo, least = S.axis ? 32 : 1024;
-    const long count = std::max(1L, std::min({8 * kUnits / across + 1, (S.positions + least - 1) / least, 1L << 15}));
+    const long across = S.axis ? (S.fo + 255) / 256 : S.fo, least = S.axis ? 32 : 1024, most = S.axis ? 4 * 1024 : 1024 * 1024;
+    const long wanted = std::min(8 * kUnits / across + 1, (S.positions + least - 1) / least);
+    const long count = std::min(std::max(wanted, (S.positions + most - 1) / most), 65535L);
     const long span = ((S.positions + count - 1) / count + 31) / 32 * 32;
     return BiasShares{(int)((S.positions + span - 1) / span), span};
 }
@@ -1582,9 +1590,9 @@ NarrowBack narrow_back(const Shape& S)
     N.tiles = tiles;
     N.groups = (unsigned)((features + kBackWaves - 1) / kBackWaves);
     N.waves = std::max((int)((features + N.groups - 1) / N.groups), (N.tiles + 1) / 2);
-    // what a chip holds at once: 40 -> 80 maps of 61 x 58 x 63 95 us, 108 with two thirds of that
+    // what a chip holds at once: 40 -> 80 maps of 61 x 58 x 63 95 us, 108 with two thirds of that; and sums of 2^16 positions at most, where many features leave few shares
     const long wanted = std::max(1L, kUnits * (12 / N.waves) / (long)N.groups), steps = (S.positions + kDepth - 1) / kDepth;
-    const long each = std::max(8L, (steps + wanted - 1) / wanted);
+    const long each = std::min(std::max(8L, (steps + wanted - 1) / wanted), kMostSpan / kDepth);
     N.span = each * kDepth;
     N.shares = (int)((S.positions + N.span - 1) / N.span);
     return N;
