@@ -72,6 +72,7 @@ class ResidualNet:
                  device="cuda:0", branches=None, gate="silu"):
         self.maps, self.blocks, self.p, self.fn, self.eps = maps, blocks, float(p), fn, eps
         self.kinds, self.gate = _kinds(blocks, branches), gate
+        znn._gate_number(gate)       # refuses what is no gate function before anything is made
         self.extents, self.device = tuple(extents), device
         self.params = {k: torch.from_numpy(np.ascontiguousarray(v)).to(device) for k, v in params.items()}
         self.random = znn.random_state(seed, device)
