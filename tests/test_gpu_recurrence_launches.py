@@ -1,4 +1,5 @@
-"""Lines across whose pieces need more threads than one launch has: every element, over operands that repeat themselves."""
+"""Lines across whose pieces need more threads than one launch has, and lines of more than 2^30 steps along: every element, over operands
+that repeat themselves."""
 import numpy as np
 import pytest
 import torch
@@ -40,7 +41,7 @@ def room(elements):
 
 # 64 lanes a wave whatever the lines are: 2^32 threads and more forward, and in launches side by side
 @pytest.mark.parametrize("reverse", [False, True])
-@pytest.mark.parametrize("periods,inner", [((1 << 19) + 1, 2), ((1 << 17) + 1, 3)])
+@pytest.mark.parametrize("periods,inner", [((1 << 19) + 1, 2), ((1 << 17) + 1, 3), ((1 << 19) + 1, 1)])
 def test_forward(periods, inner, reverse):
     print("case", periods, inner, reverse, flush=True)
     room(5 * periods * PERIOD * inner)
@@ -54,7 +55,7 @@ def test_forward(periods, inner, reverse):
 
 
 @pytest.mark.parametrize("reverse", [False, True])
-@pytest.mark.parametrize("periods,inner", [((1 << 18) + 1, 2), ((1 << 16) + 1, 3)])
+@pytest.mark.parametrize("periods,inner", [((1 << 18) + 1, 2), ((1 << 16) + 1, 3), ((1 << 18) + 1, 1)])
 def test_backward(periods, inner, reverse):
     print("case", periods, inner, reverse, flush=True)
     room(8 * periods * PERIOD * inner)
