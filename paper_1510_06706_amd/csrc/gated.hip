@@ -222,7 +222,8 @@ __device__ __forceinline__ TilePlace tile_place(const Tiles& T, unsigned number)
 // shared memory, [part][row][32 k], of which there are two: while one step is multiplied, the next one is taken apart between its instructions, a
 // pair of values at a time, and the loads of the one behind it are issued as soon as registers are free for them.
 // Results lie with their rows (the instruction's first operand) along j, so that a lane has four neighbours of a row of C.
-// Bound by the matrix cores, 56 to 60 % busy at 1.9 GHz: 8192 x 1024 from 8192 terms in 630 us, 218 TFLOP/s of fp32 work; vector instructions take half of the time beside.
+// Bound by the matrix cores, 56 to 60 % busy at 1.9 GHz: 8192 x 1024 from 8192 terms in 630 to 670 us as the card's clock has it, 205 to 218 TFLOP/s of fp32 work; vector
+// instructions take half of the time beside.
 
 constexpr int kSplitColumns = 128, kSplitWaves = 4;     // rows of waves
 
@@ -621,7 +622,10 @@ __global__ void __launch_bounds__(128 * WI, WI / 2) k_gated_fwd_split(GatedFwd G
 
 // ---------------------------------------------------------------- few positions
 // Every weight is read for a few products only, so that their bytes are all there is: a wave takes one feature, lanes quads of its two rows of weights, and N
-// positions at once.  One row of 1024 -> 4096 5.3 us (33.6 MB from the last level cache), 8 rows 13, 32 rows 41 (50 by tiles).
+// positions at once.  One row of 1024 -> 4096 5.3 us (33.6 MB from the last level cache).  All weights are read once for eight positions, and images are read a feature
+// at a time; us of kernels, so and by the shares that forward_of has for more positions: rows of 1024 -> 4096, 4 of them 6.8 and 17.7, 8 12.4 and 17.7, 9 22.1 and 17.8, 32 40.6
+// and 18.6; maps, 4 positions 8.1 and 18.8, 8 20.2 and 19.3, 32 69.3 and 21.6; rows of 256 -> 512, 8 of them 4.5 and 13.8, 32 5.6 and 14.3; maps the same.  The limit of 32
+// is right for few weights and not for many, from 9 positions on.
 
 __device__ __forceinline__ float sum_lanes(float v)
 {
@@ -690,7 +694,8 @@ __global__ void __launch_bounds__(256) k_gated_few(GatedFew G)
 // ---------------------------------------------------------------- few features in, many positions
 // Up to 128 features of a position are taken apart once and stay in registers, 16 P positions a wave; weights, taken apart beforehand, pass through
 // shared memory, 16 features (both halves) at a time, and every wave multiplies all of them.  Nothing of x is read or taken apart twice, and a step's results are
-// finished while the other workgroup of the unit multiplies.  120 -> 240 maps of 96^3 705 us (143 TFLOP/s, 1.8 TB/s; 1380 by tiles); 40 -> 80 of 64^3, kept, 61 us (4.8 TB/s).
+// finished while the other workgroup of the unit multiplies.  Over images the biases of a group are read where they are added, four pairs one after another.  120 -> 240 maps
+// of 96^3 700 to 740 us (141 TFLOP/s, 1.8 TB/s; 1380 by tiles); 40 -> 80 of 64^3, kept, 61 us (4.8 TB/s).
 
 // Weights in the order they are read: [16 features][half][step of 32 k][part][lane] of 16 bytes.  Every second step has its sign changed.
 constexpr int kNarrowSteps = 4;
@@ -1110,8 +1115,9 @@ __device__ __forceinline__ void pack_back(const float* w, int f, int fo, int til
     for (int part = 0; part < 3; ++part) *(uintx4*)(packed + (piece * 3 + part) * 1024 + lane * 16) = split::take_part8(v);
 }
 
-// gx: a wave takes 32 positions and all TILES x 16 inputs, workgroups of four waves walk over the positions.  While 16 features are multiplied, the
-// next ones' gy, u and v are on their way into registers and their weights into shared memory.  40 -> 80 maps of 61 x 58 x 63 68 us, 3.7 TB/s.
+// gx: a wave takes 32 positions and all TILES x 16 inputs, workgroups of four waves walk over the positions.  The next 16 features' gy, u and v are requested before
+// 16 are multiplied.  Their weights are copied into shared memory as well, but waited for at once: gx_again takes G by reference, so that G lies in private memory, its pointers
+// are read from there and loads through them are flat ones, which wait for everything before them.  40 -> 80 maps of 61 x 58 x 63 68 us, 3.7 TB/s.
 template <int TILES, int AXIS>
 __global__ void __launch_bounds__(256, 2) k_gated_gx(GatedBack G, const char* packed, float* gx)
 {
@@ -1265,8 +1271,9 @@ __global__ void __launch_bounds__(256, 2) k_gated_gx(GatedBack G, const char* pa
 constexpr int kBackWaves = 4;       // of a workgroup: with three on a SIMD
 
 // gw and gb: a wave takes 16 features (both halves) and all TILES x 16 inputs, workgroups a share of the positions, 32 at a time; x is taken apart by all
-// waves for all of them.  40 -> 80 maps of 61 x 58 x 63 95 us, 2.6 TB/s: loads of a step, gates and products follow each other in a wave, three waves a
-// SIMD are what its registers leave.  Workgroups behind the shares pack the weights for k_gated_gx, which comes next.
+// waves for all of them.  Workgroups behind the shares pack the weights for k_gated_gx, which comes next.  40 -> 80 maps of 61 x 58 x 63 95 us, 2.6 TB/s, bound by the
+// latency of its loads: gw_again takes G by reference, so that G lies in private memory as in k_gated_gx, and the pointers of gy and of the kept are read behind the loads of x and
+// waited for with these.  Three waves a SIMD are what the registers leave.
 template <int TILES, int AXIS>
 __global__ void __launch_bounds__(64 * kBackWaves, 3) k_gated_gw(GatedBack G, long span, int shares, int waves, float* parts, float* sums, char* packed)
 {
@@ -1450,8 +1457,8 @@ typedef Waves<4, 1, 1, 2> Tall;         // 128 x 64
 
 // Tiles of a product and into how many shares its sum goes, by what it is expected to take: a unit takes 2.6 us for a step of 32 k of a tile of 256 x 128 on the
 // bf16 matrix cores (205 TFLOP/s in all), and 1.3 us for one of 64 x 128 on the fp32 ones (100 TFLOP/s), which take three tiles side by side; sums of
-// shares move their bytes at 4 TB/s and a launch takes 3 us.  Sums of more than 2^16 terms (2048 additions one after another) go into shares whatever they
-// cost, as far as there are shares.
+// shares move their bytes at 4 TB/s and a launch takes 3 us.  Where a product may go in shares, sums of more than 2^16 terms (2048 additions one after another on the bf16
+// matrix cores) do whatever it costs, as far as there are shares.
 enum Kind { FP32, SPLIT, SPLIT_TURNED };
 struct Layout { Kind kind; Tiles T; int shares; long span; double us; };
 constexpr long kFewPositions = 32, kUnits = 256, kMostShares = 512, kLeastSpan = kDepth, kMostSpan = 1L << 16;
